@@ -305,6 +305,113 @@ int fq_gemm_w4a8(const int8_t* Aq, const float* alpha, int64_t M, int64_t N, int
                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention between the two products of a layer: the QKV product's rows are normalised, rotated and put into a cache of
+ * pages (fq_qk_norm_rope), and attended to, whole prompts at once (fq_attention_prompt) or a few drafted tokens per sequence
+ * over the cache (fq_attention_tree).  No product of the method; the paper's layers (section 2.1) are served with them.
+ *
+ * Shape limits shared by the three: act_dtype FQ_F16 or FQ_BF16; head_dim a multiple of 8, at most 128; 1 <= kv_heads <= q_heads,
+ * kv_heads dividing q_heads (query head h reads key head h / (q_heads / kv_heads)), q_heads at most 4096; strides count
+ * elements and are multiples of 8.
+ */
+
+/* Rows of heads: row r of head h is the head_dim consecutive values from data + r * row_stride + h * head_stride on.
+ * The struct is host memory, read during the call; data is device memory. */
+typedef struct fq_heads {
+    const void* data;
+    int64_t row_stride, head_stride;
+} fq_heads;
+
+/* A cache of keys and values in pages: slot s (0 <= s < pages * page_size) of head h is the head_dim consecutive values from
+ * k (or v) + (s / page_size) * page_stride + (s % page_size) * token_stride + h * head_stride on.  pages * page_size is at most
+ * 2^31 - 1.  The struct is host memory, read during the call; k and v are device memory. */
+typedef struct fq_kv_pages {
+    void* k;
+    void* v;
+    int64_t pages;
+    int page_size;
+    int64_t page_stride, token_stride, head_stride;
+} fq_kv_pages;
+
+/*
+ * fq_qk_norm_rope -- the rows of a QKV product, made ready for attention in one pass.  A row holds q_heads query heads, kv_heads
+ * key heads and kv_heads value heads of head_dim values each.  Every query and key head x becomes
+ *   y = x / sqrt(mean(x^2) + eps) * weight                                    (weight NULL: y = x)
+ * and the first rot_dim of its values are rotated by the row's position p, c = table[p][i], s = table[p][rot_dim / 2 + i]:
+ *   (y[a], y[b]) -> (y[a] c - y[b] s, y[b] c + y[a] s),   a, b = i, i + rot_dim / 2, or 2 i, 2 i + 1 (interleaved).
+ * Everything is evaluated in binary32 and rounded once.  Values are copied.
+ *
+ *   qkv              in   [tokens, (q_heads + 2 kv_heads) * head_dim], act_dtype, rows row_stride elements apart
+ *   q_weight, k_weight in [head_dim], act_dtype; NULL: no norm of the queries, of the keys
+ *   table            in   [table_rows, rot_dim] binary32: cosines, then sines (NULL when rot_dim is 0)
+ *   positions        in   [tokens] (NULL when rot_dim is 0); a position outside 0 .. table_rows - 1 takes the nearest row
+ *   q_out            out  [tokens, q_heads, head_dim], act_dtype
+ *   k_out            out  [tokens, kv_heads, head_dim], act_dtype; NULL: not written
+ *   cache, slots     out  keys and values go to slot slots[t] of the cache (NULL, NULL: they do not); a slot outside the cache
+ *                         (a negative one: padding) is not written.  Slots that are written are different ones.
+ * rot_dim: a multiple of 8, at most head_dim.  q_out, k_out and the cache must not overlap qkv or each other.
+ * tokens = 0 is a valid no-op.  Asynchronous on `stream`, one kernel, no scratch.
+ * Errors: FQ_ERR_INVALID_ARG (null pointers, sizes, strides that do not hold a row, eps negative or not finite, q_out or k_out over qkv,
+ *         neither k_out nor a cache), FQ_ERR_UNSUPPORTED (shape limits, tokens above 2^24, pointers or strides not aligned to 16 bytes), FQ_ERR_HIP.
+ */
+int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_stride, int q_heads, int kv_heads, int head_dim,
+                    const void* q_weight, const void* k_weight, float eps, const float* table, int64_t table_rows, int rot_dim,
+                    int interleaved, const int32_t* positions, void* q_out, void* k_out, const fq_kv_pages* cache,
+                    const int64_t* slots, void* stream);
+
+/*
+ * fq_attention_prompt -- causal attention over packed sequences.  Rows q_offsets[b] .. q_offsets[b+1]-1 of q and rows
+ * k_offsets[b] .. k_offsets[b+1]-1 of k and v belong to sequence b, whose last query is at its last key:
+ *   out[i, h] = sum_j softmax_j(scale * q[i, h] . k[j, h']) v[j, h'],   j <= i + (keys of b) - (queries of b)   (i, j in b)
+ * (more keys than queries: a prefix is there already; a query that sees no key gives zeros).  Scores, softmax and sums are
+ * binary32; the softmax's numerators are rounded to act_dtype for their product with the values, the result once.  What a
+ * query does not see has no part in its result, not by an infinity or a NaN either.
+ *
+ *   q, k, v        in   device rows of q_heads, kv_heads, kv_heads heads
+ *   q_offsets_host in   HOST array [sequences + 1], non-decreasing, q_offsets_host[0] = 0
+ *   k_offsets_host in   HOST array, the same for k and v; NULL: q_offsets_host
+ *   scale               positive and finite (0.0f: 1 / sqrt(head_dim))
+ *   out            out  [q_offsets_host[sequences], q_heads, head_dim], act_dtype; must not overlap an input
+ *   workspace           device scratch, >= fq_attention_prompt_workspace_bytes(...) bytes (may be NULL when that is 0)
+ * Deterministic; asynchronous on `stream`, no allocation.  No rows, or no sequences: a valid no-op.
+ * Errors: FQ_ERR_INVALID_ARG (null pointers, offsets, scale), FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, pointers or
+ *         strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
+ */
+size_t fq_attention_prompt_workspace_bytes(int q_heads, int kv_heads, int head_dim, const int32_t* q_offsets_host,
+                                           const int32_t* k_offsets_host, int sequences);
+int fq_attention_prompt(const fq_heads* q, const fq_heads* k, const fq_heads* v, int act_dtype, int q_heads, int kv_heads, int head_dim,
+                        const int32_t* q_offsets_host, const int32_t* k_offsets_host, int sequences, float scale, void* out,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * fq_attention_tree -- attention of `nodes` drafted tokens per sequence over the sequence's cache.  Sequence b has
+ * context_lens[b] tokens in the cache, its drafted tokens' keys and values in the `nodes` places behind them; place j of it is slot
+ * page_table[b][j / page_size] * page_size + j % page_size.  Node i sees the whole context, and of the drafted tokens those whose
+ * bit is set in its mask, bit j % 64 of word j / 64 for token j (a tree: the node itself and its ancestors); without a mask,
+ * tokens 0 .. i (a chain).  nodes = 1 without a mask is ordinary generation.  Numerics as fq_attention_prompt.
+ *
+ *   q            in   rows b * nodes + i of q_heads heads
+ *   cache        in   kv_heads heads
+ *   page_table   in   [sequences, table_width] device; entries that no token lies in are not read for anything.  An entry outside the
+ *                     cache is taken as the nearest page
+ *   context_lens in   [sequences] device.  A negative one: the sequence has no keys, its result is zeros.  Tokens beyond
+ *                     table_width pages are not seen
+ *   mask         in   device words, node i's at mask + b * mask_stride + i * ((nodes + 63) / 64); mask_stride = 0: one tree for all
+ *   scale, out   as fq_attention_prompt; out [sequences, nodes, q_heads, head_dim]
+ *   workspace         device scratch, >= fq_attention_tree_workspace_bytes(...) bytes (may be NULL when that is 0)
+ * Lengths and tables are read on the device when the kernels run, so that a captured call may be replayed with others; calls that
+ * share a workspace must be ordered on one stream.  Deterministic; asynchronous on `stream`, no allocation.
+ * sequences = 0 or nodes = 0: a valid no-op.
+ * Errors: FQ_ERR_INVALID_ARG, FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, 2^20 nodes or 2^24 rows in all, table_width * page_size of 2^31 or
+ *         more, pointers or strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
+ */
+size_t fq_attention_tree_workspace_bytes(int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,
+                                         int page_size);
+int fq_attention_tree(const fq_heads* q, int act_dtype, int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim,
+                      const fq_kv_pages* cache, const int32_t* page_table, int64_t table_width, const int32_t* context_lens,
+                      const uint64_t* mask, int64_t mask_stride, float scale, void* out, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/*
  * fq_gemm_describe -- writes a short text description of the kernel configuration fq_gemm
  * would use for this problem (kernel family, tile shape, block shape, split-K factor) into
  * buf (HOST memory, at most buf_bytes including the terminating 0).  For logs and benchmark

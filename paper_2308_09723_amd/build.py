@@ -24,6 +24,9 @@ SOURCES = [
     "fq_gemm.hip",
     "fq_w4a8.hip",
     "fq_probe.hip",
+    "fq_rope.hip",
+    "fq_attn_prompt.hip",
+    "fq_attn_tree.hip",
     "fq_gemm_f16_4.hip",
     "fq_gemm_f16_8.hip",
     "fq_gemm_bf16_4.hip",

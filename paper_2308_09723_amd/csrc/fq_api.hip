@@ -323,6 +323,192 @@ int fq_gemm_grouped_describe(const int32_t* offsets_host, int E, int64_t N, int6
     return FQ_OK;
 }
 
+// ------------------------------------------------------------------------------------------ attention
+// FQ_OK, or what is wrong with types and head counts
+static int check_heads(int act_dtype, int q_heads, int kv_heads, int head_dim) {
+    if (act_dtype != FQ_F16 && act_dtype != FQ_BF16) return FQ_ERR_INVALID_ARG;
+    if (q_heads <= 0 || kv_heads <= 0 || head_dim <= 0 || q_heads % kv_heads != 0) return FQ_ERR_INVALID_ARG;
+    return head_dim % 8 != 0 || head_dim > 128 || q_heads > 4096 ? FQ_ERR_UNSUPPORTED : FQ_OK;
+}
+
+static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// Whether n things a stride apart reach further than any memory does (the sums of offsets below stay within 63 bits)
+static bool too_far(int64_t n, int64_t stride) { return stride > ((int64_t)1 << 58) / (n > 0 ? n : 1); }
+
+static int check_rows(const fq_heads* x, int64_t rows, int heads) {
+    if (!x->data || x->row_stride < 0 || x->head_stride < 0) return FQ_ERR_INVALID_ARG;
+    if (!aligned16(x->data) || x->row_stride % 8 != 0 || x->head_stride % 8 != 0 || too_far(rows, x->row_stride) ||
+        too_far(heads, x->head_stride))
+        return FQ_ERR_UNSUPPORTED;
+    return FQ_OK;
+}
+
+static int check_cache(const fq_kv_pages* c, int kv_heads, int head_dim) {
+    if (!c->k || !c->v || c->pages <= 0 || c->page_size <= 0) return FQ_ERR_INVALID_ARG;
+    // (a slot's head_dim values are its own: no stride is shorter, unless there is only one of what it steps over)
+    if ((c->pages > 1 && c->page_stride < head_dim) || (c->page_size > 1 && c->token_stride < head_dim) ||
+        (kv_heads > 1 && c->head_stride < head_dim) || c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0)
+        return FQ_ERR_INVALID_ARG;
+    if (!aligned16(c->k) || !aligned16(c->v) || c->page_stride % 8 != 0 || c->token_stride % 8 != 0 || c->head_stride % 8 != 0)
+        return FQ_ERR_UNSUPPORTED;
+    if (too_far(c->pages, c->page_stride) || too_far(c->page_size, c->token_stride) || too_far(kv_heads, c->head_stride)) return FQ_ERR_UNSUPPORTED;
+    return c->pages > INT32_MAX / c->page_size ? FQ_ERR_UNSUPPORTED : FQ_OK;
+}
+
+int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_stride, int q_heads, int kv_heads, int head_dim,
+                    const void* q_weight, const void* k_weight, float eps, const float* table, int64_t table_rows, int rot_dim,
+                    int interleaved, const int32_t* positions, void* q_out, void* k_out, const fq_kv_pages* cache,
+                    const int64_t* slots, void* stream) {
+    if (tokens < 0 || rot_dim < 0 || rot_dim > head_dim || !(eps >= 0.0f && eps <= 3.4e38f)) return FQ_ERR_INVALID_ARG;
+    const int st = check_heads(act_dtype, q_heads, kv_heads, head_dim);
+    if (st != FQ_OK) return st;
+    const int64_t row = ((int64_t)q_heads + 2 * (int64_t)kv_heads) * head_dim;
+    if (row_stride < row && tokens > 1) return FQ_ERR_INVALID_ARG;
+    if (tokens > 0 && (!cache != !slots || (!k_out && !cache))) return FQ_ERR_INVALID_ARG;
+    if (rot_dim > 0 && (table_rows <= 0 || !table || (!positions && tokens > 0))) return FQ_ERR_INVALID_ARG;
+    if (rot_dim % 8 != 0 || tokens > (int64_t)1 << 24 || too_far(tokens, row_stride) || row_stride % 8 != 0) return FQ_ERR_UNSUPPORTED;
+    if (cache) {
+        const int cst = check_cache(cache, kv_heads, head_dim);
+        if (cst != FQ_OK) return cst;
+    }
+    if (tokens == 0) return FQ_OK;
+    if (!qkv || !q_out) return FQ_ERR_INVALID_ARG;
+    if (!aligned16(qkv) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_weight) || !aligned16(k_weight)) return FQ_ERR_UNSUPPORTED;
+    const size_t read = (size_t)((tokens - 1) * row_stride + row) * 2;
+    if (fq_overlaps(q_out, (size_t)tokens * q_heads * head_dim * 2, {{qkv, read}})) return FQ_ERR_INVALID_ARG;
+    if (k_out && fq_overlaps(k_out, (size_t)tokens * kv_heads * head_dim * 2, {{qkv, read}, {q_out, (size_t)tokens * q_heads * head_dim * 2}}))
+        return FQ_ERR_INVALID_ARG;
+    fq_rope_args a = {qkv, tokens, row_stride, q_heads, kv_heads, head_dim, q_weight, k_weight, eps, table, table_rows, rot_dim, interleaved != 0,
+                      positions, q_out, k_out, {}, slots};
+    if (cache) a.cache = *cache;
+    return fq_launch_qk_norm_rope(act_dtype, a, (hipStream_t)stream);
+}
+
+static int check_offsets(const int32_t* offsets, int sequences) {
+    if (offsets[0] != 0) return FQ_ERR_INVALID_ARG;
+    for (int b = 0; b < sequences; ++b)
+        if (offsets[b + 1] < offsets[b]) return FQ_ERR_INVALID_ARG;
+    return FQ_OK;
+}
+
+// The checks that need no data pointer; fills what they have seen.
+static int check_prompt(int act_dtype, int q_heads, int kv_heads, int head_dim, const int32_t* q_offsets, const int32_t* k_offsets,
+                        int sequences, fq_prompt_args* a) {
+    if (!q_offsets || sequences < 0) return FQ_ERR_INVALID_ARG;
+    if (!k_offsets) k_offsets = q_offsets;
+    int st = check_heads(act_dtype, q_heads, kv_heads, head_dim);
+    if (st != FQ_OK) return st;
+    if (sequences > 65536) return FQ_ERR_UNSUPPORTED;
+    st = check_offsets(q_offsets, sequences);
+    if (st == FQ_OK && k_offsets != q_offsets) st = check_offsets(k_offsets, sequences);
+    if (st != FQ_OK) return st;
+    a->q_heads = q_heads;
+    a->kv_heads = kv_heads;
+    a->head_dim = head_dim;
+    a->q_offsets = q_offsets;
+    a->k_offsets = k_offsets;
+    a->sequences = sequences;
+    return FQ_OK;
+}
+
+// 1 / sqrt(head_dim) for 0; false: not a scale
+static bool effective_scale(float* scale, int head_dim) {
+    if (*scale == 0.0f) *scale = 1.0f / __builtin_sqrtf((float)head_dim);
+    return *scale > 0.0f && *scale <= 3.4e38f;
+}
+
+size_t fq_attention_prompt_workspace_bytes(int q_heads, int kv_heads, int head_dim, const int32_t* q_offsets_host,
+                                           const int32_t* k_offsets_host, int sequences) {
+    fq_prompt_args a = {};
+    if (check_prompt(FQ_F16, q_heads, kv_heads, head_dim, q_offsets_host, k_offsets_host, sequences, &a) != FQ_OK) return 0;
+    return fq_prompt_bytes(a);
+}
+
+int fq_attention_prompt(const fq_heads* q, const fq_heads* k, const fq_heads* v, int act_dtype, int q_heads, int kv_heads, int head_dim,
+                        const int32_t* q_offsets_host, const int32_t* k_offsets_host, int sequences, float scale, void* out,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    fq_prompt_args a = {};
+    int st = check_prompt(act_dtype, q_heads, kv_heads, head_dim, q_offsets_host, k_offsets_host, sequences, &a);
+    if (st != FQ_OK) return st;
+    if (!effective_scale(&scale, head_dim)) return FQ_ERR_INVALID_ARG;
+    const int64_t rows = a.q_offsets[sequences], keys = a.k_offsets[sequences];
+    if (rows == 0) return FQ_OK;
+    if (!q || !out || (keys > 0 && (!k || !v))) return FQ_ERR_INVALID_ARG;
+    if ((st = check_rows(q, rows, q_heads)) != FQ_OK) return st;
+    if (keys > 0 && ((st = check_rows(k, keys, kv_heads)) != FQ_OK || (st = check_rows(v, keys, kv_heads)) != FQ_OK)) return st;
+    if (!aligned16(out)) return FQ_ERR_UNSUPPORTED;
+    const size_t bytes = (size_t)rows * q_heads * head_dim * 2;
+    auto span = [&](const fq_heads* x, int64_t n, int heads) {
+        return fq_span{x->data, (size_t)((n - 1) * x->row_stride + (heads - 1) * x->head_stride + head_dim) * 2};
+    };
+    if (fq_overlaps(out, bytes, {span(q, rows, q_heads)}) ||
+        (keys > 0 && fq_overlaps(out, bytes, {span(k, keys, kv_heads), span(v, keys, kv_heads)})))
+        return FQ_ERR_INVALID_ARG;
+    const size_t need = fq_prompt_bytes(a);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return FQ_ERR_WORKSPACE;
+    a.q = *q;
+    if (keys > 0) a.k = *k, a.v = *v;
+    a.scale = scale;
+    a.out = out;
+    return fq_launch_attention_prompt(act_dtype, a, workspace, (hipStream_t)stream);
+}
+
+static int check_tree(int act_dtype, int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,
+                      int page_size, fq_tree_args* a) {
+    if (sequences < 0 || nodes < 0 || table_width < 0 || page_size <= 0) return FQ_ERR_INVALID_ARG;
+    const int st = check_heads(act_dtype, q_heads, kv_heads, head_dim);
+    if (st != FQ_OK) return st;
+    if (sequences > 65536 || nodes > 1 << 20 || sequences * nodes > 1 << 24 || table_width > INT32_MAX / page_size) return FQ_ERR_UNSUPPORTED;
+    a->sequences = sequences;
+    a->nodes = (int)nodes;
+    a->q_heads = q_heads;
+    a->kv_heads = kv_heads;
+    a->head_dim = head_dim;
+    a->table_width = table_width;
+    a->cache.page_size = page_size;
+    return FQ_OK;
+}
+
+size_t fq_attention_tree_workspace_bytes(int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,
+                                         int page_size) {
+    fq_tree_args a = {};
+    if (check_tree(FQ_F16, sequences, nodes, q_heads, kv_heads, head_dim, table_width, page_size, &a) != FQ_OK) return 0;
+    if (sequences == 0 || nodes == 0) return 0;
+    return fq_tree_bytes(a);
+}
+
+int fq_attention_tree(const fq_heads* q, int act_dtype, int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim,
+                      const fq_kv_pages* cache, const int32_t* page_table, int64_t table_width, const int32_t* context_lens,
+                      const uint64_t* mask, int64_t mask_stride, float scale, void* out, void* workspace, size_t workspace_bytes,
+                      void* stream) {
+    if (!cache) return FQ_ERR_INVALID_ARG;
+    fq_tree_args a = {};
+    int st = check_tree(act_dtype, sequences, nodes, q_heads, kv_heads, head_dim, table_width, cache->page_size, &a);
+    if (st != FQ_OK) return st;
+    if ((st = check_cache(cache, kv_heads, head_dim)) != FQ_OK) return st;
+    if (!effective_scale(&scale, head_dim) || mask_stride < 0) return FQ_ERR_INVALID_ARG;
+    if (sequences == 0 || nodes == 0) return FQ_OK;
+    if (!q || !out || !context_lens || (!page_table && table_width > 0)) return FQ_ERR_INVALID_ARG;
+    if (mask && mask_stride != 0 && mask_stride < nodes * ((nodes + 63) / 64)) return FQ_ERR_INVALID_ARG;
+    if ((st = check_rows(q, sequences * nodes, q_heads)) != FQ_OK) return st;
+    if (!aligned16(out) || too_far(sequences, mask_stride)) return FQ_ERR_UNSUPPORTED;
+    const size_t bytes = (size_t)(sequences * nodes) * q_heads * head_dim * 2;
+    if (fq_overlaps(out, bytes, {{q->data, (size_t)((sequences * nodes - 1) * q->row_stride + (q_heads - 1) * q->head_stride + head_dim) * 2}}))
+        return FQ_ERR_INVALID_ARG;
+    const size_t need = fq_tree_bytes(a);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return FQ_ERR_WORKSPACE;
+    a.q = *q;
+    a.cache = *cache;
+    a.page_table = page_table;
+    a.context_lens = context_lens;
+    a.mask = mask;
+    a.mask_stride = mask_stride;
+    a.scale = scale;
+    a.out = out;
+    return fq_launch_attention_tree(act_dtype, a, workspace, (hipStream_t)stream);
+}
+
 int fq_gemm_describe(int64_t M, int64_t N, int64_t K, int bits, int group_size, char* buf,
                      size_t buf_bytes) {
     if (!buf || buf_bytes == 0 || M < 0) return FQ_ERR_INVALID_ARG;

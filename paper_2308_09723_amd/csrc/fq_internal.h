@@ -129,4 +129,49 @@ int fq_launch_gemm_grouped(const void* A, int act, const int32_t* offsets, int E
                            const void* codes, const void* scales, int bits, int g, void* C,
                            hipStream_t stream);
 
+
+// attention side (arguments checked; cache: pages == 0 where there is none)
+struct fq_rope_args {
+    const void* qkv;
+    int64_t tokens, row_stride;
+    int q_heads, kv_heads, head_dim;
+    const void *q_weight, *k_weight;
+    float eps;
+    const float* table;
+    int64_t table_rows;
+    int rot_dim, interleaved;
+    const int32_t* positions;
+    void *q_out, *k_out;
+    fq_kv_pages cache;
+    const int64_t* slots;
+};
+int fq_launch_qk_norm_rope(int act_dtype, const fq_rope_args& a, hipStream_t stream);
+
+struct fq_prompt_args {
+    fq_heads q, k, v;
+    int q_heads, kv_heads, head_dim;
+    const int32_t *q_offsets, *k_offsets;      // host
+    int sequences;
+    float scale;
+    void* out;
+};
+size_t fq_prompt_bytes(const fq_prompt_args& a);
+int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* workspace, hipStream_t stream);
+
+struct fq_tree_args {
+    fq_heads q;
+    int64_t sequences;
+    int nodes, q_heads, kv_heads, head_dim;
+    fq_kv_pages cache;
+    const int32_t* page_table;
+    int64_t table_width;
+    const int32_t* context_lens;
+    const uint64_t* mask;
+    int64_t mask_stride;
+    float scale;
+    void* out;
+};
+size_t fq_tree_bytes(const fq_tree_args& a);
+int fq_launch_attention_tree(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream);
+
 #endif  // FQ_INTERNAL_H_

@@ -28,6 +28,17 @@ FQ_SCALE_BF16 = 1
 _lib = None
 
 
+class Heads(ctypes.Structure):
+    """fq_heads: rows of heads in device memory, strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class KvPages(ctypes.Structure):
+    """fq_kv_pages: a cache of keys and values in pages, strides in elements."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int),
+                ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 class FqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -84,6 +95,15 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "fq_mfma_rate_probe_sink_bytes": (sz, []),
         "fq_mfma_rate_probe_flops": (ctypes.c_double, [i32, i32]),
         "fq_mfma_rate_probe": (i32, [vp, sz, vp, sz, i32, i32, i32, vp]),
+        "fq_qk_norm_rope": (i32, [vp, i32, i64, i64, i32, i32, i32, vp, vp, f32, vp, i64, i32, i32, vp, vp, vp,
+                                  ctypes.POINTER(KvPages), vp, vp]),
+        "fq_attention_prompt_workspace_bytes": (sz, [i32, i32, i32, ctypes.POINTER(ctypes.c_int32),
+                                                     ctypes.POINTER(ctypes.c_int32), i32]),
+        "fq_attention_prompt": (i32, [ctypes.POINTER(Heads), ctypes.POINTER(Heads), ctypes.POINTER(Heads), i32, i32, i32, i32,
+                                      ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32), i32, f32, vp, vp, sz, vp]),
+        "fq_attention_tree_workspace_bytes": (sz, [i64, i64, i32, i32, i32, i64, i32]),
+        "fq_attention_tree": (i32, [ctypes.POINTER(Heads), i32, i64, i64, i32, i32, i32, ctypes.POINTER(KvPages), vp, i64, vp, vp,
+                                    i64, f32, vp, vp, sz, vp]),
         "fq_status_string": (ctypes.c_char_p, [i32]),
         "fq_version": (ctypes.c_char_p, []),
     }
@@ -104,6 +124,8 @@ EXPORTED = [
     "fq_stream_read_probe", "fq_gemm_noalloc", "fq_gemm_noalloc_scratch_bytes",
     "fq_mfma_rate_probe_operand_bytes", "fq_mfma_rate_probe_sink_bytes", "fq_mfma_rate_probe_flops", "fq_mfma_rate_probe",
     "fq_zscale_bytes", "fq_unpack_w4a8", "fq_quantize_w4a8", "fq_quantize_act_i8", "fq_gemm_w4a8_workspace_bytes", "fq_gemm_w4a8",
+    "fq_qk_norm_rope", "fq_attention_prompt_workspace_bytes", "fq_attention_prompt", "fq_attention_tree_workspace_bytes",
+    "fq_attention_tree",
 ]
 
 
@@ -287,6 +309,40 @@ def gemm_w4a8_raw(Aq_ptr, alpha_ptr, M, N, K, codes_ptr, z_ptr, t_ptr, group_siz
                   stream=0):
     return int(load().fq_gemm_w4a8(Aq_ptr, alpha_ptr, M, N, K, codes_ptr, z_ptr, t_ptr, group_size, C_ptr, out_dtype,
                                    ws_ptr, ws_bytes, stream))
+
+
+def qk_norm_rope_raw(qkv_ptr, act_dtype, tokens, row_stride, q_heads, kv_heads, head_dim, q_weight_ptr, k_weight_ptr, eps,
+                     table_ptr, table_rows, rot_dim, interleaved, positions_ptr, q_out_ptr, k_out_ptr, cache=None,
+                     slots_ptr=None, stream=0):
+    return int(load().fq_qk_norm_rope(qkv_ptr, act_dtype, tokens, row_stride, q_heads, kv_heads, head_dim, q_weight_ptr,
+                                      k_weight_ptr, eps, table_ptr, table_rows, rot_dim, interleaved, positions_ptr, q_out_ptr,
+                                      k_out_ptr, cache, slots_ptr, stream))
+
+
+def attention_prompt_workspace_bytes(q_heads, kv_heads, head_dim, q_offsets, k_offsets=None):
+    return int(load().fq_attention_prompt_workspace_bytes(q_heads, kv_heads, head_dim, _int32_array(q_offsets),
+                                                          None if k_offsets is None else _int32_array(k_offsets),
+                                                          len(q_offsets) - 1))
+
+
+def attention_prompt_raw(q, k, v, act_dtype, q_heads, kv_heads, head_dim, q_offsets, k_offsets, scale, out_ptr, ws_ptr=None,
+                         ws_bytes=0, stream=0):
+    """q, k, v: Heads."""
+    return int(load().fq_attention_prompt(q, k, v, act_dtype, q_heads, kv_heads, head_dim, _int32_array(q_offsets),
+                                          None if k_offsets is None else _int32_array(k_offsets), len(q_offsets) - 1, scale,
+                                          out_ptr, ws_ptr, ws_bytes, stream))
+
+
+def attention_tree_workspace_bytes(sequences, nodes, q_heads, kv_heads, head_dim, table_width, page_size):
+    return int(load().fq_attention_tree_workspace_bytes(sequences, nodes, q_heads, kv_heads, head_dim, table_width, page_size))
+
+
+def attention_tree_raw(q, act_dtype, sequences, nodes, q_heads, kv_heads, head_dim, cache, page_table_ptr, table_width,
+                       context_lens_ptr, mask_ptr, mask_stride, scale, out_ptr, ws_ptr=None, ws_bytes=0, stream=0):
+    """q: Heads; cache: KvPages."""
+    return int(load().fq_attention_tree(q, act_dtype, sequences, nodes, q_heads, kv_heads, head_dim, cache, page_table_ptr,
+                                        table_width, context_lens_ptr, mask_ptr, mask_stride, scale, out_ptr, ws_ptr, ws_bytes,
+                                        stream))
 
 
 # ------------------------------------------------------------------ torch-tensor conveniences
@@ -528,3 +584,165 @@ def gemm_w4a8(Aq, alpha, codes, z, t, group_size, out_dtype, out=None, workspace
         status = gemm_w4a8_raw(*args, workspace.data_ptr(), size, _stream())
     _check(status, "fq_gemm_w4a8")
     return C
+
+
+# ------------------------------------------------------------------ attention
+def _require(condition, where):
+    if not condition:
+        raise FqError(FQ_ERR_INVALID_ARG, where)
+
+
+def _plain(t, dtype, device, where):
+    """Whether t is a contiguous tensor of this type on this device."""
+    _require(t.dtype == dtype and t.device == device and t.is_contiguous(), where)
+
+
+def rope_table(rows, rot_dim, base=10000.0, device="cuda"):
+    """The table of qk_norm_rope for positions 0 .. rows - 1: cosines, then sines, of position * base^(-2 i / rot_dim);
+    float32 [rows, rot_dim]."""
+    torch = _torch_mod or _torch()
+    turns = base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
+    angle = torch.arange(rows, dtype=torch.float64)[:, None] * turns
+    return torch.cat([angle.cos(), angle.sin()], 1).float().to(device)
+
+
+def tree_mask(parents, device="cuda"):
+    """Masks of attention_tree for drafted trees: parents[i] < i is the node that node i hangs from, -1 for the context itself (one
+    list, or one of the same length per sequence) -> int64 [nodes, words] or [sequences, nodes, words]: each node's ancestors and itself."""
+    torch = _torch_mod or _torch()
+
+    def words(tree):
+        seen = []
+        for i, p in enumerate(tree):
+            if not -1 <= p < i:
+                raise ValueError(f"node {i} hangs from {p}: -1 or a node before it")
+            seen.append((seen[p] if p >= 0 else 0) | 1 << i)
+        rows = [[s >> 64 * w & (1 << 64) - 1 for w in range((len(tree) + 63) // 64)] for s in seen]
+        return [[x - (1 << 64) if x >> 63 else x for x in row] for row in rows]
+
+    several = len(parents) > 0 and not isinstance(parents[0], int)
+    return torch.tensor([words(t) for t in parents] if several else words(parents), dtype=torch.int64, device=device)
+
+
+def _heads(t, where):
+    """Heads of a tensor [rows, heads, head_dim]."""
+    _require(t.is_cuda and t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] <= 1), where)
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _pages(k_cache, v_cache, like, kv_heads, head_dim, where):
+    """KvPages of two tensors [pages, page_size, kv_heads, head_dim] with the same strides."""
+    for c in (k_cache, v_cache):
+        _require(c.dim() == 4 and c.dtype == like.dtype and c.device == like.device and c.stride(3) == 1, where)
+        _require(c.shape[2] == kv_heads and c.shape[3] == head_dim, where)
+    _require(k_cache.shape == v_cache.shape and k_cache.stride() == v_cache.stride(), where)
+    return KvPages(k_cache.data_ptr(), v_cache.data_ptr(), k_cache.shape[0], k_cache.shape[1], *k_cache.stride()[:3])
+
+
+def _output(out, shape, like, where):
+    torch = _torch_mod or _torch()
+    if out is None:
+        return torch.empty(shape, dtype=like.dtype, device=like.device)
+    _require(tuple(out.shape) == tuple(shape), where)
+    _plain(out, like.dtype, like.device, where)
+    return out
+
+
+def qk_norm_rope(qkv, heads, kv_heads, table, positions, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, q_out=None,
+                 k_out=None, k_cache=None, v_cache=None, slots=None):
+    """qkv: cuda [tokens, (heads + 2 kv_heads) * head_dim] float16/bfloat16, rows of any stride -> (q [tokens, heads, head_dim],
+    k [tokens, kv_heads, head_dim]), normalised (with q_weight, k_weight [head_dim]) and rotated by positions (int32 [tokens]) with
+    table (rope_table; None: not rotated).  With k_cache, v_cache [pages, page_size, kv_heads, head_dim] and slots (int64 [tokens])
+    keys and values go to the cache, and k is None unless k_out is given."""
+    torch = _torch_mod or _torch()
+    where = "fq_qk_norm_rope"
+    _require(qkv.is_cuda and qkv.dim() == 2 and heads > 0 and kv_heads > 0 and qkv.shape[1] % (heads + 2 * kv_heads) == 0, where)
+    _require(qkv.stride(1) == 1, where)
+    tokens, D = qkv.shape[0], qkv.shape[1] // (heads + 2 * kv_heads)
+    act = _act_code(qkv)
+    for w in (q_weight, k_weight):
+        if w is not None:
+            _require(w.numel() == D, where)
+            _plain(w, qkv.dtype, qkv.device, where)
+    rot = 0
+    if table is not None:
+        _require(table.dim() == 2 and positions is not None and positions.numel() == tokens, where)
+        _plain(table, torch.float32, qkv.device, where)
+        _plain(positions, torch.int32, qkv.device, where)
+        rot = table.shape[1]
+    cache = None
+    _require((k_cache is None) == (v_cache is None) == (slots is None), where)
+    if k_cache is not None:
+        cache = _pages(k_cache, v_cache, qkv, kv_heads, D, where)
+        _require(slots.numel() == tokens, where)
+        _plain(slots, torch.int64, qkv.device, where)
+    q = _output(q_out, (tokens, heads, D), qkv, where)
+    k = _output(k_out, (tokens, kv_heads, D), qkv, where) if k_out is not None or cache is None else None
+
+    def at(t):
+        return None if t is None else t.data_ptr()
+
+    _check(qk_norm_rope_raw(qkv.data_ptr(), act, tokens, qkv.stride(0), heads, kv_heads, D, at(q_weight), at(k_weight), eps,
+                            at(table) if rot else None, table.shape[0] if rot else 0, rot, int(interleaved),
+                            at(positions) if rot else None, q.data_ptr(), at(k), cache, at(slots), _stream()), where)
+    return q, k
+
+
+def attention_prompt(q, k, v, q_offsets, k_offsets=None, scale=None, out=None, workspace=None):
+    """Causal attention over packed sequences: q cuda [rows, heads, head_dim], k and v [keys, kv_heads, head_dim] (float16 or bfloat16,
+    any row and head strides), sequence b's rows q_offsets[b] .. q_offsets[b + 1] - 1 (host integers) and keys k_offsets[b] .. (None: the
+    same) -> [rows, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given."""
+    torch = _torch_mod or _torch()
+    where = "fq_attention_prompt"
+    act = _act_code(q)
+    hq, hk, hv = _heads(q, where), _heads(k, where), _heads(v, where)
+    (rows, heads, D), (keys, kv_heads, _) = q.shape, k.shape
+    for t in (k, v):
+        _require(tuple(t.shape) == (keys, kv_heads, D) and t.dtype == q.dtype and t.device == q.device, where)
+    _require(len(q_offsets) >= 1 and q_offsets[-1] == rows, where)
+    _require(k_offsets is None or len(k_offsets) == len(q_offsets), where)
+    _require((q_offsets if k_offsets is None else k_offsets)[-1] == keys, where)
+    _require(scale is None or scale > 0, where)
+    o = _output(out, (rows, heads, D), q, where)
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    need = attention_prompt_workspace_bytes(heads, kv_heads, D, q_offsets, k_offsets)
+    if size < need:
+        workspace, size = torch.empty(need, dtype=torch.uint8, device=q.device), need
+    _check(attention_prompt_raw(hq, hk, hv, act, heads, kv_heads, D, q_offsets, k_offsets, scale or 0.0, o.data_ptr(),
+                                workspace.data_ptr() if size else None, size, _stream()), where)
+    return o
+
+
+def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, scale=None, out=None, workspace=None):
+    """Attention of drafted tokens over a paged cache: q cuda [sequences, nodes, heads, head_dim] (float16 or bfloat16), caches
+    [pages, page_size, kv_heads, head_dim], page_table int32 [sequences, width], context_lens int32 [sequences] (tokens in the cache
+    before the drafted ones, whose keys and values lie in the places behind them), mask int64 [nodes, words] or [sequences, nodes, words] (tree_mask;
+    None: a chain) -> [sequences, nodes, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given."""
+    torch = _torch_mod or _torch()
+    where = "fq_attention_tree"
+    act = _act_code(q)
+    _require(q.is_cuda and q.dim() == 4 and (q.stride(3) == 1 or q.shape[3] <= 1), where)
+    sequences, nodes, heads, D = q.shape
+    _require(q.stride(0) == nodes * q.stride(1) or sequences <= 1, where)
+    kv_heads = k_cache.shape[2] if k_cache.dim() == 4 else 0
+    cache = _pages(k_cache, v_cache, q, kv_heads, D, where)
+    _require(page_table.dim() == 2 and page_table.shape[0] == sequences and context_lens.numel() == sequences, where)
+    _plain(page_table, torch.int32, q.device, where)
+    _plain(context_lens, torch.int32, q.device, where)
+    stride = 0
+    if mask is not None:
+        words = (nodes + 63) // 64
+        _plain(mask, torch.int64, q.device, where)
+        _require(tuple(mask.shape) in ((nodes, words), (sequences, nodes, words)), where)
+        stride = nodes * words if mask.dim() == 3 else 0
+    _require(scale is None or scale > 0, where)
+    o = _output(out, (sequences, nodes, heads, D), q, where)
+    width, page = page_table.shape[1], k_cache.shape[1]
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    need = attention_tree_workspace_bytes(sequences, nodes, heads, kv_heads, D, width, page)
+    if size < need:
+        workspace, size = torch.empty(need, dtype=torch.uint8, device=q.device), need
+    _check(attention_tree_raw(Heads(q.data_ptr(), q.stride(1), q.stride(2)), act, sequences, nodes, heads, kv_heads, D, cache,
+                              page_table.data_ptr(), width, context_lens.data_ptr(), None if mask is None else mask.data_ptr(), stride,
+                              scale or 0.0, o.data_ptr(), workspace.data_ptr() if size else None, size, _stream()), where)
+    return o
