@@ -1,14 +1,16 @@
 // Causal attention over packed sequences (fq_attention_prompt).
 #include <hip/hip_runtime.h>
 #include <algorithm>
+#include <atomic>
 
-#include "fq_attn.h"
+#include "fq_attn_tile.h"
+#include "fq_lds_limit.h"
 
 namespace {
 
 using namespace fqa;
 
-constexpr int TILE = 4;              // queries per block
+constexpr int TILE = ROWS;           // queries per block
 constexpr int SEQUENCES = 128;       // per launch: their table is a kernel argument
 
 // The sequences of a launch, longest first, and the order of their query tiles: the last tiles of the longest sequences, which
@@ -33,24 +35,95 @@ __device__ inline void find_tile(const prompt_items& items, int rank, int* seque
     *tile = items.tiles[s] - 1 - level;
 }
 
-template <int ACT>
-__global__ __launch_bounds__(256) void fq_attention_prompt_kernel(fq_heads q, fq_heads k, fq_heads v, int q_heads, int group, int D,
-                                                                  float factor, uint16_t* out, prompt_items items) {
+template <int ACT, int DP>
+__global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q, fq_heads k, fq_heads v, int q_heads, int group, int D,
+                                                                     float factor, uint16_t* out, prompt_items items) {
+    typedef tile_shape<DP> SH;
+    extern __shared__ __align__(16) char lds[];
     int sequence, tile;
-    find_tile(items, blockIdx.x, &sequence, &tile);
-    const int i = tile * TILE + (threadIdx.x >> 6), h = blockIdx.y;
+    find_tile(items, blockIdx.x / q_heads, &sequence, &tile);
+    const int h = blockIdx.x % q_heads;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int queries = items.q_len[sequence], keys = items.k_len[sequence];
-    if (i >= queries) return;
+    const int first = tile * ROWS + wave * 32, i = first + (lane & 31);       // the wave's first query; the lane's
     packed_rows rows;
     rows.k = (const uint16_t*)k.data + items.k_start[sequence] * k.row_stride + h / group * k.head_stride;
     rows.v = (const uint16_t*)v.data + items.k_start[sequence] * v.row_stride + h / group * v.head_stride;
     rows.k_stride = k.row_stride;
     rows.v_stride = v.row_stride;
-    const int64_t row = (int64_t)items.q_start[sequence] + i;
-    const int end = max(0, i + 1 + keys - queries);
-    float o[2], m, l;
-    attend_one<ACT>((const uint16_t*)q.data + row * q.row_stride + h * q.head_stride, rows, sees_first{end}, 0, end, D, factor, o, &m, &l);
-    store_one<ACT>(out + (row * q_heads + h) * D, o, l, D);
+    const int ahead = keys - queries;        // query i sees keys 0 .. i + ahead
+    const int tiles = (min(queries, (tile + 1) * ROWS) + ahead + KEYS - 1) / KEYS;      // of keys that the block's last query sees
+
+    // units of a head that no load fills are zeros from here on
+    if (D < SH::UNITS * 8) {
+        const u32x4 zero = {0, 0, 0, 0};
+        for (int x = threadIdx.x; x < SH::LDS / 16; x += 256) ((u32x4*)lds)[x] = zero;
+        __syncthreads();
+    }
+    // A thread loads unit (its place in LDS: lane % UNITS) of rows that lie 256 / UNITS apart, which move it alike.
+    constexpr int STEP = 256 / SH::UNITS;
+    const int row0 = threadIdx.x / SH::UNITS, place = threadIdx.x % SH::UNITS;
+    const int key_at = key_unit<SH::UNITS>(row0, place) * 8, value_at = value_unit<SH::UNITS>(row0, place) * 8;
+    auto load = [&](int t, int buffer) {
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + buffer * 2 * SH::BYTES) + wave * 1024;
+#pragma unroll
+        for (int j = 0; j < SH::LOADS; ++j) {
+            const int row = min(t * KEYS + row0 + j * STEP, keys - 1);
+            if (key_at < D) load_lds16(to + j * 4096, rows.key(row) + key_at);
+            if (value_at < D) load_lds16(to + SH::BYTES + j * 4096, rows.value(row) + value_at);
+        }
+    };
+    wave_state<ACT, DP> w;
+    w.clear();
+    if (tiles > 0) load(0, 0);
+    const int64_t row = (int64_t)items.q_start[sequence] + min(i, queries - 1);
+    const uint16_t* query = (const uint16_t*)q.data + row * q.row_stride + h * q.head_stride;
+    w.load_queries(query, D);
+    const int end = i + 1 + ahead;           // keys that the lane's query sees
+    for (int t = 0; t < tiles; ++t) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (t + 1 < tiles) load(t + 1, (t + 1) & 1);
+        const int base = t * KEYS;
+        if (first < queries && base < first + 32 + ahead) {
+            const int left = end - base - 4 * (lane >> 5);
+            const char* at = lds + (t & 1) * 2 * SH::BYTES;
+            w.tile(at, at + SH::BYTES, factor, base + KEYS > first + 1 + ahead, [&](int s, int x) { return 32 * s + 8 * (x >> 2) + (x & 3) < left; });
+        }
+    }
+    const float l = other_half_sum(w.l);
+    w.l = l;
+    if (!w.finite()) {
+        for (int x = 0; x < 32 && first + x < queries; ++x) {
+            const int64_t r = (int64_t)items.q_start[sequence] + first + x;
+            const int sees = max(0, first + x + 1 + ahead);
+            float o[2], m, sum;
+            attend_one<ACT>((const uint16_t*)q.data + r * q.row_stride + h * q.head_stride, rows, sees_first{sees}, 0, sees, D, factor, o, &m, &sum);
+            store_one<ACT>(out + (r * q_heads + h) * D, o, sum, D);
+        }
+    } else if (i < queries) {
+        w.store(out + (row * q_heads + h) * D, l == 0.0f ? 0.0f : 1.0f / l, D);
+    }
+}
+
+template <int ACT, int DP>
+int launch(const fq_prompt_args& a, const prompt_items& items, int total, hipStream_t stream) {
+    static std::atomic<uint64_t> raised{0};
+    constexpr int LDS = tile_shape<DP>::LDS;
+    if (LDS > 65536) {
+        const int st = fqd::raise_lds_limit((const void*)fq_attention_prompt_kernel<ACT, DP>, raised);
+        if (st != FQ_OK) return st;
+    }
+    fq_attention_prompt_kernel<ACT, DP><<<dim3((unsigned)(total * a.q_heads)), 256, LDS, stream>>>(
+        a.q, a.k, a.v, a.q_heads, a.q_heads / a.kv_heads, a.head_dim, a.scale * LOG2E, (uint16_t*)a.out, items);
+    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
+template <int ACT>
+int launch(const fq_prompt_args& a, const prompt_items& items, int total, hipStream_t stream) {
+    if (a.head_dim <= 64) return launch<ACT, 64>(a, items, total, stream);
+    if (a.head_dim <= 96) return launch<ACT, 96>(a, items, total, stream);
+    return launch<ACT, 128>(a, items, total, stream);
 }
 
 }  // namespace
@@ -87,14 +160,9 @@ int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* wor
             total += (s + 1) * (items.tiles[s] - (s + 1 < n ? items.tiles[s + 1] : 0));
         }
         if (total == 0) continue;
-        const dim3 grid((unsigned)total, (unsigned)a.q_heads);
-        const float factor = a.scale * LOG2E;
-        const int group = a.q_heads / a.kv_heads;
-        if (act_dtype == FQ_F16)
-            fq_attention_prompt_kernel<FQ_F16><<<grid, 64 * TILE, 0, stream>>>(a.q, a.k, a.v, a.q_heads, group, a.head_dim, factor, (uint16_t*)a.out, items);
-        else
-            fq_attention_prompt_kernel<FQ_BF16><<<grid, 64 * TILE, 0, stream>>>(a.q, a.k, a.v, a.q_heads, group, a.head_dim, factor, (uint16_t*)a.out, items);
-        if (hipGetLastError() != hipSuccess) return FQ_ERR_HIP;
+        if ((int64_t)total * a.q_heads >= 1 << 24) return FQ_ERR_UNSUPPORTED;      // (2^32 threads)
+        const int st = act_dtype == FQ_F16 ? launch<FQ_F16>(a, items, total, stream) : launch<FQ_BF16>(a, items, total, stream);
+        if (st != FQ_OK) return st;
     }
     return FQ_OK;
 }

@@ -1,0 +1,215 @@
+// Attention of 128 queries at a time on the matrix cores.
+//
+// A block is four waves of 32 queries; keys and values come through LDS in tiles of 64, the next tile's loads in flight while the
+// present one is multiplied.  Both products are computed transposed, with 32 x 32 x 16 products whose columns are the wave's
+// queries: S^T = K Q^T, then O^T = V^T P^T.  A lane then holds one query's scores (half of a tile's keys; lane + 32 the others), so
+// that the softmax's maximum and sum need one exchange between two lanes, and the numerators leave it in the order in which the
+// second product takes them: the sum over keys may be taken in any order, and V's transposed reads follow the one that S^T
+// comes in.  Neither scores nor numerators pass through LDS.
+//
+// Running maximum: numerators are taken relative to a maximum that is renewed only when a score exceeds it by 2^8 (times
+// factor), so that most tiles leave the sums alone.  The numerators are at most 2^8 then, which binary16 holds with the same relative error.
+//
+// What a query does not see has weight zero in the products, and zero times an infinity or a NaN is a NaN: a wave whose
+// results are not finite computes its queries again, one by one and seen keys alone (attend_one).
+#ifndef FQ_ATTN_TILE_H_
+#define FQ_ATTN_TILE_H_
+
+#include "fq_attn.h"
+
+namespace fqa {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int ACT>
+__device__ inline f32x16 mfma32(const u32x4& a, const u32x4& b, const f32x16& c) {
+    if constexpr (ACT == FQ_F16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// two values, rounded to nearest
+template <int ACT>
+__device__ inline uint32_t pack2(float a, float b) {
+    typedef typename type16<ACT>::t T;
+    typedef T vec2 __attribute__((ext_vector_type(2)));
+    f32x2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, vec2));
+}
+
+__device__ inline float other_half_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float other_half_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Direct load global -> LDS, 16 bytes per lane (lane l to base + 16 l; base wave-uniform).  Assembly, since the builtin's wait
+// handling would drain every load in flight; the waits are written out.  M0 needs a wait state behind its write.
+__device__ inline void load_lds16(uint32_t base, const void* src) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"(src) : "memory", "m0");
+}
+
+constexpr int KEYS = 64;             // per tile
+constexpr int ROWS = 128;            // queries per block
+
+// Where 16-byte unit `unit` of key row `row` lies in a tile: units are moved about within their row so that the lanes of a read
+// fall on different banks.  Keys are read 16 bytes a lane, 32 rows of one unit at a time; values eight rows x four units.
+template <int UNITS>
+__device__ constexpr int key_unit(int row, int unit) { return unit ^ (UNITS == 16 ? row & 15 : row >> 1 & 7); }
+template <int UNITS>
+__device__ constexpr int value_unit(int row, int unit) {
+    return unit ^ (UNITS == 16 ? (row & 3) * 4 + (row >> 2 & 3) : (row >> 1 & 1) * 4 + (row >> 2 & 3));
+}
+
+// DP: head_dim as the matrix cores take it, 64, 96 or 128 (the rest of a head is zeros)
+template <int DP>
+struct tile_shape {
+    static constexpr int UNITS = DP == 64 ? 8 : 16;           // 16-byte units of a row in LDS (96: four of them idle)
+    static constexpr int PITCH = UNITS * 16;                  // bytes
+    static constexpr int BYTES = KEYS * PITCH;                // of keys, or of values
+    static constexpr int LOADS = BYTES / 4096;                // 16-byte loads per thread for either
+    static constexpr int STEPS = DP / 16;                     // of the first product
+    static constexpr int TILES = DP / 32;                     // of the second
+    static constexpr int LDS = 4 * BYTES;                     // two buffers
+};
+
+// One wave's state: 32 queries (lane l: query l % 32; both halves of the wave hold the same)
+template <int ACT, int DP>
+struct wave_state {
+    typedef tile_shape<DP> SH;
+    u32x4 q[SH::STEPS];
+    f32x16 o[SH::TILES];
+    float m, c, l;       // maximum that the numerators are relative to (raw scores), the same times factor (0: none yet), this lane's sum
+
+    __device__ void clear() {
+#pragma unroll
+        for (int t = 0; t < SH::TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+        m = -__builtin_inff();
+        c = l = 0.0f;
+    }
+
+    // the lane's query row
+    __device__ void load_queries(const uint16_t* row, int D) {
+        const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int s = 0; s < SH::STEPS; ++s) {
+            const int unit = 2 * s + half;
+            const u32x4 zero = {0, 0, 0, 0};
+            q[s] = unit * 8 < D ? *(const u32x4*)(row + unit * 8) : zero;
+        }
+    }
+
+    // One tile of keys and values in LDS.  mask(s, i): whether the lane's query sees the key of score i of half-tile s.
+    template <typename MASK>
+    __device__ __forceinline__ void tile(const char* keys, const char* values, float factor, bool masked, const MASK& mask) {
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+        f32x16 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+        for (int step = 0; step < SH::STEPS; ++step)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int row = lane & 31;
+                const u32x4 k = *(const u32x4*)(keys + (t * 32 + row) * SH::PITCH + key_unit<SH::UNITS>(row, 2 * step + half) * 16);
+                s[t] = mfma32<ACT>(k, q[step], s[t]);
+            }
+        if (masked) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] = mask(t, i) ? s[t][i] : -__builtin_inff();
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) top = __builtin_fmaxf(top, s[i >> 4][i & 15]);
+        top = other_half_max(top);
+        if (__any(top * factor > m * factor + 8.0f)) {
+            const float now = __builtin_fmaxf(m, top), next = now == -__builtin_inff() ? 0.0f : now * factor;
+            const float again = __builtin_amdgcn_exp2f(m * factor - next);       // (0 where there was none)
+            m = now;
+            c = next;
+            l *= again;
+#pragma unroll
+            for (int t = 0; t < SH::TILES; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][i] *= again;
+        }
+        u32x4 p[4];
+        float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], factor, -c));
+                sum[i & 1] += s[t][i];
+            }
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) p[2 * t + i / 8][i / 2 % 4] = pack2<ACT>(s[t][i], s[t][i + 1]);
+        }
+        l += sum[0] + sum[1];
+        // V^T: lane l takes column l % 32 of the 32; a transposed read hands each lane four keys of its column, from four rows
+        // of which each lane of sixteen points at a quarter
+        const int row = 4 * half + (lane & 15) / 4, unit = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), in = (lane & 1) * 8;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int t = 0; t < SH::TILES; ++t) {
+                u32x4 v;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = row + 8 * e;
+                    const char* at = values + (16 * k + r) * SH::PITCH + value_unit<SH::UNITS>(r, 4 * t + unit) * 16 + in;
+                    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4*)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)at);
+                    const u32x2 y = __builtin_bit_cast(u32x2, x);
+                    v[2 * e] = y[0];
+                    v[2 * e + 1] = y[1];
+                }
+                o[t] = mfma32<ACT>(v, p[k], o[t]);
+            }
+    }
+
+    // whether every sum of the wave's queries is finite
+    __device__ bool finite() const {
+        float x = l * 0.0f;
+#pragma unroll
+        for (int t = 0; t < SH::TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[t][i], 0.0f, x);
+        return __all(x == 0.0f);
+    }
+
+    // The lane's half of its query's result, times r.
+    __device__ void store(uint16_t* row, float r, int D) const {
+        const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int t = 0; t < SH::TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int d = 32 * t + 2 * i + 4 * half;
+                u32x2 x;
+                x[0] = pack2<ACT>(o[t][i] * r, o[t][i + 1] * r);
+                x[1] = pack2<ACT>(o[t][i + 2] * r, o[t][i + 3] * r);
+                if (d < D) *(u32x2*)(row + d) = x;
+            }
+    }
+};
+
+}  // namespace fqa
+
+#endif  // FQ_ATTN_TILE_H_
