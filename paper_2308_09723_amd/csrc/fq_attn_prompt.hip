@@ -55,9 +55,10 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
     const int tiles = (min(queries, (tile + 1) * ROWS) + ahead + KEYS - 1) / KEYS;      // of keys that the block's last query sees
 
     // units of a head that no load fills are zeros from here on
+    constexpr int TILE_BYTES = 2 * SH::BYTES;      // of keys, or of values
     if (D < SH::UNITS * 8) {
         const u32x4 zero = {0, 0, 0, 0};
-        for (int x = threadIdx.x; x < SH::LDS / 16; x += 256) ((u32x4*)lds)[x] = zero;
+        for (int x = threadIdx.x; x < 4 * TILE_BYTES / 16; x += 256) ((u32x4*)lds)[x] = zero;
         __syncthreads();
     }
     // A thread loads unit (its place in LDS: lane % UNITS) of rows that lie 256 / UNITS apart, which move it alike.
@@ -65,20 +66,20 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
     const int row0 = threadIdx.x / SH::UNITS, place = threadIdx.x % SH::UNITS;
     const int key_at = key_unit<SH::UNITS>(row0, place) * 8, value_at = value_unit<SH::UNITS>(row0, place) * 8;
     auto load = [&](int t, int buffer) {
-        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + buffer * 2 * SH::BYTES) + wave * 1024;
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + buffer * 2 * TILE_BYTES) + wave * 1024;
 #pragma unroll
-        for (int j = 0; j < SH::LOADS; ++j) {
+        for (int j = 0; j < TILE_BYTES / 4096; ++j) {
             const int row = min(t * KEYS + row0 + j * STEP, keys - 1);
             if (key_at < D) load_lds16(to + j * 4096, rows.key(row) + key_at);
-            if (value_at < D) load_lds16(to + SH::BYTES + j * 4096, rows.value(row) + value_at);
+            if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, rows.value(row) + value_at);
         }
     };
-    wave_state<ACT, DP> w;
+    wave_state<ACT, DP, 1> w;
     w.clear();
     if (tiles > 0) load(0, 0);
     const int64_t row = (int64_t)items.q_start[sequence] + min(i, queries - 1);
     const uint16_t* query = (const uint16_t*)q.data + row * q.row_stride + h * q.head_stride;
-    w.load_queries(query, D);
+    w.load_queries(0, query, D);
     const int end = i + 1 + ahead;           // keys that the lane's query sees
     for (int t = 0; t < tiles; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -86,13 +87,19 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
         if (t + 1 < tiles) load(t + 1, (t + 1) & 1);
         const int base = t * KEYS;
         if (first < queries && base < first + 32 + ahead) {
-            const int left = end - base - 4 * (lane >> 5);
-            const char* at = lds + (t & 1) * 2 * SH::BYTES;
-            w.tile(at, at + SH::BYTES, factor, base + KEYS > first + 1 + ahead, [&](int s, int x) { return 32 * s + 8 * (x >> 2) + (x & 3) < left; });
+            const char* at = lds + (t & 1) * 2 * TILE_BYTES;
+            f32x16 s[1][2];
+            u32x4 p[1][4];
+            w.template scores<2>(at, s);
+            if (base + KEYS > first + 1 + ahead) {
+                keep_seen(s[0][0], low_bits(end - base));
+                keep_seen(s[0][1], low_bits(end - base - HALF));
+            }
+            w.template soften<2>(0, s[0], factor, p[0]);
+            w.template accumulate<2>(at + TILE_BYTES, p);
         }
     }
-    const float l = other_half_sum(w.l);
-    w.l = l;
+    const float l = w.l[0] = other_half_sum(w.l[0]);
     if (!w.finite()) {
         for (int x = 0; x < 32 && first + x < queries; ++x) {
             const int64_t r = (int64_t)items.q_start[sequence] + first + x;
@@ -102,14 +109,20 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
             store_one<ACT>(out + (r * q_heads + h) * D, o, sum, D);
         }
     } else if (i < queries) {
-        w.store(out + (row * q_heads + h) * D, l == 0.0f ? 0.0f : 1.0f / l, D);
+        const float r = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
+        uint16_t* to = out + (row * q_heads + h) * D;
+        w.quads([&](int d, int x, int t) {
+            const f32x16& o = w.o[0][t];
+            const u32x2 v = {pack2<ACT>(o[x] * r, o[x + 1] * r), pack2<ACT>(o[x + 2] * r, o[x + 3] * r)};
+            if (d < D) *(u32x2*)(to + d) = v;
+        });
     }
 }
 
 template <int ACT, int DP>
 int launch(const fq_prompt_args& a, const prompt_items& items, int total, hipStream_t stream) {
     static std::atomic<uint64_t> raised{0};
-    constexpr int LDS = tile_shape<DP>::LDS;
+    constexpr int LDS = 8 * tile_shape<DP>::BYTES;      // two tiles of keys and of values
     if (LDS > 65536) {
         const int st = fqd::raise_lds_limit((const void*)fq_attention_prompt_kernel<ACT, DP>, raised);
         if (st != FQ_OK) return st;

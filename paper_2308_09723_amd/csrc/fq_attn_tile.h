@@ -20,6 +20,7 @@
 namespace fqa {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -34,6 +35,15 @@ __device__ inline f32x16 mfma32(const u32x4& a, const u32x4& b, const f32x16& c)
     else
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
+
+// Values of the lane's keys that its query sees, bit 8 (i / 4) + 4 (lane / 32) + i % 4 for score i: the others become -infinity.
+__device__ __forceinline__ void keep_seen(f32x16& s, uint32_t seen) {
+    const uint32_t mine = seen >> ((threadIdx.x & 32) >> 3);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = mine >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -__builtin_inff();
+}
+// the lowest n bits (none below 0, all from 32 on)
+__device__ inline uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
 // two values, rounded to nearest
 template <int ACT>
@@ -59,8 +69,9 @@ __device__ inline void load_lds16(uint32_t base, const void* src) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"(src) : "memory", "m0");
 }
 
-constexpr int KEYS = 64;             // per tile
-constexpr int ROWS = 128;            // queries per block
+constexpr int HALF = 32;             // keys of half a tile: the first product's rows
+constexpr int KEYS = 2 * HALF;       // of a tile that a block shares
+constexpr int ROWS = 128;            // queries of a block that shares its tiles
 
 // Where 16-byte unit `unit` of key row `row` lies in a tile: units are moved about within their row so that the lanes of a read
 // fall on different banks.  Keys are read 16 bytes a lane, 32 rows of one unit at a time; values eight rows x four units.
@@ -76,97 +87,102 @@ template <int DP>
 struct tile_shape {
     static constexpr int UNITS = DP == 64 ? 8 : 16;           // 16-byte units of a row in LDS (96: four of them idle)
     static constexpr int PITCH = UNITS * 16;                  // bytes
-    static constexpr int BYTES = KEYS * PITCH;                // of keys, or of values
-    static constexpr int LOADS = BYTES / 4096;                // 16-byte loads per thread for either
+    static constexpr int BYTES = HALF * PITCH;                // of half a tile of keys, or of values
     static constexpr int STEPS = DP / 16;                     // of the first product
     static constexpr int TILES = DP / 32;                     // of the second
-    static constexpr int LDS = 4 * BYTES;                     // two buffers
 };
 
-// One wave's state: 32 queries (lane l: query l % 32; both halves of the wave hold the same)
-template <int ACT, int DP>
+// One wave's state: RG groups of 32 queries (lane l: query l % 32 of each; the wave's halves hold the same queries)
+template <int ACT, int DP, int RG>
 struct wave_state {
     typedef tile_shape<DP> SH;
-    u32x4 q[SH::STEPS];
-    f32x16 o[SH::TILES];
-    float m, c, l;       // maximum that the numerators are relative to (raw scores), the same times factor (0: none yet), this lane's sum
+    u32x4 q[RG][SH::STEPS];
+    f32x16 o[RG][SH::TILES];
+    float m[RG], c[RG], l[RG];   // maximum that the numerators are relative to (raw scores), the same times factor (0: none yet), this lane's sum
 
-    __device__ void clear() {
+    __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int t = 0; t < SH::TILES; ++t)
+        for (int g = 0; g < RG; ++g) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
-        m = -__builtin_inff();
-        c = l = 0.0f;
+            for (int t = 0; t < SH::TILES; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[g][t][i] = 0.0f;
+            m[g] = -__builtin_inff();
+            c[g] = l[g] = 0.0f;
+        }
     }
 
-    // the lane's query row
-    __device__ void load_queries(const uint16_t* row, int D) {
+    // the lane's query of group g
+    __device__ __forceinline__ void load_queries(int g, const uint16_t* row, int D) {
         const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
         for (int s = 0; s < SH::STEPS; ++s) {
             const int unit = 2 * s + half;
             const u32x4 zero = {0, 0, 0, 0};
-            q[s] = unit * 8 < D ? *(const u32x4*)(row + unit * 8) : zero;
+            q[g][s] = unit * 8 < D ? *(const u32x4*)(row + unit * 8) : zero;
         }
     }
 
-    // One tile of keys and values in LDS.  mask(s, i): whether the lane's query sees the key of score i of half-tile s.
-    template <typename MASK>
-    __device__ __forceinline__ void tile(const char* keys, const char* values, float factor, bool masked, const MASK& mask) {
-        const int lane = threadIdx.x & 63, half = lane >> 5;
-        f32x16 s[2];
+    // S^T of H half-tiles of keys in LDS.  Score i of half-tile t belongs to key 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4.
+    template <int H>
+    __device__ __forceinline__ void scores(const char* keys, f32x16 (&s)[RG][H]) const {
+        const int lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int g = 0; g < RG; ++g)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+            for (int t = 0; t < H; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[g][t][i] = 0.0f;
 #pragma unroll
         for (int step = 0; step < SH::STEPS; ++step)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int row = lane & 31;
-                const u32x4 k = *(const u32x4*)(keys + (t * 32 + row) * SH::PITCH + key_unit<SH::UNITS>(row, 2 * step + half) * 16);
-                s[t] = mfma32<ACT>(k, q[step], s[t]);
+            for (int t = 0; t < H; ++t) {
+                const u32x4 k = *(const u32x4*)(keys + t * SH::BYTES + row * SH::PITCH + key_unit<SH::UNITS>(row, 2 * step + half) * 16);
+#pragma unroll
+                for (int g = 0; g < RG; ++g) s[g][t] = mfma32<ACT>(k, q[g][step], s[g][t]);
             }
-        if (masked) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[t][i] = mask(t, i) ? s[t][i] : -__builtin_inff();
-        }
+    }
+
+    // Numerators of group g's scores, in the order that accumulate() takes; maximum, sum and results brought along.
+    template <int H>
+    __device__ __forceinline__ void soften(int g, f32x16 (&s)[H], float factor, u32x4 (&p)[2 * H]) {
         float top = s[0][0];
 #pragma unroll
-        for (int i = 1; i < 32; ++i) top = __builtin_fmaxf(top, s[i >> 4][i & 15]);
+        for (int i = 1; i < 16 * H; ++i) top = __builtin_fmaxf(top, s[i >> 4][i & 15]);
         top = other_half_max(top);
-        if (__any(top * factor > m * factor + 8.0f)) {
-            const float now = __builtin_fmaxf(m, top), next = now == -__builtin_inff() ? 0.0f : now * factor;
-            const float again = __builtin_amdgcn_exp2f(m * factor - next);       // (0 where there was none)
-            m = now;
-            c = next;
-            l *= again;
+        if (__any(top * factor > m[g] * factor + 8.0f)) {
+            const float now = __builtin_fmaxf(m[g], top), next = now == -__builtin_inff() ? 0.0f : now * factor;
+            const float again = __builtin_amdgcn_exp2f(m[g] * factor - next);       // (0 where there was none)
+            m[g] = now;
+            c[g] = next;
+            l[g] *= again;
 #pragma unroll
             for (int t = 0; t < SH::TILES; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][i] *= again;
+                for (int i = 0; i < 16; ++i) o[g][t][i] *= again;
         }
-        u32x4 p[4];
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < H; ++t) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], factor, -c));
+                s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], factor, -c[g]));
                 sum[i & 1] += s[t][i];
             }
 #pragma unroll
             for (int i = 0; i < 16; i += 2) p[2 * t + i / 8][i / 2 % 4] = pack2<ACT>(s[t][i], s[t][i + 1]);
         }
-        l += sum[0] + sum[1];
-        // V^T: lane l takes column l % 32 of the 32; a transposed read hands each lane four keys of its column, from four rows
-        // of which each lane of sixteen points at a quarter
-        const int row = 4 * half + (lane & 15) / 4, unit = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), in = (lane & 1) * 8;
+        l[g] += sum[0] + sum[1];
+    }
+
+    // O^T += V^T P^T over H half-tiles of values in LDS.  V^T: lane l takes column l % 32 of 32; a transposed read hands each lane
+    // four keys of its column, out of four rows of which each lane of sixteen points at a quarter.
+    template <int H>
+    __device__ __forceinline__ void accumulate(const char* values, const u32x4 (&p)[RG][2 * H]) {
+        const int lane = threadIdx.x & 63;
+        const int row = 4 * (lane >> 5) + (lane & 15) / 4, unit = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), in = (lane & 1) * 8;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 2 * H; ++k)
 #pragma unroll
             for (int t = 0; t < SH::TILES; ++t) {
                 u32x4 v;
@@ -180,33 +196,33 @@ struct wave_state {
                     v[2 * e] = y[0];
                     v[2 * e + 1] = y[1];
                 }
-                o[t] = mfma32<ACT>(v, p[k], o[t]);
+#pragma unroll
+                for (int g = 0; g < RG; ++g) o[g][t] = mfma32<ACT>(v, p[g][k], o[g][t]);
             }
     }
 
     // whether every sum of the wave's queries is finite
-    __device__ bool finite() const {
-        float x = l * 0.0f;
+    __device__ __forceinline__ bool finite() const {
+        float x = 0.0f;
 #pragma unroll
-        for (int t = 0; t < SH::TILES; ++t)
+        for (int g = 0; g < RG; ++g) {
+            x = __builtin_fmaf(l[g], 0.0f, x);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[t][i], 0.0f, x);
+            for (int t = 0; t < SH::TILES; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[g][t][i], 0.0f, x);
+        }
         return __all(x == 0.0f);
     }
 
-    // The lane's half of its query's result, times r.
-    __device__ void store(uint16_t* row, float r, int D) const {
+    // f(d, i, t): the lane's results i .. i + 3 of block t are values d .. d + 3 of its query
+    template <typename F>
+    __device__ __forceinline__ static void quads(F f) {
         const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
         for (int t = 0; t < SH::TILES; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int d = 32 * t + 2 * i + 4 * half;
-                u32x2 x;
-                x[0] = pack2<ACT>(o[t][i] * r, o[t][i + 1] * r);
-                x[1] = pack2<ACT>(o[t][i + 2] * r, o[t][i + 3] * r);
-                if (d < D) *(u32x2*)(row + d) = x;
-            }
+            for (int i = 0; i < 16; i += 4) f(32 * t + 2 * i + 4 * half, i, t);
     }
 };
 

@@ -1,55 +1,562 @@
 // Attention of drafted tokens over the pages of a cache (fq_attention_tree).
+//
+// The rows that share a key head's keys are the sequence's nodes times the query heads of the group: one token of four heads a group
+// is four rows, 48 nodes are 192.  Up to 64 rows the call is bound by the cache's bytes (fq_attention_tree_stream_kernel: every wave
+// brings its own keys in), above by the products (fq_attention_tree_tile_kernel: 128 rows a block, four waves on the same keys).
+//
+// Work is dealt out evenly whatever the sequences' lengths are: all sequences' key tiles, key head by key head, make one line, and
+// each block takes an equal piece of it, cut where it likes.  Lengths are read on the device, so each block finds its own place (a
+// scan over the lengths by each wave).  Where a unit (a sequence's rows of one key head) is cut, the pieces leave their sums,
+// not divided, and the maxima they are relative to in the workspace, and a second kernel joins them.
 #include <hip/hip_runtime.h>
+#include <atomic>
 
-#include "fq_attn.h"
+#include "fq_attn_tile.h"
+#include "fq_lds_limit.h"
 
 namespace {
 
 using namespace fqa;
 
-template <int ACT>
-__global__ __launch_bounds__(256) void fq_attention_tree_kernel(fq_tree_args a, float factor) {
-    const int64_t pair = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);      // a node and a query head
-    if (pair >= a.sequences * a.nodes * a.q_heads) return;
-    const int64_t row = pair / a.q_heads;
-    const int h = (int)(pair - row * a.q_heads);
-    const int b = (int)(row / a.nodes), i = (int)(row - (int64_t)b * a.nodes);
-    const int hk = h / (a.q_heads / a.kv_heads);
-    paged_rows rows;
-    rows.k = (const uint16_t*)a.cache.k + hk * a.cache.head_stride;
-    rows.v = (const uint16_t*)a.cache.v + hk * a.cache.head_stride;
-    rows.page_stride = a.cache.page_stride;
-    rows.token_stride = a.cache.token_stride;
-    rows.table = a.page_table + b * a.table_width;
-    rows.page_size = (uint32_t)a.cache.page_size;
-    rows.last_page = (uint32_t)(a.cache.pages - 1);
-    const int capacity = (int)a.table_width * a.cache.page_size, context = a.context_lens[b];
-    const int end = context < 0 ? 0 : (int)min((int64_t)capacity, (int64_t)context + a.nodes);
-    const uint16_t* q = (const uint16_t*)a.q.data + row * a.q.row_stride + h * a.q.head_stride;
-    float o[2], m, l;
-    if (a.mask) {
-        const sees_tree sees{context, a.nodes, a.mask + b * a.mask_stride + (int64_t)i * ((a.nodes + 63) / 64)};
-        attend_one<ACT>(q, rows, sees, 0, end, a.head_dim, factor, o, &m, &l);
-    } else {
-        const int64_t last = (int64_t)context + i + 1;
-        const sees_first sees{(int)min((int64_t)end, last)};
-        attend_one<ACT>(q, rows, sees, 0, context < 0 ? 0 : sees.end, a.head_dim, factor, o, &m, &l);
+constexpr int TABLE = 1024;          // entries of the page table that a block has in LDS
+
+// What the host has made of a call.
+struct tree_plan {
+    int group, rows;                 // query heads per key head; rows of a key head
+    int row_tiles, unit_rows;        // units of unit_rows rows that they are cut into
+    int tile;                        // keys of a tile
+    int blocks;                      // at most
+    int slot_rows;                   // rows of a slot of the workspace
+    float factor;
+    float* slots;                    // two per block: [slot_rows][head_dim] sums, [slot_rows] maxima (log2), [slot_rows] sums of numerators
+};
+
+__device__ inline int64_t slot_floats(const tree_plan& p, int D) { return (int64_t)p.slot_rows * (D + 2); }
+
+__device__ inline int keys_of(const fq_tree_args& a, int context) {
+    return context < 0 ? 0 : (int)min(a.table_width * a.cache.page_size, (int64_t)context + a.nodes);
+}
+__device__ inline int tiles_of(const fq_tree_args& a, const tree_plan& p, int b) {      // (one without keys: its zeros are somebody's)
+    return max(1, (keys_of(a, a.context_lens[b]) + p.tile - 1) / p.tile);
+}
+
+__device__ inline int64_t wave_sum64(int64_t x) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+
+// The line of tiles: sequence by sequence, in it unit by unit.
+struct line {
+    int64_t per_block;               // tiles
+    int64_t total;
+    int units;                       // of a sequence
+
+    __device__ line(const fq_tree_args& a, const tree_plan& p) {
+        units = a.kv_heads * p.row_tiles;
+        int64_t sum = 0;
+        for (int b = threadIdx.x & 63; b < a.sequences; b += 64) sum += tiles_of(a, p, b);
+        total = wave_sum64(sum) * units;
+        per_block = (total + p.blocks - 1) / p.blocks;
     }
-    store_one<ACT>((uint16_t*)a.out + (row * a.q_heads + h) * a.head_dim, o, l, a.head_dim);
+    // the sequence whose tiles the line has at `at`, and where they begin
+    __device__ void find(const fq_tree_args& a, const tree_plan& p, int64_t at, int* sequence, int64_t* begin) const {
+        const int lane = threadIdx.x & 63;
+        const int64_t target = at / units;        // in tiles of one unit
+        int64_t before = 0;
+        for (int first = 0;; first += 64) {
+            const int b = first + lane, n = b < a.sequences ? tiles_of(a, p, b) : 0;
+            int64_t upto = n;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int64_t x = __shfl_up(upto, d);
+                if (lane >= d) upto += x;
+            }
+            const int64_t all = __shfl(upto, 63);
+            if (target < before + all || first + 64 >= a.sequences) {
+                const int k = min(63, __builtin_popcountll(__ballot(before + upto <= target)));
+                *sequence = __builtin_amdgcn_readfirstlane(min(first + k, (int)a.sequences - 1));
+                *begin = (before + __shfl(upto - n, k)) * units;
+                return;
+            }
+            before += all;
+        }
+    }
+};
+
+// Rows of a unit: where a row's query lies, where its result goes, and what it sees.
+struct unit_rows {
+    const fq_tree_args& a;
+    const tree_plan& p;
+    int b, head, first, count;       // sequence; key head; first row, rows
+    int context, keys;
+
+    __device__ unit_rows(const fq_tree_args& a, const tree_plan& p, int b, int u) : a(a), p(p), b(b) {
+        head = u / p.row_tiles;
+        first = (u - head * p.row_tiles) * p.unit_rows;
+        count = min(p.unit_rows, p.rows - first);
+        context = __builtin_amdgcn_readfirstlane(a.context_lens[b]);
+        keys = keys_of(a, context);
+    }
+    __device__ const uint16_t* query(int r) const {
+        const int node = (first + r) / p.group, h = head * p.group + (first + r) - node * p.group;
+        return (const uint16_t*)a.q.data + ((int64_t)b * a.nodes + node) * a.q.row_stride + h * a.q.head_stride;
+    }
+    __device__ uint16_t* result(int r) const {
+        const int node = (first + r) / p.group, h = head * p.group + (first + r) - node * p.group;
+        return (uint16_t*)a.out + (((int64_t)b * a.nodes + node) * a.q_heads + h) * a.head_dim;
+    }
+    __device__ paged_rows pages() const {
+        paged_rows x;
+        x.k = (const uint16_t*)a.cache.k + head * a.cache.head_stride;
+        x.v = (const uint16_t*)a.cache.v + head * a.cache.head_stride;
+        x.page_stride = a.cache.page_stride;
+        x.token_stride = a.cache.token_stride;
+        x.table = a.page_table + b * a.table_width;
+        x.page_size = (uint32_t)a.cache.page_size;
+        x.last_page = (uint32_t)(a.cache.pages - 1);
+        return x;
+    }
+    __device__ const uint64_t* words(int r) const {
+        return a.mask + b * a.mask_stride + (int64_t)((first + r) / p.group) * ((a.nodes + 63) / 64);
+    }
+    // which of keys base .. base + 31 row r sees
+    __device__ uint32_t seen(int r, int base) const {
+        uint32_t bits = low_bits(keys - base);
+        const int d = base - context;          // the drafted token that bit 0 stands for
+        if (d <= -32) return bits;
+        if (!a.mask) return bits & low_bits((first + r) / p.group + 1 - d);
+        const uint64_t* w = words(r);
+        const int n = max(0, d), last = (a.nodes + 63) / 64 - 1;
+        uint32_t drafted = 0;
+        if (n < a.nodes) {
+            const int at = n >> 6, by = n & 63;
+            uint64_t x = w[at] >> by;
+            if (by > 32 && at < last) x |= w[at + 1] << (64 - by);
+            drafted = (uint32_t)x & low_bits(a.nodes - n);
+        }
+        return bits & (d < 0 ? low_bits(-d) | drafted << -d : drafted);
+    }
+    // row r over keys begin .. end - 1 by one wave, seen keys alone
+    template <int ACT>
+    __device__ void one(int r, int begin, int end, float* o, float* c, float* l) const {
+        if (a.mask) {
+            attend_one<ACT>(query(r), pages(), sees_tree{context, a.nodes, words(r)}, begin, end, a.head_dim, p.factor, o, c, l);
+        } else {
+            const int last = (int)min((int64_t)end, (int64_t)context + (first + r) / p.group + 1);
+            attend_one<ACT>(query(r), pages(), sees_first{last}, begin, min(end, last), a.head_dim, p.factor, o, c, l);
+        }
+    }
+    // the whole piece in that way, rows dealt to the block's waves
+    template <int ACT>
+    __device__ void one_by_one(int begin, int end, float* slot) const {
+        const int lane = threadIdx.x & 63;
+        for (int r = threadIdx.x >> 6; r < count; r += 4) {
+            float o[2], c, l;
+            one<ACT>(r, begin, end, o, &c, &l);
+            if (!slot) {
+                store_one<ACT>(result(r), o, l, a.head_dim);
+            } else {
+                if (2 * lane < a.head_dim) slot[r * a.head_dim + 2 * lane] = o[0], slot[r * a.head_dim + 2 * lane + 1] = o[1];
+                if (lane == 0) slot[p.slot_rows * a.head_dim + r] = c, slot[p.slot_rows * (a.head_dim + 1) + r] = l;
+            }
+        }
+    }
+};
+
+// Keys n0 * page_size and on of a piece: the page table's entries in LDS, and where a key lies.
+struct table_part {
+    const int32_t* entries;          // LDS
+    uint32_t first, page_size;
+    int shift;                       // page_size = 1 << shift, or -1
+    int64_t page_stride, token_stride;
+    __device__ int64_t place(int j) const {
+        const uint32_t n = shift >= 0 ? (uint32_t)j >> shift : (uint32_t)j / page_size;
+        return entries[n - first] * page_stride + (int64_t)((uint32_t)j - n * page_size) * token_stride;
+    }
+};
+
+// Brings in the entries of keys begin .. end - 1 (few enough, table_keys()); the caller waits.
+__device__ inline table_part load_table(const fq_tree_args& a, const unit_rows& u, int begin, int end, int32_t* entries) {
+    table_part t;
+    t.entries = entries;
+    t.page_size = (uint32_t)a.cache.page_size;
+    t.shift = (a.cache.page_size & (a.cache.page_size - 1)) == 0 ? __builtin_ctz(a.cache.page_size) : -1;
+    t.first = (uint32_t)begin / t.page_size;
+    t.page_stride = a.cache.page_stride;
+    t.token_stride = a.cache.token_stride;
+    const int count = (int)((uint32_t)(end - 1) / t.page_size - t.first) + 1;
+    const int32_t* row = a.page_table + u.b * a.table_width + t.first;
+    for (int i = threadIdx.x; i < count; i += 256) {
+        const int32_t page = row[i];
+        entries[i] = page < 0 ? 0 : (int32_t)min((uint32_t)page, (uint32_t)(a.cache.pages - 1));
+    }
+    return t;
+}
+// How many keys' entries fit, in whole tiles
+__device__ inline int table_keys(const fq_tree_args& a, int tile) {
+    return (int)min((int64_t)1 << 30, (int64_t)(TABLE - 1) * a.cache.page_size) / tile * tile;
+}
+
+// ------------------------------------------------------------------------------------------ up to 64 rows
+// A block's four waves take 32 keys each of a tile of 128, every one its own: keys and values of a wave lie in 2 x 32 rows of LDS
+// that no other wave touches, and the next keys are on their way while the present ones are used, values likewise, without a
+// barrier.  Two blocks of 64 KiB fill a compute unit.  At the end of a piece the waves' sums are joined through LDS.
+template <int ACT, int DP, int RG>
+__global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tree_args a, tree_plan p) {
+    typedef tile_shape<DP> SH;
+    constexpr int LOADS = SH::BYTES / 1024;             // 16-byte loads per lane for 32 rows
+    constexpr int STEP = 64 / SH::UNITS;                // rows per load
+    constexpr int JOIN = 32 * DP * 4;                   // bytes of 32 rows of sums
+    constexpr int WAVE_BYTES = 2 * SH::BYTES > JOIN ? 2 * SH::BYTES : JOIN;
+    extern __shared__ __align__(16) char lds[];
+    int32_t* entries = (int32_t*)(lds + 4 * WAVE_BYTES);
+    float* stats = (float*)(entries + TABLE);           // [4][32][2], and a flag
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int D = a.head_dim;
+    char* mine = lds + wave * WAVE_BYTES;
+    const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+    const int row0 = lane / SH::UNITS, spot = lane % SH::UNITS;
+
+    const line all(a, p);
+    const int64_t begin = blockIdx.x * all.per_block, stop = min(all.total, begin + all.per_block);
+    if (begin >= stop) return;
+    int b;
+    int64_t at_b;
+    all.find(a, p, begin, &b, &at_b);
+    int tiles = tiles_of(a, p, b);
+    int u = (int)((begin - at_b) / tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
+    wave_state<ACT, DP, RG> w;
+
+    for (int64_t pos = begin; pos < stop;) {
+        const unit_rows rows(a, p, b, u);
+        const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slots + (2 * (int64_t)blockIdx.x + (pos != begin)) * slot_floats(p, D);
+        const int key0 = t0 * 128, key1 = min(rows.keys, t1 * 128);
+#pragma unroll
+        for (int g = 0; g < RG; ++g) w.load_queries(g, rows.query(min(32 * g + (lane & 31), rows.count - 1)), D);
+        w.clear();
+        const int most = table_keys(a, 128);
+        for (int part = key0; part < key1; part += most) {
+            const int part_end = min(key1, part + most);
+            __syncthreads();                            // (entries and sums of the piece before are read)
+            const table_part table = load_table(a, rows, part, part_end, entries);
+            if (D < SH::UNITS * 8) {                    // units that no load fills: zeros
+                const u32x4 zero = {0, 0, 0, 0};
+                for (int x = lane; x < 2 * SH::BYTES / 16; x += 64) ((u32x4*)mine)[x] = zero;
+            }
+            __syncthreads();
+            const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
+            auto load = [&](const uint16_t* from, int base, uint32_t to, bool values) {
+#pragma unroll
+                for (int j = 0; j < LOADS; ++j) {
+                    const int row = row0 + j * STEP;
+                    const int unit = values ? value_unit<SH::UNITS>(row, spot) : key_unit<SH::UNITS>(row, spot);
+                    const uint16_t* src = from + table.place(min(base + row, part_end - 1)) + unit * 8;
+                    if (unit * 8 < D) load_lds16(to + j * 1024, src);
+                }
+            };
+            int base = part + wave * 32;
+            if (base < part_end) {
+                load(k, base, mine_at, false);
+                load(v, base, mine_at + SH::BYTES, true);
+            }
+            for (; base < part_end; base += 128) {
+                const bool more = base + 128 < part_end;
+                f32x16 s[RG][1];
+                u32x4 x[RG][2];
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");       // keys are here
+                w.template scores<1>(mine, s);
+                if (more) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    load(k, base + 128, mine_at, false);
+                }
+                const bool masked = base + 32 > min(rows.context, part_end);
+#pragma unroll
+                for (int g = 0; g < RG; ++g) {
+                    if (masked) keep_seen(s[g][0], rows.seen(min(32 * g + (lane & 31), rows.count - 1), base));
+                    w.template soften<1>(g, s[g], p.factor, x[g]);
+                }
+                if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");       // values are here
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                w.template accumulate<1>(mine + SH::BYTES, x);
+                if (more) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    load(v, base + 128, mine_at + SH::BYTES, true);
+                }
+            }
+        }
+        // join the waves' sums
+#pragma unroll
+        for (int g = 0; g < RG; ++g) w.l[g] = other_half_sum(w.l[g]);
+        __syncthreads();
+        if (threadIdx.x == 0) stats[256] = 0.0f;
+        __syncthreads();
+        if (!w.finite() && lane == 0) stats[256] = 1.0f;
+        __syncthreads();
+        const bool again = stats[256] != 0.0f;
+        if (again) {
+            rows.one_by_one<ACT>(key0, key1, slot);
+        } else {
+#pragma unroll
+            for (int g = 0; g < RG; ++g) {
+                if (32 * g >= rows.count) break;
+                if (lane < 32) {
+                    stats[(wave * 32 + lane) * 2] = w.m[g] == -__builtin_inff() ? -__builtin_inff() : w.c[g];
+                    stats[(wave * 32 + lane) * 2 + 1] = w.l[g];
+                }
+                float* sums = (float*)mine;
+                w.quads([&](int d, int i, int t) {
+                    const f32x16& o = w.o[g][t];
+                    const f32x4 x = {o[i], o[i + 1], o[i + 2], o[i + 3]};
+                    const int r = lane & 31;
+                    *(f32x4*)(sums + r * DP + ((d / 4) ^ (r & (DP / 4 == 24 ? 7 : 15))) * 4) = x;
+                });
+                __syncthreads();
+                for (int x = threadIdx.x; x < 32 * DP / 4; x += 256) {
+                    const int r = x / (DP / 4), d = x % (DP / 4) * 4;
+                    if (32 * g + r >= rows.count || d >= D) continue;
+                    float c = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) c = __builtin_fmaxf(c, stats[(y * 32 + r) * 2]);
+                    const float from = c == -__builtin_inff() ? 0.0f : c;
+                    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const float weight = __builtin_amdgcn_exp2f(stats[(y * 32 + r) * 2] - from);
+                        const f32x4 z = *(const f32x4*)((const float*)(lds + y * WAVE_BYTES) + r * DP + ((d / 4) ^ (r & (DP / 4 == 24 ? 7 : 15))) * 4);
+                        l += weight * stats[(y * 32 + r) * 2 + 1];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
+                    }
+                    if (!slot) {
+                        const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+                        const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+                        *(u32x2*)(rows.result(32 * g + r) + d) = z;
+                    } else {
+                        const int at = 32 * g + r;
+                        *(f32x4*)(slot + at * D + d) = o;
+                        if (d == 0) slot[p.slot_rows * D + at] = c, slot[p.slot_rows * (D + 1) + at] = l;
+                    }
+                }
+                __syncthreads();
+            }
+        }
+        pos += t1 - t0;
+        t0 = 0;
+        if (++u == all.units) {
+            u = 0;
+            if (++b < a.sequences) tiles = tiles_of(a, p, b);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ above 64 rows
+// 128 rows a block, 32 to a wave; tiles of 64 keys that all four waves read, two of them in LDS, as for prompts.
+template <int ACT, int DP>
+__global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_args a, tree_plan p) {
+    typedef tile_shape<DP> SH;
+    constexpr int TILE_BYTES = 2 * SH::BYTES;
+    constexpr int STEP = 256 / SH::UNITS;
+    extern __shared__ __align__(16) char lds[];
+    int32_t* entries = (int32_t*)(lds + 4 * TILE_BYTES);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int D = a.head_dim;
+    const int row0 = threadIdx.x / SH::UNITS, spot = threadIdx.x % SH::UNITS;
+    const int key_at = key_unit<SH::UNITS>(row0, spot) * 8, value_at = value_unit<SH::UNITS>(row0, spot) * 8;
+
+    const line all(a, p);
+    const int64_t begin = blockIdx.x * all.per_block, stop = min(all.total, begin + all.per_block);
+    if (begin >= stop) return;
+    int b;
+    int64_t at_b;
+    all.find(a, p, begin, &b, &at_b);
+    int tiles = tiles_of(a, p, b);
+    int u = (int)((begin - at_b) / tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
+    wave_state<ACT, DP, 1> w;
+    if (D < SH::UNITS * 8) {
+        const u32x4 zero = {0, 0, 0, 0};
+        for (int x = threadIdx.x; x < 4 * TILE_BYTES / 16; x += 256) ((u32x4*)lds)[x] = zero;
+    }
+
+    for (int64_t pos = begin; pos < stop;) {
+        const unit_rows rows(a, p, b, u);
+        const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slots + (2 * (int64_t)blockIdx.x + (pos != begin)) * slot_floats(p, D);
+        const int key0 = t0 * KEYS, key1 = min(rows.keys, t1 * KEYS);
+        const int r = wave * 32 + (lane & 31), row = min(r, rows.count - 1);
+        const bool busy = wave * 32 < rows.count;
+        w.load_queries(0, rows.query(row), D);
+        w.clear();
+        const int most = table_keys(a, KEYS);
+        for (int part = key0; part < key1; part += most) {
+            const int part_end = min(key1, part + most);
+            __syncthreads();
+            const table_part table = load_table(a, rows, part, part_end, entries);
+            __syncthreads();
+            const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
+            auto load = [&](int base, int buffer) {
+                const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + buffer * 2 * TILE_BYTES) + wave * 1024;
+#pragma unroll
+                for (int j = 0; j < TILE_BYTES / 4096; ++j) {
+                    const int64_t place = table.place(min(base + row0 + j * STEP, part_end - 1));
+                    if (key_at < D) load_lds16(to + j * 4096, k + place + key_at);
+                    if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, v + place + value_at);
+                }
+            };
+            load(part, 0);
+            for (int base = part, buffer = 0; base < part_end; base += KEYS, buffer ^= 1) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                if (base + KEYS < part_end) load(base + KEYS, buffer ^ 1);
+                if (!busy) continue;
+                const char* at = lds + buffer * 2 * TILE_BYTES;
+                f32x16 s[1][2];
+                u32x4 x[1][4];
+                w.template scores<2>(at, s);
+                if (base + KEYS > min(rows.context, part_end)) {
+                    keep_seen(s[0][0], rows.seen(row, base));
+                    keep_seen(s[0][1], rows.seen(row, base + HALF));
+                }
+                w.template soften<2>(0, s[0], p.factor, x[0]);
+                w.template accumulate<2>(at + TILE_BYTES, x);
+            }
+        }
+        const float l = w.l[0] = other_half_sum(w.l[0]);
+        if (!w.finite()) {
+            for (int i = wave * 32; i < min(wave * 32 + 32, rows.count); ++i) {
+                float o[2], c, sum;
+                rows.one<ACT>(i, key0, key1, o, &c, &sum);
+                if (!slot) {
+                    store_one<ACT>(rows.result(i), o, sum, D);
+                } else {
+                    if (2 * lane < D) slot[i * D + 2 * lane] = o[0], slot[i * D + 2 * lane + 1] = o[1];
+                    if (lane == 0) slot[p.slot_rows * D + i] = c, slot[p.slot_rows * (D + 1) + i] = sum;
+                }
+            }
+        } else if (r < rows.count) {
+            const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+            uint16_t* to = rows.result(r);
+            w.quads([&](int d, int i, int t) {
+                const f32x16& o = w.o[0][t];
+                if (d >= D) return;
+                if (!slot) {
+                    const u32x2 z = {pack2<ACT>(o[i] * scale, o[i + 1] * scale), pack2<ACT>(o[i + 2] * scale, o[i + 3] * scale)};
+                    *(u32x2*)(to + d) = z;
+                } else {
+                    const f32x4 z = {o[i], o[i + 1], o[i + 2], o[i + 3]};
+                    *(f32x4*)(slot + r * D + d) = z;
+                }
+            });
+            if (slot && lane < 32) {
+                slot[p.slot_rows * D + r] = w.m[0] == -__builtin_inff() ? -__builtin_inff() : w.c[0];
+                slot[p.slot_rows * (D + 1) + r] = l;
+            }
+        }
+        pos += t1 - t0;
+        t0 = 0;
+        if (++u == all.units) {
+            u = 0;
+            if (++b < a.sequences) tiles = tiles_of(a, p, b);
+        }
+    }
+}
+
+// Joins the pieces of a unit that was cut: one block per unit, piece after piece in the line's order.
+template <int ACT>
+__global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_args a, tree_plan p) {
+    const line all(a, p);
+    const int b = (int)(blockIdx.x / all.units), u = (int)(blockIdx.x - (int64_t)b * all.units);
+    int64_t before = 0;
+    for (int x = threadIdx.x & 63; x < b; x += 64) before += tiles_of(a, p, x);
+    const int tiles = tiles_of(a, p, b);
+    const int64_t begin = wave_sum64(before) * all.units + (int64_t)u * tiles, end = begin + tiles;
+    const int64_t from = begin / all.per_block, to = (end - 1) / all.per_block;        // blocks that have pieces of it
+    if (from == to) return;
+    const unit_rows rows(a, p, b, u);
+    const int D = a.head_dim, quads = D / 4;
+    const int64_t size = slot_floats(p, D);
+    const bool whole = begin == from * all.per_block;        // (the first block's first piece, or its last)
+    for (int x = threadIdx.x; x < rows.count * quads; x += 256) {
+        const int r = x / quads, d = (x - r * quads) * 4;
+        float c = -__builtin_inff();
+        for (int64_t y = from; y <= to; ++y) c = __builtin_fmaxf(c, p.slots[(2 * y + (y == from && !whole)) * size + p.slot_rows * D + r]);
+        const float base = c == -__builtin_inff() ? 0.0f : c;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        float l = 0.0f;
+        for (int64_t y = from; y <= to; ++y) {
+            const float* slot = p.slots + (2 * y + (y == from && !whole)) * size;
+            const float weight = __builtin_amdgcn_exp2f(slot[p.slot_rows * D + r] - base);
+            const f32x4 z = *(const f32x4*)(slot + r * D + d);
+            l += weight * slot[p.slot_rows * (D + 1) + r];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
+        }
+        const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+        const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+        *(u32x2*)(rows.result(r) + d) = z;
+    }
+}
+
+tree_plan plan_tree(const fq_tree_args& a) {
+    tree_plan p = {};
+    p.group = a.q_heads / a.kv_heads;
+    p.rows = a.nodes * p.group;
+    const bool stream = p.rows <= 64;
+    p.unit_rows = stream ? 64 : ROWS;
+    p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
+    p.slot_rows = p.rows < p.unit_rows ? p.rows : p.unit_rows;
+    p.tile = stream ? 128 : KEYS;
+    p.blocks = 2 * fq_cu_count();
+    p.factor = a.scale * LOG2E;
+    return p;
+}
+
+template <int ACT, int DP>
+int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
+    constexpr int HALF_BYTES = tile_shape<DP>::BYTES;
+    const unsigned blocks = (unsigned)p.blocks;
+    if (p.rows <= 64) {
+        constexpr int WAVE_BYTES = 2 * HALF_BYTES > 128 * DP ? 2 * HALF_BYTES : 128 * DP;
+        constexpr int LDS = 4 * WAVE_BYTES + TABLE * 4 + 257 * 4;
+        static std::atomic<uint64_t> raised1{0}, raised2{0};
+        if (p.rows <= 32) {
+            const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_stream_kernel<ACT, DP, 1>, raised1);
+            if (st != FQ_OK) return st;
+            fq_attention_tree_stream_kernel<ACT, DP, 1><<<blocks, 256, LDS, stream>>>(a, p);
+        } else {
+            const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_stream_kernel<ACT, DP, 2>, raised2);
+            if (st != FQ_OK) return st;
+            fq_attention_tree_stream_kernel<ACT, DP, 2><<<blocks, 256, LDS, stream>>>(a, p);
+        }
+    } else {
+        static std::atomic<uint64_t> raised{0};
+        const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_tile_kernel<ACT, DP>, raised);
+        if (st != FQ_OK) return st;
+        fq_attention_tree_tile_kernel<ACT, DP><<<blocks, 256, 8 * HALF_BYTES + TABLE * 4, stream>>>(a, p);
+    }
+    if (hipGetLastError() != hipSuccess) return FQ_ERR_HIP;
+    fq_attention_tree_join_kernel<ACT><<<(unsigned)(a.sequences * a.kv_heads * p.row_tiles), 256, 0, stream>>>(a, p);
+    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
+template <int ACT>
+int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
+    if (a.head_dim <= 64) return launch<ACT, 64>(a, p, stream);
+    if (a.head_dim <= 96) return launch<ACT, 96>(a, p, stream);
+    return launch<ACT, 128>(a, p, stream);
 }
 
 }  // namespace
 
 size_t fq_tree_bytes(const fq_tree_args& a) {
-    (void)a;
-    return 0;
+    const tree_plan p = plan_tree(a);
+    return (size_t)p.blocks * 2 * p.slot_rows * (a.head_dim + 2) * sizeof(float);
 }
 
 int fq_launch_attention_tree(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream) {
-    (void)workspace;
-    const dim3 grid((unsigned)((a.sequences * a.nodes * a.q_heads + 3) / 4));
-    const float factor = a.scale * LOG2E;
-    if (act_dtype == FQ_F16) fq_attention_tree_kernel<FQ_F16><<<grid, 256, 0, stream>>>(a, factor);
-    else fq_attention_tree_kernel<FQ_BF16><<<grid, 256, 0, stream>>>(a, factor);
-    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+    tree_plan p = plan_tree(a);
+    p.slots = (float*)workspace;
+    if (a.sequences * a.kv_heads * p.row_tiles >= 1 << 24) return FQ_ERR_UNSUPPORTED;
+    return act_dtype == FQ_F16 ? launch<FQ_F16>(a, p, stream) : launch<FQ_BF16>(a, p, stream);
 }
