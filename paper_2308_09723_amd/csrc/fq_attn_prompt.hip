@@ -74,12 +74,12 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
             if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, rows.value(row) + value_at);
         }
     };
-    wave_state<ACT, DP, 1> w;
+    wave_state<ACT, DP> w;
     w.clear();
     if (tiles > 0) load(0, 0);
     const int64_t row = (int64_t)items.q_start[sequence] + min(i, queries - 1);
     const uint16_t* query = (const uint16_t*)q.data + row * q.row_stride + h * q.head_stride;
-    w.load_queries(0, query, D);
+    w.load_query(query, D);
     const int end = i + 1 + ahead;           // keys that the lane's query sees
     for (int t = 0; t < tiles; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -88,18 +88,18 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
         const int base = t * KEYS;
         if (first < queries && base < first + 32 + ahead) {
             const char* at = lds + (t & 1) * 2 * TILE_BYTES;
-            f32x16 s[1][2];
-            u32x4 p[1][4];
+            f32x16 s[2];
+            u32x4 p[4];
             w.template scores<2>(at, s);
             if (base + KEYS > first + 1 + ahead) {
-                keep_seen(s[0][0], low_bits(end - base));
-                keep_seen(s[0][1], low_bits(end - base - HALF));
+                keep_seen(s[0], low_bits(end - base));
+                keep_seen(s[1], low_bits(end - base - HALF));
             }
-            w.template soften<2>(0, s[0], factor, p[0]);
+            w.template soften<2>(s, factor, p);
             w.template accumulate<2>(at + TILE_BYTES, p);
         }
     }
-    const float l = w.l[0] = other_half_sum(w.l[0]);
+    const float l = w.l = other_half_sum(w.l);
     if (!w.finite()) {
         for (int x = 0; x < 32 && first + x < queries; ++x) {
             const int64_t r = (int64_t)items.q_start[sequence] + first + x;
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
         const float r = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
         uint16_t* to = out + (row * q_heads + h) * D;
         w.quads([&](int d, int x, int t) {
-            const f32x16& o = w.o[0][t];
+            const f32x16& o = w.o[t];
             const u32x2 v = {pack2<ACT>(o[x] * r, o[x + 1] * r), pack2<ACT>(o[x + 2] * r, o[x + 3] * r)};
             if (d < D) *(u32x2*)(to + d) = v;
         });

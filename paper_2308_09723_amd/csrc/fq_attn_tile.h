@@ -63,10 +63,23 @@ __device__ inline float other_half_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// What all lanes hold alike, in scalar registers
+__device__ inline int64_t uniform(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ inline const void* uniform(const void* p) { return (const void*)uniform((int64_t)(uintptr_t)p); }
+
 // Direct load global -> LDS, 16 bytes per lane (lane l to base + 16 l; base wave-uniform).  Assembly, since the builtin's wait
 // handling would drain every load in flight; the waits are written out.  M0 needs a wait state behind its write.
 __device__ inline void load_lds16(uint32_t base, const void* src) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"(src) : "memory", "m0");
+}
+
+// The same from an address that all lanes share + a 32-bit lane offset (bytes).
+__device__ inline void load_lds16(uint32_t base, const void* shared, uint32_t offset) {
+    const void* from = uniform(shared);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(base), "v"(offset), "s"(from) : "memory", "m0");
 }
 
 constexpr int HALF = 32;             // keys of half a tile: the first product's rows
@@ -92,93 +105,87 @@ struct tile_shape {
     static constexpr int TILES = DP / 32;                     // of the second
 };
 
-// One wave's state: RG groups of 32 queries (lane l: query l % 32 of each; the wave's halves hold the same queries)
-template <int ACT, int DP, int RG>
+// One wave's state: 32 queries (lane l: query l % 32; the wave's halves hold the same queries)
+template <int ACT, int DP>
 struct wave_state {
     typedef tile_shape<DP> SH;
-    u32x4 q[RG][SH::STEPS];
-    f32x16 o[RG][SH::TILES];
-    float m[RG], c[RG], l[RG];   // maximum that the numerators are relative to (raw scores), the same times factor (0: none yet), this lane's sum
+    u32x4 q[SH::STEPS];
+    f32x16 o[SH::TILES];
+    float m, c, l;       // maximum that the numerators are relative to (raw scores), the same times factor (0: none yet), this lane's sum
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
-        for (int g = 0; g < RG; ++g) {
+        for (int t = 0; t < SH::TILES; ++t)
 #pragma unroll
-            for (int t = 0; t < SH::TILES; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[g][t][i] = 0.0f;
-            m[g] = -__builtin_inff();
-            c[g] = l[g] = 0.0f;
-        }
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+        m = -__builtin_inff();
+        c = l = 0.0f;
     }
 
-    // the lane's query of group g
-    __device__ __forceinline__ void load_queries(int g, const uint16_t* row, int D) {
+    // the lane's query
+    __device__ __forceinline__ void load_query(const uint16_t* row, int D) {
         const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
         for (int s = 0; s < SH::STEPS; ++s) {
             const int unit = 2 * s + half;
             const u32x4 zero = {0, 0, 0, 0};
-            q[g][s] = unit * 8 < D ? *(const u32x4*)(row + unit * 8) : zero;
+            q[s] = unit * 8 < D ? *(const u32x4*)(row + unit * 8) : zero;
         }
     }
 
     // S^T of H half-tiles of keys in LDS.  Score i of half-tile t belongs to key 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4.
     template <int H>
-    __device__ __forceinline__ void scores(const char* keys, f32x16 (&s)[RG][H]) const {
+    __device__ __forceinline__ void scores(const char* keys, f32x16 (&s)[H]) const {
         const int lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31;
 #pragma unroll
-        for (int g = 0; g < RG; ++g)
+        for (int t = 0; t < H; ++t)
 #pragma unroll
-            for (int t = 0; t < H; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[g][t][i] = 0.0f;
+            for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
 #pragma unroll
         for (int step = 0; step < SH::STEPS; ++step)
 #pragma unroll
             for (int t = 0; t < H; ++t) {
                 const u32x4 k = *(const u32x4*)(keys + t * SH::BYTES + row * SH::PITCH + key_unit<SH::UNITS>(row, 2 * step + half) * 16);
-#pragma unroll
-                for (int g = 0; g < RG; ++g) s[g][t] = mfma32<ACT>(k, q[g][step], s[g][t]);
+                s[t] = mfma32<ACT>(k, q[step], s[t]);
             }
     }
 
-    // Numerators of group g's scores, in the order that accumulate() takes; maximum, sum and results brought along.
+    // Numerators of the scores, in the order that accumulate() takes; maximum, sum and results brought along.
     template <int H>
-    __device__ __forceinline__ void soften(int g, f32x16 (&s)[H], float factor, u32x4 (&p)[2 * H]) {
+    __device__ __forceinline__ void soften(f32x16 (&s)[H], float factor, u32x4 (&p)[2 * H]) {
         float top = s[0][0];
 #pragma unroll
         for (int i = 1; i < 16 * H; ++i) top = __builtin_fmaxf(top, s[i >> 4][i & 15]);
         top = other_half_max(top);
-        if (__any(top * factor > m[g] * factor + 8.0f)) {
-            const float now = __builtin_fmaxf(m[g], top), next = now == -__builtin_inff() ? 0.0f : now * factor;
-            const float again = __builtin_amdgcn_exp2f(m[g] * factor - next);       // (0 where there was none)
-            m[g] = now;
-            c[g] = next;
-            l[g] *= again;
+        if (__any(top * factor > m * factor + 8.0f)) {
+            const float now = __builtin_fmaxf(m, top), next = now == -__builtin_inff() ? 0.0f : now * factor;
+            const float again = __builtin_amdgcn_exp2f(m * factor - next);       // (0 where there was none)
+            m = now;
+            c = next;
+            l *= again;
 #pragma unroll
             for (int t = 0; t < SH::TILES; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[g][t][i] *= again;
+                for (int i = 0; i < 16; ++i) o[t][i] *= again;
         }
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int t = 0; t < H; ++t) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], factor, -c[g]));
+                s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], factor, -c));
                 sum[i & 1] += s[t][i];
             }
 #pragma unroll
             for (int i = 0; i < 16; i += 2) p[2 * t + i / 8][i / 2 % 4] = pack2<ACT>(s[t][i], s[t][i + 1]);
         }
-        l[g] += sum[0] + sum[1];
+        l += sum[0] + sum[1];
     }
 
     // O^T += V^T P^T over H half-tiles of values in LDS.  V^T: lane l takes column l % 32 of 32; a transposed read hands each lane
     // four keys of its column, out of four rows of which each lane of sixteen points at a quarter.
     template <int H>
-    __device__ __forceinline__ void accumulate(const char* values, const u32x4 (&p)[RG][2 * H]) {
+    __device__ __forceinline__ void accumulate(const char* values, const u32x4 (&p)[2 * H]) {
         const int lane = threadIdx.x & 63;
         const int row = 4 * (lane >> 5) + (lane & 15) / 4, unit = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), in = (lane & 1) * 8;
 #pragma unroll
@@ -196,22 +203,17 @@ struct wave_state {
                     v[2 * e] = y[0];
                     v[2 * e + 1] = y[1];
                 }
-#pragma unroll
-                for (int g = 0; g < RG; ++g) o[g][t] = mfma32<ACT>(v, p[g][k], o[g][t]);
+                o[t] = mfma32<ACT>(v, p[k], o[t]);
             }
     }
 
     // whether every sum of the wave's queries is finite
     __device__ __forceinline__ bool finite() const {
-        float x = 0.0f;
+        float x = l * 0.0f;
 #pragma unroll
-        for (int g = 0; g < RG; ++g) {
-            x = __builtin_fmaf(l[g], 0.0f, x);
+        for (int t = 0; t < SH::TILES; ++t)
 #pragma unroll
-            for (int t = 0; t < SH::TILES; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[g][t][i], 0.0f, x);
-        }
+            for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[t][i], 0.0f, x);
         return __all(x == 0.0f);
     }
 

@@ -56,7 +56,7 @@ struct line {
         units = a.kv_heads * p.row_tiles;
         int64_t sum = 0;
         for (int b = threadIdx.x & 63; b < a.sequences; b += 64) sum += tiles_of(a, p, b);
-        total = wave_sum64(sum) * units;
+        total = uniform(wave_sum64(sum)) * units;
         per_block = (total + p.blocks - 1) / p.blocks;
     }
     // the sequence whose tiles the line has at `at`, and where they begin
@@ -72,11 +72,11 @@ struct line {
                 const int64_t x = __shfl_up(upto, d);
                 if (lane >= d) upto += x;
             }
-            const int64_t all = __shfl(upto, 63);
+            const int64_t all = uniform(__shfl(upto, 63));
             if (target < before + all || first + 64 >= a.sequences) {
                 const int k = min(63, __builtin_popcountll(__ballot(before + upto <= target)));
                 *sequence = __builtin_amdgcn_readfirstlane(min(first + k, (int)a.sequences - 1));
-                *begin = (before + __shfl(upto - n, k)) * units;
+                *begin = uniform(before + __shfl(upto - n, k)) * units;
                 return;
             }
             before += all;
@@ -164,20 +164,25 @@ struct unit_rows {
     }
 };
 
-// Keys n0 * page_size and on of a piece: the page table's entries in LDS, and where a key lies.
+// Where the keys of a part of a piece lie: the page table's entries for it, in LDS.
 struct table_part {
-    const int32_t* entries;          // LDS
+    const int32_t* entries;
     uint32_t first, page_size;
     int shift;                       // page_size = 1 << shift, or -1
     int64_t page_stride, token_stride;
-    __device__ int64_t place(int j) const {
+    __device__ __forceinline__ int64_t place(int j) const {
         const uint32_t n = shift >= 0 ? (uint32_t)j >> shift : (uint32_t)j / page_size;
         return entries[n - first] * page_stride + (int64_t)((uint32_t)j - n * page_size) * token_stride;
     }
+    // for a key that all lanes ask for (page_size a power of two)
+    __device__ __forceinline__ int64_t one_place(int j) const {
+        const uint32_t n = (uint32_t)j >> shift;
+        return __builtin_amdgcn_readfirstlane(entries[n - first]) * page_stride + (int64_t)((uint32_t)j & (page_size - 1)) * token_stride;
+    }
 };
 
-// Brings in the entries of keys begin .. end - 1 (few enough, table_keys()); the caller waits.
-__device__ inline table_part load_table(const fq_tree_args& a, const unit_rows& u, int begin, int end, int32_t* entries) {
+// Brings in the entries of keys begin .. end - 1 (few enough: table_keys()); the caller waits.
+__device__ inline table_part load_table(const fq_tree_args& a, int b, int begin, int end, int32_t* entries) {
     table_part t;
     t.entries = entries;
     t.page_size = (uint32_t)a.cache.page_size;
@@ -186,7 +191,7 @@ __device__ inline table_part load_table(const fq_tree_args& a, const unit_rows& 
     t.page_stride = a.cache.page_stride;
     t.token_stride = a.cache.token_stride;
     const int count = (int)((uint32_t)(end - 1) / t.page_size - t.first) + 1;
-    const int32_t* row = a.page_table + u.b * a.table_width + t.first;
+    const int32_t* row = a.page_table + b * a.table_width + t.first;
     for (int i = threadIdx.x; i < count; i += 256) {
         const int32_t page = row[i];
         entries[i] = page < 0 ? 0 : (int32_t)min((uint32_t)page, (uint32_t)(a.cache.pages - 1));
@@ -197,26 +202,44 @@ __device__ inline table_part load_table(const fq_tree_args& a, const unit_rows& 
 __device__ inline int table_keys(const fq_tree_args& a, int tile) {
     return (int)min((int64_t)1 << 30, (int64_t)(TABLE - 1) * a.cache.page_size) / tile * tile;
 }
+// Whether the few neighbouring keys of one load lie in one page and within 32 bits of each other
+__device__ inline bool near_keys(const fq_tree_args& a, int keys) {
+    const int page = a.cache.page_size;
+    return (page & (page - 1)) == 0 && page >= keys && a.cache.token_stride < (int64_t)1 << 24;
+}
 
 // ------------------------------------------------------------------------------------------ up to 64 rows
-// A block's four waves take 32 keys each of a tile of 128, every one its own: keys and values of a wave lie in 2 x 32 rows of LDS
-// that no other wave touches, and the next keys are on their way while the present ones are used, values likewise, without a
-// barrier.  Two blocks of 64 KiB fill a compute unit.  At the end of a piece the waves' sums are joined through LDS.
-template <int ACT, int DP, int RG>
+// Up to 32 rows a block's four waves take 32 keys each of a tile of 128, up to 64 rows two pairs of waves 32 of a tile of 64, a pair
+// sharing the rows: every wave has its keys' and values' 2 x 32 rows of LDS to itself, the next keys are on their way while the
+// present ones are used, values likewise, and no barrier is needed.  Two blocks of 64 KiB fill a compute unit.  At the end of
+// a piece the waves' sums are joined through LDS.
+template <int ACT, int DP, int GROUPS>
 __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tree_args a, tree_plan p) {
     typedef tile_shape<DP> SH;
     constexpr int LOADS = SH::BYTES / 1024;             // 16-byte loads per lane for 32 rows
     constexpr int STEP = 64 / SH::UNITS;                // rows per load
+    constexpr int PERIOD = LOADS < 4 ? LOADS : 4;       // loads after which the rows' units lie alike again
     constexpr int JOIN = 32 * DP * 4;                   // bytes of 32 rows of sums
     constexpr int WAVE_BYTES = 2 * SH::BYTES > JOIN ? 2 * SH::BYTES : JOIN;
+    constexpr int PARTS = 4 / GROUPS;                   // waves that share 32 rows
+    constexpr int TILE = 32 * PARTS;
+    constexpr int TURN = DP / 4 == 24 ? 7 : 15;         // sums: units of four moved about by row
     extern __shared__ __align__(16) char lds[];
     int32_t* entries = (int32_t*)(lds + 4 * WAVE_BYTES);
     float* stats = (float*)(entries + TABLE);           // [4][32][2], and a flag
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = wave % GROUPS, part_of = wave / GROUPS;
     const int D = a.head_dim;
     char* mine = lds + wave * WAVE_BYTES;
     const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
     const int row0 = lane / SH::UNITS, spot = lane % SH::UNITS;
+    const bool near = near_keys(a, STEP);
+    uint32_t key_off[PERIOD], value_off[PERIOD];        // lane offsets of a load, bytes
+#pragma unroll
+    for (int j = 0; j < PERIOD; ++j) {
+        key_off[j] = (uint32_t)row0 * (uint32_t)a.cache.token_stride * 2 + key_unit<SH::UNITS>(row0 + j * STEP, spot) * 16;
+        value_off[j] = (uint32_t)row0 * (uint32_t)a.cache.token_stride * 2 + value_unit<SH::UNITS>(row0 + j * STEP, spot) * 16;
+    }
 
     const line all(a, p);
     const int64_t begin = blockIdx.x * all.per_block, stop = min(all.total, begin + all.per_block);
@@ -226,122 +249,119 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
     all.find(a, p, begin, &b, &at_b);
     int tiles = tiles_of(a, p, b);
     int u = (int)((begin - at_b) / tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
-    wave_state<ACT, DP, RG> w;
+    wave_state<ACT, DP> w;
 
     for (int64_t pos = begin; pos < stop;) {
         const unit_rows rows(a, p, b, u);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
         float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slots + (2 * (int64_t)blockIdx.x + (pos != begin)) * slot_floats(p, D);
-        const int key0 = t0 * 128, key1 = min(rows.keys, t1 * 128);
-#pragma unroll
-        for (int g = 0; g < RG; ++g) w.load_queries(g, rows.query(min(32 * g + (lane & 31), rows.count - 1)), D);
+        const int key0 = t0 * TILE, key1 = min(rows.keys, t1 * TILE);
+        const int row = min(32 * group + (lane & 31), rows.count - 1);
+        w.load_query(rows.query(row), D);
         w.clear();
-        const int most = table_keys(a, 128);
+        const int most = table_keys(a, TILE);
         for (int part = key0; part < key1; part += most) {
             const int part_end = min(key1, part + most);
             __syncthreads();                            // (entries and sums of the piece before are read)
-            const table_part table = load_table(a, rows, part, part_end, entries);
+            const table_part table = load_table(a, b, part, part_end, entries);
             if (D < SH::UNITS * 8) {                    // units that no load fills: zeros
                 const u32x4 zero = {0, 0, 0, 0};
                 for (int x = lane; x < 2 * SH::BYTES / 16; x += 64) ((u32x4*)mine)[x] = zero;
             }
             __syncthreads();
             const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
-            auto load = [&](const uint16_t* from, int base, uint32_t to, bool values) {
+            auto load = [&](const uint16_t* from, int base, uint32_t to, const uint32_t (&off)[PERIOD], bool values) {
+                if (near && base + 32 <= part_end) {
 #pragma unroll
-                for (int j = 0; j < LOADS; ++j) {
-                    const int row = row0 + j * STEP;
-                    const int unit = values ? value_unit<SH::UNITS>(row, spot) : key_unit<SH::UNITS>(row, spot);
-                    const uint16_t* src = from + table.place(min(base + row, part_end - 1)) + unit * 8;
-                    if (unit * 8 < D) load_lds16(to + j * 1024, src);
+                    for (int j = 0; j < LOADS; ++j) {
+                        const int unit = values ? value_unit<SH::UNITS>(row0 + j * STEP, spot) : key_unit<SH::UNITS>(row0 + j * STEP, spot);
+                        const uint16_t* src = from + table.one_place(base + j * STEP);
+                        if (unit * 8 < D) load_lds16(to + j * 1024, src, off[j % PERIOD]);
+                    }
+                } else {                                // (no row behind the last: what lies there may be anything)
+#pragma unroll 1
+                    for (int j = 0; j < LOADS; ++j) {
+                        const int r = row0 + j * STEP;
+                        const int unit = values ? value_unit<SH::UNITS>(r, spot) : key_unit<SH::UNITS>(r, spot);
+                        const uint16_t* src = from + table.place(min(base + r, part_end - 1)) + unit * 8;
+                        if (unit * 8 < D) load_lds16(to + j * 1024, src);
+                    }
                 }
             };
-            int base = part + wave * 32;
+            int base = part + part_of * 32;
             if (base < part_end) {
-                load(k, base, mine_at, false);
-                load(v, base, mine_at + SH::BYTES, true);
+                load(k, base, mine_at, key_off, false);
+                load(v, base, mine_at + SH::BYTES, value_off, true);
             }
-            for (; base < part_end; base += 128) {
-                const bool more = base + 128 < part_end;
-                f32x16 s[RG][1];
-                u32x4 x[RG][2];
+            for (; base < part_end; base += TILE) {
+                const bool more = base + TILE < part_end;
+                f32x16 s[1];
+                u32x4 x[2];
                 asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");       // keys are here
                 w.template scores<1>(mine, s);
                 if (more) {
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    load(k, base + 128, mine_at, false);
+                    load(k, base + TILE, mine_at, key_off, false);
                 }
-                const bool masked = base + 32 > min(rows.context, part_end);
-#pragma unroll
-                for (int g = 0; g < RG; ++g) {
-                    if (masked) keep_seen(s[g][0], rows.seen(min(32 * g + (lane & 31), rows.count - 1), base));
-                    w.template soften<1>(g, s[g], p.factor, x[g]);
-                }
+                if (base + 32 > min(rows.context, part_end)) keep_seen(s[0], rows.seen(row, base));
+                w.template soften<1>(s, p.factor, x);
                 if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");       // values are here
                 else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 w.template accumulate<1>(mine + SH::BYTES, x);
                 if (more) {
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    load(v, base + 128, mine_at + SH::BYTES, true);
+                    load(v, base + TILE, mine_at + SH::BYTES, value_off, true);
                 }
             }
         }
         // join the waves' sums
-#pragma unroll
-        for (int g = 0; g < RG; ++g) w.l[g] = other_half_sum(w.l[g]);
+        w.l = other_half_sum(w.l);
         __syncthreads();
         if (threadIdx.x == 0) stats[256] = 0.0f;
         __syncthreads();
         if (!w.finite() && lane == 0) stats[256] = 1.0f;
+        if (lane < 32) {
+            stats[(wave * 32 + lane) * 2] = w.m == -__builtin_inff() ? -__builtin_inff() : w.c;
+            stats[(wave * 32 + lane) * 2 + 1] = w.l;
+        }
+        w.quads([&](int d, int i, int t) {
+            const f32x16& o = w.o[t];
+            const f32x4 x = {o[i], o[i + 1], o[i + 2], o[i + 3]};
+            const int r = lane & 31;
+            *(f32x4*)((float*)mine + r * DP + ((d / 4) ^ (r & TURN)) * 4) = x;
+        });
         __syncthreads();
-        const bool again = stats[256] != 0.0f;
-        if (again) {
+        if (stats[256] != 0.0f) {
             rows.one_by_one<ACT>(key0, key1, slot);
         } else {
+            for (int x = threadIdx.x; x < min(rows.count, 32 * GROUPS) * (DP / 4); x += 256) {
+                const int at = x / (DP / 4), d = x % (DP / 4) * 4, r = at & 31, g = at >> 5;
+                if (d >= D) continue;
+                float c = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-            for (int g = 0; g < RG; ++g) {
-                if (32 * g >= rows.count) break;
-                if (lane < 32) {
-                    stats[(wave * 32 + lane) * 2] = w.m[g] == -__builtin_inff() ? -__builtin_inff() : w.c[g];
-                    stats[(wave * 32 + lane) * 2 + 1] = w.l[g];
+                for (int y = 0; y < PARTS; ++y) c = __builtin_fmaxf(c, stats[((y * GROUPS + g) * 32 + r) * 2]);
+                const float from = c == -__builtin_inff() ? 0.0f : c;
+                f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int y = 0; y < PARTS; ++y) {
+                    const int other = y * GROUPS + g;
+                    const float weight = __builtin_amdgcn_exp2f(stats[(other * 32 + r) * 2] - from);
+                    const f32x4 z = *(const f32x4*)((const float*)(lds + other * WAVE_BYTES) + r * DP + ((d / 4) ^ (r & TURN)) * 4);
+                    l += weight * stats[(other * 32 + r) * 2 + 1];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
                 }
-                float* sums = (float*)mine;
-                w.quads([&](int d, int i, int t) {
-                    const f32x16& o = w.o[g][t];
-                    const f32x4 x = {o[i], o[i + 1], o[i + 2], o[i + 3]};
-                    const int r = lane & 31;
-                    *(f32x4*)(sums + r * DP + ((d / 4) ^ (r & (DP / 4 == 24 ? 7 : 15))) * 4) = x;
-                });
-                __syncthreads();
-                for (int x = threadIdx.x; x < 32 * DP / 4; x += 256) {
-                    const int r = x / (DP / 4), d = x % (DP / 4) * 4;
-                    if (32 * g + r >= rows.count || d >= D) continue;
-                    float c = -__builtin_inff(), l = 0.0f;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) c = __builtin_fmaxf(c, stats[(y * 32 + r) * 2]);
-                    const float from = c == -__builtin_inff() ? 0.0f : c;
-                    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const float weight = __builtin_amdgcn_exp2f(stats[(y * 32 + r) * 2] - from);
-                        const f32x4 z = *(const f32x4*)((const float*)(lds + y * WAVE_BYTES) + r * DP + ((d / 4) ^ (r & (DP / 4 == 24 ? 7 : 15))) * 4);
-                        l += weight * stats[(y * 32 + r) * 2 + 1];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
-                    }
-                    if (!slot) {
-                        const float scale = l == 0.0f ? 0.0f : 1.0f / l;
-                        const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
-                        *(u32x2*)(rows.result(32 * g + r) + d) = z;
-                    } else {
-                        const int at = 32 * g + r;
-                        *(f32x4*)(slot + at * D + d) = o;
-                        if (d == 0) slot[p.slot_rows * D + at] = c, slot[p.slot_rows * (D + 1) + at] = l;
-                    }
+                if (!slot) {
+                    const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+                    const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+                    *(u32x2*)(rows.result(at) + d) = z;
+                } else {
+                    *(f32x4*)(slot + at * D + d) = o;
+                    if (d == 0) slot[p.slot_rows * D + at] = c, slot[p.slot_rows * (D + 1) + at] = l;
                 }
-                __syncthreads();
             }
         }
+        __syncthreads();
         pos += t1 - t0;
         t0 = 0;
         if (++u == all.units) {
@@ -364,6 +384,8 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     const int D = a.head_dim;
     const int row0 = threadIdx.x / SH::UNITS, spot = threadIdx.x % SH::UNITS;
     const int key_at = key_unit<SH::UNITS>(row0, spot) * 8, value_at = value_unit<SH::UNITS>(row0, spot) * 8;
+    const bool near = near_keys(a, STEP / 4);
+    const uint32_t in_page = (uint32_t)(lane / SH::UNITS) * (uint32_t)a.cache.token_stride * 2, key_off = in_page + key_at * 2, value_off = in_page + value_at * 2;
 
     const line all(a, p);
     const int64_t begin = blockIdx.x * all.per_block, stop = min(all.total, begin + all.per_block);
@@ -373,7 +395,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     all.find(a, p, begin, &b, &at_b);
     int tiles = tiles_of(a, p, b);
     int u = (int)((begin - at_b) / tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
-    wave_state<ACT, DP, 1> w;
+    wave_state<ACT, DP> w;
     if (D < SH::UNITS * 8) {
         const u32x4 zero = {0, 0, 0, 0};
         for (int x = threadIdx.x; x < 4 * TILE_BYTES / 16; x += 256) ((u32x4*)lds)[x] = zero;
@@ -386,22 +408,31 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
         const int key0 = t0 * KEYS, key1 = min(rows.keys, t1 * KEYS);
         const int r = wave * 32 + (lane & 31), row = min(r, rows.count - 1);
         const bool busy = wave * 32 < rows.count;
-        w.load_queries(0, rows.query(row), D);
+        w.load_query(rows.query(row), D);
         w.clear();
         const int most = table_keys(a, KEYS);
         for (int part = key0; part < key1; part += most) {
             const int part_end = min(key1, part + most);
             __syncthreads();
-            const table_part table = load_table(a, rows, part, part_end, entries);
+            const table_part table = load_table(a, b, part, part_end, entries);
             __syncthreads();
             const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
             auto load = [&](int base, int buffer) {
                 const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + buffer * 2 * TILE_BYTES) + wave * 1024;
+                if (near && base + KEYS <= part_end) {
 #pragma unroll
-                for (int j = 0; j < TILE_BYTES / 4096; ++j) {
-                    const int64_t place = table.place(min(base + row0 + j * STEP, part_end - 1));
-                    if (key_at < D) load_lds16(to + j * 4096, k + place + key_at);
-                    if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, v + place + value_at);
+                    for (int j = 0; j < TILE_BYTES / 4096; ++j) {
+                        const int64_t place = table.one_place(base + wave * (STEP / 4) + j * STEP);
+                        if (key_at < D) load_lds16(to + j * 4096, k + place, key_off);
+                        if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, v + place, value_off);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int j = 0; j < TILE_BYTES / 4096; ++j) {
+                        const int64_t place = table.place(min(base + row0 + j * STEP, part_end - 1));
+                        if (key_at < D) load_lds16(to + j * 4096, k + place + key_at);
+                        if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, v + place + value_at);
+                    }
                 }
             };
             load(part, 0);
@@ -411,18 +442,18 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
                 if (base + KEYS < part_end) load(base + KEYS, buffer ^ 1);
                 if (!busy) continue;
                 const char* at = lds + buffer * 2 * TILE_BYTES;
-                f32x16 s[1][2];
-                u32x4 x[1][4];
+                f32x16 s[2];
+                u32x4 x[4];
                 w.template scores<2>(at, s);
                 if (base + KEYS > min(rows.context, part_end)) {
-                    keep_seen(s[0][0], rows.seen(row, base));
-                    keep_seen(s[0][1], rows.seen(row, base + HALF));
+                    keep_seen(s[0], rows.seen(row, base));
+                    keep_seen(s[1], rows.seen(row, base + HALF));
                 }
-                w.template soften<2>(0, s[0], p.factor, x[0]);
+                w.template soften<2>(s, p.factor, x);
                 w.template accumulate<2>(at + TILE_BYTES, x);
             }
         }
-        const float l = w.l[0] = other_half_sum(w.l[0]);
+        const float l = w.l = other_half_sum(w.l);
         if (!w.finite()) {
             for (int i = wave * 32; i < min(wave * 32 + 32, rows.count); ++i) {
                 float o[2], c, sum;
@@ -438,7 +469,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
             const float scale = l == 0.0f ? 0.0f : 1.0f / l;
             uint16_t* to = rows.result(r);
             w.quads([&](int d, int i, int t) {
-                const f32x16& o = w.o[0][t];
+                const f32x16& o = w.o[t];
                 if (d >= D) return;
                 if (!slot) {
                     const u32x2 z = {pack2<ACT>(o[i] * scale, o[i + 1] * scale), pack2<ACT>(o[i + 2] * scale, o[i + 3] * scale)};
@@ -449,7 +480,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
                 }
             });
             if (slot && lane < 32) {
-                slot[p.slot_rows * D + r] = w.m[0] == -__builtin_inff() ? -__builtin_inff() : w.c[0];
+                slot[p.slot_rows * D + r] = w.m == -__builtin_inff() ? -__builtin_inff() : w.c;
                 slot[p.slot_rows * (D + 1) + r] = l;
             }
         }
@@ -462,9 +493,12 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     }
 }
 
-// Joins the pieces of a unit that was cut: one block per unit, piece after piece in the line's order.
+// Joins the pieces of a unit that was cut, two rows per block: a lane has four values of a row, the four waves a quarter of the
+// pieces each, all of them in the line's order.
 template <int ACT>
 __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_args a, tree_plan p) {
+    __shared__ f32x4 sums[4][64];
+    __shared__ float stats[4][64][2];
     const line all(a, p);
     const int b = (int)(blockIdx.x / all.units), u = (int)(blockIdx.x - (int64_t)b * all.units);
     int64_t before = 0;
@@ -474,28 +508,39 @@ __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_arg
     const int64_t from = begin / all.per_block, to = (end - 1) / all.per_block;        // blocks that have pieces of it
     if (from == to) return;
     const unit_rows rows(a, p, b, u);
-    const int D = a.head_dim, quads = D / 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int D = a.head_dim, r = blockIdx.y * 2 + (lane >> 5), d = (lane & 31) * 4;
+    const bool there = r < rows.count && d < D;
     const int64_t size = slot_floats(p, D);
     const bool whole = begin == from * all.per_block;        // (the first block's first piece, or its last)
-    for (int x = threadIdx.x; x < rows.count * quads; x += 256) {
-        const int r = x / quads, d = (x - r * quads) * 4;
-        float c = -__builtin_inff();
-        for (int64_t y = from; y <= to; ++y) c = __builtin_fmaxf(c, p.slots[(2 * y + (y == from && !whole)) * size + p.slot_rows * D + r]);
-        const float base = c == -__builtin_inff() ? 0.0f : c;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        float l = 0.0f;
-        for (int64_t y = from; y <= to; ++y) {
-            const float* slot = p.slots + (2 * y + (y == from && !whole)) * size;
-            const float weight = __builtin_amdgcn_exp2f(slot[p.slot_rows * D + r] - base);
-            const f32x4 z = *(const f32x4*)(slot + r * D + d);
-            l += weight * slot[p.slot_rows * (D + 1) + r];
+    const int share = (int)((to - from + 4) / 4);
+    float c = -__builtin_inff(), l = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](float c1, float l1, const f32x4& o1) {
+        const float top = __builtin_fmaxf(c, c1), base = top == -__builtin_inff() ? 0.0f : top;
+        const float mine = __builtin_amdgcn_exp2f(c - base), its = __builtin_amdgcn_exp2f(c1 - base);
+        c = top;
+        l = l * mine + l1 * its;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
+        for (int i = 0; i < 4; ++i) o[i] = o[i] * mine + o1[i] * its;
+    };
+    if (there) {
+        const int64_t last = min(to + 1, from + (wave + 1) * share);
+#pragma unroll 4
+        for (int64_t y = from + wave * share; y < last; ++y) {
+            const float* slot = p.slots + (2 * y + (y == from && !whole)) * size;
+            add(slot[p.slot_rows * D + r], slot[p.slot_rows * (D + 1) + r], *(const f32x4*)(slot + r * D + d));
         }
-        const float scale = l == 0.0f ? 0.0f : 1.0f / l;
-        const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
-        *(u32x2*)(rows.result(r) + d) = z;
     }
+    sums[wave][lane] = o;
+    stats[wave][lane][0] = c;
+    stats[wave][lane][1] = l;
+    __syncthreads();
+    if (wave != 0 || !there) return;
+    for (int y = 1; y < 4; ++y) add(stats[y][lane][0], stats[y][lane][1], sums[y][lane]);
+    const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+    const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+    *(u32x2*)(rows.result(r) + d) = z;
 }
 
 tree_plan plan_tree(const fq_tree_args& a) {
@@ -506,7 +551,7 @@ tree_plan plan_tree(const fq_tree_args& a) {
     p.unit_rows = stream ? 64 : ROWS;
     p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
     p.slot_rows = p.rows < p.unit_rows ? p.rows : p.unit_rows;
-    p.tile = stream ? 128 : KEYS;
+    p.tile = stream && p.rows <= 32 ? 128 : KEYS;
     p.blocks = 2 * fq_cu_count();
     p.factor = a.scale * LOG2E;
     return p;
@@ -536,7 +581,7 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
         fq_attention_tree_tile_kernel<ACT, DP><<<blocks, 256, 8 * HALF_BYTES + TABLE * 4, stream>>>(a, p);
     }
     if (hipGetLastError() != hipSuccess) return FQ_ERR_HIP;
-    fq_attention_tree_join_kernel<ACT><<<(unsigned)(a.sequences * a.kv_heads * p.row_tiles), 256, 0, stream>>>(a, p);
+    fq_attention_tree_join_kernel<ACT><<<dim3((unsigned)(a.sequences * a.kv_heads * p.row_tiles), (unsigned)(p.slot_rows + 1) / 2), 256, 0, stream>>>(a, p);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
