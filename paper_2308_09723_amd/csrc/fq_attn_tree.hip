@@ -23,15 +23,18 @@ constexpr int TABLE = 1024;          // entries of the page table that a block h
 // What the host has made of a call.
 struct tree_plan {
     int group, rows;                 // query heads per key head; rows of a key head
-    int row_tiles, unit_rows;        // units of unit_rows rows that they are cut into
+    int heads;                       // key heads that a block takes together
+    int row_tiles, unit_rows;        // tiles of unit_rows rows that a head's are cut into
     int tile;                        // keys of a tile
     int blocks;                      // at most
     int slot_rows;                   // rows of a slot of the workspace
     float factor;
-    float* slots;                    // two per block: [slot_rows][head_dim] sums, [slot_rows] maxima (log2), [slot_rows] sums of numerators
-};
+    float* slots;                    // two per block and head of it: [slot_rows][head_dim] sums, [slot_rows] maxima (log2), [slot_rows] sums of numerators
 
-__device__ inline int64_t slot_floats(const tree_plan& p, int D) { return (int64_t)p.slot_rows * (D + 2); }
+    __host__ __device__ int64_t slot_floats(int D) const { return (int64_t)slot_rows * (D + 2); }
+    // a block's first piece, or its last, of head h of the heads it takes together
+    __device__ float* slot(int64_t block, bool first, int h, int D) const { return slots + ((2 * block + !first) * heads + h) * slot_floats(D); }
+};
 
 __device__ inline int keys_of(const fq_tree_args& a, int context) {
     return context < 0 ? 0 : (int)min(a.table_width * a.cache.page_size, (int64_t)context + a.nodes);
@@ -53,7 +56,7 @@ struct line {
     int units;                       // of a sequence
 
     __device__ line(const fq_tree_args& a, const tree_plan& p) {
-        units = a.kv_heads * p.row_tiles;
+        units = a.kv_heads / p.heads * p.row_tiles;
         int64_t sum = 0;
         for (int b = threadIdx.x & 63; b < a.sequences; b += 64) sum += tiles_of(a, p, b);
         total = uniform(wave_sum64(sum)) * units;
@@ -91,9 +94,11 @@ struct unit_rows {
     int b, head, first, count;       // sequence; key head; first row, rows
     int context, keys;
 
-    __device__ unit_rows(const fq_tree_args& a, const tree_plan& p, int b, int u) : a(a), p(p), b(b) {
-        head = u / p.row_tiles;
-        first = (u - head * p.row_tiles) * p.unit_rows;
+    // unit u of sequence b, head h of its heads
+    __device__ unit_rows(const fq_tree_args& a, const tree_plan& p, int b, int u, int h) : a(a), p(p), b(b) {
+        const int set = u / p.row_tiles;
+        head = set * p.heads + h;
+        first = (u - set * p.row_tiles) * p.unit_rows;
         count = min(p.unit_rows, p.rows - first);
         context = __builtin_amdgcn_readfirstlane(a.context_lens[b]);
         keys = keys_of(a, context);
@@ -147,20 +152,43 @@ struct unit_rows {
             attend_one<ACT>(query(r), pages(), sees_first{last}, begin, min(end, last), a.head_dim, p.factor, o, c, l);
         }
     }
-    // the whole piece in that way, rows dealt to the block's waves
+    // rows from .. to - 1 of a piece in that way, every step-th
     template <int ACT>
-    __device__ void one_by_one(int begin, int end, float* slot) const {
+    __device__ void one_by_one(int begin, int end, float* slot, int from, int to, int step) const {
         const int lane = threadIdx.x & 63;
-        for (int r = threadIdx.x >> 6; r < count; r += 4) {
+        for (int r = from; r < to; r += step) {
             float o[2], c, l;
             one<ACT>(r, begin, end, o, &c, &l);
             if (!slot) {
                 store_one<ACT>(result(r), o, l, a.head_dim);
             } else {
                 if (2 * lane < a.head_dim) slot[r * a.head_dim + 2 * lane] = o[0], slot[r * a.head_dim + 2 * lane + 1] = o[1];
-                if (lane == 0) slot[p.slot_rows * a.head_dim + r] = c, slot[p.slot_rows * (a.head_dim + 1) + r] = l;
+                if (lane == 0) put_stats(slot, r, c, l);
             }
         }
+    }
+    __device__ void put_stats(float* slot, int r, float c, float l) const {
+        slot[p.slot_rows * a.head_dim + r] = c;
+        slot[p.slot_rows * (a.head_dim + 1) + r] = l;
+    }
+    // the lane's row r of a wave's sums
+    template <int ACT, int DP>
+    __device__ __forceinline__ void put(const wave_state<ACT, DP>& w, float* slot, int r) const {
+        const float scale = w.l == 0.0f ? 0.0f : 1.0f / w.l;       // (no key seen: zeros)
+        const int D = a.head_dim;
+        uint16_t* to = result(r);
+        w.quads([&](int d, int i, int t) {
+            const f32x16& o = w.o[t];
+            if (d >= D) return;
+            if (!slot) {
+                const u32x2 z = {pack2<ACT>(o[i] * scale, o[i + 1] * scale), pack2<ACT>(o[i + 2] * scale, o[i + 3] * scale)};
+                *(u32x2*)(to + d) = z;
+            } else {
+                const f32x4 z = {o[i], o[i + 1], o[i + 2], o[i + 3]};
+                *(f32x4*)(slot + r * D + d) = z;
+            }
+        });
+        if (slot && (threadIdx.x & 32) == 0) put_stats(slot, r, w.top(), w.l);
     }
 };
 
@@ -174,14 +202,19 @@ struct table_part {
         const uint32_t n = shift >= 0 ? (uint32_t)j >> shift : (uint32_t)j / page_size;
         return entries[n - first] * page_stride + (int64_t)((uint32_t)j - n * page_size) * token_stride;
     }
-    // for a key that all lanes ask for (page_size a power of two)
-    __device__ __forceinline__ int64_t one_place(int j) const {
-        const uint32_t n = (uint32_t)j >> shift;
-        return __builtin_amdgcn_readfirstlane(entries[n - first]) * page_stride + (int64_t)((uint32_t)j & (page_size - 1)) * token_stride;
+    // The places of keys j, j + step, ... (N of them), the same for all lanes (page_size a power of two): one read of the entries,
+    // a lane for each.
+    template <int N>
+    __device__ __forceinline__ void places(int j, int step, int64_t (&at)[N]) const {
+        const int e = entries[((uint32_t)(j + (int)(threadIdx.x % N) * step) >> shift) - first];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            at[i] = (int64_t)__builtin_amdgcn_readlane(e, i) * page_stride + (int64_t)((uint32_t)(j + i * step) & (page_size - 1)) * token_stride;
     }
 };
 
 // Brings in the entries of keys begin .. end - 1 (few enough: table_keys()); the caller waits.
+template <int THREADS>
 __device__ inline table_part load_table(const fq_tree_args& a, int b, int begin, int end, int32_t* entries) {
     table_part t;
     t.entries = entries;
@@ -192,15 +225,15 @@ __device__ inline table_part load_table(const fq_tree_args& a, int b, int begin,
     t.token_stride = a.cache.token_stride;
     const int count = (int)((uint32_t)(end - 1) / t.page_size - t.first) + 1;
     const int32_t* row = a.page_table + b * a.table_width + t.first;
-    for (int i = threadIdx.x; i < count; i += 256) {
+    for (int i = threadIdx.x % THREADS; i < count; i += THREADS) {
         const int32_t page = row[i];
         entries[i] = page < 0 ? 0 : (int32_t)min((uint32_t)page, (uint32_t)(a.cache.pages - 1));
     }
     return t;
 }
 // How many keys' entries fit, in whole tiles
-__device__ inline int table_keys(const fq_tree_args& a, int tile) {
-    return (int)min((int64_t)1 << 30, (int64_t)(TABLE - 1) * a.cache.page_size) / tile * tile;
+__device__ inline int table_keys(const fq_tree_args& a, int entries, int tile) {
+    return (int)min((int64_t)1 << 30, (int64_t)(entries - 1) * a.cache.page_size) / tile * tile;
 }
 // Whether the few neighbouring keys of one load lie in one page and within 32 bits of each other
 __device__ inline bool near_keys(const fq_tree_args& a, int keys) {
@@ -209,11 +242,11 @@ __device__ inline bool near_keys(const fq_tree_args& a, int keys) {
 }
 
 // ------------------------------------------------------------------------------------------ up to 64 rows
-// Up to 32 rows a block's four waves take 32 keys each of a tile of 128, up to 64 rows two pairs of waves 32 of a tile of 64, a pair
-// sharing the rows: every wave has its keys' and values' 2 x 32 rows of LDS to itself, the next keys are on their way while the
-// present ones are used, values likewise, and no barrier is needed.  Two blocks of 64 KiB fill a compute unit.  At the end of
-// a piece the waves' sums are joined through LDS.
-template <int ACT, int DP, int GROUPS>
+// A wave takes 32 rows of one key head and 32 keys at a time, which it brings into 2 x 32 rows of LDS of its own: the next keys
+// are on their way while the present ones are used, values likewise, and no barrier is needed.  Two blocks of 64 KiB fill a
+// compute unit.  A block's four waves are GROUPS groups of rows x HEADS key heads x PARTS parts of a tile of 32 PARTS keys; where they
+// share the keys out, they join their sums through LDS at the end of a piece.
+template <int ACT, int DP, int GROUPS, int HEADS>
 __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tree_args a, tree_plan p) {
     typedef tile_shape<DP> SH;
     constexpr int LOADS = SH::BYTES / 1024;             // 16-byte loads per lane for 32 rows
@@ -221,14 +254,15 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
     constexpr int PERIOD = LOADS < 4 ? LOADS : 4;       // loads after which the rows' units lie alike again
     constexpr int JOIN = 32 * DP * 4;                   // bytes of 32 rows of sums
     constexpr int WAVE_BYTES = 2 * SH::BYTES > JOIN ? 2 * SH::BYTES : JOIN;
-    constexpr int PARTS = 4 / GROUPS;                   // waves that share 32 rows
+    constexpr int PARTS = 4 / (GROUPS * HEADS);
     constexpr int TILE = 32 * PARTS;
     constexpr int TURN = DP / 4 == 24 ? 7 : 15;         // sums: units of four moved about by row
+    constexpr bool ONCE = GROUPS == 1;
     extern __shared__ __align__(16) char lds[];
-    int32_t* entries = (int32_t*)(lds + 4 * WAVE_BYTES);
-    float* stats = (float*)(entries + TABLE);           // [4][32][2], and a flag
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int group = wave % GROUPS, part_of = wave / GROUPS;
+    const int group = wave % GROUPS, head = wave / GROUPS % HEADS, part_of = wave / (GROUPS * HEADS);
+    int32_t* entries = (int32_t*)(lds + 4 * WAVE_BYTES) + wave * (TABLE / 4);
+    float* stats = (float*)(lds + 4 * WAVE_BYTES + TABLE * 4);       // [4][32][2], and a flag
     const int D = a.head_dim;
     char* mine = lds + wave * WAVE_BYTES;
     const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
@@ -252,31 +286,30 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
     wave_state<ACT, DP> w;
 
     for (int64_t pos = begin; pos < stop;) {
-        const unit_rows rows(a, p, b, u);
+        const unit_rows rows(a, p, b, u, head);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
-        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slots + (2 * (int64_t)blockIdx.x + (pos != begin)) * slot_floats(p, D);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, head, D);
         const int key0 = t0 * TILE, key1 = min(rows.keys, t1 * TILE);
         const int row = min(32 * group + (lane & 31), rows.count - 1);
         w.load_query(rows.query(row), D);
         w.clear();
-        const int most = table_keys(a, TILE);
+        const int most = table_keys(a, TABLE / 4, TILE);
         for (int part = key0; part < key1; part += most) {
             const int part_end = min(key1, part + most);
-            __syncthreads();                            // (entries and sums of the piece before are read)
-            const table_part table = load_table(a, b, part, part_end, entries);
+            const table_part table = load_table<64>(a, b, part, part_end, entries);
             if (D < SH::UNITS * 8) {                    // units that no load fills: zeros
                 const u32x4 zero = {0, 0, 0, 0};
                 for (int x = lane; x < 2 * SH::BYTES / 16; x += 64) ((u32x4*)mine)[x] = zero;
             }
-            __syncthreads();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the wave's own: no barrier)
             const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
+            int64_t at[LOADS];                          // places of the loads' first rows, where a load lies in a page
             auto load = [&](const uint16_t* from, int base, uint32_t to, const uint32_t (&off)[PERIOD], bool values) {
                 if (near && base + 32 <= part_end) {
 #pragma unroll
                     for (int j = 0; j < LOADS; ++j) {
                         const int unit = values ? value_unit<SH::UNITS>(row0 + j * STEP, spot) : key_unit<SH::UNITS>(row0 + j * STEP, spot);
-                        const uint16_t* src = from + table.one_place(base + j * STEP);
-                        if (unit * 8 < D) load_lds16(to + j * 1024, src, off[j % PERIOD]);
+                        if (unit * 8 < D) load_lds16<ONCE>(to + j * 1024, from + at[j], off[j % PERIOD]);
                     }
                 } else {                                // (no row behind the last: what lies there may be anything)
 #pragma unroll 1
@@ -290,6 +323,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
             };
             int base = part + part_of * 32;
             if (base < part_end) {
+                if (near && base + 32 <= part_end) table.template places<LOADS>(base, STEP, at);
                 load(k, base, mine_at, key_off, false);
                 load(v, base, mine_at + SH::BYTES, value_off, true);
             }
@@ -297,6 +331,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
                 const bool more = base + TILE < part_end;
                 f32x16 s[1];
                 u32x4 x[2];
+                if (near && base + TILE + 32 <= part_end) table.template places<LOADS>(base + TILE, STEP, at);
                 asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");       // keys are here
                 w.template scores<1>(mine, s);
                 if (more) {
@@ -308,60 +343,61 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
                 if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");       // values are here
                 else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 w.template accumulate<1>(mine + SH::BYTES, x);
-                if (more) {
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    load(v, base + TILE, mine_at + SH::BYTES, value_off, true);
-                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (more) load(v, base + TILE, mine_at + SH::BYTES, value_off, true);
             }
         }
-        // join the waves' sums
         w.l = other_half_sum(w.l);
-        __syncthreads();
-        if (threadIdx.x == 0) stats[256] = 0.0f;
-        __syncthreads();
-        if (!w.finite() && lane == 0) stats[256] = 1.0f;
-        if (lane < 32) {
-            stats[(wave * 32 + lane) * 2] = w.m == -__builtin_inff() ? -__builtin_inff() : w.c;
-            stats[(wave * 32 + lane) * 2 + 1] = w.l;
-        }
-        w.quads([&](int d, int i, int t) {
-            const f32x16& o = w.o[t];
-            const f32x4 x = {o[i], o[i + 1], o[i + 2], o[i + 3]};
-            const int r = lane & 31;
-            *(f32x4*)((float*)mine + r * DP + ((d / 4) ^ (r & TURN)) * 4) = x;
-        });
-        __syncthreads();
-        if (stats[256] != 0.0f) {
-            rows.one_by_one<ACT>(key0, key1, slot);
+        if constexpr (PARTS == 1) {
+            if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, 32 * group, min(rows.count, 32 * group + 32), 1);
+            else if (32 * group + (lane & 31) < rows.count) rows.put(w, slot, row);
         } else {
-            for (int x = threadIdx.x; x < min(rows.count, 32 * GROUPS) * (DP / 4); x += 256) {
-                const int at = x / (DP / 4), d = x % (DP / 4) * 4, r = at & 31, g = at >> 5;
-                if (d >= D) continue;
-                float c = -__builtin_inff(), l = 0.0f;
+            if (threadIdx.x == 0) stats[256] = 0.0f;
+            __syncthreads();
+            if (!w.finite() && lane == 0) stats[256] = 1.0f;
+            if (lane < 32) {
+                stats[(wave * 32 + lane) * 2] = w.top();
+                stats[(wave * 32 + lane) * 2 + 1] = w.l;
+            }
+            w.quads([&](int d, int i, int t) {
+                const f32x16& o = w.o[t];
+                const f32x4 x = {o[i], o[i + 1], o[i + 2], o[i + 3]};
+                const int r = lane & 31;
+                *(f32x4*)((float*)mine + r * DP + ((d / 4) ^ (r & TURN)) * 4) = x;
+            });
+            __syncthreads();
+            if (stats[256] != 0.0f) {
+                rows.one_by_one<ACT>(key0, key1, slot, 32 * group + part_of, min(rows.count, 32 * group + 32), PARTS);
+            } else {
+                for (int x = (part_of * 64 + lane); x < 32 * (DP / 4); x += 64 * PARTS) {
+                    const int r = x / (DP / 4), d = x % (DP / 4) * 4, at = 32 * group + r;
+                    if (at >= rows.count || d >= D) continue;
+                    float c = -__builtin_inff(), l = 0.0f;
 #pragma unroll
-                for (int y = 0; y < PARTS; ++y) c = __builtin_fmaxf(c, stats[((y * GROUPS + g) * 32 + r) * 2]);
-                const float from = c == -__builtin_inff() ? 0.0f : c;
-                f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int y = 0; y < PARTS; ++y) c = __builtin_fmaxf(c, stats[((y * HEADS + head) * GROUPS + group) * 64 + r * 2]);
+                    const float from = c == -__builtin_inff() ? 0.0f : c;
+                    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int y = 0; y < PARTS; ++y) {
-                    const int other = y * GROUPS + g;
-                    const float weight = __builtin_amdgcn_exp2f(stats[(other * 32 + r) * 2] - from);
-                    const f32x4 z = *(const f32x4*)((const float*)(lds + other * WAVE_BYTES) + r * DP + ((d / 4) ^ (r & TURN)) * 4);
-                    l += weight * stats[(other * 32 + r) * 2 + 1];
+                    for (int y = 0; y < PARTS; ++y) {
+                        const int other = (y * HEADS + head) * GROUPS + group;
+                        const float weight = __builtin_amdgcn_exp2f(stats[other * 64 + r * 2] - from);
+                        const f32x4 z = *(const f32x4*)((const float*)(lds + other * WAVE_BYTES) + r * DP + ((d / 4) ^ (r & TURN)) * 4);
+                        l += weight * stats[other * 64 + r * 2 + 1];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
-                }
-                if (!slot) {
-                    const float scale = l == 0.0f ? 0.0f : 1.0f / l;
-                    const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
-                    *(u32x2*)(rows.result(at) + d) = z;
-                } else {
-                    *(f32x4*)(slot + at * D + d) = o;
-                    if (d == 0) slot[p.slot_rows * D + at] = c, slot[p.slot_rows * (D + 1) + at] = l;
+                        for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
+                    }
+                    if (!slot) {
+                        const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+                        const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+                        *(u32x2*)(rows.result(at) + d) = z;
+                    } else {
+                        *(f32x4*)(slot + at * D + d) = o;
+                        if (d == 0) rows.put_stats(slot, at, c, l);
+                    }
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();
         pos += t1 - t0;
         t0 = 0;
         if (++u == all.units) {
@@ -402,29 +438,30 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     }
 
     for (int64_t pos = begin; pos < stop;) {
-        const unit_rows rows(a, p, b, u);
+        const unit_rows rows(a, p, b, u, 0);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
-        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slots + (2 * (int64_t)blockIdx.x + (pos != begin)) * slot_floats(p, D);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, 0, D);
         const int key0 = t0 * KEYS, key1 = min(rows.keys, t1 * KEYS);
         const int r = wave * 32 + (lane & 31), row = min(r, rows.count - 1);
         const bool busy = wave * 32 < rows.count;
         w.load_query(rows.query(row), D);
         w.clear();
-        const int most = table_keys(a, KEYS);
+        const int most = table_keys(a, TABLE, KEYS);
         for (int part = key0; part < key1; part += most) {
             const int part_end = min(key1, part + most);
             __syncthreads();
-            const table_part table = load_table(a, b, part, part_end, entries);
+            const table_part table = load_table<256>(a, b, part, part_end, entries);
             __syncthreads();
             const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
             auto load = [&](int base, int buffer) {
                 const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + buffer * 2 * TILE_BYTES) + wave * 1024;
                 if (near && base + KEYS <= part_end) {
+                    int64_t place[TILE_BYTES / 4096];
+                    table.template places<TILE_BYTES / 4096>(base + wave * (STEP / 4), STEP, place);
 #pragma unroll
                     for (int j = 0; j < TILE_BYTES / 4096; ++j) {
-                        const int64_t place = table.one_place(base + wave * (STEP / 4) + j * STEP);
-                        if (key_at < D) load_lds16(to + j * 4096, k + place, key_off);
-                        if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, v + place, value_off);
+                        if (key_at < D) load_lds16<false>(to + j * 4096, k + place[j], key_off);
+                        if (value_at < D) load_lds16<false>(to + TILE_BYTES + j * 4096, v + place[j], value_off);
                     }
                 } else {
 #pragma unroll 1
@@ -453,37 +490,9 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
                 w.template accumulate<2>(at + TILE_BYTES, x);
             }
         }
-        const float l = w.l = other_half_sum(w.l);
-        if (!w.finite()) {
-            for (int i = wave * 32; i < min(wave * 32 + 32, rows.count); ++i) {
-                float o[2], c, sum;
-                rows.one<ACT>(i, key0, key1, o, &c, &sum);
-                if (!slot) {
-                    store_one<ACT>(rows.result(i), o, sum, D);
-                } else {
-                    if (2 * lane < D) slot[i * D + 2 * lane] = o[0], slot[i * D + 2 * lane + 1] = o[1];
-                    if (lane == 0) slot[p.slot_rows * D + i] = c, slot[p.slot_rows * (D + 1) + i] = sum;
-                }
-            }
-        } else if (r < rows.count) {
-            const float scale = l == 0.0f ? 0.0f : 1.0f / l;
-            uint16_t* to = rows.result(r);
-            w.quads([&](int d, int i, int t) {
-                const f32x16& o = w.o[t];
-                if (d >= D) return;
-                if (!slot) {
-                    const u32x2 z = {pack2<ACT>(o[i] * scale, o[i + 1] * scale), pack2<ACT>(o[i + 2] * scale, o[i + 3] * scale)};
-                    *(u32x2*)(to + d) = z;
-                } else {
-                    const f32x4 z = {o[i], o[i + 1], o[i + 2], o[i + 3]};
-                    *(f32x4*)(slot + r * D + d) = z;
-                }
-            });
-            if (slot && lane < 32) {
-                slot[p.slot_rows * D + r] = w.m == -__builtin_inff() ? -__builtin_inff() : w.c;
-                slot[p.slot_rows * (D + 1) + r] = l;
-            }
-        }
+        w.l = other_half_sum(w.l);
+        if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, wave * 32, min(wave * 32 + 32, rows.count), 1);
+        else if (r < rows.count) rows.put(w, slot, r);
         pos += t1 - t0;
         t0 = 0;
         if (++u == all.units) {
@@ -507,11 +516,11 @@ __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_arg
     const int64_t begin = wave_sum64(before) * all.units + (int64_t)u * tiles, end = begin + tiles;
     const int64_t from = begin / all.per_block, to = (end - 1) / all.per_block;        // blocks that have pieces of it
     if (from == to) return;
-    const unit_rows rows(a, p, b, u);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int D = a.head_dim, r = blockIdx.y * 2 + (lane >> 5), d = (lane & 31) * 4;
-    const bool there = r < rows.count && d < D;
-    const int64_t size = slot_floats(p, D);
+    const int pair = blockIdx.y * 2 + (lane >> 5), head = pair / p.slot_rows, r = pair - head * p.slot_rows;
+    const int D = a.head_dim, d = (lane & 31) * 4;
+    const unit_rows rows(a, p, b, u, head);
+    const bool there = head < p.heads && r < rows.count && d < D;
     const bool whole = begin == from * all.per_block;        // (the first block's first piece, or its last)
     const int share = (int)((to - from + 4) / 4);
     float c = -__builtin_inff(), l = 0.0f;
@@ -528,7 +537,7 @@ __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_arg
         const int64_t last = min(to + 1, from + (wave + 1) * share);
 #pragma unroll 4
         for (int64_t y = from + wave * share; y < last; ++y) {
-            const float* slot = p.slots + (2 * y + (y == from && !whole)) * size;
+            const float* slot = p.slot(y, y != from || whole, head, D);
             add(slot[p.slot_rows * D + r], slot[p.slot_rows * (D + 1) + r], *(const f32x4*)(slot + r * D + d));
         }
     }
@@ -548,40 +557,47 @@ tree_plan plan_tree(const fq_tree_args& a) {
     p.group = a.q_heads / a.kv_heads;
     p.rows = a.nodes * p.group;
     const bool stream = p.rows <= 64;
+    // Few rows: the waves take neighbouring heads, whose rows of a token lie side by side: 4 x 256 bytes come in 10 % faster than
+    // 256.  That makes four times as many pieces as waves that share the keys out, of sums that are no longer few from 16 rows on.
+    p.heads = p.rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
     p.unit_rows = stream ? 64 : ROWS;
     p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
     p.slot_rows = p.rows < p.unit_rows ? p.rows : p.unit_rows;
-    p.tile = stream && p.rows <= 32 ? 128 : KEYS;
+    p.tile = p.rows > 32 ? KEYS : 128 / p.heads;
     p.blocks = 2 * fq_cu_count();
     p.factor = a.scale * LOG2E;
     return p;
 }
 
+template <int ACT, int DP, int GROUPS, int HEADS>
+int launch_stream(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
+    constexpr int WAVE_BYTES = 2 * tile_shape<DP>::BYTES > 128 * DP ? 2 * tile_shape<DP>::BYTES : 128 * DP;
+    static std::atomic<uint64_t> raised{0};
+    const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_stream_kernel<ACT, DP, GROUPS, HEADS>, raised);
+    if (st != FQ_OK) return st;
+    fq_attention_tree_stream_kernel<ACT, DP, GROUPS, HEADS><<<(unsigned)p.blocks, 256, 4 * WAVE_BYTES + TABLE * 4 + 257 * 4, stream>>>(a, p);
+    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
+template <int ACT, int DP>
+int launch_tiles(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
+    static std::atomic<uint64_t> raised{0};
+    const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_tile_kernel<ACT, DP>, raised);
+    if (st != FQ_OK) return st;
+    fq_attention_tree_tile_kernel<ACT, DP><<<(unsigned)p.blocks, 256, 8 * tile_shape<DP>::BYTES + TABLE * 4, stream>>>(a, p);
+    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
 template <int ACT, int DP>
 int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
-    constexpr int HALF_BYTES = tile_shape<DP>::BYTES;
-    const unsigned blocks = (unsigned)p.blocks;
-    if (p.rows <= 64) {
-        constexpr int WAVE_BYTES = 2 * HALF_BYTES > 128 * DP ? 2 * HALF_BYTES : 128 * DP;
-        constexpr int LDS = 4 * WAVE_BYTES + TABLE * 4 + 257 * 4;
-        static std::atomic<uint64_t> raised1{0}, raised2{0};
-        if (p.rows <= 32) {
-            const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_stream_kernel<ACT, DP, 1>, raised1);
-            if (st != FQ_OK) return st;
-            fq_attention_tree_stream_kernel<ACT, DP, 1><<<blocks, 256, LDS, stream>>>(a, p);
-        } else {
-            const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_stream_kernel<ACT, DP, 2>, raised2);
-            if (st != FQ_OK) return st;
-            fq_attention_tree_stream_kernel<ACT, DP, 2><<<blocks, 256, LDS, stream>>>(a, p);
-        }
-    } else {
-        static std::atomic<uint64_t> raised{0};
-        const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_tile_kernel<ACT, DP>, raised);
-        if (st != FQ_OK) return st;
-        fq_attention_tree_tile_kernel<ACT, DP><<<blocks, 256, 8 * HALF_BYTES + TABLE * 4, stream>>>(a, p);
-    }
-    if (hipGetLastError() != hipSuccess) return FQ_ERR_HIP;
-    fq_attention_tree_join_kernel<ACT><<<dim3((unsigned)(a.sequences * a.kv_heads * p.row_tiles), (unsigned)(p.slot_rows + 1) / 2), 256, 0, stream>>>(a, p);
+    const int st = p.rows > 64    ? launch_tiles<ACT, DP>(a, p, stream)
+                   : p.rows > 32  ? launch_stream<ACT, DP, 2, 1>(a, p, stream)
+                   : p.heads == 4 ? launch_stream<ACT, DP, 1, 4>(a, p, stream)
+                   : p.heads == 2 ? launch_stream<ACT, DP, 1, 2>(a, p, stream)
+                                  : launch_stream<ACT, DP, 1, 1>(a, p, stream);
+    if (st != FQ_OK) return st;
+    const dim3 grid((unsigned)(a.sequences * (a.kv_heads / p.heads) * p.row_tiles), (unsigned)(p.heads * p.slot_rows + 1) / 2);
+    fq_attention_tree_join_kernel<ACT><<<grid, 256, 0, stream>>>(a, p);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
@@ -596,7 +612,7 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
 
 size_t fq_tree_bytes(const fq_tree_args& a) {
     const tree_plan p = plan_tree(a);
-    return (size_t)p.blocks * 2 * p.slot_rows * (a.head_dim + 2) * sizeof(float);
+    return (size_t)p.blocks * 2 * p.heads * p.slot_floats(a.head_dim) * sizeof(float);
 }
 
 int fq_launch_attention_tree(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream) {
