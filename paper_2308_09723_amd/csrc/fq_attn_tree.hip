@@ -31,6 +31,8 @@ struct tree_plan {
     float factor;
     float* slots;                    // two per block and head of it: [slot_rows][head_dim] sums, [slot_rows] maxima (log2), [slot_rows] sums of numerators
 
+    // blocks that follow each other in the line share a die's cache (blocks go to the eight dies in turn)
+    __device__ int in_line(int block) const { return blocks % 8 == 0 ? block % 8 * (blocks / 8) + block / 8 : block; }
     __host__ __device__ int64_t slot_floats(int D) const { return (int64_t)slot_rows * (D + 2); }
     // a block's first piece, or its last, of head h of the heads it takes together
     __device__ float* slot(int64_t block, bool first, int h, int D) const { return slots + ((2 * block + !first) * heads + h) * slot_floats(D); }
@@ -241,12 +243,67 @@ __device__ inline bool near_keys(const fq_tree_args& a, int keys) {
     return (page & (page - 1)) == 0 && page >= keys && a.cache.token_stride < (int64_t)1 << 24;
 }
 
-// ------------------------------------------------------------------------------------------ up to 64 rows
+// The end of a piece whose keys PARTS waves of a block have shared out: wave first + i * step has part i of the rows from 32 group on.
+// Their sums go through LDS, 32 rows in `bytes` of each wave; stats: [4][32][2] and a flag.
+template <int ACT, int DP, int PARTS>
+__device__ __forceinline__ void join_parts(const unit_rows& rows, const wave_state<ACT, DP>& w, char* lds, int bytes, float* stats, int first,
+                                           int step, int part, int group, int key0, int key1, float* slot) {
+    constexpr int TURN = DP / 4 == 24 ? 7 : 15;         // units of four sums are moved about by row
+    const int lane = threadIdx.x & 63, wave = first + part * step, D = rows.a.head_dim;
+    __syncthreads();                                    // (nobody reads the keys and values that lay here, nor the sums of the piece before)
+    if (threadIdx.x == 0) stats[256] = 0.0f;
+    __syncthreads();
+    if (!w.finite() && lane == 0) stats[256] = 1.0f;
+    if (lane < 32) {
+        stats[(wave * 32 + lane) * 2] = w.top();
+        stats[(wave * 32 + lane) * 2 + 1] = w.l;
+    }
+    w.quads([&](int d, int i, int t) {
+        const f32x16& o = w.o[t];
+        const f32x4 x = {o[i], o[i + 1], o[i + 2], o[i + 3]};
+        const int r = lane & 31;
+        *(f32x4*)((float*)(lds + wave * bytes) + r * DP + ((d / 4) ^ (r & TURN)) * 4) = x;
+    });
+    __syncthreads();
+    if (stats[256] != 0.0f) {
+        rows.one_by_one<ACT>(key0, key1, slot, 32 * group + part, min(rows.count, 32 * group + 32), PARTS);
+    } else {
+        for (int x = part * 64 + lane; x < 32 * (DP / 4); x += 64 * PARTS) {
+            const int r = x / (DP / 4), d = x % (DP / 4) * 4, at = 32 * group + r;
+            if (at >= rows.count || d >= D) continue;
+            float c = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+            for (int y = 0; y < PARTS; ++y) c = __builtin_fmaxf(c, stats[(first + y * step) * 64 + r * 2]);
+            const float from = c == -__builtin_inff() ? 0.0f : c;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int y = 0; y < PARTS; ++y) {
+                const int other = first + y * step;
+                const float weight = __builtin_amdgcn_exp2f(stats[other * 64 + r * 2] - from);
+                const f32x4 z = *(const f32x4*)((const float*)(lds + other * bytes) + r * DP + ((d / 4) ^ (r & TURN)) * 4);
+                l += weight * stats[other * 64 + r * 2 + 1];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
+            }
+            if (!slot) {
+                const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+                const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+                *(u32x2*)(rows.result(at) + d) = z;
+            } else {
+                *(f32x4*)(slot + at * D + d) = o;
+                if (d == 0) rows.put_stats(slot, at, c, l);
+            }
+        }
+    }
+    __syncthreads();
+}
+
+// ------------------------------------------------------------------------------------------ up to 32 rows
 // A wave takes 32 rows of one key head and 32 keys at a time, which it brings into 2 x 32 rows of LDS of its own: the next keys
 // are on their way while the present ones are used, values likewise, and no barrier is needed.  Two blocks of 64 KiB fill a
-// compute unit.  A block's four waves are GROUPS groups of rows x HEADS key heads x PARTS parts of a tile of 32 PARTS keys; where they
-// share the keys out, they join their sums through LDS at the end of a piece.
-template <int ACT, int DP, int GROUPS, int HEADS>
+// compute unit.  A block's four waves are HEADS key heads x PARTS parts of a tile of 32 PARTS keys; where they share the keys out, they
+// join their sums through LDS at the end of a piece.
+template <int ACT, int DP, int HEADS>
 __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tree_args a, tree_plan p) {
     typedef tile_shape<DP> SH;
     constexpr int LOADS = SH::BYTES / 1024;             // 16-byte loads per lane for 32 rows
@@ -254,13 +311,11 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
     constexpr int PERIOD = LOADS < 4 ? LOADS : 4;       // loads after which the rows' units lie alike again
     constexpr int JOIN = 32 * DP * 4;                   // bytes of 32 rows of sums
     constexpr int WAVE_BYTES = 2 * SH::BYTES > JOIN ? 2 * SH::BYTES : JOIN;
-    constexpr int PARTS = 4 / (GROUPS * HEADS);
+    constexpr int PARTS = 4 / HEADS;
     constexpr int TILE = 32 * PARTS;
-    constexpr int TURN = DP / 4 == 24 ? 7 : 15;         // sums: units of four moved about by row
-    constexpr bool ONCE = GROUPS == 1;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int group = wave % GROUPS, head = wave / GROUPS % HEADS, part_of = wave / (GROUPS * HEADS);
+    const int head = wave % HEADS, part_of = wave / HEADS;
     int32_t* entries = (int32_t*)(lds + 4 * WAVE_BYTES) + wave * (TABLE / 4);
     float* stats = (float*)(lds + 4 * WAVE_BYTES + TABLE * 4);       // [4][32][2], and a flag
     const int D = a.head_dim;
@@ -290,7 +345,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
         float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, head, D);
         const int key0 = t0 * TILE, key1 = min(rows.keys, t1 * TILE);
-        const int row = min(32 * group + (lane & 31), rows.count - 1);
+        const int row = min(lane & 31, rows.count - 1);
         w.load_query(rows.query(row), D);
         w.clear();
         const int most = table_keys(a, TABLE / 4, TILE);
@@ -309,7 +364,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
 #pragma unroll
                     for (int j = 0; j < LOADS; ++j) {
                         const int unit = values ? value_unit<SH::UNITS>(row0 + j * STEP, spot) : key_unit<SH::UNITS>(row0 + j * STEP, spot);
-                        if (unit * 8 < D) load_lds16<ONCE>(to + j * 1024, from + at[j], off[j % PERIOD]);
+                        if (unit * 8 < D) load_lds16<true>(to + j * 1024, from + at[j], off[j % PERIOD]);
                     }
                 } else {                                // (no row behind the last: what lies there may be anything)
 #pragma unroll 1
@@ -349,54 +404,10 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         }
         w.l = other_half_sum(w.l);
         if constexpr (PARTS == 1) {
-            if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, 32 * group, min(rows.count, 32 * group + 32), 1);
-            else if (32 * group + (lane & 31) < rows.count) rows.put(w, slot, row);
+            if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
+            else if ((lane & 31) < rows.count) rows.put(w, slot, row);
         } else {
-            if (threadIdx.x == 0) stats[256] = 0.0f;
-            __syncthreads();
-            if (!w.finite() && lane == 0) stats[256] = 1.0f;
-            if (lane < 32) {
-                stats[(wave * 32 + lane) * 2] = w.top();
-                stats[(wave * 32 + lane) * 2 + 1] = w.l;
-            }
-            w.quads([&](int d, int i, int t) {
-                const f32x16& o = w.o[t];
-                const f32x4 x = {o[i], o[i + 1], o[i + 2], o[i + 3]};
-                const int r = lane & 31;
-                *(f32x4*)((float*)mine + r * DP + ((d / 4) ^ (r & TURN)) * 4) = x;
-            });
-            __syncthreads();
-            if (stats[256] != 0.0f) {
-                rows.one_by_one<ACT>(key0, key1, slot, 32 * group + part_of, min(rows.count, 32 * group + 32), PARTS);
-            } else {
-                for (int x = (part_of * 64 + lane); x < 32 * (DP / 4); x += 64 * PARTS) {
-                    const int r = x / (DP / 4), d = x % (DP / 4) * 4, at = 32 * group + r;
-                    if (at >= rows.count || d >= D) continue;
-                    float c = -__builtin_inff(), l = 0.0f;
-#pragma unroll
-                    for (int y = 0; y < PARTS; ++y) c = __builtin_fmaxf(c, stats[((y * HEADS + head) * GROUPS + group) * 64 + r * 2]);
-                    const float from = c == -__builtin_inff() ? 0.0f : c;
-                    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int y = 0; y < PARTS; ++y) {
-                        const int other = (y * HEADS + head) * GROUPS + group;
-                        const float weight = __builtin_amdgcn_exp2f(stats[other * 64 + r * 2] - from);
-                        const f32x4 z = *(const f32x4*)((const float*)(lds + other * WAVE_BYTES) + r * DP + ((d / 4) ^ (r & TURN)) * 4);
-                        l += weight * stats[other * 64 + r * 2 + 1];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
-                    }
-                    if (!slot) {
-                        const float scale = l == 0.0f ? 0.0f : 1.0f / l;
-                        const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
-                        *(u32x2*)(rows.result(at) + d) = z;
-                    } else {
-                        *(f32x4*)(slot + at * D + d) = o;
-                        if (d == 0) rows.put_stats(slot, at, c, l);
-                    }
-                }
-            }
-            __syncthreads();
+            join_parts<ACT, DP, PARTS>(rows, w, lds, WAVE_BYTES, stats, head, HEADS, part_of, 0, key0, key1, slot);
         }
         pos += t1 - t0;
         t0 = 0;
@@ -407,16 +418,22 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
     }
 }
 
-// ------------------------------------------------------------------------------------------ above 64 rows
-// 128 rows a block, 32 to a wave; tiles of 64 keys that all four waves read, two of them in LDS, as for prompts.
-template <int ACT, int DP>
+// ------------------------------------------------------------------------------------------ above 32 rows
+// GROUPS x 32 rows a block; tiles of 64 keys that all waves read, two of them in LDS, as for prompts.  Four groups: every wave takes
+// all keys of a tile.  Two (up to 64 rows): two pairs of waves take half a tile each, and join their sums.
+template <int ACT, int DP, int GROUPS>
 __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_args a, tree_plan p) {
     typedef tile_shape<DP> SH;
     constexpr int TILE_BYTES = 2 * SH::BYTES;
     constexpr int STEP = 256 / SH::UNITS;
+    constexpr int JOIN = 32 * DP * 4;                   // bytes of 32 rows of sums
+    static_assert(4 * JOIN <= 4 * TILE_BYTES, "");
     extern __shared__ __align__(16) char lds[];
+    constexpr int PARTS = 4 / GROUPS, HALVES = 2 / PARTS;
     int32_t* entries = (int32_t*)(lds + 4 * TILE_BYTES);
+    float* stats = (float*)(entries + TABLE);           // [4][32][2], and a flag
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = wave % GROUPS, part_of = wave / GROUPS;
     const int D = a.head_dim;
     const int row0 = threadIdx.x / SH::UNITS, spot = threadIdx.x % SH::UNITS;
     const int key_at = key_unit<SH::UNITS>(row0, spot) * 8, value_at = value_unit<SH::UNITS>(row0, spot) * 8;
@@ -424,7 +441,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     const uint32_t in_page = (uint32_t)(lane / SH::UNITS) * (uint32_t)a.cache.token_stride * 2, key_off = in_page + key_at * 2, value_off = in_page + value_at * 2;
 
     const line all(a, p);
-    const int64_t begin = blockIdx.x * all.per_block, stop = min(all.total, begin + all.per_block);
+    const int64_t block = p.in_line(blockIdx.x), begin = block * all.per_block, stop = min(all.total, begin + all.per_block);
     if (begin >= stop) return;
     int b;
     int64_t at_b;
@@ -432,18 +449,14 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     int tiles = tiles_of(a, p, b);
     int u = (int)((begin - at_b) / tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
     wave_state<ACT, DP> w;
-    if (D < SH::UNITS * 8) {
-        const u32x4 zero = {0, 0, 0, 0};
-        for (int x = threadIdx.x; x < 4 * TILE_BYTES / 16; x += 256) ((u32x4*)lds)[x] = zero;
-    }
 
     for (int64_t pos = begin; pos < stop;) {
         const unit_rows rows(a, p, b, u, 0);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
-        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, 0, D);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(block, pos == begin, 0, D);
         const int key0 = t0 * KEYS, key1 = min(rows.keys, t1 * KEYS);
-        const int r = wave * 32 + (lane & 31), row = min(r, rows.count - 1);
-        const bool busy = wave * 32 < rows.count;
+        const int r = group * 32 + (lane & 31), row = min(r, rows.count - 1);
+        const bool busy = group * 32 < rows.count;
         w.load_query(rows.query(row), D);
         w.clear();
         const int most = table_keys(a, TABLE, KEYS);
@@ -451,6 +464,10 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
             const int part_end = min(key1, part + most);
             __syncthreads();
             const table_part table = load_table<256>(a, b, part, part_end, entries);
+            if (D < SH::UNITS * 8) {                    // units that no load fills: zeros
+                const u32x4 zero = {0, 0, 0, 0};
+                for (int x = threadIdx.x; x < 4 * TILE_BYTES / 16; x += 256) ((u32x4*)lds)[x] = zero;
+            }
             __syncthreads();
             const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
             auto load = [&](int base, int buffer) {
@@ -478,21 +495,26 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
                 __syncthreads();
                 if (base + KEYS < part_end) load(base + KEYS, buffer ^ 1);
                 if (!busy) continue;
-                const char* at = lds + buffer * 2 * TILE_BYTES;
-                f32x16 s[2];
-                u32x4 x[4];
-                w.template scores<2>(at, s);
-                if (base + KEYS > min(rows.context, part_end)) {
-                    keep_seen(s[0], rows.seen(row, base));
-                    keep_seen(s[1], rows.seen(row, base + HALF));
+                const char* at = lds + buffer * 2 * TILE_BYTES + part_of * SH::BYTES;
+                const int from = base + part_of * HALF;
+                f32x16 s[HALVES];
+                u32x4 x[2 * HALVES];
+                w.template scores<HALVES>(at, s);
+                if (from + HALVES * HALF > min(rows.context, part_end)) {
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) keep_seen(s[h], rows.seen(row, from + h * HALF));
                 }
-                w.template soften<2>(s, p.factor, x);
-                w.template accumulate<2>(at + TILE_BYTES, x);
+                w.template soften<HALVES>(s, p.factor, x);
+                w.template accumulate<HALVES>(at + TILE_BYTES, x);
             }
         }
         w.l = other_half_sum(w.l);
-        if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, wave * 32, min(wave * 32 + 32, rows.count), 1);
-        else if (r < rows.count) rows.put(w, slot, r);
+        if constexpr (PARTS > 1) {
+            join_parts<ACT, DP, PARTS>(rows, w, lds, JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
+        } else {
+            if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
+            else if (r < rows.count) rows.put(w, slot, r);
+        }
         pos += t1 - t0;
         t0 = 0;
         if (++u == all.units) {
@@ -502,8 +524,8 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     }
 }
 
-// Joins the pieces of a unit that was cut, two rows per block: a lane has four values of a row, the four waves a quarter of the
-// pieces each, all of them in the line's order.
+// Joins the pieces of a unit that was cut.  A lane has four values of a row, a wave two rows.  A unit of few pieces: each wave its own
+// rows; of many: the four waves a quarter of the pieces each of the same rows.  Pieces are added in the line's order.
 template <int ACT>
 __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_args a, tree_plan p) {
     __shared__ f32x4 sums[4][64];
@@ -513,54 +535,75 @@ __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_arg
     int64_t before = 0;
     for (int x = threadIdx.x & 63; x < b; x += 64) before += tiles_of(a, p, x);
     const int tiles = tiles_of(a, p, b);
-    const int64_t begin = wave_sum64(before) * all.units + (int64_t)u * tiles, end = begin + tiles;
+    const int64_t begin = uniform(wave_sum64(before)) * all.units + (int64_t)u * tiles, end = begin + tiles;
     const int64_t from = begin / all.per_block, to = (end - 1) / all.per_block;        // blocks that have pieces of it
     if (from == to) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int pair = blockIdx.y * 2 + (lane >> 5), head = pair / p.slot_rows, r = pair - head * p.slot_rows;
     const int D = a.head_dim, d = (lane & 31) * 4;
-    const unit_rows rows(a, p, b, u, head);
-    const bool there = head < p.heads && r < rows.count && d < D;
     const bool whole = begin == from * all.per_block;        // (the first block's first piece, or its last)
-    const int share = (int)((to - from + 4) / 4);
-    float c = -__builtin_inff(), l = 0.0f;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto add = [&](float c1, float l1, const f32x4& o1) {
-        const float top = __builtin_fmaxf(c, c1), base = top == -__builtin_inff() ? 0.0f : top;
-        const float mine = __builtin_amdgcn_exp2f(c - base), its = __builtin_amdgcn_exp2f(c1 - base);
-        c = top;
-        l = l * mine + l1 * its;
+    const bool many = to - from >= 8;
+    const int share = many ? (int)((to - from + 4) / 4) : (int)(to - from + 1), mine = many ? wave : 0;
+    const int at_once = many ? 2 : 8;
+    for (int base = blockIdx.y * at_once; base < p.heads * p.slot_rows; base += gridDim.y * at_once) {
+        const int row = base + (many ? 0 : 2 * wave) + (lane >> 5), head = row / p.slot_rows, r = row - head * p.slot_rows;
+        const unit_rows rows(a, p, b, u, min(head, p.heads - 1));
+        const bool there = head < p.heads && r < rows.count && d < D;
+        float c = -__builtin_inff(), l = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        auto add = [&](float c1, float l1, const f32x4& o1) {
+            const float top = __builtin_fmaxf(c, c1), base = top == -__builtin_inff() ? 0.0f : top;
+            const float mine = __builtin_amdgcn_exp2f(c - base), its = __builtin_amdgcn_exp2f(c1 - base);
+            c = top;
+            l = l * mine + l1 * its;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = o[i] * mine + o1[i] * its;
-    };
-    if (there) {
-        const int64_t last = min(to + 1, from + (wave + 1) * share);
-#pragma unroll 4
-        for (int64_t y = from + wave * share; y < last; ++y) {
-            const float* slot = p.slot(y, y != from || whole, head, D);
-            add(slot[p.slot_rows * D + r], slot[p.slot_rows * (D + 1) + r], *(const f32x4*)(slot + r * D + d));
+            for (int i = 0; i < 4; ++i) o[i] = o[i] * mine + o1[i] * its;
+        };
+        if (there) {
+            const int64_t stride = 2 * p.heads * p.slot_floats(D);       // from block to block
+            const float* first = p.slot(from, true, head, D);
+            const int n0 = mine * share, n1 = min((int)(to - from) + 1, n0 + share);
+            constexpr int BATCH = 8;                        // pieces on their way at once
+            for (int n = n0; n < n1; n += BATCH) {
+                float c1[BATCH], l1[BATCH];
+                f32x4 o1[BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int y = min(n + i, n1 - 1);
+                    const float* slot = y == 0 && !whole ? p.slot(from, false, head, D) : first + y * stride;
+                    c1[i] = slot[p.slot_rows * D + r];
+                    l1[i] = slot[p.slot_rows * (D + 1) + r];
+                    o1[i] = *(const f32x4*)(slot + r * D + d);
+                }
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i)
+                    if (n + i < n1) add(c1[i], l1[i], o1[i]);
+            }
+        }
+        if (many) {
+            __syncthreads();
+            sums[wave][lane] = o;
+            stats[wave][lane][0] = c;
+            stats[wave][lane][1] = l;
+            __syncthreads();
+            if (wave == 0)
+                for (int y = 1; y < 4; ++y) add(stats[y][lane][0], stats[y][lane][1], sums[y][lane]);
+        }
+        if (there && (wave == 0 || !many)) {
+            const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+            const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+            *(u32x2*)(rows.result(r) + d) = z;
         }
     }
-    sums[wave][lane] = o;
-    stats[wave][lane][0] = c;
-    stats[wave][lane][1] = l;
-    __syncthreads();
-    if (wave != 0 || !there) return;
-    for (int y = 1; y < 4; ++y) add(stats[y][lane][0], stats[y][lane][1], sums[y][lane]);
-    const float scale = l == 0.0f ? 0.0f : 1.0f / l;
-    const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
-    *(u32x2*)(rows.result(r) + d) = z;
 }
 
 tree_plan plan_tree(const fq_tree_args& a) {
     tree_plan p = {};
     p.group = a.q_heads / a.kv_heads;
     p.rows = a.nodes * p.group;
-    const bool stream = p.rows <= 64;
     // Few rows: the waves take neighbouring heads, whose rows of a token lie side by side: 4 x 256 bytes come in 10 % faster than
     // 256.  That makes four times as many pieces as waves that share the keys out, of sums that are no longer few from 16 rows on.
     p.heads = p.rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
-    p.unit_rows = stream ? 64 : ROWS;
+    p.unit_rows = p.rows <= 64 ? 64 : ROWS;
     p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
     p.slot_rows = p.rows < p.unit_rows ? p.rows : p.unit_rows;
     p.tile = p.rows > 32 ? KEYS : 128 / p.heads;
@@ -569,34 +612,37 @@ tree_plan plan_tree(const fq_tree_args& a) {
     return p;
 }
 
-template <int ACT, int DP, int GROUPS, int HEADS>
+template <int ACT, int DP, int HEADS>
 int launch_stream(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
     constexpr int WAVE_BYTES = 2 * tile_shape<DP>::BYTES > 128 * DP ? 2 * tile_shape<DP>::BYTES : 128 * DP;
     static std::atomic<uint64_t> raised{0};
-    const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_stream_kernel<ACT, DP, GROUPS, HEADS>, raised);
+    const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_stream_kernel<ACT, DP, HEADS>, raised);
     if (st != FQ_OK) return st;
-    fq_attention_tree_stream_kernel<ACT, DP, GROUPS, HEADS><<<(unsigned)p.blocks, 256, 4 * WAVE_BYTES + TABLE * 4 + 257 * 4, stream>>>(a, p);
+    fq_attention_tree_stream_kernel<ACT, DP, HEADS><<<(unsigned)p.blocks, 256, 4 * WAVE_BYTES + TABLE * 4 + 257 * 4, stream>>>(a, p);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
-template <int ACT, int DP>
+template <int ACT, int DP, int GROUPS>
 int launch_tiles(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
     static std::atomic<uint64_t> raised{0};
-    const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_tile_kernel<ACT, DP>, raised);
+    const int st = fqd::raise_lds_limit((const void*)fq_attention_tree_tile_kernel<ACT, DP, GROUPS>, raised);
     if (st != FQ_OK) return st;
-    fq_attention_tree_tile_kernel<ACT, DP><<<(unsigned)p.blocks, 256, 8 * tile_shape<DP>::BYTES + TABLE * 4, stream>>>(a, p);
+    fq_attention_tree_tile_kernel<ACT, DP, GROUPS><<<(unsigned)p.blocks, 256, 8 * tile_shape<DP>::BYTES + TABLE * 4 + 257 * 4, stream>>>(a, p);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
 template <int ACT, int DP>
 int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
-    const int st = p.rows > 64    ? launch_tiles<ACT, DP>(a, p, stream)
-                   : p.rows > 32  ? launch_stream<ACT, DP, 2, 1>(a, p, stream)
-                   : p.heads == 4 ? launch_stream<ACT, DP, 1, 4>(a, p, stream)
-                   : p.heads == 2 ? launch_stream<ACT, DP, 1, 2>(a, p, stream)
-                                  : launch_stream<ACT, DP, 1, 1>(a, p, stream);
+    const int st = p.rows > 64    ? launch_tiles<ACT, DP, 4>(a, p, stream)
+                   : p.rows > 32  ? launch_tiles<ACT, DP, 2>(a, p, stream)
+                   : p.heads == 4 ? launch_stream<ACT, DP, 4>(a, p, stream)
+                   : p.heads == 2 ? launch_stream<ACT, DP, 2>(a, p, stream)
+                                  : launch_stream<ACT, DP, 1>(a, p, stream);
     if (st != FQ_OK) return st;
-    const dim3 grid((unsigned)(a.sequences * (a.kv_heads / p.heads) * p.row_tiles), (unsigned)(p.heads * p.slot_rows + 1) / 2);
+    // (a block for each unit at least, more for its rows while they are few)
+    const int64_t units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
+    const int64_t most = (p.heads * p.slot_rows + 1) / 2, wanted = 1024 / units;
+    const dim3 grid((unsigned)units, (unsigned)(wanted < 1 ? 1 : wanted < most ? wanted : most));
     fq_attention_tree_join_kernel<ACT><<<grid, 256, 0, stream>>>(a, p);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
