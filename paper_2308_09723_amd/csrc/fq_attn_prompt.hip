@@ -155,7 +155,7 @@ int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* wor
             order[i] = i;
             tiles[i] = (a.q_offsets[first + i + 1] - a.q_offsets[first + i] + TILE - 1) / TILE;
         }
-        std::stable_sort(order, order + n, [&](int x, int y) { return tiles[x] > tiles[y]; });
+        std::sort(order, order + n, [&](int x, int y) { return tiles[x] != tiles[y] ? tiles[x] > tiles[y] : x < y; });
         prompt_items items = {};
         items.count = n;
         int total = 0;

@@ -40,6 +40,11 @@ struct {
     decltype(&fq_codes_bytes) codes_bytes;
     decltype(&fq_scales_bytes) scales_bytes;
     decltype(&fq_zscale_bytes) zscale_bytes;
+    decltype(&fq_qk_norm_rope) qk_norm_rope;
+    decltype(&fq_attention_prompt) attention_prompt;
+    decltype(&fq_attention_prompt_workspace_bytes) attention_prompt_workspace_bytes;
+    decltype(&fq_attention_tree) attention_tree;
+    decltype(&fq_attention_tree_workspace_bytes) attention_tree_workspace_bytes;
 } lib;
 
 PyObject* fq_error;       // fq.FqError
@@ -250,6 +255,204 @@ PyObject* quantize_w4a8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ------------------------------------------------------------------------------------------ attention
+void require(bool condition) {
+    if (!condition) throw not_plain();
+}
+
+double number(PyObject* o) {
+    if (PyFloat_CheckExact(o)) return PyFloat_AS_DOUBLE(o);
+    return integer(o);
+}
+
+bool truth(PyObject* o) {
+    require(PyBool_Check(o));
+    return o == Py_True;
+}
+
+// a contiguous tensor of this type beside `like`
+const at::Tensor& plain(PyObject* o, at::ScalarType type, const at::Tensor& like) {
+    const at::Tensor& t = tensor(o);
+    require(t.scalar_type() == type && t.device() == like.device() && t.is_contiguous());
+    return t;
+}
+
+at::Tensor output(PyObject* o, at::IntArrayRef size, const at::Tensor& like) {
+    if (o == Py_None) return empty(size, like.scalar_type(), like);
+    const at::Tensor& t = plain(o, like.scalar_type(), like);
+    require(t.sizes() == size);
+    return t;
+}
+
+fq_kv_pages pages(PyObject* ko, PyObject* vo, const at::Tensor& like, int64_t kv_heads, int64_t head_dim) {
+    const at::Tensor &k = tensor(ko), &v = tensor(vo);
+    for (const at::Tensor* t : {&k, &v})
+        require(t->dim() == 4 && t->scalar_type() == like.scalar_type() && t->device() == like.device() && t->stride(3) == 1 &&
+                t->size(2) == kv_heads && t->size(3) == head_dim);
+    require(k.sizes() == v.sizes() && k.strides() == v.strides() && k.size(1) <= INT_MAX);
+    return {k.data_ptr(), v.data_ptr(), k.size(0), (int)k.size(1), k.stride(0), k.stride(1), k.stride(2)};
+}
+
+fq_heads heads(const at::Tensor& t) {
+    require(t.dim() == 3 && t.stride(2) == 1 && t.size(1) <= INT_MAX && t.size(2) <= INT_MAX);
+    return {t.data_ptr(), t.stride(0), t.stride(1)};
+}
+
+// qk_norm_rope(qkv, heads, kv_heads, table, positions, q_weight, k_weight, eps, interleaved, q_out, k_out, k_cache, v_cache, slots)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 14);
+        const at::Tensor& qkv = tensor(a[0]);
+        const int hq = integer(a[1]), hk = integer(a[2]), act = type16(qkv.scalar_type());
+        require(qkv.dim() == 2 && hq > 0 && hk > 0 && qkv.stride(1) == 1 && qkv.size(1) % ((int64_t)hq + 2 * (int64_t)hk) == 0);
+        const int64_t tokens = qkv.size(0), D = qkv.size(1) / ((int64_t)hq + 2 * (int64_t)hk);
+        require(tokens > 0 && D <= INT_MAX);
+        const void* weight[2] = {};
+        for (int i = 0; i < 2; ++i)
+            if (a[5 + i] != Py_None) {
+                const at::Tensor& w = plain(a[5 + i], qkv.scalar_type(), qkv);
+                require(w.numel() == D);
+                weight[i] = w.data_ptr();
+            }
+        const float* table = nullptr;
+        const int32_t* positions = nullptr;
+        int64_t rows = 0, rot = 0;
+        if (a[3] != Py_None) {
+            const at::Tensor &t = plain(a[3], at::kFloat, qkv), &p = plain(a[4], at::kInt, qkv);
+            require(t.dim() == 2 && p.numel() == tokens && t.size(1) > 0 && t.size(1) <= INT_MAX);
+            table = (const float*)t.data_ptr();
+            positions = (const int32_t*)p.data_ptr();
+            rows = t.size(0);
+            rot = t.size(1);
+        }
+        fq_kv_pages cache = {};
+        const int64_t* slots = nullptr;
+        const bool cached = a[11] != Py_None;
+        require(cached == (a[12] != Py_None) && cached == (a[13] != Py_None));
+        if (cached) {
+            cache = pages(a[11], a[12], qkv, hk, D);
+            const at::Tensor& s = plain(a[13], at::kLong, qkv);
+            require(s.numel() == tokens);
+            slots = (const int64_t*)s.data_ptr();
+        }
+        const float eps = (float)number(a[7]);
+        const int interleaved = truth(a[8]);
+        at::Tensor q = output(a[9], {tokens, hq, D}, qkv), k;
+        const bool keys = !cached || a[10] != Py_None;
+        if (keys) k = output(a[10], {tokens, hk, D}, qkv);
+        const void* from = qkv.data_ptr();
+        const int64_t stride = qkv.stride(0);
+        void *qp = q.data_ptr(), *kp = keys ? k.data_ptr() : nullptr, *s = stream();
+        call("fq_qk_norm_rope", [&] {
+            return lib.qk_norm_rope(from, act, tokens, stride, hq, hk, (int)D, weight[0], weight[1], eps, table, rows, (int)rot, interleaved, positions, qp,
+                                    kp, cached ? &cache : nullptr, slots, s);
+        });
+        PyObject* first = result(a[9], std::move(q));
+        if (keys) return Py_BuildValue("(NN)", first, result(a[10], std::move(k)));
+        return Py_BuildValue("(NO)", first, Py_None);
+    });
+}
+
+// host offsets of up to 1024 sequences, as int32
+struct offsets32 {
+    int32_t at[1025];
+    int count = 0;
+    explicit offsets32(PyObject* o) {
+        require(PyList_CheckExact(o) || PyTuple_CheckExact(o));
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+        require(n >= 1 && n <= 1025);
+        for (Py_ssize_t i = 0; i < n; ++i) at[i] = integer(PySequence_Fast_GET_ITEM(o, i));
+        count = (int)n;
+    }
+};
+
+// a scale that was given; 0 for the library's own
+float given_scale(PyObject* o) {
+    if (o == Py_None) return 0.0f;
+    const float x = (float)number(o);
+    require(x > 0.0f);
+    return x;
+}
+
+// a caller's workspace where it is large enough, or a new one of `need` bytes
+void* scratch_of(PyObject* o, const at::Tensor& like, size_t need, size_t* size, at::Tensor* own) {
+    if (o != Py_None) {
+        const at::Tensor& t = tensor(o);
+        *size = (size_t)t.numel() * t.element_size();
+        if (*size >= need) return t.data_ptr();
+    }
+    *size = need;
+    if (need == 0) return nullptr;
+    *own = empty({(int64_t)need}, at::kByte, like);
+    return own->data_ptr();
+}
+
+// attention_prompt(q, k, v, q_offsets, k_offsets, scale, out, workspace)
+PyObject* attention_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 8);
+        const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
+        const int act = type16(q.scalar_type());
+        const fq_heads qh = heads(q), kh = heads(k), vh = heads(v);
+        for (const at::Tensor* t : {&k, &v})
+            require(t->sizes() == k.sizes() && t->size(2) == q.size(2) && t->scalar_type() == q.scalar_type() && t->device() == q.device());
+        const int hq = (int)q.size(1), hk = (int)k.size(1), D = (int)q.size(2);
+        const offsets32 qo(a[3]);
+        const bool own_keys = a[4] != Py_None;
+        const offsets32 ko(own_keys ? a[4] : a[3]);
+        require(ko.count == qo.count && qo.at[qo.count - 1] == q.size(0) && ko.at[ko.count - 1] == k.size(0));
+        const int32_t* kp = own_keys ? ko.at : nullptr;
+        const float scale = given_scale(a[5]);
+        at::Tensor out = output(a[6], q.sizes(), q), own;
+        size_t size = 0;
+        void* ws = scratch_of(a[7], q, lib.attention_prompt_workspace_bytes(hq, hk, D, qo.at, kp, qo.count - 1), &size, &own);
+        void *op = out.data_ptr(), *s = stream();
+        call("fq_attention_prompt",
+             [&] { return lib.attention_prompt(&qh, &kh, &vh, act, hq, hk, D, qo.at, kp, qo.count - 1, scale, op, ws, size, s); });
+        return result(a[6], std::move(out));
+    });
+}
+
+// attention_tree(q, k_cache, v_cache, page_table, context_lens, mask, scale, out, workspace)
+PyObject* attention_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 9);
+        const at::Tensor& q = tensor(a[0]);
+        const int act = type16(q.scalar_type());
+        require(q.dim() == 4 && q.stride(3) == 1);
+        const int64_t B = q.size(0), nodes = q.size(1), hq = q.size(2), D = q.size(3);
+        require((q.stride(0) == nodes * q.stride(1) || B <= 1) && hq <= INT_MAX && D <= INT_MAX);
+        const at::Tensor& kc = tensor(a[1]);
+        const int64_t hk = kc.dim() == 4 ? kc.size(2) : 0;
+        require(hk <= INT_MAX);
+        const fq_kv_pages cache = pages(a[1], a[2], q, hk, D);
+        const at::Tensor &table = plain(a[3], at::kInt, q), &lens = plain(a[4], at::kInt, q);
+        require(table.dim() == 2 && table.size(0) == B && lens.numel() == B);
+        const uint64_t* mask = nullptr;
+        int64_t stride = 0;
+        if (a[5] != Py_None) {
+            const at::Tensor& m = plain(a[5], at::kLong, q);
+            const int64_t words = (nodes + 63) / 64;
+            const bool shared = m.dim() == 2;
+            require(shared ? m.size(0) == nodes && m.size(1) == words : m.dim() == 3 && m.size(0) == B && m.size(1) == nodes && m.size(2) == words);
+            mask = (const uint64_t*)m.data_ptr();
+            stride = shared ? 0 : nodes * words;
+        }
+        const float scale = given_scale(a[6]);
+        at::Tensor out = output(a[7], q.sizes(), q), own;
+        size_t size = 0;
+        const int64_t width = table.size(1);
+        void* ws = scratch_of(a[8], q, lib.attention_tree_workspace_bytes(B, nodes, (int)hq, (int)hk, (int)D, width, cache.page_size), &size, &own);
+        const fq_heads qh = {q.data_ptr(), q.stride(1), q.stride(2)};
+        const int32_t *tp = (const int32_t*)table.data_ptr(), *lp = (const int32_t*)lens.data_ptr();
+        void *op = out.data_ptr(), *s = stream();
+        call("fq_attention_tree", [&] {
+            return lib.attention_tree(&qh, act, B, nodes, (int)hq, (int)hk, (int)D, &cache, tp, width, lp, mask, stride, scale, op, ws, size, s);
+        });
+        return result(a[7], std::move(out));
+    });
+}
+
 // bind(FqError, addresses of the functions of `lib`, in its order)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     constexpr Py_ssize_t count = sizeof(lib) / sizeof(void*);
@@ -273,7 +476,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FQ_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FQ_METHOD(gemm),     FQ_METHOD(gemm_grouped),  FQ_METHOD(quantize_act_i8), FQ_METHOD(gemm_w4a8),
-                         FQ_METHOD(quantize), FQ_METHOD(quantize_w4a8), FQ_METHOD(bind),            {nullptr, nullptr, 0, nullptr}};
+                         FQ_METHOD(quantize), FQ_METHOD(quantize_w4a8), FQ_METHOD(qk_norm_rope),    FQ_METHOD(attention_prompt),
+                         FQ_METHOD(attention_tree), FQ_METHOD(bind),    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fqcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -372,7 +372,9 @@ _torch_mod = _raw_stream = _device = None
 # may come after launches, it raises itself.)
 NATIVE_PATH = os.path.join(_HERE, "_fqcall.so")
 _NATIVE_FUNCTIONS = ("fq_gemm_sf", "fq_gemm_workspace_bytes", "fq_gemm_grouped_sf", "fq_gemm_w4a8", "fq_gemm_w4a8_workspace_bytes",
-                     "fq_quantize_act_i8", "fq_quantize_sf", "fq_quantize_w4a8", "fq_codes_bytes", "fq_scales_bytes", "fq_zscale_bytes")
+                     "fq_quantize_act_i8", "fq_quantize_sf", "fq_quantize_w4a8", "fq_codes_bytes", "fq_scales_bytes", "fq_zscale_bytes",
+                     "fq_qk_norm_rope", "fq_attention_prompt", "fq_attention_prompt_workspace_bytes", "fq_attention_tree",
+                     "fq_attention_tree_workspace_bytes")
 _native = None
 
 
@@ -655,6 +657,10 @@ def qk_norm_rope(qkv, heads, kv_heads, table, positions, q_weight=None, k_weight
     table (rope_table; None: not rotated).  With k_cache, v_cache [pages, page_size, kv_heads, head_dim] and slots (int64 [tokens])
     keys and values go to the cache, and k is None unless k_out is given."""
     torch = _torch_mod or _torch()
+    done = _native.qk_norm_rope(qkv, heads, kv_heads, table, positions, q_weight, k_weight, eps, interleaved, q_out, k_out, k_cache,
+                                v_cache, slots)
+    if done is not None:
+        return done
     where = "fq_qk_norm_rope"
     _require(qkv.is_cuda and qkv.dim() == 2 and heads > 0 and kv_heads > 0 and qkv.shape[1] % (heads + 2 * kv_heads) == 0, where)
     _require(qkv.stride(1) == 1, where)
@@ -693,6 +699,9 @@ def attention_prompt(q, k, v, q_offsets, k_offsets=None, scale=None, out=None, w
     any row and head strides), sequence b's rows q_offsets[b] .. q_offsets[b + 1] - 1 (host integers) and keys k_offsets[b] .. (None: the
     same) -> [rows, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given."""
     torch = _torch_mod or _torch()
+    done = _native.attention_prompt(q, k, v, q_offsets, k_offsets, scale, out, workspace)
+    if done is not None:
+        return done
     where = "fq_attention_prompt"
     act = _act_code(q)
     hq, hk, hv = _heads(q, where), _heads(k, where), _heads(v, where)
@@ -719,6 +728,9 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
     before the drafted ones, whose keys and values lie in the places behind them), mask int64 [nodes, words] or [sequences, nodes, words] (tree_mask;
     None: a chain) -> [sequences, nodes, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given."""
     torch = _torch_mod or _torch()
+    done = _native.attention_tree(q, k_cache, v_cache, page_table, context_lens, mask, scale, out, workspace)
+    if done is not None:
+        return done
     where = "fq_attention_tree"
     act = _act_code(q)
     _require(q.is_cuda and q.dim() == 4 and (q.stride(3) == 1 or q.shape[3] <= 1), where)

@@ -457,3 +457,74 @@ def test_one_token_is_the_prompts_last_row():
         got = fq.attention_tree(q[None, n - nodes:].cuda(), *caches, torch.tensor([n - nodes], dtype=torch.int32, device="cuda"))
         ref.compare(got[0], want[n - nodes:], tol[n - nodes:], "tree")
         ref.compare(whole[n - nodes:], want[n - nodes:], tol[n - nodes:], "prompt")
+
+
+# ------------------------------------------------------------------------------------------------ the native calls and the Python they stand in for
+def test_native_calls_and_python_give_the_same(monkeypatch):
+    tokens, hq, hk, D = 40, 8, 2, 64
+    qkv = _normal((tokens, (hq + 2 * hk) * D), F16, 80).cuda()
+    w = _normal((D,), F16, 81).cuda()
+    table, positions = fq.rope_table(64, D), torch.arange(tokens, dtype=torch.int32, device="cuda")
+    slots = torch.arange(tokens, device="cuda")
+    pages = torch.arange(3, dtype=torch.int32, device="cuda")[None]
+    lens = torch.tensor([tokens - 4], dtype=torch.int32, device="cuda")
+    mask = fq.tree_mask([-1, 0, 0, 1])
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+
+    def everything():
+        kc, vc = (torch.zeros((3, 16, hk, D), dtype=F16, device="cuda") for _ in range(2))
+        q, k = fq.qk_norm_rope(qkv, hq, hk, table, positions, w, w)
+        q2, none = fq.qk_norm_rope(qkv, hq, hk, table, positions, q_weight=w, k_cache=kc, v_cache=vc, slots=slots)
+        assert none is None
+        given = torch.empty_like(k)
+        assert fq.qk_norm_rope(qkv, hq, hk, None, None, k_weight=w, interleaved=True, k_out=given, k_cache=kc, v_cache=vc, slots=slots)[1] is given
+        v = qkv.view(tokens, -1, D)[:, hq + hk:]
+        out = torch.empty_like(q)
+        assert fq.attention_prompt(q, k, v, [0, 10, tokens], out=out) is out
+        p2 = fq.attention_prompt(q[:30], k, v, (0, 10, 30), (0, 10, tokens), scale=0.3, workspace=small)
+        drafted = q[tokens - 4:][None]
+        t = fq.attention_tree(drafted, kc, vc, pages, lens, mask=mask)
+        t2 = fq.attention_tree(drafted, kc, vc, pages, lens, mask=mask[None], scale=1, workspace=small)
+        return [q, k, q2, given, kc, vc, out, p2, t, t2, fq.attention_tree(drafted, kc, vc, pages, lens)]
+
+    first = everything()
+    with monkeypatch.context() as m:
+        m.setattr(fq, "_native", fq._NoNative())
+        second = everything()
+    for a, b in zip(first, second):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_torch_calls_refuse_what_does_not_fit(monkeypatch, native):
+    if not native:
+        monkeypatch.setattr(fq, "_native", fq._NoNative())
+    x = torch.zeros((8, 768), dtype=F16, device="cuda")
+    q, k = x.view(8, 6, 128), x.view(8, 6, 128)[:, :2]
+    cache = torch.zeros((2, 16, 2, 128), dtype=F16, device="cuda")
+    q4, table, lens = x.view(1, 8, 6, 128), torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    positions, rope = torch.zeros(8, dtype=torch.int32, device="cuda"), fq.rope_table(4, 128)
+    slots = torch.arange(8, device="cuda")
+    for call in (
+        lambda: fq.attention_prompt(q, k, k, [0, 7]), lambda: fq.attention_prompt(q, k, k, [0, 9]), lambda: fq.attention_prompt(q, k, k, [0, 5, 3, 8]),
+        lambda: fq.attention_prompt(q, k, k, [0, 8], [0, 4, 8]), lambda: fq.attention_prompt(q, k[:7], k, [0, 8], [0, 8]),
+        lambda: fq.attention_prompt(q, k.bfloat16(), k, [0, 8]), lambda: fq.attention_prompt(q, k, k, [0, 8], scale=-1.0),
+        lambda: fq.attention_prompt(q, k, k, [0, 8], scale=0.0), lambda: fq.attention_prompt(q, k, k, [0, 8], out=q[:, :5]),
+        lambda: fq.attention_prompt(q, k, k, [0, 8], out=q), lambda: fq.attention_prompt(q[:, :5], k, k, [0, 8]),
+        lambda: fq.attention_prompt(q[..., 1:], k[..., 1:], k[..., 1:], [0, 8]),
+        lambda: fq.attention_tree(q4, cache, cache[:1], table, lens), lambda: fq.attention_tree(q4, cache, cache.bfloat16(), table, lens),
+        lambda: fq.attention_tree(q4, cache, cache, table.long(), lens), lambda: fq.attention_tree(q4, cache, cache, table[0], lens),
+        lambda: fq.attention_tree(q4, cache, cache, table, lens.cpu()), lambda: fq.attention_tree(q4, cache, cache, table, lens, mask=slots[:4, None]),
+        lambda: fq.attention_tree(q4, cache, cache, table, lens, mask=slots.int()[:, None]), lambda: fq.attention_tree(q4, cache, cache, table, lens, scale=-1.0),
+        lambda: fq.attention_tree(q4, cache, cache, table, lens, out=q4), lambda: fq.attention_tree(x.view(1, 8, 12, 64), cache, cache, table, lens),
+        lambda: fq.qk_norm_rope(x, 2, 2, rope, None), lambda: fq.qk_norm_rope(x, 2, 2, rope, positions.long()), lambda: fq.qk_norm_rope(x, 2, 3, None, None),
+        lambda: fq.qk_norm_rope(x, 2, 2, rope, positions, k_cache=cache, v_cache=cache), lambda: fq.qk_norm_rope(x, 2, 2, rope, positions, q_weight=x[0, :64]),
+        lambda: fq.qk_norm_rope(x, 2, 2, rope, positions, k_cache=cache[:, :, :1], v_cache=cache[:, :, :1], slots=slots),
+        lambda: fq.qk_norm_rope(x, 2, 2, rope, positions, eps=-1.0), lambda: fq.qk_norm_rope(x, 2, 2, fq.rope_table(4, 136), positions),
+        lambda: fq.qk_norm_rope(x, 2, 2, rope, positions, k_cache=cache, v_cache=cache, slots=slots[:4]),
+    ):
+        with pytest.raises(fq.FqError):
+            call()
+    with pytest.raises(TypeError):
+        fq.attention_tree(q4.float(), cache, cache, table, lens)
+    torch.cuda.synchronize()
