@@ -373,8 +373,8 @@ int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_
  *   out            out  [q_offsets_host[sequences], q_heads, head_dim], act_dtype; must not overlap an input
  *   workspace           device scratch, >= fq_attention_prompt_workspace_bytes(...) bytes (may be NULL when that is 0)
  * Deterministic; asynchronous on `stream`, no allocation.  No rows, or no sequences: a valid no-op.
- * Errors: FQ_ERR_INVALID_ARG (null pointers, offsets, scale), FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, pointers or
- *         strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
+ * Errors: FQ_ERR_INVALID_ARG (null pointers, offsets, scale), FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, 2^31 - 1025 rows or keys, or 2^24
+ *         blocks of 128 rows and a head, pointers or strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
  */
 size_t fq_attention_prompt_workspace_bytes(int q_heads, int kv_heads, int head_dim, const int32_t* q_offsets_host,
                                            const int32_t* k_offsets_host, int sequences);
@@ -401,8 +401,8 @@ int fq_attention_prompt(const fq_heads* q, const fq_heads* k, const fq_heads* v,
  * Lengths and tables are read on the device when the kernels run, so that a captured call may be replayed with others; calls that
  * share a workspace must be ordered on one stream.  Deterministic; asynchronous on `stream`, no allocation.
  * sequences = 0 or nodes = 0: a valid no-op.
- * Errors: FQ_ERR_INVALID_ARG, FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, 2^20 nodes or 2^24 rows in all, table_width * page_size of 2^31 or
- *         more, pointers or strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
+ * Errors: FQ_ERR_INVALID_ARG, FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, 2^20 nodes or 2^24 rows in all, table_width * page_size above
+ *         2^31 - 1025, pointers or strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
  */
 size_t fq_attention_tree_workspace_bytes(int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,
                                          int page_size);

@@ -385,6 +385,8 @@ int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_
     return fq_launch_qk_norm_rope(act_dtype, a, (hipStream_t)stream);
 }
 
+static constexpr int32_t MOST_PLACES = INT32_MAX - 1024;
+
 static int check_offsets(const int32_t* offsets, int sequences) {
     if (offsets[0] != 0) return FQ_ERR_INVALID_ARG;
     for (int b = 0; b < sequences; ++b)
@@ -400,6 +402,8 @@ static int check_prompt(int act_dtype, int q_heads, int kv_heads, int head_dim, 
     int st = check_heads(act_dtype, q_heads, kv_heads, head_dim);
     if (st != FQ_OK) return st;
     if (sequences > 65536) return FQ_ERR_UNSUPPORTED;
+    // (the kernels count up to a few tiles behind the last row)
+    if (q_offsets[sequences] > MOST_PLACES || k_offsets[sequences] > MOST_PLACES) return FQ_ERR_UNSUPPORTED;
     st = check_offsets(q_offsets, sequences);
     if (st == FQ_OK && k_offsets != q_offsets) st = check_offsets(k_offsets, sequences);
     if (st != FQ_OK) return st;
@@ -459,7 +463,7 @@ static int check_tree(int act_dtype, int64_t sequences, int64_t nodes, int q_hea
     if (sequences < 0 || nodes < 0 || table_width < 0 || page_size <= 0) return FQ_ERR_INVALID_ARG;
     const int st = check_heads(act_dtype, q_heads, kv_heads, head_dim);
     if (st != FQ_OK) return st;
-    if (sequences > 65536 || nodes > 1 << 20 || sequences * nodes > 1 << 24 || table_width > INT32_MAX / page_size) return FQ_ERR_UNSUPPORTED;
+    if (sequences > 65536 || nodes > 1 << 20 || sequences * nodes > 1 << 24 || table_width > MOST_PLACES / page_size) return FQ_ERR_UNSUPPORTED;
     a->sequences = sequences;
     a->nodes = (int)nodes;
     a->q_heads = q_heads;

@@ -10,7 +10,6 @@ namespace {
 
 using namespace fqa;
 
-constexpr int TILE = ROWS;           // queries per block
 constexpr int SEQUENCES = 128;       // per launch: their table is a kernel argument
 
 // The sequences of a launch, longest first, and the order of their query tiles: the last tiles of the longest sequences, which
@@ -35,24 +34,37 @@ __device__ inline void find_tile(const prompt_items& items, int rank, int* seque
     *tile = items.tiles[s] - 1 - level;
 }
 
+// What the host has made of a launch.
+struct prompt_plan {
+    int q_heads, group, D;
+    float factor;
+    int splits;                      // pieces that a query tile's keys are cut into
+    float* slots;                    // one per query tile, head and piece: [ROWS][D] sums, [ROWS] maxima (log2), [ROWS] sums of numerators
+
+    __host__ __device__ int64_t slot_floats() const { return (int64_t)ROWS * (D + 2); }
+    __device__ float* slot(int tile_of_head, int piece) const { return slots + ((int64_t)tile_of_head * splits + piece) * slot_floats(); }
+};
+
 template <int ACT, int DP>
-__global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q, fq_heads k, fq_heads v, int q_heads, int group, int D,
-                                                                     float factor, uint16_t* out, prompt_items items) {
+__global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q, fq_heads k, fq_heads v, prompt_plan p, uint16_t* out,
+                                                                     prompt_items items) {
     typedef tile_shape<DP> SH;
     extern __shared__ __align__(16) char lds[];
+    const int unit = blockIdx.x / p.splits, piece = blockIdx.x - unit * p.splits;      // query tile and head; piece of its keys
+    const int rank = unit / p.q_heads, h = unit - rank * p.q_heads, D = p.D;
     int sequence, tile;
-    find_tile(items, blockIdx.x / q_heads, &sequence, &tile);
-    const int h = blockIdx.x % q_heads;
+    find_tile(items, rank, &sequence, &tile);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int queries = items.q_len[sequence], keys = items.k_len[sequence];
     const int first = tile * ROWS + wave * 32, i = first + (lane & 31);       // the wave's first query; the lane's
     packed_rows rows;
-    rows.k = (const uint16_t*)k.data + items.k_start[sequence] * k.row_stride + h / group * k.head_stride;
-    rows.v = (const uint16_t*)v.data + items.k_start[sequence] * v.row_stride + h / group * v.head_stride;
+    rows.k = (const uint16_t*)k.data + items.k_start[sequence] * k.row_stride + h / p.group * k.head_stride;
+    rows.v = (const uint16_t*)v.data + items.k_start[sequence] * v.row_stride + h / p.group * v.head_stride;
     rows.k_stride = k.row_stride;
     rows.v_stride = v.row_stride;
     const int ahead = keys - queries;        // query i sees keys 0 .. i + ahead
-    const int tiles = (min(queries, (tile + 1) * ROWS) + ahead + KEYS - 1) / KEYS;      // of keys that the block's last query sees
+    const int all = max(0, (min(queries, (tile + 1) * ROWS) + ahead + KEYS - 1) / KEYS);      // tiles of keys that the block's last query sees
+    const int t0 = (int)((int64_t)all * piece / p.splits), t1 = (int)((int64_t)all * (piece + 1) / p.splits);
 
     // units of a head that no load fills are zeros from here on
     constexpr int TILE_BYTES = 2 * SH::BYTES;      // of keys, or of values
@@ -76,89 +88,135 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
     };
     wave_state<ACT, DP> w;
     w.clear();
-    if (tiles > 0) load(0, 0);
+    if (t0 < t1) load(t0, 0);
     const int64_t row = (int64_t)items.q_start[sequence] + min(i, queries - 1);
     const uint16_t* query = (const uint16_t*)q.data + row * q.row_stride + h * q.head_stride;
     w.load_query(query, D);
     const int end = i + 1 + ahead;           // keys that the lane's query sees
-    for (int t = 0; t < tiles; ++t) {
+    for (int t = t0; t < t1; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (t + 1 < tiles) load(t + 1, (t + 1) & 1);
+        const int buffer = (t - t0) & 1;
+        if (t + 1 < t1) load(t + 1, buffer ^ 1);
         const int base = t * KEYS;
         if (first < queries && base < first + 32 + ahead) {
-            const char* at = lds + (t & 1) * 2 * TILE_BYTES;
+            const char* at = lds + buffer * 2 * TILE_BYTES;
             f32x16 s[2];
-            u32x4 p[4];
+            u32x4 x[4];
             w.template scores<2>(at, s);
             if (base + KEYS > first + 1 + ahead) {
                 keep_seen(s[0], low_bits(end - base));
                 keep_seen(s[1], low_bits(end - base - HALF));
             }
-            w.template soften<2>(s, factor, p);
-            w.template accumulate<2>(at + TILE_BYTES, p);
+            w.template soften<2>(s, p.factor, x);
+            w.template accumulate<2>(at + TILE_BYTES, x);
         }
     }
-    const float l = w.l = other_half_sum(w.l);
+    w.l = other_half_sum(w.l);
+    float* slot = p.splits > 1 ? p.slot(unit, piece) : nullptr;
     if (!w.finite()) {
         for (int x = 0; x < 32 && first + x < queries; ++x) {
             const int64_t r = (int64_t)items.q_start[sequence] + first + x;
-            const int sees = max(0, first + x + 1 + ahead);
-            float o[2], m, sum;
-            attend_one<ACT>((const uint16_t*)q.data + r * q.row_stride + h * q.head_stride, rows, sees_first{sees}, 0, sees, D, factor, o, &m, &sum);
-            store_one<ACT>(out + (r * q_heads + h) * D, o, sum, D);
+            const int sees = first + x + 1 + ahead;
+            float o[2], c, sum;
+            attend_one<ACT>((const uint16_t*)q.data + r * q.row_stride + h * q.head_stride, rows, sees_first{sees}, t0 * KEYS, min(sees, t1 * KEYS), D,
+                            p.factor, o, &c, &sum);
+            put_one<ACT>(out + (r * p.q_heads + h) * D, slot, ROWS, wave * 32 + x, o, c, sum, D);
         }
     } else if (i < queries) {
-        const float r = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
-        uint16_t* to = out + (row * q_heads + h) * D;
-        w.quads([&](int d, int x, int t) {
-            const f32x16& o = w.o[t];
-            const u32x2 v = {pack2<ACT>(o[x] * r, o[x + 1] * r), pack2<ACT>(o[x + 2] * r, o[x + 3] * r)};
-            if (d < D) *(u32x2*)(to + d) = v;
-        });
+        w.put(out + (row * p.q_heads + h) * D, slot, ROWS, wave * 32 + (lane & 31), D);
+    }
+}
+
+// Joins the pieces of a query tile: a lane has four values of a row, a wave two rows at a time.
+template <int ACT>
+__global__ __launch_bounds__(256) void fq_attention_prompt_join_kernel(prompt_plan p, uint16_t* out, prompt_items items) {
+    const int unit = blockIdx.x, rank = unit / p.q_heads, h = unit - rank * p.q_heads, D = p.D;
+    int sequence, tile;
+    find_tile(items, rank, &sequence, &tile);
+    const int lane = threadIdx.x & 63, d = (lane & 31) * 4;
+    const int count = min(ROWS, items.q_len[sequence] - tile * ROWS);
+    for (int r = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 2 + (lane >> 5); r < count; r += 8 * gridDim.y) {
+        if (d >= D) continue;
+        partial_sums all;
+        all.clear();
+        all.add(p.slot(unit, 0), p.slot_floats(), p.splits, ROWS, r, d, D);
+        all.template store<ACT>(out + (((int64_t)items.q_start[sequence] + tile * ROWS + r) * p.q_heads + h) * D + d);
     }
 }
 
 template <int ACT, int DP>
-int launch(const fq_prompt_args& a, const prompt_items& items, int total, hipStream_t stream) {
+int launch(const fq_prompt_args& a, const prompt_plan& p, const prompt_items& items, int total, hipStream_t stream) {
     static std::atomic<uint64_t> raised{0};
     constexpr int LDS = 8 * tile_shape<DP>::BYTES;      // two tiles of keys and of values
     if (LDS > 65536) {
         const int st = fqd::raise_lds_limit((const void*)fq_attention_prompt_kernel<ACT, DP>, raised);
         if (st != FQ_OK) return st;
     }
-    fq_attention_prompt_kernel<ACT, DP><<<dim3((unsigned)(total * a.q_heads)), 256, LDS, stream>>>(
-        a.q, a.k, a.v, a.q_heads, a.q_heads / a.kv_heads, a.head_dim, a.scale * LOG2E, (uint16_t*)a.out, items);
+    fq_attention_prompt_kernel<ACT, DP><<<dim3((unsigned)(total * a.q_heads * p.splits)), 256, LDS, stream>>>(a.q, a.k, a.v, p, (uint16_t*)a.out, items);
+    if (hipGetLastError() != hipSuccess) return FQ_ERR_HIP;
+    if (p.splits == 1) return FQ_OK;
+    fq_attention_prompt_join_kernel<ACT><<<dim3((unsigned)(total * a.q_heads), 4), 256, 0, stream>>>(p, (uint16_t*)a.out, items);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
 template <int ACT>
-int launch(const fq_prompt_args& a, const prompt_items& items, int total, hipStream_t stream) {
-    if (a.head_dim <= 64) return launch<ACT, 64>(a, items, total, stream);
-    if (a.head_dim <= 96) return launch<ACT, 96>(a, items, total, stream);
-    return launch<ACT, 128>(a, items, total, stream);
+int launch(const fq_prompt_args& a, const prompt_plan& p, const prompt_items& items, int total, hipStream_t stream) {
+    if (a.head_dim <= 64) return launch<ACT, 64>(a, p, items, total, stream);
+    if (a.head_dim <= 96) return launch<ACT, 96>(a, p, items, total, stream);
+    return launch<ACT, 128>(a, p, items, total, stream);
+}
+
+// Query tiles of sequences first .. first + n - 1, and the most key tiles that one of them has.
+void count_tiles(const fq_prompt_args& a, int first, int n, int64_t* total, int* longest) {
+    *total = 0;
+    *longest = 0;
+    for (int b = first; b < first + n; ++b) {
+        const int queries = a.q_offsets[b + 1] - a.q_offsets[b], keys = a.k_offsets[b + 1] - a.k_offsets[b];
+        *total += (queries + ROWS - 1) / ROWS;
+        if (queries > 0) *longest = std::max(*longest, (keys + KEYS - 1) / KEYS);
+    }
+}
+
+// Pieces for the keys of a launch's query tiles: as many as bring the blocks up to the number that run at once, of eight key tiles
+// and more (a piece's sums are written and read again, which costs as much as two tiles, and joining them is a launch).
+int plan_splits(const fq_prompt_args& a, int64_t total, int longest) {
+    const int64_t units = total * a.q_heads, room = 2 * fq_cu_count();
+    if (units == 0 || units * 2 > room) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(2 * room / units, longest / 8));
 }
 
 }  // namespace
 
 size_t fq_prompt_bytes(const fq_prompt_args& a) {
-    (void)a;
-    return 0;
+    size_t most = 0;
+    for (int first = 0; first < a.sequences; first += SEQUENCES) {
+        int64_t total;
+        int longest;
+        count_tiles(a, first, std::min(SEQUENCES, a.sequences - first), &total, &longest);
+        const int splits = plan_splits(a, total, longest);
+        if (splits > 1) most = std::max(most, (size_t)(total * a.q_heads * splits) * ROWS * (a.head_dim + 2) * sizeof(float));
+    }
+    return most;
 }
 
 int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* workspace, hipStream_t stream) {
-    (void)workspace;
     for (int first = 0; first < a.sequences; first += SEQUENCES) {
         const int n = std::min(SEQUENCES, a.sequences - first);
+        int64_t total;
+        int longest;
+        count_tiles(a, first, n, &total, &longest);
+        if (total == 0) continue;
+        prompt_plan p = {a.q_heads, a.q_heads / a.kv_heads, a.head_dim, a.scale * LOG2E, plan_splits(a, total, longest), (float*)workspace};
+        if (total * a.q_heads >= 1 << 24) return FQ_ERR_UNSUPPORTED;      // (2^32 threads)
         int order[SEQUENCES], tiles[SEQUENCES];
         for (int i = 0; i < n; ++i) {
             order[i] = i;
-            tiles[i] = (a.q_offsets[first + i + 1] - a.q_offsets[first + i] + TILE - 1) / TILE;
+            tiles[i] = (a.q_offsets[first + i + 1] - a.q_offsets[first + i] + ROWS - 1) / ROWS;
         }
         std::sort(order, order + n, [&](int x, int y) { return tiles[x] != tiles[y] ? tiles[x] > tiles[y] : x < y; });
         prompt_items items = {};
         items.count = n;
-        int total = 0;
         for (int s = 0; s < n; ++s) {
             const int b = first + order[s];
             items.q_start[s] = a.q_offsets[b];
@@ -168,13 +226,11 @@ int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* wor
             items.tiles[s] = tiles[order[s]];
         }
         // levels from the longest sequence's last tile down: those that sequences 0 .. s have and s + 1 has not
-        for (int s = 0; s < n; ++s) {
-            items.before[s] = total;
-            total += (s + 1) * (items.tiles[s] - (s + 1 < n ? items.tiles[s + 1] : 0));
+        for (int s = 0, before = 0; s < n; ++s) {
+            items.before[s] = before;
+            before += (s + 1) * (items.tiles[s] - (s + 1 < n ? items.tiles[s + 1] : 0));
         }
-        if (total == 0) continue;
-        if ((int64_t)total * a.q_heads >= 1 << 24) return FQ_ERR_UNSUPPORTED;      // (2^32 threads)
-        const int st = act_dtype == FQ_F16 ? launch<FQ_F16>(a, items, total, stream) : launch<FQ_BF16>(a, items, total, stream);
+        const int st = act_dtype == FQ_F16 ? launch<FQ_F16>(a, p, items, (int)total, stream) : launch<FQ_BF16>(a, p, items, (int)total, stream);
         if (st != FQ_OK) return st;
     }
     return FQ_OK;

@@ -110,6 +110,64 @@ struct tile_shape {
     static constexpr int TILES = DP / 32;                     // of the second
 };
 
+// Sums that are not a query's whole result are left in slots: [slot_rows][D] sums, not divided, then [slot_rows] maxima that they are
+// relative to (log2; -infinity: no key seen) and [slot_rows] sums of numerators.
+__device__ inline void put_stats(float* slot, int slot_rows, int r, int D, float c, float l) {
+    slot[slot_rows * D + r] = c;
+    slot[slot_rows * (D + 1) + r] = l;
+}
+// attend_one's result, or its sums to row r of a slot
+template <int ACT>
+__device__ inline void put_one(uint16_t* out, float* slot, int slot_rows, int r, const float* o, float c, float l, int D) {
+    const int lane = threadIdx.x & 63;
+    if (!slot) return store_one<ACT>(out, o, l, D);
+    if (2 * lane < D) slot[r * D + 2 * lane] = o[0], slot[r * D + 2 * lane + 1] = o[1];
+    if (lane == 0) put_stats(slot, slot_rows, r, D, c, l);
+}
+
+// Values d .. d + 3 of a row, joined from slots.
+struct partial_sums {
+    float c, l;
+    f32x4 o;
+    __device__ void clear() {
+        c = -__builtin_inff();
+        l = 0.0f;
+        o = {0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    __device__ void add(float c1, float l1, const f32x4& o1) {
+        const float top = __builtin_fmaxf(c, c1), base = top == -__builtin_inff() ? 0.0f : top;
+        const float mine = __builtin_amdgcn_exp2f(c - base), its = __builtin_amdgcn_exp2f(c1 - base);
+        c = top;
+        l = l * mine + l1 * its;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = o[i] * mine + o1[i] * its;
+    }
+    // row r of `count` slots that lie `stride` values apart, in their order, eight of them on their way at once
+    __device__ void add(const float* slot, int64_t stride, int count, int slot_rows, int r, int d, int D) {
+        constexpr int BATCH = 8;
+        for (int n = 0; n < count; n += BATCH) {
+            float c1[BATCH], l1[BATCH];
+            f32x4 o1[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const float* from = slot + min(n + i, count - 1) * stride;
+                c1[i] = from[slot_rows * D + r];
+                l1[i] = from[slot_rows * (D + 1) + r];
+                o1[i] = *(const f32x4*)(from + r * D + d);
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (n + i < count) add(c1[i], l1[i], o1[i]);
+        }
+    }
+    template <int ACT>
+    __device__ void store(uint16_t* out) const {
+        const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+        const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+        *(u32x2*)out = z;
+    }
+};
+
 // One wave's state: 32 queries (lane l: query l % 32; the wave's halves hold the same queries)
 template <int ACT, int DP>
 struct wave_state {
@@ -223,6 +281,22 @@ struct wave_state {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x = __builtin_fmaf(o[t][i], 0.0f, x);
         return __all(x == 0.0f);
+    }
+
+    // The lane's query's result, or its sums to row r of a slot.
+    __device__ __forceinline__ void put(uint16_t* out, float* slot, int slot_rows, int r, int D) const {
+        const float scale = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
+        quads([&](int d, int i, int t) {
+            if (d >= D) return;
+            if (!slot) {
+                const u32x2 z = {pack2<ACT>(o[t][i] * scale, o[t][i + 1] * scale), pack2<ACT>(o[t][i + 2] * scale, o[t][i + 3] * scale)};
+                *(u32x2*)(out + d) = z;
+            } else {
+                const f32x4 z = {o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+                *(f32x4*)(slot + r * D + d) = z;
+            }
+        });
+        if (slot && (threadIdx.x & 32) == 0) put_stats(slot, slot_rows, r, D, top(), l);
     }
 
     // f(d, i, t): the lane's results i .. i + 3 of block t are values d .. d + 3 of its query

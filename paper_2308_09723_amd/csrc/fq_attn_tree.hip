@@ -161,36 +161,8 @@ struct unit_rows {
         for (int r = from; r < to; r += step) {
             float o[2], c, l;
             one<ACT>(r, begin, end, o, &c, &l);
-            if (!slot) {
-                store_one<ACT>(result(r), o, l, a.head_dim);
-            } else {
-                if (2 * lane < a.head_dim) slot[r * a.head_dim + 2 * lane] = o[0], slot[r * a.head_dim + 2 * lane + 1] = o[1];
-                if (lane == 0) put_stats(slot, r, c, l);
-            }
+            put_one<ACT>(result(r), slot, p.slot_rows, r, o, c, l, a.head_dim);
         }
-    }
-    __device__ void put_stats(float* slot, int r, float c, float l) const {
-        slot[p.slot_rows * a.head_dim + r] = c;
-        slot[p.slot_rows * (a.head_dim + 1) + r] = l;
-    }
-    // the lane's row r of a wave's sums
-    template <int ACT, int DP>
-    __device__ __forceinline__ void put(const wave_state<ACT, DP>& w, float* slot, int r) const {
-        const float scale = w.l == 0.0f ? 0.0f : 1.0f / w.l;       // (no key seen: zeros)
-        const int D = a.head_dim;
-        uint16_t* to = result(r);
-        w.quads([&](int d, int i, int t) {
-            const f32x16& o = w.o[t];
-            if (d >= D) return;
-            if (!slot) {
-                const u32x2 z = {pack2<ACT>(o[i] * scale, o[i + 1] * scale), pack2<ACT>(o[i + 2] * scale, o[i + 3] * scale)};
-                *(u32x2*)(to + d) = z;
-            } else {
-                const f32x4 z = {o[i], o[i + 1], o[i + 2], o[i + 3]};
-                *(f32x4*)(slot + r * D + d) = z;
-            }
-        });
-        if (slot && (threadIdx.x & 32) == 0) put_stats(slot, r, w.top(), w.l);
     }
 };
 
@@ -291,7 +263,7 @@ __device__ __forceinline__ void join_parts(const unit_rows& rows, const wave_sta
                 *(u32x2*)(rows.result(at) + d) = z;
             } else {
                 *(f32x4*)(slot + at * D + d) = o;
-                if (d == 0) rows.put_stats(slot, at, c, l);
+                if (d == 0) put_stats(slot, rows.p.slot_rows, at, D, c, l);
             }
         }
     }
@@ -405,7 +377,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         w.l = other_half_sum(w.l);
         if constexpr (PARTS == 1) {
             if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
-            else if ((lane & 31) < rows.count) rows.put(w, slot, row);
+            else if ((lane & 31) < rows.count) w.put(rows.result(row), slot, p.slot_rows, row, D);
         } else {
             join_parts<ACT, DP, PARTS>(rows, w, lds, WAVE_BYTES, stats, head, HEADS, part_of, 0, key0, key1, slot);
         }
@@ -513,7 +485,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
             join_parts<ACT, DP, PARTS>(rows, w, lds, JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
         } else {
             if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
-            else if (r < rows.count) rows.put(w, slot, r);
+            else if (r < rows.count) w.put(rows.result(r), slot, p.slot_rows, r, D);
         }
         pos += t1 - t0;
         t0 = 0;
@@ -548,51 +520,28 @@ __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_arg
         const int row = base + (many ? 0 : 2 * wave) + (lane >> 5), head = row / p.slot_rows, r = row - head * p.slot_rows;
         const unit_rows rows(a, p, b, u, min(head, p.heads - 1));
         const bool there = head < p.heads && r < rows.count && d < D;
-        float c = -__builtin_inff(), l = 0.0f;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        auto add = [&](float c1, float l1, const f32x4& o1) {
-            const float top = __builtin_fmaxf(c, c1), base = top == -__builtin_inff() ? 0.0f : top;
-            const float mine = __builtin_amdgcn_exp2f(c - base), its = __builtin_amdgcn_exp2f(c1 - base);
-            c = top;
-            l = l * mine + l1 * its;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = o[i] * mine + o1[i] * its;
-        };
+        partial_sums all_pieces;
+        all_pieces.clear();
         if (there) {
-            const int64_t stride = 2 * p.heads * p.slot_floats(D);       // from block to block
-            const float* first = p.slot(from, true, head, D);
-            const int n0 = mine * share, n1 = min((int)(to - from) + 1, n0 + share);
-            constexpr int BATCH = 8;                        // pieces on their way at once
-            for (int n = n0; n < n1; n += BATCH) {
-                float c1[BATCH], l1[BATCH];
-                f32x4 o1[BATCH];
-#pragma unroll
-                for (int i = 0; i < BATCH; ++i) {
-                    const int y = min(n + i, n1 - 1);
-                    const float* slot = y == 0 && !whole ? p.slot(from, false, head, D) : first + y * stride;
-                    c1[i] = slot[p.slot_rows * D + r];
-                    l1[i] = slot[p.slot_rows * (D + 1) + r];
-                    o1[i] = *(const f32x4*)(slot + r * D + d);
-                }
-#pragma unroll
-                for (int i = 0; i < BATCH; ++i)
-                    if (n + i < n1) add(c1[i], l1[i], o1[i]);
+            // (a unit's first piece may be its block's last one, the others are their blocks' first)
+            int n0 = mine * share;
+            const int n1 = min((int)(to - from) + 1, n0 + share);
+            if (n0 == 0 && !whole) {
+                all_pieces.add(p.slot(from, false, head, D), 0, 1, p.slot_rows, r, d, D);
+                n0 = 1;
             }
+            if (n0 < n1) all_pieces.add(p.slot(from + n0, true, head, D), 2 * p.heads * p.slot_floats(D), n1 - n0, p.slot_rows, r, d, D);
         }
         if (many) {
             __syncthreads();
-            sums[wave][lane] = o;
-            stats[wave][lane][0] = c;
-            stats[wave][lane][1] = l;
+            sums[wave][lane] = all_pieces.o;
+            stats[wave][lane][0] = all_pieces.c;
+            stats[wave][lane][1] = all_pieces.l;
             __syncthreads();
             if (wave == 0)
-                for (int y = 1; y < 4; ++y) add(stats[y][lane][0], stats[y][lane][1], sums[y][lane]);
+                for (int y = 1; y < 4; ++y) all_pieces.add(stats[y][lane][0], stats[y][lane][1], sums[y][lane]);
         }
-        if (there && (wave == 0 || !many)) {
-            const float scale = l == 0.0f ? 0.0f : 1.0f / l;
-            const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
-            *(u32x2*)(rows.result(r) + d) = z;
-        }
+        if (there && (wave == 0 || !many)) all_pieces.template store<ACT>(rows.result(r) + d);
     }
 }
 
