@@ -92,6 +92,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
     const int64_t row = (int64_t)items.q_start[sequence] + min(i, queries - 1);
     const uint16_t* query = (const uint16_t*)q.data + row * q.row_stride + h * q.head_stride;
     w.load_query(query, D);
+    w.query_is_here();
     const int end = i + 1 + ahead;           // keys that the lane's query sees
     for (int t = t0; t < t1; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

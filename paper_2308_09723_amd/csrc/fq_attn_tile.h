@@ -195,6 +195,11 @@ struct wave_state {
             q[s] = unit * 8 < D ? *(const u32x4*)(row + unit * 8) : zero;
         }
     }
+    // Waits for the query here, not at its first use in a loop, where the wait would take in the loads that the loop has under way.
+    __device__ __forceinline__ void query_is_here() {
+#pragma unroll
+        for (int s = 0; s < SH::STEPS; ++s) asm volatile("" : "+v"(q[s]));
+    }
 
     // S^T of H half-tiles of keys in LDS.  Score i of half-tile t belongs to key 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4.
     template <int H>
@@ -204,13 +209,23 @@ struct wave_state {
         for (int t = 0; t < H; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+        // keys are read AHEAD products before they are multiplied (left to itself the compiler reads them one product ahead, which
+        // has every product wait for LDS)
+        constexpr int N = SH::STEPS * H, AHEAD = N < 8 ? N : 8;
+        u32x4 k[AHEAD];
+        auto read = [&](int n) {
+            const int t = n % H, step = n / H;
+            k[n % AHEAD] = *(const u32x4*)(keys + t * SH::BYTES + row * SH::PITCH + key_unit<SH::UNITS>(row, 2 * step + half) * 16);
+        };
 #pragma unroll
-        for (int step = 0; step < SH::STEPS; ++step)
+        for (int n = 0; n < AHEAD; ++n) read(n);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < H; ++t) {
-                const u32x4 k = *(const u32x4*)(keys + t * SH::BYTES + row * SH::PITCH + key_unit<SH::UNITS>(row, 2 * step + half) * 16);
-                s[t] = mfma32<ACT>(k, q[step], s[t]);
-            }
+        for (int n = 0; n < N; ++n) {
+            s[n % H] = mfma32<ACT>(k[n % AHEAD], q[n / H], s[n % H]);
+            if (n + AHEAD < N) read(n + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
 
     // Numerators of the scores, in the order that accumulate() takes; maximum, sum and results brought along.

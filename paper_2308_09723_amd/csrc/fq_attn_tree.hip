@@ -319,6 +319,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         const int key0 = t0 * TILE, key1 = min(rows.keys, t1 * TILE);
         const int row = min(lane & 31, rows.count - 1);
         w.load_query(rows.query(row), D);
+        w.query_is_here();
         w.clear();
         const int most = table_keys(a, TABLE / 4, TILE);
         for (int part = key0; part < key1; part += most) {
@@ -430,6 +431,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
         const int r = group * 32 + (lane & 31), row = min(r, rows.count - 1);
         const bool busy = group * 32 < rows.count;
         w.load_query(rows.query(row), D);
+        w.query_is_here();
         w.clear();
         const int most = table_keys(a, TABLE, KEYS);
         for (int part = key0; part < key1; part += most) {
