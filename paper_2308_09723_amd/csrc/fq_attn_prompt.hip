@@ -41,6 +41,9 @@ struct prompt_plan {
     int splits;                      // pieces that a query tile's keys are cut into
     float* slots;                    // one per query tile, head and piece: [ROWS][D] sums, [ROWS] maxima (log2), [ROWS] sums of numerators
 
+    // Blocks go to the eight dies in turn: neighbouring heads, which share keys, to the same die and its cache (8192 tokens, 32 heads
+    // over 8: 518 -> 510 us, 24 ragged prompts 122 -> 113).
+    __device__ int head(int i) const { return q_heads % 8 == 0 ? i % 8 * (q_heads / 8) + i / 8 : i; }
     __host__ __device__ int64_t slot_floats() const { return (int64_t)ROWS * (D + 2); }
     __device__ float* slot(int tile_of_head, int piece) const { return slots + ((int64_t)tile_of_head * splits + piece) * slot_floats(); }
 };
@@ -50,8 +53,8 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
                                                                      prompt_items items) {
     typedef tile_shape<DP> SH;
     extern __shared__ __align__(16) char lds[];
-    const int unit = blockIdx.x / p.splits, piece = blockIdx.x - unit * p.splits;      // query tile and head; piece of its keys
-    const int rank = unit / p.q_heads, h = unit - rank * p.q_heads, D = p.D;
+    const int units = gridDim.x / p.splits, piece = blockIdx.x / units, unit = blockIdx.x - piece * units;      // piece of its keys; query tile and head
+    const int rank = unit / p.q_heads, h = p.head(unit - rank * p.q_heads), D = p.D;
     int sequence, tile;
     find_tile(items, rank, &sequence, &tile);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -77,13 +80,28 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
     constexpr int STEP = 256 / SH::UNITS;
     const int row0 = threadIdx.x / SH::UNITS, place = threadIdx.x % SH::UNITS;
     const int key_at = key_unit<SH::UNITS>(row0, place) * 8, value_at = value_unit<SH::UNITS>(row0, place) * 8;
+    // (64 rows within 32 bits of each other: scalar address and lane offset)
+    const bool near = k.row_stride < (int64_t)1 << 24 && v.row_stride < (int64_t)1 << 24;
+    const uint32_t key_off = (uint32_t)((row0 * (uint32_t)k.row_stride + key_at) * 2), value_off = (uint32_t)((row0 * (uint32_t)v.row_stride + value_at) * 2);
     auto load = [&](int t, int buffer) {
         const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + buffer * 2 * TILE_BYTES) + wave * 1024;
+        if (near && (t + 1) * KEYS <= keys) {
+            const uint16_t *key = rows.key(t * KEYS), *value = rows.value(t * KEYS);
+            if (key_at < D) {
 #pragma unroll
-        for (int j = 0; j < TILE_BYTES / 4096; ++j) {
-            const int row = min(t * KEYS + row0 + j * STEP, keys - 1);
-            if (key_at < D) load_lds16(to + j * 4096, rows.key(row) + key_at);
-            if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, rows.value(row) + value_at);
+                for (int j = 0; j < TILE_BYTES / 4096; ++j) load_lds16<false>(to + j * 4096, key + j * STEP * k.row_stride, key_off);
+            }
+            if (value_at < D) {
+#pragma unroll
+                for (int j = 0; j < TILE_BYTES / 4096; ++j) load_lds16<false>(to + TILE_BYTES + j * 4096, value + j * STEP * v.row_stride, value_off);
+            }
+        } else {                                // (no row behind the last: what lies there may be anything)
+#pragma unroll 1
+            for (int j = 0; j < TILE_BYTES / 4096; ++j) {
+                const int row = min(t * KEYS + row0 + j * STEP, keys - 1);
+                if (key_at < D) load_lds16(to + j * 4096, rows.key(row) + key_at);
+                if (value_at < D) load_lds16(to + TILE_BYTES + j * 4096, rows.value(row) + value_at);
+            }
         }
     };
     wave_state<ACT, DP> w;
@@ -132,7 +150,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
 // Joins the pieces of a query tile: a lane has four values of a row, a wave two rows at a time.
 template <int ACT>
 __global__ __launch_bounds__(256) void fq_attention_prompt_join_kernel(prompt_plan p, uint16_t* out, prompt_items items) {
-    const int unit = blockIdx.x, rank = unit / p.q_heads, h = unit - rank * p.q_heads, D = p.D;
+    const int unit = blockIdx.x, rank = unit / p.q_heads, h = p.head(unit - rank * p.q_heads), D = p.D;
     int sequence, tile;
     find_tile(items, rank, &sequence, &tile);
     const int lane = threadIdx.x & 63, d = (lane & 31) * 4;

@@ -9,6 +9,8 @@
 //
 // Running maximum: numerators are taken relative to a maximum that is renewed only when a score exceeds it by 2^8 (times
 // factor), so that most tiles leave the sums alone.  The numerators are at most 2^8 then, which binary16 holds with the same relative error.
+// bfloat16 numerators may be as large as binary32's: there the maximum of a tile is not even looked for until the numerators' sum
+// has passed 2^60 (8192 tokens: 518 -> 508 us); one that passes 2^128 within a tile shows in the result, and the queries are computed one by one.
 //
 // What a query does not see has weight zero in the products, and zero times an infinity or a NaN is a NaN: a wave whose
 // results are not finite computes its queries again, one by one and seen keys alone (attend_one).
@@ -174,6 +176,7 @@ struct wave_state {
     typedef tile_shape<DP> SH;
     u32x4 q[SH::STEPS];
     f32x16 o[SH::TILES];
+    bool stale;          // whether the next tile's maximum is looked for (bfloat16)
     float m, c, l;       // maximum that the numerators are relative to (raw scores), the same times factor (0: none yet), this lane's sum
 
     __device__ __forceinline__ void clear() {
@@ -181,6 +184,7 @@ struct wave_state {
         for (int t = 0; t < SH::TILES; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+        stale = true;
         m = -__builtin_inff();
         c = l = 0.0f;
     }
@@ -231,20 +235,22 @@ struct wave_state {
     // Numerators of the scores, in the order that accumulate() takes; maximum, sum and results brought along.
     template <int H>
     __device__ __forceinline__ void soften(f32x16 (&s)[H], float factor, u32x4 (&p)[2 * H]) {
-        float top = s[0][0];
+        if (ACT == FQ_F16 || stale) {
+            float top = s[0][0];
 #pragma unroll
-        for (int i = 1; i < 16 * H; ++i) top = __builtin_fmaxf(top, s[i >> 4][i & 15]);
-        top = other_half_max(top);
-        if (__any(top * factor > m * factor + 8.0f)) {
-            const float now = __builtin_fmaxf(m, top), next = now == -__builtin_inff() ? 0.0f : now * factor;
-            const float again = __builtin_amdgcn_exp2f(m * factor - next);       // (0 where there was none)
-            m = now;
-            c = next;
-            l *= again;
+            for (int i = 1; i < 16 * H; ++i) top = __builtin_fmaxf(top, s[i >> 4][i & 15]);
+            top = other_half_max(top);
+            if (__any(top * factor > m * factor + 8.0f)) {
+                const float now = __builtin_fmaxf(m, top), next = now == -__builtin_inff() ? 0.0f : now * factor;
+                const float again = __builtin_amdgcn_exp2f(m * factor - next);       // (0 where there was none)
+                m = now;
+                c = next;
+                l *= again;
 #pragma unroll
-            for (int t = 0; t < SH::TILES; ++t)
+                for (int t = 0; t < SH::TILES; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][i] *= again;
+                    for (int i = 0; i < 16; ++i) o[t][i] *= again;
+            }
         }
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -257,7 +263,9 @@ struct wave_state {
 #pragma unroll
             for (int i = 0; i < 16; i += 2) p[2 * t + i / 8][i / 2 % 4] = pack2<ACT>(s[t][i], s[t][i + 1]);
         }
-        l += sum[0] + sum[1];
+        const float both = sum[0] + sum[1];
+        l += both;
+        if (ACT == FQ_BF16) stale = __any(both > 0x1p60f || m == -__builtin_inff());
     }
 
     // O^T += V^T P^T over H half-tiles of values in LDS.  V^T: lane l takes column l % 32 of 32; a transposed read hands each lane
