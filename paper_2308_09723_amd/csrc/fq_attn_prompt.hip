@@ -41,9 +41,21 @@ struct prompt_plan {
     int splits;                      // pieces that a query tile's keys are cut into
     float* slots;                    // one per query tile, head and piece: [ROWS][D] sums, [ROWS] maxima (log2), [ROWS] sums of numerators
 
-    // Blocks go to the eight dies in turn: neighbouring heads, which share keys, to the same die and its cache (8192 tokens, 32 heads
-    // over 8: 518 -> 510 us, 24 ragged prompts 122 -> 113).
-    __device__ int head(int i) const { return q_heads % 8 == 0 ? i % 8 * (q_heads / 8) + i / 8 : i; }
+    int together;                    // heads of a die that it works on at the same time
+    // Blocks go to the eight dies in turn.  Neighbouring heads, which share keys, go to the same die and its cache (8192 tokens, 32
+    // heads over 8: 518 -> 510 us, 24 ragged prompts 122 -> 113), some of them at a time where the keys of all would not stay there
+    // (96 heads, two sequences of 2048 tokens: 235 -> 223 us); within them all query tiles in the order of the items.
+    __device__ void find(int unit, int units, int* rank, int* h) const {
+        if (q_heads % 8 != 0) {
+            *rank = unit / q_heads;
+            *h = unit - *rank * q_heads;
+            return;
+        }
+        const int of_die = q_heads / 8, tiles = units / q_heads, i = unit / 8;
+        const int set = i / (tiles * together), in = i - set * tiles * together, heads = min(together, of_die - set * together);
+        *rank = in / heads;
+        *h = unit % 8 * of_die + set * together + in - *rank * heads;
+    }
     __host__ __device__ int64_t slot_floats() const { return (int64_t)ROWS * (D + 2); }
     __device__ float* slot(int tile_of_head, int piece) const { return slots + ((int64_t)tile_of_head * splits + piece) * slot_floats(); }
 };
@@ -54,8 +66,9 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
     typedef tile_shape<DP> SH;
     extern __shared__ __align__(16) char lds[];
     const int units = gridDim.x / p.splits, piece = blockIdx.x / units, unit = blockIdx.x - piece * units;      // piece of its keys; query tile and head
-    const int rank = unit / p.q_heads, h = p.head(unit - rank * p.q_heads), D = p.D;
-    int sequence, tile;
+    const int D = p.D;
+    int rank, h, sequence, tile;
+    p.find(unit, units, &rank, &h);
     find_tile(items, rank, &sequence, &tile);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int queries = items.q_len[sequence], keys = items.k_len[sequence];
@@ -150,8 +163,9 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
 // Joins the pieces of a query tile: a lane has four values of a row, a wave two rows at a time.
 template <int ACT>
 __global__ __launch_bounds__(256) void fq_attention_prompt_join_kernel(prompt_plan p, uint16_t* out, prompt_items items) {
-    const int unit = blockIdx.x, rank = unit / p.q_heads, h = p.head(unit - rank * p.q_heads), D = p.D;
-    int sequence, tile;
+    const int unit = blockIdx.x, D = p.D;
+    int rank, h, sequence, tile;
+    p.find(unit, gridDim.x, &rank, &h);
     find_tile(items, rank, &sequence, &tile);
     const int lane = threadIdx.x & 63, d = (lane & 31) * 4;
     const int count = min(ROWS, items.q_len[sequence] - tile * ROWS);
@@ -205,6 +219,13 @@ int plan_splits(const fq_prompt_args& a, int64_t total, int longest) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(2 * room / units, longest / 8));
 }
 
+// Heads of a die whose keys and values, of all sequences of a launch, its 4 MiB of cache holds.
+int heads_together(const fq_prompt_args& a, int first, int n) {
+    const int64_t keys = (int64_t)a.k_offsets[first + n] - a.k_offsets[first], bytes = std::max<int64_t>(1, keys * a.head_dim * 4);
+    const int group = a.q_heads / a.kv_heads, of_die = std::max(1, a.q_heads / 8);
+    return (int)std::min<int64_t>(of_die, std::max<int64_t>(1, (4 << 20) / bytes) * group);
+}
+
 }  // namespace
 
 size_t fq_prompt_bytes(const fq_prompt_args& a) {
@@ -226,7 +247,8 @@ int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* wor
         int longest;
         count_tiles(a, first, n, &total, &longest);
         if (total == 0) continue;
-        prompt_plan p = {a.q_heads, a.q_heads / a.kv_heads, a.head_dim, a.scale * LOG2E, plan_splits(a, total, longest), (float*)workspace};
+        prompt_plan p = {a.q_heads, a.q_heads / a.kv_heads, a.head_dim, a.scale * LOG2E, plan_splits(a, total, longest), (float*)workspace, 0};
+        p.together = p.splits > 1 ? std::max(1, a.q_heads / 8) : heads_together(a, first, n);       // (pieces: all blocks run at once anyway)
         if (total * a.q_heads >= 1 << 24) return FQ_ERR_UNSUPPORTED;      // (2^32 threads)
         int order[SEQUENCES], tiles[SEQUENCES];
         for (int i = 0; i < n; ++i) {
