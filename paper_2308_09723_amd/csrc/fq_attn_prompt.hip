@@ -144,6 +144,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
             w.template accumulate<2>(at + TILE_BYTES, x);
         }
     }
+    __syncthreads();                         // (nobody reads keys and values any more)
     w.l = other_half_sum(w.l);
     float* slot = p.splits > 1 ? p.slot(unit, piece) : nullptr;
     if (!w.finite()) {
@@ -155,8 +156,11 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
                             p.factor, o, &c, &sum);
             put_one<ACT>(out + (r * p.q_heads + h) * D, slot, ROWS, wave * 32 + x, o, c, sum, D);
         }
-    } else if (i < queries) {
-        w.put(out + (row * p.q_heads + h) * D, slot, ROWS, wave * 32 + (lane & 31), D);
+    } else if (slot) {
+        if (i < queries) w.put(nullptr, slot, ROWS, wave * 32 + (lane & 31), D);
+    } else if (first < queries) {
+        w.put_rows(lds + wave * 2 * SH::BYTES, out + (((int64_t)items.q_start[sequence] + first) * p.q_heads + h) * D, (int64_t)p.q_heads * D,
+                   queries - first, D);
     }
 }
 

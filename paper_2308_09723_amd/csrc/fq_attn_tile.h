@@ -322,6 +322,27 @@ struct wave_state {
         if (slot && (threadIdx.x & 32) == 0) put_stats(slot, slot_rows, r, D, top(), l);
     }
 
+    // The wave's results to rows out + r * stride (32 of them, `count` there), whole lines at a time: through 32 rows of LDS of its
+    // own, where the lanes of a store find neighbouring values (stored as the lanes have them a line takes eight writes).
+    __device__ __forceinline__ void put_rows(char* mine, uint16_t* out, int64_t stride, int count, int D) const {
+        const int lane = threadIdx.x & 63;
+        const float scale = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
+        quads([&](int d, int i, int t) {
+            const u32x2 z = {pack2<ACT>(o[t][i] * scale, o[t][i + 1] * scale), pack2<ACT>(o[t][i + 2] * scale, o[t][i + 3] * scale)};
+            const int r = lane & 31;
+            *(u32x2*)(mine + r * SH::PITCH + key_unit<SH::UNITS>(r, d / 8) * 16 + (d & 4) * 2) = z;
+        });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the wave's own: no barrier)
+        constexpr int STEP = 64 / SH::UNITS;
+        const int unit = lane % SH::UNITS;
+#pragma unroll
+        for (int j = 0; j < 32 / STEP; ++j) {
+            const int r = lane / SH::UNITS + j * STEP;
+            const u32x4 z = *(const u32x4*)(mine + r * SH::PITCH + key_unit<SH::UNITS>(r, unit) * 16);
+            if (r < count && unit * 8 < D) *(u32x4*)(out + r * stride + unit * 8) = z;
+        }
+    }
+
     // f(d, i, t): the lane's results i .. i + 3 of block t are values d .. d + 3 of its query
     template <typename F>
     __device__ __forceinline__ static void quads(F f) {
