@@ -120,10 +120,21 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
     wave_state<ACT, DP> w;
     w.clear();
     if (t0 < t1) load(t0, 0);
-    const int64_t row = (int64_t)items.q_start[sequence] + min(i, queries - 1);
-    const uint16_t* query = (const uint16_t*)q.data + row * q.row_stride + h * q.head_stride;
-    w.load_query(query, D);
-    w.query_is_here();
+    {
+        // the wave's queries, into the second buffer, whole lines at a time
+        const int r0 = lane / SH::UNITS;
+        char* mine = lds + 2 * TILE_BYTES + wave * SH::BYTES;
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+        const uint16_t* from = (const uint16_t*)q.data + (int64_t)items.q_start[sequence] * q.row_stride + h * q.head_stride;
+#pragma unroll
+        for (int j = 0; j < SH::BYTES / 1024; ++j) {
+            const int r = r0 + j * (64 / SH::UNITS), at = key_unit<SH::UNITS>(r, place) * 8;
+            if (at < D) load_lds16(to + j * 1024, from + (int64_t)min(first + r, queries - 1) * q.row_stride + at);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        w.read_query(mine);
+        w.query_is_here();
+    }
     const int end = i + 1 + ahead;           // keys that the lane's query sees
     for (int t = t0; t < t1; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

@@ -205,6 +205,13 @@ struct wave_state {
         for (int s = 0; s < SH::STEPS; ++s) asm volatile("" : "+v"(q[s]));
     }
 
+    // The same out of 32 rows in LDS that lie as keys do
+    __device__ __forceinline__ void read_query(const char* rows) {
+        const int lane = threadIdx.x & 63, r = lane & 31;
+#pragma unroll
+        for (int s = 0; s < SH::STEPS; ++s) q[s] = *(const u32x4*)(rows + r * SH::PITCH + key_unit<SH::UNITS>(r, 2 * s + (lane >> 5)) * 16);
+    }
+
     // S^T of H half-tiles of keys in LDS.  Score i of half-tile t belongs to key 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4.
     template <int H>
     __device__ __forceinline__ void scores(const char* keys, f32x16 (&s)[H]) const {
