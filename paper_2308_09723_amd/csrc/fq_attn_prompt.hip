@@ -39,7 +39,7 @@ struct prompt_plan {
     int q_heads, group, D;
     float factor;
     int splits;                      // pieces that a query tile's keys are cut into
-    float* slots;                    // one per query tile, head and piece: [ROWS][D] sums, [ROWS] maxima (log2), [ROWS] sums of numerators
+    float* slots;                    // one per query tile, head and piece
 
     int together;                    // heads of a die that it works on at the same time
     // Blocks go to the eight dies in turn.  Neighbouring heads, which share keys, go to the same die and its cache (8192 tokens, 32
@@ -56,8 +56,8 @@ struct prompt_plan {
         *rank = in / heads;
         *h = unit % 8 * of_die + set * together + in - *rank * heads;
     }
-    __host__ __device__ int64_t slot_floats() const { return (int64_t)ROWS * (D + 2); }
-    __device__ float* slot(int tile_of_head, int piece) const { return slots + ((int64_t)tile_of_head * splits + piece) * slot_floats(); }
+    __host__ __device__ slot_shape shape() const { return {ROWS, D}; }
+    __device__ float* slot(int unit, int piece) const { return slots + ((int64_t)unit * splits + piece) * shape().floats(); }
 };
 
 template <int ACT, int DP>
@@ -165,30 +165,30 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
             float o[2], c, sum;
             attend_one<ACT>((const uint16_t*)q.data + r * q.row_stride + h * q.head_stride, rows, sees_first{sees}, t0 * KEYS, min(sees, t1 * KEYS), D,
                             p.factor, o, &c, &sum);
-            put_one<ACT>(out + (r * p.q_heads + h) * D, slot, ROWS, wave * 32 + x, o, c, sum, D);
+            put_one<ACT>(out + (r * p.q_heads + h) * D, slot, p.shape(), wave * 32 + x, o, c, sum);
         }
     } else if (slot) {
-        if (i < queries) w.put(nullptr, slot, ROWS, wave * 32 + (lane & 31), D);
+        if (i < queries) w.put(nullptr, slot, p.shape(), wave * 32 + (lane & 31));
     } else if (first < queries) {
-        w.put_rows(lds + wave * 2 * SH::BYTES, out + (((int64_t)items.q_start[sequence] + first) * p.q_heads + h) * D, (int64_t)p.q_heads * D,
-                   queries - first, D);
+        uint16_t* to = out + (((int64_t)items.q_start[sequence] + first) * p.q_heads + h) * D;
+        w.put_rows(lds + wave * 2 * SH::BYTES, [&](int r) { return to + (int64_t)r * p.q_heads * D; }, queries - first, D);
     }
 }
 
-// Joins the pieces of a query tile: a lane has four values of a row, a wave two rows at a time.
+// Joins the pieces of a query tile: a lane has four values of a row, a wave 32 rows of eight.
 template <int ACT>
 __global__ __launch_bounds__(256) void fq_attention_prompt_join_kernel(prompt_plan p, uint16_t* out, prompt_items items) {
     const int unit = blockIdx.x, D = p.D;
     int rank, h, sequence, tile;
     p.find(unit, gridDim.x, &rank, &h);
     find_tile(items, rank, &sequence, &tile);
-    const int lane = threadIdx.x & 63, d = (lane & 31) * 4;
-    const int count = min(ROWS, items.q_len[sequence] - tile * ROWS);
-    for (int r = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 2 + (lane >> 5); r < count; r += 8 * gridDim.y) {
-        if (d >= D) continue;
+    const int count = min(ROWS, items.q_len[sequence] - tile * ROWS), groups = (count + 31) / 32;
+    for (int x = blockIdx.y * 256 + threadIdx.x; x < groups * (D / 4) * 32; x += 256 * gridDim.y) {
+        const int y = x / 32, group = y / (D / 4), d = (y - group * (D / 4)) * 4, r = group * 32 + x % 32;
+        if (r >= count) continue;
         partial_sums all;
         all.clear();
-        all.add(p.slot(unit, 0), p.slot_floats(), p.splits, ROWS, r, d, D);
+        all.add(0, p.splits, [&](int y) { return p.slot(unit, y); }, p.shape(), r, d);
         all.template store<ACT>(out + (((int64_t)items.q_start[sequence] + tile * ROWS + r) * p.q_heads + h) * D + d);
     }
 }

@@ -112,19 +112,32 @@ struct tile_shape {
     static constexpr int TILES = DP / 32;                     // of the second
 };
 
-// Sums that are not a query's whole result are left in slots: [slot_rows][D] sums, not divided, then [slot_rows] maxima that they are
-// relative to (log2; -infinity: no key seen) and [slot_rows] sums of numerators.
-__device__ inline void put_stats(float* slot, int slot_rows, int r, int D, float c, float l) {
-    slot[slot_rows * D + r] = c;
-    slot[slot_rows * (D + 1) + r] = l;
-}
+// Sums that are not a query's whole result are left in slots: sums, not divided, four of a row together and up to 32 rows side by side, as
+// a wave has them (whole lines at a time: a slot is written and read once more), then the maxima that they are relative to (log2;
+// -infinity: no key seen) and the sums of numerators.
+struct slot_shape {
+    int rows, D;                     // rows: fewer than 32, or a multiple of them
+    __host__ __device__ int64_t floats() const { return (int64_t)rows * (D + 2); }
+    __device__ int at(int r, int d) const {
+        const int side = rows < 32 ? rows : 32, of = r / 32;
+        return ((of * (D / 4) + d / 4) * side + r - of * 32) * 4 + (d & 3);
+    }
+    __device__ void put_stats(float* slot, int r, float c, float l) const {
+        slot[rows * D + r] = c;
+        slot[rows * (D + 1) + r] = l;
+    }
+};
 // attend_one's result, or its sums to row r of a slot
 template <int ACT>
-__device__ inline void put_one(uint16_t* out, float* slot, int slot_rows, int r, const float* o, float c, float l, int D) {
+__device__ inline void put_one(uint16_t* out, float* slot, const slot_shape& shape, int r, const float* o, float c, float l) {
     const int lane = threadIdx.x & 63;
-    if (!slot) return store_one<ACT>(out, o, l, D);
-    if (2 * lane < D) slot[r * D + 2 * lane] = o[0], slot[r * D + 2 * lane + 1] = o[1];
-    if (lane == 0) put_stats(slot, slot_rows, r, D, c, l);
+    if (!slot) return store_one<ACT>(out, o, l, shape.D);
+    if (2 * lane < shape.D) {
+        float* to = slot + shape.at(r, 2 * lane);
+        to[0] = o[0];
+        to[1] = o[1];
+    }
+    if (lane == 0) shape.put_stats(slot, r, c, l);
 }
 
 // Values d .. d + 3 of a row, joined from slots.
@@ -144,22 +157,25 @@ struct partial_sums {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = o[i] * mine + o1[i] * its;
     }
-    // row r of `count` slots that lie `stride` values apart, in their order, eight of them on their way at once
-    __device__ void add(const float* slot, int64_t stride, int count, int slot_rows, int r, int d, int D) {
-        constexpr int BATCH = 8;
-        for (int n = 0; n < count; n += BATCH) {
+    // values d .. d + 3 of row r of slots slot(begin) .. slot(end - 1), in their order, four of them on their way at once
+    template <typename SLOT>
+    __device__ void add(int begin, int end, const SLOT& slot, const slot_shape& shape, int r, int d) {
+        constexpr int BATCH = 4;
+        const int at = shape.at(r, d), stats = shape.rows * shape.D + r;
+        for (int n = begin; n < end; n += BATCH) {
             float c1[BATCH], l1[BATCH];
             f32x4 o1[BATCH];
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
-                const float* from = slot + min(n + i, count - 1) * stride;
-                c1[i] = from[slot_rows * D + r];
-                l1[i] = from[slot_rows * (D + 1) + r];
-                o1[i] = *(const f32x4*)(from + r * D + d);
+                if (n + i >= end) break;
+                const float* from = slot(n + i);
+                c1[i] = from[stats];
+                l1[i] = from[stats + shape.rows];
+                o1[i] = *(const f32x4*)(from + at);
             }
 #pragma unroll
             for (int i = 0; i < BATCH; ++i)
-                if (n + i < count) add(c1[i], l1[i], o1[i]);
+                if (n + i < end) add(c1[i], l1[i], o1[i]);
         }
     }
     template <int ACT>
@@ -314,24 +330,28 @@ struct wave_state {
     }
 
     // The lane's query's result, or its sums to row r of a slot.
-    __device__ __forceinline__ void put(uint16_t* out, float* slot, int slot_rows, int r, int D) const {
+    __device__ __forceinline__ void put(uint16_t* out, float* slot, const slot_shape& shape, int r) const {
+        if (slot) {
+            float* to = slot + shape.at(r, (threadIdx.x & 32) >> 3);
+            const int step = shape.at(0, 8);
+            quads([&](int d, int i, int t) {
+                const f32x4 z = {o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+                if (d < shape.D) *(f32x4*)(to + (4 * t + i / 4) * step) = z;
+            });
+            if ((threadIdx.x & 32) == 0) shape.put_stats(slot, r, top(), l);
+            return;
+        }
         const float scale = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
         quads([&](int d, int i, int t) {
-            if (d >= D) return;
-            if (!slot) {
-                const u32x2 z = {pack2<ACT>(o[t][i] * scale, o[t][i + 1] * scale), pack2<ACT>(o[t][i + 2] * scale, o[t][i + 3] * scale)};
-                *(u32x2*)(out + d) = z;
-            } else {
-                const f32x4 z = {o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
-                *(f32x4*)(slot + r * D + d) = z;
-            }
+            const u32x2 z = {pack2<ACT>(o[t][i] * scale, o[t][i + 1] * scale), pack2<ACT>(o[t][i + 2] * scale, o[t][i + 3] * scale)};
+            if (d < shape.D) *(u32x2*)(out + d) = z;
         });
-        if (slot && (threadIdx.x & 32) == 0) put_stats(slot, slot_rows, r, D, top(), l);
     }
 
-    // The wave's results to rows out + r * stride (32 of them, `count` there), whole lines at a time: through 32 rows of LDS of its
-    // own, where the lanes of a store find neighbouring values (stored as the lanes have them a line takes eight writes).
-    __device__ __forceinline__ void put_rows(char* mine, uint16_t* out, int64_t stride, int count, int D) const {
+    // The wave's results to rows out(r) (32 of them, `count` there), whole lines at a time: through 32 rows of LDS of its own, where the
+    // lanes of a store find neighbouring values (stored as the lanes have them a line takes eight writes).
+    template <typename OUT>
+    __device__ __forceinline__ void put_rows(char* mine, const OUT& out, int count, int D) const {
         const int lane = threadIdx.x & 63;
         const float scale = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
         quads([&](int d, int i, int t) {
@@ -342,11 +362,11 @@ struct wave_state {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the wave's own: no barrier)
         constexpr int STEP = 64 / SH::UNITS;
         const int unit = lane % SH::UNITS;
-#pragma unroll
+#pragma unroll 2
         for (int j = 0; j < 32 / STEP; ++j) {
             const int r = lane / SH::UNITS + j * STEP;
             const u32x4 z = *(const u32x4*)(mine + r * SH::PITCH + key_unit<SH::UNITS>(r, unit) * 16);
-            if (r < count && unit * 8 < D) *(u32x4*)(out + r * stride + unit * 8) = z;
+            if (r < count && unit * 8 < D) *(u32x4*)(out(r) + unit * 8) = z;
         }
     }
 

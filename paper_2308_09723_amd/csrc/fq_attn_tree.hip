@@ -28,14 +28,15 @@ struct tree_plan {
     int tile;                        // keys of a tile
     int blocks;                      // at most
     int slot_rows;                   // rows of a slot of the workspace
+    int D;
     float factor;
-    float* slots;                    // two per block and head of it: [slot_rows][head_dim] sums, [slot_rows] maxima (log2), [slot_rows] sums of numerators
+    float* slots;                    // two per block and head of it
 
     // blocks that follow each other in the line share a die's cache (blocks go to the eight dies in turn)
     __device__ int in_line(int block) const { return blocks % 8 == 0 ? block % 8 * (blocks / 8) + block / 8 : block; }
-    __host__ __device__ int64_t slot_floats(int D) const { return (int64_t)slot_rows * (D + 2); }
+    __host__ __device__ slot_shape shape() const { return {slot_rows, D}; }
     // a block's first piece, or its last, of head h of the heads it takes together
-    __device__ float* slot(int64_t block, bool first, int h, int D) const { return slots + ((2 * block + !first) * heads + h) * slot_floats(D); }
+    __device__ float* slot(int64_t block, bool first, int h) const { return slots + ((2 * block + !first) * heads + h) * shape().floats(); }
 };
 
 __device__ inline int keys_of(const fq_tree_args& a, int context) {
@@ -161,7 +162,7 @@ struct unit_rows {
         for (int r = from; r < to; r += step) {
             float o[2], c, l;
             one<ACT>(r, begin, end, o, &c, &l);
-            put_one<ACT>(result(r), slot, p.slot_rows, r, o, c, l, a.head_dim);
+            put_one<ACT>(result(r), slot, p.shape(), r, o, c, l);
         }
     }
 };
@@ -262,8 +263,8 @@ __device__ __forceinline__ void join_parts(const unit_rows& rows, const wave_sta
                 const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
                 *(u32x2*)(rows.result(at) + d) = z;
             } else {
-                *(f32x4*)(slot + at * D + d) = o;
-                if (d == 0) put_stats(slot, rows.p.slot_rows, at, D, c, l);
+                *(f32x4*)(slot + rows.p.shape().at(at, d)) = o;
+                if (d == 0) rows.p.shape().put_stats(slot, at, c, l);
             }
         }
     }
@@ -315,7 +316,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
     for (int64_t pos = begin; pos < stop;) {
         const unit_rows rows(a, p, b, u, head);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
-        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, head, D);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, head);
         const int key0 = t0 * TILE, key1 = min(rows.keys, t1 * TILE);
         const int row = min(lane & 31, rows.count - 1);
         w.load_query(rows.query(row), D);
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         w.l = other_half_sum(w.l);
         if constexpr (PARTS == 1) {
             if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
-            else if ((lane & 31) < rows.count) w.put(rows.result(row), slot, p.slot_rows, row, D);
+            else if ((lane & 31) < rows.count) w.put(rows.result(row), slot, p.shape(), row);
         } else {
             join_parts<ACT, DP, PARTS>(rows, w, lds, WAVE_BYTES, stats, head, HEADS, part_of, 0, key0, key1, slot);
         }
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     for (int64_t pos = begin; pos < stop;) {
         const unit_rows rows(a, p, b, u, 0);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
-        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(block, pos == begin, 0, D);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(block, pos == begin, 0);
         const int key0 = t0 * KEYS, key1 = min(rows.keys, t1 * KEYS);
         const int r = group * 32 + (lane & 31), row = min(r, rows.count - 1);
         const bool busy = group * 32 < rows.count;
@@ -487,7 +488,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
             join_parts<ACT, DP, PARTS>(rows, w, lds, JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
         } else {
             if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
-            else if (r < rows.count) w.put(rows.result(r), slot, p.slot_rows, r, D);
+            else if (r < rows.count) w.put(rows.result(r), slot, p.shape(), r);
         }
         pos += t1 - t0;
         t0 = 0;
@@ -498,8 +499,8 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     }
 }
 
-// Joins the pieces of a unit that was cut.  A lane has four values of a row, a wave two rows.  A unit of few pieces: each wave its own
-// rows; of many: the four waves a quarter of the pieces each of the same rows.  Pieces are added in the line's order.
+// Joins the pieces of a unit that was cut.  A lane has four values of a row, a wave up to 32 rows of them.  A unit of few pieces: each
+// wave its own; of many: the four waves a quarter of the pieces each of the same values.  Pieces are added in the line's order.
 template <int ACT>
 __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_args a, tree_plan p) {
     __shared__ f32x4 sums[4][64];
@@ -512,38 +513,34 @@ __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_arg
     const int64_t begin = uniform(wave_sum64(before)) * all.units + (int64_t)u * tiles, end = begin + tiles;
     const int64_t from = begin / all.per_block, to = (end - 1) / all.per_block;        // blocks that have pieces of it
     if (from == to) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int D = a.head_dim, d = (lane & 31) * 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.head_dim;
     const bool whole = begin == from * all.per_block;        // (the first block's first piece, or its last)
     const bool many = to - from >= 8;
     const int share = many ? (int)((to - from + 4) / 4) : (int)(to - from + 1), mine = many ? wave : 0;
-    const int at_once = many ? 2 : 8;
-    for (int base = blockIdx.y * at_once; base < p.heads * p.slot_rows; base += gridDim.y * at_once) {
-        const int row = base + (many ? 0 : 2 * wave) + (lane >> 5), head = row / p.slot_rows, r = row - head * p.slot_rows;
+    const int at_once = many ? 64 : 256, rows_at_once = min(32, p.rows);
+    const int groups = (p.slot_rows + 31) / 32, units = p.heads * groups * (D / 4) * rows_at_once;
+    for (int base = blockIdx.y * at_once; base < units; base += gridDim.y * at_once) {
+        const int x = base + (many ? lane : (int)threadIdx.x), y = x / rows_at_once, z = y / (D / 4), d = (y - z * (D / 4)) * 4;
+        const int head = z / groups, r = (z - head * groups) * 32 + x - y * rows_at_once;
         const unit_rows rows(a, p, b, u, min(head, p.heads - 1));
-        const bool there = head < p.heads && r < rows.count && d < D;
-        partial_sums all_pieces;
-        all_pieces.clear();
+        const bool there = head < p.heads && r < rows.count;
+        partial_sums sum;
+        sum.clear();
         if (there) {
             // (a unit's first piece may be its block's last one, the others are their blocks' first)
-            int n0 = mine * share;
-            const int n1 = min((int)(to - from) + 1, n0 + share);
-            if (n0 == 0 && !whole) {
-                all_pieces.add(p.slot(from, false, head, D), 0, 1, p.slot_rows, r, d, D);
-                n0 = 1;
-            }
-            if (n0 < n1) all_pieces.add(p.slot(from + n0, true, head, D), 2 * p.heads * p.slot_floats(D), n1 - n0, p.slot_rows, r, d, D);
+            const int n0 = mine * share, n1 = min((int)(to - from) + 1, n0 + share);
+            sum.add(n0, n1, [&](int y) { return p.slot(from + y, y > 0 || whole, head); }, p.shape(), r, d);
         }
         if (many) {
             __syncthreads();
-            sums[wave][lane] = all_pieces.o;
-            stats[wave][lane][0] = all_pieces.c;
-            stats[wave][lane][1] = all_pieces.l;
+            sums[wave][lane] = sum.o;
+            stats[wave][lane][0] = sum.c;
+            stats[wave][lane][1] = sum.l;
             __syncthreads();
             if (wave == 0)
-                for (int y = 1; y < 4; ++y) all_pieces.add(stats[y][lane][0], stats[y][lane][1], sums[y][lane]);
+                for (int i = 1; i < 4; ++i) sum.add(stats[i][lane][0], stats[i][lane][1], sums[i][lane]);
         }
-        if (there && (wave == 0 || !many)) all_pieces.template store<ACT>(rows.result(r) + d);
+        if (there && (wave == 0 || !many)) sum.template store<ACT>(rows.result(r) + d);
     }
 }
 
@@ -556,7 +553,8 @@ tree_plan plan_tree(const fq_tree_args& a) {
     p.heads = p.rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
     p.unit_rows = p.rows <= 64 ? 64 : ROWS;
     p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
-    p.slot_rows = p.rows < p.unit_rows ? p.rows : p.unit_rows;
+    p.slot_rows = p.rows < 32 ? p.rows : ((p.rows < p.unit_rows ? p.rows : p.unit_rows) + 31) / 32 * 32;
+    p.D = a.head_dim;
     p.tile = p.rows > 32 ? KEYS : 128 / p.heads;
     p.blocks = 2 * fq_cu_count();
     p.factor = a.scale * LOG2E;
@@ -592,7 +590,7 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
     if (st != FQ_OK) return st;
     // (a block for each unit at least, more for its rows while they are few)
     const int64_t units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
-    const int64_t most = (p.heads * p.slot_rows + 1) / 2, wanted = 1024 / units;
+    const int64_t most = (p.heads * (p.slot_rows < p.rows ? p.slot_rows : p.rows) + 1) / 2, wanted = 1024 / units;
     const dim3 grid((unsigned)units, (unsigned)(wanted < 1 ? 1 : wanted < most ? wanted : most));
     fq_attention_tree_join_kernel<ACT><<<grid, 256, 0, stream>>>(a, p);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
@@ -609,7 +607,7 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
 
 size_t fq_tree_bytes(const fq_tree_args& a) {
     const tree_plan p = plan_tree(a);
-    return (size_t)p.blocks * 2 * p.heads * p.slot_floats(a.head_dim) * sizeof(float);
+    return (size_t)p.blocks * 2 * p.heads * p.shape().floats() * sizeof(float);
 }
 
 int fq_launch_attention_tree(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream) {
