@@ -20,9 +20,22 @@ using namespace fqa;
 
 constexpr int TABLE = 1024;          // entries of the page table that a block has in LDS
 
+// Quotients of numbers below 2^31 by one that the host knows, 1 to 2^31: a multiplication (by m = ceil(2^(31 + k) / d), where 2^k is the
+// first power of two that is not below d: the error of n m / 2^(31 + k) is below n / 2^(31 + k) <= 1 / d).
+struct divisor {
+    uint32_t d, m, shift;
+    static divisor of(uint32_t d) {
+        uint32_t k = 0;
+        while (((uint64_t)1 << k) < d) ++k;
+        return {d, k == 0 ? 0 : (uint32_t)((((uint64_t)1 << (31 + k)) + d - 1) / d), k - 1};
+    }
+    __device__ int quotient(int n) const { return m == 0 ? n : (int)(__umulhi((uint32_t)n, m) >> shift); }
+};
+
 // What the host has made of a call.
 struct tree_plan {
     int group, rows;                 // query heads per key head; rows of a key head
+    divisor by_group, by_quads, by_side;       // divisors: group; head_dim / 4; rows of a slot that lie side by side
     int heads;                       // key heads that a block takes together
     int row_tiles, unit_rows;        // tiles of unit_rows rows that a head's are cut into
     int tile;                        // keys of a tile
@@ -46,6 +59,12 @@ __device__ inline int tiles_of(const fq_tree_args& a, const tree_plan& p, int b)
     return max(1, (keys_of(a, a.context_lens[b]) + p.tile - 1) / p.tile);
 }
 
+// a / b of numbers that are hardly ever long (a division in 64 bits takes a microsecond)
+__device__ inline int64_t quotient(int64_t a, int64_t b) {
+    if (((uint64_t)(a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+    return a / b;
+}
+
 __device__ inline int64_t wave_sum64(int64_t x) {
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
@@ -63,12 +82,12 @@ struct line {
         int64_t sum = 0;
         for (int b = threadIdx.x & 63; b < a.sequences; b += 64) sum += tiles_of(a, p, b);
         total = uniform(wave_sum64(sum)) * units;
-        per_block = (total + p.blocks - 1) / p.blocks;
+        per_block = quotient(total + p.blocks - 1, p.blocks);
     }
     // the sequence whose tiles the line has at `at`, and where they begin
     __device__ void find(const fq_tree_args& a, const tree_plan& p, int64_t at, int* sequence, int64_t* begin) const {
         const int lane = threadIdx.x & 63;
-        const int64_t target = at / units;        // in tiles of one unit
+        const int64_t target = quotient(at, units);        // in tiles of one unit
         int64_t before = 0;
         for (int first = 0;; first += 64) {
             const int b = first + lane, n = b < a.sequences ? tiles_of(a, p, b) : 0;
@@ -107,11 +126,11 @@ struct unit_rows {
         keys = keys_of(a, context);
     }
     __device__ const uint16_t* query(int r) const {
-        const int node = (first + r) / p.group, h = head * p.group + (first + r) - node * p.group;
+        const int node = p.by_group.quotient(first + r), h = head * p.group + (first + r) - node * p.group;
         return (const uint16_t*)a.q.data + ((int64_t)b * a.nodes + node) * a.q.row_stride + h * a.q.head_stride;
     }
     __device__ uint16_t* result(int r) const {
-        const int node = (first + r) / p.group, h = head * p.group + (first + r) - node * p.group;
+        const int node = p.by_group.quotient(first + r), h = head * p.group + (first + r) - node * p.group;
         return (uint16_t*)a.out + (((int64_t)b * a.nodes + node) * a.q_heads + h) * a.head_dim;
     }
     __device__ paged_rows pages() const {
@@ -126,14 +145,14 @@ struct unit_rows {
         return x;
     }
     __device__ const uint64_t* words(int r) const {
-        return a.mask + b * a.mask_stride + (int64_t)((first + r) / p.group) * ((a.nodes + 63) / 64);
+        return a.mask + b * a.mask_stride + (int64_t)p.by_group.quotient(first + r) * ((a.nodes + 63) / 64);
     }
     // which of keys base .. base + 31 row r sees
     __device__ uint32_t seen(int r, int base) const {
         uint32_t bits = low_bits(keys - base);
         const int d = base - context;          // the drafted token that bit 0 stands for
         if (d <= -32) return bits;
-        if (!a.mask) return bits & low_bits((first + r) / p.group + 1 - d);
+        if (!a.mask) return bits & low_bits(p.by_group.quotient(first + r) + 1 - d);
         const uint64_t* w = words(r);
         const int n = max(0, d), last = (a.nodes + 63) / 64 - 1;
         uint32_t drafted = 0;
@@ -151,7 +170,7 @@ struct unit_rows {
         if (a.mask) {
             attend_one<ACT>(query(r), pages(), sees_tree{context, a.nodes, words(r)}, begin, end, a.head_dim, p.factor, o, c, l);
         } else {
-            const int last = (int)min((int64_t)end, (int64_t)context + (first + r) / p.group + 1);
+            const int last = (int)min((int64_t)end, (int64_t)context + p.by_group.quotient(first + r) + 1);
             attend_one<ACT>(query(r), pages(), sees_first{last}, begin, min(end, last), a.head_dim, p.factor, o, c, l);
         }
     }
@@ -310,7 +329,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
     int64_t at_b;
     all.find(a, p, begin, &b, &at_b);
     int tiles = tiles_of(a, p, b);
-    int u = (int)((begin - at_b) / tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
+    int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
     wave_state<ACT, DP> w;
 
     for (int64_t pos = begin; pos < stop;) {
@@ -421,7 +440,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     int64_t at_b;
     all.find(a, p, begin, &b, &at_b);
     int tiles = tiles_of(a, p, b);
-    int u = (int)((begin - at_b) / tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
+    int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
     wave_state<ACT, DP> w;
 
     for (int64_t pos = begin; pos < stop;) {
@@ -500,30 +519,33 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
 }
 
 // Joins the pieces of a unit that was cut.  A lane has four values of a row, a wave up to 32 rows of them.  A unit of few pieces: each
-// wave its own; of many: the four waves a quarter of the pieces each of the same values.  Pieces are added in the line's order.
+// wave its own; of many: the waves share the pieces of the same values out.  Pieces are added in the line's order.
 template <int ACT>
-__global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_args a, tree_plan p) {
-    __shared__ f32x4 sums[4][64];
-    __shared__ float stats[4][64][2];
+__global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_args a, tree_plan p) {
+    __shared__ f32x4 sums[16][64];
+    __shared__ float stats[16][64][2];
+    const int waves = blockDim.x / 64;
     const line all(a, p);
     const int b = (int)(blockIdx.x / all.units), u = (int)(blockIdx.x - (int64_t)b * all.units);
     int64_t before = 0;
     for (int x = threadIdx.x & 63; x < b; x += 64) before += tiles_of(a, p, x);
     const int tiles = tiles_of(a, p, b);
     const int64_t begin = uniform(wave_sum64(before)) * all.units + (int64_t)u * tiles, end = begin + tiles;
-    const int64_t from = begin / all.per_block, to = (end - 1) / all.per_block;        // blocks that have pieces of it
+    const int64_t from = quotient(begin, all.per_block), to = quotient(end - 1, all.per_block);        // blocks that have pieces of it
     if (from == to) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.head_dim;
     const bool whole = begin == from * all.per_block;        // (the first block's first piece, or its last)
     const bool many = to - from >= 8;
-    const int share = many ? (int)((to - from + 4) / 4) : (int)(to - from + 1), mine = many ? wave : 0;
-    const int at_once = many ? 64 : 256, rows_at_once = min(32, p.rows);
-    const int groups = (p.slot_rows + 31) / 32, units = p.heads * groups * (D / 4) * rows_at_once;
-    for (int base = blockIdx.y * at_once; base < units; base += gridDim.y * at_once) {
-        const int x = base + (many ? lane : (int)threadIdx.x), y = x / rows_at_once, z = y / (D / 4), d = (y - z * (D / 4)) * 4;
-        const int head = z / groups, r = (z - head * groups) * 32 + x - y * rows_at_once;
+    const int share = many ? ((int)(to - from) + waves) / waves : (int)(to - from + 1), mine = many ? wave : 0;
+    // lanes: rows that lie side by side, of as many quads as a wave has room for
+    const int side = min(32, p.rows), groups = (p.slot_rows + 31) / 32, quads = 64 / side;
+    const int sub = p.by_side.quotient(lane), r0 = lane - sub * side, units = p.heads * groups * (D / 4);
+    const int step = quads * (many ? 1 : waves);
+    for (int base = blockIdx.y * step; base < units; base += gridDim.y * step) {
+        const int y = base + (many ? 0 : wave * quads) + sub, z = p.by_quads.quotient(y), d = (y - z * (D / 4)) * 4;
+        const int head = groups == 1 ? z : z / groups, r = (z - head * groups) * 32 + r0;
         const unit_rows rows(a, p, b, u, min(head, p.heads - 1));
-        const bool there = head < p.heads && r < rows.count;
+        const bool there = sub < quads && y < units && r < rows.count;
         partial_sums sum;
         sum.clear();
         if (there) {
@@ -538,7 +560,7 @@ __global__ __launch_bounds__(256) void fq_attention_tree_join_kernel(fq_tree_arg
             stats[wave][lane][1] = sum.l;
             __syncthreads();
             if (wave == 0)
-                for (int i = 1; i < 4; ++i) sum.add(stats[i][lane][0], stats[i][lane][1], sums[i][lane]);
+                for (int i = 1; i < waves; ++i) sum.add(stats[i][lane][0], stats[i][lane][1], sums[i][lane]);
         }
         if (there && (wave == 0 || !many)) sum.template store<ACT>(rows.result(r) + d);
     }
@@ -555,6 +577,9 @@ tree_plan plan_tree(const fq_tree_args& a) {
     p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
     p.slot_rows = p.rows < 32 ? p.rows : ((p.rows < p.unit_rows ? p.rows : p.unit_rows) + 31) / 32 * 32;
     p.D = a.head_dim;
+    p.by_group = divisor::of((uint32_t)p.group);
+    p.by_quads = divisor::of((uint32_t)a.head_dim / 4);
+    p.by_side = divisor::of((uint32_t)(p.rows < 32 ? p.rows : 32));
     p.tile = p.rows > 32 ? KEYS : 128 / p.heads;
     p.blocks = 2 * fq_cu_count();
     p.factor = a.scale * LOG2E;
@@ -588,11 +613,11 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
                    : p.heads == 2 ? launch_stream<ACT, DP, 2>(a, p, stream)
                                   : launch_stream<ACT, DP, 1>(a, p, stream);
     if (st != FQ_OK) return st;
-    // (a block for each unit at least, more for its rows while they are few)
+    // A block for each unit at least, more for its rows while units are few; sixteen waves where few units may be of hundreds of pieces.
     const int64_t units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
     const int64_t most = (p.heads * (p.slot_rows < p.rows ? p.slot_rows : p.rows) + 1) / 2, wanted = 1024 / units;
     const dim3 grid((unsigned)units, (unsigned)(wanted < 1 ? 1 : wanted < most ? wanted : most));
-    fq_attention_tree_join_kernel<ACT><<<grid, 256, 0, stream>>>(a, p);
+    fq_attention_tree_join_kernel<ACT><<<grid, units < 16 ? 1024 : 256, 0, stream>>>(a, p);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
