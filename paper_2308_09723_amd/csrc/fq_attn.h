@@ -15,6 +15,18 @@ template <> struct type16<FQ_BF16> { typedef __bf16 t; };
 
 constexpr float LOG2E = 1.44269504088896340736f;
 
+// Quotients of numbers below 2^31 by one that the host knows, 1 to 2^31: a multiplication (by m = ceil(2^(31 + k) / d), where 2^k is the
+// first power of two that is not below d: the error of n m / 2^(31 + k) is below n / 2^(31 + k) <= 1 / d).
+struct divisor {
+    uint32_t d, m, shift;
+    static divisor of(uint32_t d) {
+        uint32_t k = 0;
+        while (((uint64_t)1 << k) < d) ++k;
+        return {d, k == 0 ? 0 : (uint32_t)((((uint64_t)1 << (31 + k)) + d - 1) / d), k - 1};
+    }
+    __device__ int quotient(int n) const { return m == 0 ? n : (int)(__umulhi((uint32_t)n, m) >> shift); }
+};
+
 // One key head's keys and values of a sequence, packed: rows a stride apart.
 struct packed_rows {
     const uint16_t *k, *v;

@@ -28,8 +28,7 @@ __device__ inline void find_tile(const prompt_items& items, int rank, int* seque
     for (int i = 0; i < SEQUENCES; i += 64)
         s += __builtin_popcountll(__ballot(i + lane < items.count && items.before[i + lane] <= rank));
     s = __builtin_amdgcn_readfirstlane(s - 1);
-    const int in = rank - items.before[s];
-    const int level = in / (s + 1);
+    const int in = rank - items.before[s], level = s == 0 ? in : in / (s + 1);
     *sequence = in - level * (s + 1);
     *tile = items.tiles[s] - 1 - level;
 }
@@ -37,23 +36,27 @@ __device__ inline void find_tile(const prompt_items& items, int rank, int* seque
 // What the host has made of a launch.
 struct prompt_plan {
     int q_heads, group, D;
+    divisor by_group;
     float factor;
     int splits;                      // pieces that a query tile's keys are cut into
     float* slots;                    // one per query tile, head and piece
 
-    int together;                    // heads of a die that it works on at the same time
+    int units;                       // query tiles times heads
+    int together, of_set;            // heads of a die that it works on at the same time; blocks of it that have them
+    divisor by_units, by_heads, by_set, by_together;
     // Blocks go to the eight dies in turn.  Neighbouring heads, which share keys, go to the same die and its cache (8192 tokens, 32
     // heads over 8: 518 -> 510 us, 24 ragged prompts 122 -> 113), some of them at a time where the keys of all would not stay there
     // (96 heads, two sequences of 2048 tokens: 235 -> 223 us); within them all query tiles in the order of the items.
-    __device__ void find(int unit, int units, int* rank, int* h) const {
+    __device__ void find(int unit, int* rank, int* h) const {
         if (q_heads % 8 != 0) {
-            *rank = unit / q_heads;
+            *rank = by_heads.quotient(unit);
             *h = unit - *rank * q_heads;
             return;
         }
-        const int of_die = q_heads / 8, tiles = units / q_heads, i = unit / 8;
-        const int set = i / (tiles * together), in = i - set * tiles * together, heads = min(together, of_die - set * together);
-        *rank = in / heads;
+        const int of_die = q_heads / 8, i = unit / 8;
+        const int set = by_set.quotient(i), in = i - set * of_set, left = of_die - set * together;
+        const int heads = left < together ? left : together;
+        *rank = heads == together ? by_together.quotient(in) : in / heads;
         *h = unit % 8 * of_die + set * together + in - *rank * heads;
     }
     __host__ __device__ slot_shape shape() const { return {ROWS, D}; }
@@ -65,22 +68,23 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
                                                                      prompt_items items) {
     typedef tile_shape<DP> SH;
     extern __shared__ __align__(16) char lds[];
-    const int units = gridDim.x / p.splits, piece = blockIdx.x / units, unit = blockIdx.x - piece * units;      // piece of its keys; query tile and head
+    const int piece = p.by_units.quotient(blockIdx.x), unit = blockIdx.x - piece * p.units;      // piece of its keys; query tile and head
     const int D = p.D;
     int rank, h, sequence, tile;
-    p.find(unit, units, &rank, &h);
+    p.find(unit, &rank, &h);
     find_tile(items, rank, &sequence, &tile);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int queries = items.q_len[sequence], keys = items.k_len[sequence];
     const int first = tile * ROWS + wave * 32, i = first + (lane & 31);       // the wave's first query; the lane's
     packed_rows rows;
-    rows.k = (const uint16_t*)k.data + items.k_start[sequence] * k.row_stride + h / p.group * k.head_stride;
-    rows.v = (const uint16_t*)v.data + items.k_start[sequence] * v.row_stride + h / p.group * v.head_stride;
+    rows.k = (const uint16_t*)k.data + items.k_start[sequence] * k.row_stride + p.by_group.quotient(h) * k.head_stride;
+    rows.v = (const uint16_t*)v.data + items.k_start[sequence] * v.row_stride + p.by_group.quotient(h) * v.head_stride;
     rows.k_stride = k.row_stride;
     rows.v_stride = v.row_stride;
     const int ahead = keys - queries;        // query i sees keys 0 .. i + ahead
     const int all = max(0, (min(queries, (tile + 1) * ROWS) + ahead + KEYS - 1) / KEYS);      // tiles of keys that the block's last query sees
-    const int t0 = (int)((int64_t)all * piece / p.splits), t1 = (int)((int64_t)all * (piece + 1) / p.splits);
+    const int t0 = p.splits == 1 ? 0 : (int)((uint32_t)all * (uint32_t)piece / (uint32_t)p.splits);
+    const int t1 = p.splits == 1 ? all : (int)((uint32_t)all * (uint32_t)(piece + 1) / (uint32_t)p.splits);      // (at most 2^25 tiles, 128 pieces)
 
     // units of a head that no load fills are zeros from here on
     constexpr int TILE_BYTES = 2 * SH::BYTES;      // of keys, or of values
@@ -180,7 +184,7 @@ template <int ACT>
 __global__ __launch_bounds__(256) void fq_attention_prompt_join_kernel(prompt_plan p, uint16_t* out, prompt_items items) {
     const int unit = blockIdx.x, D = p.D;
     int rank, h, sequence, tile;
-    p.find(unit, gridDim.x, &rank, &h);
+    p.find(unit, &rank, &h);
     find_tile(items, rank, &sequence, &tile);
     const int count = min(ROWS, items.q_len[sequence] - tile * ROWS), groups = (count + 31) / 32;
     for (int x = blockIdx.y * 256 + threadIdx.x; x < groups * (D / 4) * 32; x += 256 * gridDim.y) {
@@ -231,7 +235,7 @@ void count_tiles(const fq_prompt_args& a, int first, int n, int64_t* total, int*
 int plan_splits(const fq_prompt_args& a, int64_t total, int longest) {
     const int64_t units = total * a.q_heads, room = 2 * fq_cu_count();
     if (units == 0 || units * 2 > room) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(2 * room / units, longest / 8));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(64, std::min<int64_t>(2 * room / units, longest / 8)));
 }
 
 // Heads of a die whose keys and values, of all sequences of a launch, its 4 MiB of cache holds.
@@ -262,9 +266,22 @@ int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* wor
         int longest;
         count_tiles(a, first, n, &total, &longest);
         if (total == 0) continue;
-        prompt_plan p = {a.q_heads, a.q_heads / a.kv_heads, a.head_dim, a.scale * LOG2E, plan_splits(a, total, longest), (float*)workspace, 0};
-        p.together = p.splits > 1 ? std::max(1, a.q_heads / 8) : heads_together(a, first, n);       // (pieces: all blocks run at once anyway)
+        prompt_plan p = {};
+        p.q_heads = a.q_heads;
+        p.group = a.q_heads / a.kv_heads;
+        p.by_group = divisor::of((uint32_t)p.group);
+        p.D = a.head_dim;
+        p.factor = a.scale * LOG2E;
+        p.splits = plan_splits(a, total, longest);
+        p.slots = (float*)workspace;
         if (total * a.q_heads >= 1 << 24) return FQ_ERR_UNSUPPORTED;      // (2^32 threads)
+        p.units = (int)total * a.q_heads;
+        p.together = p.splits > 1 ? std::max(1, a.q_heads / 8) : heads_together(a, first, n);       // (pieces: all blocks run at once anyway)
+        p.of_set = (int)total * p.together;
+        p.by_units = divisor::of((uint32_t)p.units);
+        p.by_heads = divisor::of((uint32_t)p.q_heads);
+        p.by_set = divisor::of((uint32_t)p.of_set);
+        p.by_together = divisor::of((uint32_t)p.together);
         int order[SEQUENCES], tiles[SEQUENCES];
         for (int i = 0; i < n; ++i) {
             order[i] = i;

@@ -20,18 +20,6 @@ using namespace fqa;
 
 constexpr int TABLE = 1024;          // entries of the page table that a block has in LDS
 
-// Quotients of numbers below 2^31 by one that the host knows, 1 to 2^31: a multiplication (by m = ceil(2^(31 + k) / d), where 2^k is the
-// first power of two that is not below d: the error of n m / 2^(31 + k) is below n / 2^(31 + k) <= 1 / d).
-struct divisor {
-    uint32_t d, m, shift;
-    static divisor of(uint32_t d) {
-        uint32_t k = 0;
-        while (((uint64_t)1 << k) < d) ++k;
-        return {d, k == 0 ? 0 : (uint32_t)((((uint64_t)1 << (31 + k)) + d - 1) / d), k - 1};
-    }
-    __device__ int quotient(int n) const { return m == 0 ? n : (int)(__umulhi((uint32_t)n, m) >> shift); }
-};
-
 // What the host has made of a call.
 struct tree_plan {
     int group, rows;                 // query heads per key head; rows of a key head
@@ -55,8 +43,8 @@ struct tree_plan {
 __device__ inline int keys_of(const fq_tree_args& a, int context) {
     return context < 0 ? 0 : (int)min(a.table_width * a.cache.page_size, (int64_t)context + a.nodes);
 }
-__device__ inline int tiles_of(const fq_tree_args& a, const tree_plan& p, int b) {      // (one without keys: its zeros are somebody's)
-    return max(1, (keys_of(a, a.context_lens[b]) + p.tile - 1) / p.tile);
+__device__ inline int tiles_of(const fq_tree_args& a, const tree_plan& p, int context) {      // (one without keys: its zeros are somebody's)
+    return max(1, (keys_of(a, context) + p.tile - 1) / p.tile);
 }
 
 // a / b of numbers that are hardly ever long (a division in 64 bits takes a microsecond)
@@ -70,27 +58,66 @@ __device__ inline int64_t wave_sum64(int64_t x) {
     for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
     return x;
 }
+// the sum of x over the lanes up to this one
+__device__ inline int sum_upto(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // from 1, 2, 4, 8 lanes below in the row of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row 0's sum to row 1, 2's to 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // rows 0 and 1's sum to rows 2 and 3
+    return x;
+}
 
-// The line of tiles: sequence by sequence, in it unit by unit.
+// The line of tiles: sequence by sequence, in it unit by unit.  Up to 64 sequences: a lane has one sequence's length, and no length is
+// read twice.
 struct line {
+    const fq_tree_args& a;
+    const tree_plan& p;
     int64_t per_block;               // tiles
     int64_t total;
     int units;                       // of a sequence
+    int mine, tiles, upto;           // up to 64 sequences: the lane's length, its tiles, all tiles up to it
 
-    __device__ line(const fq_tree_args& a, const tree_plan& p) {
+    __device__ line(const fq_tree_args& a, const tree_plan& p) : a(a), p(p) {
+        const int lane = threadIdx.x & 63;
         units = a.kv_heads / p.heads * p.row_tiles;
-        int64_t sum = 0;
-        for (int b = threadIdx.x & 63; b < a.sequences; b += 64) sum += tiles_of(a, p, b);
-        total = uniform(wave_sum64(sum)) * units;
+        mine = tiles = upto = 0;
+        if (a.sequences <= 64) {
+            if (lane < a.sequences) {
+                mine = a.context_lens[lane];
+                tiles = tiles_of(a, p, mine);
+            }
+            upto = sum_upto(tiles);
+            total = (int64_t)__builtin_amdgcn_readlane(upto, 63) * units;
+        } else {
+            int64_t sum = 0;
+            for (int b = lane; b < a.sequences; b += 64) sum += tiles_of(a, p, a.context_lens[b]);
+            total = uniform(wave_sum64(sum)) * units;
+        }
         per_block = quotient(total + p.blocks - 1, p.blocks);
     }
+    __device__ int context(int b) const { return a.sequences <= 64 ? __builtin_amdgcn_readlane(mine, b) : __builtin_amdgcn_readfirstlane(a.context_lens[b]); }
+    // where sequence b's tiles begin
+    __device__ int64_t begin(int b) const {
+        if (a.sequences <= 64) return (int64_t)(__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(tiles, b)) * units;
+        int64_t before = 0;
+        for (int x = threadIdx.x & 63; x < b; x += 64) before += tiles_of(a, p, a.context_lens[x]);
+        return uniform(wave_sum64(before)) * units;
+    }
     // the sequence whose tiles the line has at `at`, and where they begin
-    __device__ void find(const fq_tree_args& a, const tree_plan& p, int64_t at, int* sequence, int64_t* begin) const {
+    __device__ void find(int64_t at, int* sequence, int64_t* begin) const {
         const int lane = threadIdx.x & 63;
         const int64_t target = quotient(at, units);        // in tiles of one unit
+        if (a.sequences <= 64) {
+            const int b = __builtin_popcountll(__ballot(lane < a.sequences && upto <= target));
+            *sequence = min(b, (int)a.sequences - 1);
+            *begin = this->begin(*sequence);
+            return;
+        }
         int64_t before = 0;
         for (int first = 0;; first += 64) {
-            const int b = first + lane, n = b < a.sequences ? tiles_of(a, p, b) : 0;
+            const int b = first + lane, n = b < a.sequences ? tiles_of(a, p, a.context_lens[b]) : 0;
             int64_t upto = n;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
@@ -117,12 +144,11 @@ struct unit_rows {
     int context, keys;
 
     // unit u of sequence b, head h of its heads
-    __device__ unit_rows(const fq_tree_args& a, const tree_plan& p, int b, int u, int h) : a(a), p(p), b(b) {
+    __device__ unit_rows(const fq_tree_args& a, const tree_plan& p, int b, int u, int h, int context) : a(a), p(p), b(b), context(context) {
         const int set = u / p.row_tiles;
         head = set * p.heads + h;
         first = (u - set * p.row_tiles) * p.unit_rows;
         count = min(p.unit_rows, p.rows - first);
-        context = __builtin_amdgcn_readfirstlane(a.context_lens[b]);
         keys = keys_of(a, context);
     }
     __device__ const uint16_t* query(int r) const {
@@ -327,13 +353,13 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
     if (begin >= stop) return;
     int b;
     int64_t at_b;
-    all.find(a, p, begin, &b, &at_b);
-    int tiles = tiles_of(a, p, b);
+    all.find(begin, &b, &at_b);
+    int context = all.context(b), tiles = tiles_of(a, p, context);
     int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
     wave_state<ACT, DP> w;
 
     for (int64_t pos = begin; pos < stop;) {
-        const unit_rows rows(a, p, b, u, head);
+        const unit_rows rows(a, p, b, u, head, context);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
         float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, head);
         const int key0 = t0 * TILE, key1 = min(rows.keys, t1 * TILE);
@@ -406,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         t0 = 0;
         if (++u == all.units) {
             u = 0;
-            if (++b < a.sequences) tiles = tiles_of(a, p, b);
+            if (++b < a.sequences) context = all.context(b), tiles = tiles_of(a, p, context);
         }
     }
 }
@@ -438,13 +464,13 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
     if (begin >= stop) return;
     int b;
     int64_t at_b;
-    all.find(a, p, begin, &b, &at_b);
-    int tiles = tiles_of(a, p, b);
+    all.find(begin, &b, &at_b);
+    int context = all.context(b), tiles = tiles_of(a, p, context);
     int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
     wave_state<ACT, DP> w;
 
     for (int64_t pos = begin; pos < stop;) {
-        const unit_rows rows(a, p, b, u, 0);
+        const unit_rows rows(a, p, b, u, 0, context);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
         float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(block, pos == begin, 0);
         const int key0 = t0 * KEYS, key1 = min(rows.keys, t1 * KEYS);
@@ -513,7 +539,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
         t0 = 0;
         if (++u == all.units) {
             u = 0;
-            if (++b < a.sequences) tiles = tiles_of(a, p, b);
+            if (++b < a.sequences) context = all.context(b), tiles = tiles_of(a, p, context);
         }
     }
 }
@@ -526,11 +552,9 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
     __shared__ float stats[16][64][2];
     const int waves = blockDim.x / 64;
     const line all(a, p);
-    const int b = (int)(blockIdx.x / all.units), u = (int)(blockIdx.x - (int64_t)b * all.units);
-    int64_t before = 0;
-    for (int x = threadIdx.x & 63; x < b; x += 64) before += tiles_of(a, p, x);
-    const int tiles = tiles_of(a, p, b);
-    const int64_t begin = uniform(wave_sum64(before)) * all.units + (int64_t)u * tiles, end = begin + tiles;
+    const int b = (int)(blockIdx.x / (unsigned)all.units), u = (int)blockIdx.x - b * all.units;
+    const int context = all.context(b), tiles = tiles_of(a, p, context);
+    const int64_t begin = all.begin(b) + (int64_t)u * tiles, end = begin + tiles;
     const int64_t from = quotient(begin, all.per_block), to = quotient(end - 1, all.per_block);        // blocks that have pieces of it
     if (from == to) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.head_dim;
@@ -544,7 +568,7 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
     for (int base = blockIdx.y * step; base < units; base += gridDim.y * step) {
         const int y = base + (many ? 0 : wave * quads) + sub, z = p.by_quads.quotient(y), d = (y - z * (D / 4)) * 4;
         const int head = groups == 1 ? z : z / groups, r = (z - head * groups) * 32 + r0;
-        const unit_rows rows(a, p, b, u, min(head, p.heads - 1));
+        const unit_rows rows(a, p, b, u, min(head, p.heads - 1), context);
         const bool there = sub < quads && y < units && r < rows.count;
         partial_sums sum;
         sum.clear();
@@ -617,7 +641,8 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
     const int64_t units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
     const int64_t most = (p.heads * (p.slot_rows < p.rows ? p.slot_rows : p.rows) + 1) / 2, wanted = 1024 / units;
     const dim3 grid((unsigned)units, (unsigned)(wanted < 1 ? 1 : wanted < most ? wanted : most));
-    fq_attention_tree_join_kernel<ACT><<<grid, units < 16 ? 1024 : 256, 0, stream>>>(a, p);
+    const bool hundreds = units < 16 && a.table_width * a.cache.page_size > 64 * (int64_t)p.tile;
+    fq_attention_tree_join_kernel<ACT><<<grid, hundreds ? 1024 : 256, 0, stream>>>(a, p);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 

@@ -528,3 +528,14 @@ def test_torch_calls_refuse_what_does_not_fit(monkeypatch, native):
     with pytest.raises(TypeError):
         fq.attention_tree(q4.float(), cache, cache, table, lens)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("count", [2, 15, 16, 17, 33, 63, 64, 65, 127, 128, 200])
+def test_tree_many_sequences_find_their_places(count):
+    """The line of tiles over few and many sequences, lengths that make units of one tile and of several."""
+    lens = [(i * 37) % 230 if i % 5 else -1 if i % 2 else 0 for i in range(count)]
+    _tree_case(lens, 1, 2, 1, 64, 16, F16, False, count)
+    _tree_case(lens, 3, 8, 2, 64, 16, BF16, True, count)
+    if count < 70:
+        _tree_case(lens, 40, 2, 1, 64, 16, F16, "shared", count)
+        _tree_case(lens, 70, 2, 1, 64, 16, F16, "shared", count)
