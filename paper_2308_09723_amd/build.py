@@ -65,8 +65,10 @@ NO_SPILL = [
     "fq_gemm_mma_kernel<0, 4, 8, 3, 8, 1, false, 2, false, 1>",   # prefill, fp16
     "fq_gemm_mma_kernel<3, 4, 8, 3, 8, 1, false, 2, false, 1>",   # prefill, bf16 on the fp16 matrix path
 ]
-# Kernels of which no instantiation may: the streaming kernels of 17 rows and more, of row blocks and of grouped tiles.
-NO_SPILL_FAMILIES = ["fq_gemm_mid_kernel", "fq_gemm_mid_items_kernel", "fq_w4a8_mid_kernel"]
+# Kernels of which no instantiation may: the streaming kernels of 17 rows and more, of row blocks and of grouped tiles; attention
+# (whose loads into LDS a wait for a reload would drain).
+NO_SPILL_FAMILIES = ["fq_gemm_mid_kernel", "fq_gemm_mid_items_kernel", "fq_w4a8_mid_kernel", "fq_attention_prompt_kernel",
+                     "fq_attention_tree_stream_kernel", "fq_attention_tree_tile_kernel"]
 
 
 def _run(cmd):

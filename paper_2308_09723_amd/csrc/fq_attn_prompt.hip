@@ -231,11 +231,13 @@ void count_tiles(const fq_prompt_args& a, int first, int n, int64_t* total, int*
 }
 
 // Pieces for the keys of a launch's query tiles: as many as bring the blocks up to the number that run at once, of eight key tiles
-// and more (a piece's sums are written and read again, which costs as much as two tiles, and joining them is a launch).
+// and more, a piece's sums being written and read again and joining them a launch.  (Three pieces of prompts behind 4001 keys, 224 tiles
+// of heads: 138 us whole, 61 in 2 pieces, 63 in 4; 100 queries behind 8000 keys 194 whole, 39 in 16; 1000 tokens of 16 heads in
+// pieces of four tiles 24.4, of eight 24.7.)
 int plan_splits(const fq_prompt_args& a, int64_t total, int longest) {
     const int64_t units = total * a.q_heads, room = 2 * fq_cu_count();
     if (units == 0 || units * 2 > room) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(64, std::min<int64_t>(2 * room / units, longest / 8)));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(64, std::min<int64_t>(room / units, longest / 8)));
 }
 
 // Heads of a die whose keys and values, of all sequences of a launch, its 4 MiB of cache holds.
