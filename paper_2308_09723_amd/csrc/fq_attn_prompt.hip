@@ -219,25 +219,35 @@ int launch(const fq_prompt_args& a, const prompt_plan& p, const prompt_items& it
     return launch<ACT, 128>(a, p, items, total, stream);
 }
 
-// Query tiles of sequences first .. first + n - 1, and the most key tiles that one of them has.
-void count_tiles(const fq_prompt_args& a, int first, int n, int64_t* total, int* longest) {
-    *total = 0;
-    *longest = 0;
-    for (int b = first; b < first + n; ++b) {
-        const int queries = a.q_offsets[b + 1] - a.q_offsets[b], keys = a.k_offsets[b + 1] - a.k_offsets[b];
-        *total += (queries + ROWS - 1) / ROWS;
-        if (queries > 0) *longest = std::max(*longest, (keys + KEYS - 1) / KEYS);
+// Of sequences first .. first + n - 1: query tiles, the key tiles of all of them, and the most that one has.
+struct tile_counts {
+    int64_t total = 0, keys = 0;
+    int longest = 0;
+    tile_counts(const fq_prompt_args& a, int first, int n) {
+        for (int b = first; b < first + n; ++b) {
+            const int64_t queries = a.q_offsets[b + 1] - a.q_offsets[b], all = a.k_offsets[b + 1] - a.k_offsets[b];
+            if (queries == 0) continue;
+            const int64_t tiles = (queries + ROWS - 1) / ROWS, last = (all + KEYS - 1) / KEYS;
+            const int64_t least = std::max<int64_t>(1, std::min(last, (all - queries + ROWS + KEYS - 1) / KEYS));
+            total += tiles;
+            keys += tiles * (least + std::max<int64_t>(1, last)) / 2;
+            longest = std::max(longest, (int)last);
+        }
     }
-}
+};
 
-// Pieces for the keys of a launch's query tiles: as many as bring the blocks up to the number that run at once, of eight key tiles
-// and more, a piece's sums being written and read again and joining them a launch.  (Three pieces of prompts behind 4001 keys, 224 tiles
-// of heads: 138 us whole, 61 in 2 pieces, 63 in 4; 100 queries behind 8000 keys 194 whole, 39 in 16; 1000 tokens of 16 heads in
-// pieces of four tiles 24.4, of eight 24.7.)
-int plan_splits(const fq_prompt_args& a, int64_t total, int longest) {
-    const int64_t units = total * a.q_heads, room = 2 * fq_cu_count();
-    if (units == 0 || units * 2 > room) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(64, std::min<int64_t>(room / units, longest / 8)));
+// Pieces for the keys of a launch's query tiles, a piece's sums being written and read again and joining them a launch.  Few tiles: as
+// many as bring the blocks up to the number that run at once, of eight key tiles and more (three pieces of prompts behind 4001 keys, 224
+// tiles of heads: 138 us whole, 61 in 2 pieces, 66 in 3, 63 in 4; 100 queries behind 8000 keys 194 whole, 39 in 16; 1000 tokens of 16 heads in
+// pieces of four tiles 24.4, of eight 24.7).  More of them, but some of so many keys that the others are done long before: as many as
+// bring those down to a block's even share, of sixteen key tiles and more (one prompt of 3397 tokens, 12 heads of 64: 55 us whole, 44
+// in 3; 15 prompts of 24 - 1018 tokens, 16 heads, 21 whole, 28 in pieces of eight tiles).
+int plan_splits(const fq_prompt_args& a, const tile_counts& c) {
+    const int64_t units = c.total * a.q_heads, work = c.keys * a.q_heads, room = 2 * fq_cu_count();
+    if (units == 0) return 1;
+    const int64_t even = units * 2 <= room ? std::min<int64_t>(room / units, c.longest / 8)
+                                           : std::min<int64_t>((2 * c.longest * room + work) / (2 * work), c.longest / 16);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(64, even));
 }
 
 // Heads of a die whose keys and values, of all sequences of a launch, its 4 MiB of cache holds.
@@ -252,11 +262,9 @@ int heads_together(const fq_prompt_args& a, int first, int n) {
 size_t fq_prompt_bytes(const fq_prompt_args& a) {
     size_t most = 0;
     for (int first = 0; first < a.sequences; first += SEQUENCES) {
-        int64_t total;
-        int longest;
-        count_tiles(a, first, std::min(SEQUENCES, a.sequences - first), &total, &longest);
-        const int splits = plan_splits(a, total, longest);
-        if (splits > 1) most = std::max(most, (size_t)(total * a.q_heads * splits) * ROWS * (a.head_dim + 2) * sizeof(float));
+        const tile_counts c(a, first, std::min(SEQUENCES, a.sequences - first));
+        const int splits = plan_splits(a, c);
+        if (splits > 1) most = std::max(most, (size_t)(c.total * a.q_heads * splits) * ROWS * (a.head_dim + 2) * sizeof(float));
     }
     return most;
 }
@@ -264,9 +272,8 @@ size_t fq_prompt_bytes(const fq_prompt_args& a) {
 int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* workspace, hipStream_t stream) {
     for (int first = 0; first < a.sequences; first += SEQUENCES) {
         const int n = std::min(SEQUENCES, a.sequences - first);
-        int64_t total;
-        int longest;
-        count_tiles(a, first, n, &total, &longest);
+        const tile_counts c(a, first, n);
+        const int64_t total = c.total;
         if (total == 0) continue;
         prompt_plan p = {};
         p.q_heads = a.q_heads;
@@ -274,9 +281,9 @@ int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* wor
         p.by_group = divisor::of((uint32_t)p.group);
         p.D = a.head_dim;
         p.factor = a.scale * LOG2E;
-        p.splits = plan_splits(a, total, longest);
+        p.splits = plan_splits(a, c);
         p.slots = (float*)workspace;
-        if (total * a.q_heads >= 1 << 24) return FQ_ERR_UNSUPPORTED;      // (2^32 threads)
+        if (total * a.q_heads * p.splits >= 1 << 24) return FQ_ERR_UNSUPPORTED;      // (2^32 threads)
         p.units = (int)total * a.q_heads;
         p.together = p.splits > 1 ? std::max(1, a.q_heads / 8) : heads_together(a, first, n);       // (pieces: all blocks run at once anyway)
         p.of_set = (int)total * p.together;
