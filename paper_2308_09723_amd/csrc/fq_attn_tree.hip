@@ -546,7 +546,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
 }
 
 // Joins the pieces of a unit that was cut.  A lane has four values of a row, a wave up to 32 rows of them.  A unit of few pieces: each
-// wave its own; of many: the waves share the pieces of the same values out.  Pieces are added in the line's order.
+// wave its own values; of many: the waves share the pieces of the same values out.  Pieces are added in the line's order.
 template <int ACT>
 __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_args a, tree_plan p) {
     __shared__ f32x4 sums[16][64];
@@ -560,11 +560,13 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
     if (from == to) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.head_dim;
     const bool whole = begin == from * all.per_block;        // (the first block's first piece, or its last)
-    const bool many = to - from >= 8;
-    const int share = many ? ((int)(to - from) + waves) / waves : (int)(to - from + 1), mine = many ? wave : 0;
     // lanes: rows that lie side by side, of as many quads as a wave has room for
     const int side = min(32, p.rows), groups = (p.slot_rows + 31) / 32, quads = 64 / side;
     const int sub = p.by_side.quotient(lane), r0 = lane - sub * side, units = p.heads * groups * (D / 4);
+    // Waves share pieces out where a unit's values leave blocks with little else to do, or where there are very many (64 drafted tokens, 8
+    // sequences, 9 pieces and 64 values for each wave: shared out 18.5 us, a wave its own values 12.8).
+    const bool many = to - from >= (units <= 2 * quads * (int)gridDim.y ? 8 : 32);
+    const int share = many ? ((int)(to - from) + waves) / waves : (int)(to - from + 1), mine = many ? wave : 0;
     const int step = quads * (many ? 1 : waves);
     for (int base = blockIdx.y * step; base < units; base += gridDim.y * step) {
         const int y = base + (many ? 0 : wave * quads) + sub, z = p.by_quads.quotient(y), d = (y - z * (D / 4)) * 4;
@@ -598,7 +600,9 @@ tree_plan plan_tree(const fq_tree_args& a) {
     // Few rows: the waves take neighbouring heads, whose rows of a token lie side by side: 4 x 256 bytes come in 10 % faster than
     // 256.  That makes four times as many pieces as waves that share the keys out, of sums that are no longer few from 16 rows on.
     p.heads = p.rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
-    p.unit_rows = p.rows <= 64 ? 64 : ROWS;
+    // (129 - 192 rows, heads above 96: three tiles of 64 rather than two of 128, a quarter of whose waves had nothing to do: 48 drafted tokens of
+    // eight sequences of 500 - 4095, groups of four: 49.8 -> 45.6 us; heads of 96, 160 rows, 32.6, in three 33.4)
+    p.unit_rows = p.rows <= 64 || (p.rows > 128 && p.rows <= 192 && a.head_dim > 96) ? 64 : ROWS;
     p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
     p.slot_rows = p.rows < 32 ? p.rows : ((p.rows < p.unit_rows ? p.rows : p.unit_rows) + 31) / 32 * 32;
     p.D = a.head_dim;
@@ -636,11 +640,11 @@ int launch_tiles(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) 
 
 template <int ACT, int DP>
 int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
-    const int st = p.rows > 64    ? launch_tiles<ACT, DP, 4>(a, p, stream)
-                   : p.rows > 32  ? launch_tiles<ACT, DP, 2>(a, p, stream)
-                   : p.heads == 4 ? launch_stream<ACT, DP, 4>(a, p, stream)
-                   : p.heads == 2 ? launch_stream<ACT, DP, 2>(a, p, stream)
-                                  : launch_stream<ACT, DP, 1>(a, p, stream);
+    const int st = p.unit_rows > 64 ? launch_tiles<ACT, DP, 4>(a, p, stream)
+                   : p.rows > 32    ? launch_tiles<ACT, DP, 2>(a, p, stream)
+                   : p.heads == 4   ? launch_stream<ACT, DP, 4>(a, p, stream)
+                   : p.heads == 2   ? launch_stream<ACT, DP, 2>(a, p, stream)
+                                    : launch_stream<ACT, DP, 1>(a, p, stream);
     if (st != FQ_OK || p.whole) return st;
     // A block for each unit at least, more for its rows while units are few; sixteen waves where few units may be of hundreds of pieces.
     const int64_t units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
