@@ -18,16 +18,14 @@ struct prompt_items {
     int32_t q_start[SEQUENCES], q_len[SEQUENCES], k_start[SEQUENCES], k_len[SEQUENCES];
     int32_t tiles[SEQUENCES];
     int32_t before[SEQUENCES];       // tiles that come before the levels of which sequence s is the shortest end
-    int32_t count;
+    int32_t count, step;             // step: the largest power of two below count, or 0
 };
 
 // Tile `rank` in that order: its sequence, and its number within it.
 __device__ inline void find_tile(const prompt_items& items, int rank, int* sequence, int* tile) {
-    const int lane = threadIdx.x & 63;
     int s = 0;
-    for (int i = 0; i < SEQUENCES; i += 64)
-        s += __builtin_popcountll(__ballot(i + lane < items.count && items.before[i + lane] <= rank));
-    s = __builtin_amdgcn_readfirstlane(s - 1);
+    for (int step = items.step; step > 0; step /= 2)
+        if (s + step < items.count && items.before[s + step] <= rank) s += step;
     const int in = rank - items.before[s], level = s == 0 ? in : in / (s + 1);
     *sequence = in - level * (s + 1);
     *tile = items.tiles[s] - 1 - level;
@@ -299,6 +297,7 @@ int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* wor
         std::sort(order, order + n, [&](int x, int y) { return tiles[x] != tiles[y] ? tiles[x] > tiles[y] : x < y; });
         prompt_items items = {};
         items.count = n;
+        while (2 * items.step + !items.step < n) items.step = 2 * items.step + !items.step;
         for (int s = 0; s < n; ++s) {
             const int b = first + order[s];
             items.q_start[s] = a.q_offsets[b];

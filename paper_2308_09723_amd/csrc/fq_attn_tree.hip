@@ -366,7 +366,6 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         const int key0 = t0 * TILE, key1 = p.whole ? rows.keys : min(rows.keys, t1 * TILE);
         const int row = min(lane & 31, rows.count - 1);
         w.load_query(rows.query(row), D);
-        w.query_is_here();
         w.clear();
         const int most = table_keys(a, TABLE / 4, TILE);
         for (int part = key0; part < key1; part += most) {
@@ -377,6 +376,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
                 for (int x = lane; x < 2 * SH::BYTES / 16; x += 64) ((u32x4*)mine)[x] = zero;
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the wave's own: no barrier)
+            w.query_is_here();                          // (with the table)
             const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
             int64_t at[LOADS];                          // places of the loads' first rows, where a load lies in a page
             auto load = [&](const uint16_t* from, int base, uint32_t to, const uint32_t (&off)[PERIOD], bool values) {
@@ -478,7 +478,6 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
         const int r = group * 32 + (lane & 31), row = min(r, rows.count - 1);
         const bool busy = group * 32 < rows.count;
         w.load_query(rows.query(row), D);
-        w.query_is_here();
         w.clear();
         const int most = table_keys(a, TABLE, KEYS);
         for (int part = key0; part < key1; part += most) {
@@ -490,6 +489,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
                 for (int x = threadIdx.x; x < 4 * TILE_BYTES / 16; x += 256) ((u32x4*)lds)[x] = zero;
             }
             __syncthreads();
+            w.query_is_here();                          // (with the table)
             const uint16_t *k = (const uint16_t*)a.cache.k + rows.head * a.cache.head_stride, *v = (const uint16_t*)a.cache.v + rows.head * a.cache.head_stride;
             auto load = [&](int base, int buffer) {
                 const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + buffer * 2 * TILE_BYTES) + wave * 1024;
