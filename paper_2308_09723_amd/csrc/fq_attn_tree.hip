@@ -1,8 +1,9 @@
 // Attention of drafted tokens over the pages of a cache (fq_attention_tree).
 //
 // The rows that share a key head's keys are the sequence's nodes times the query heads of the group: one token of four heads a group
-// is four rows, 48 nodes are 192.  Up to 64 rows the call is bound by the cache's bytes (fq_attention_tree_stream_kernel: every wave
-// brings its own keys in), above by the products (fq_attention_tree_tile_kernel: 128 rows a block, four waves on the same keys).
+// is four rows, 48 nodes are 192.  A key and its value are 4 D bytes, and 4 D operations for each row; the card does 170 operations in the
+// time of a byte.  So few rows are bound by the cache's bytes: up to 32, every wave brings in keys of its own (fq_attention_tree_stream_kernel);
+// above, four waves share them (fq_attention_tree_tile_kernel).
 //
 // Work is dealt out evenly whatever the sequences' lengths are: all sequences' key tiles, key head by key head, make one line, and
 // each block takes an equal piece of it, cut where it likes.  Lengths are read on the device, so each block finds its own place (a
@@ -10,6 +11,7 @@
 // not divided, and the maxima they are relative to in the workspace, and a second kernel joins them.
 #include <hip/hip_runtime.h>
 #include <atomic>
+#include <type_traits>
 
 #include "fq_attn_tile.h"
 #include "fq_lds_limit.h"
@@ -28,6 +30,7 @@ struct tree_plan {
     int row_tiles, unit_rows;        // tiles of unit_rows rows that a head's are cut into
     int tile;                        // keys of a tile
     bool whole;                      // units are not cut: each counts as one tile
+    bool once;                       // tiles of 64 rows: keys and values are read past the caches
     int blocks;                      // at most
     int slot_rows;                   // rows of a slot of the workspace
     int D;
@@ -322,6 +325,10 @@ __device__ __forceinline__ void join_parts(const unit_rows& rows, const wave_sta
 // are on their way while the present ones are used, values likewise, and no barrier is needed.  Two blocks of 64 KiB fill a
 // compute unit.  A block's four waves are HEADS key heads x PARTS parts of a tile of 32 PARTS keys; where they share the keys out, they
 // join their sums through LDS at the end of a piece.
+//
+// Bound by the cache's bytes: 64 sequences of 100 - 8191 tokens, one new token each, 32 heads over 8 of 128 values in bfloat16, 437 MB
+// in 75 us = 5.8 TB/s (a kernel that only reads: 7.1).  By latency where keys are few: one sequence of 777 tokens 9 us, reads that
+// wait for each other (lengths, page table, keys, sums).
 template <int ACT, int DP, int HEADS>
 __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tree_args a, tree_plan p) {
     typedef tile_shape<DP> SH;
@@ -440,7 +447,11 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
 
 // ------------------------------------------------------------------------------------------ above 32 rows
 // GROUPS x 32 rows a block; tiles of 64 keys that all waves read, two of them in LDS, as for prompts.  Four groups: every wave takes
-// all keys of a tile.  Two (up to 64 rows): two pairs of waves take half a tile each, and join their sums.
+// all keys of a tile.  Two (tiles of 64 rows): two pairs of waves take half a tile each, and join their sums.
+//
+// 131 000 tokens, 16 drafted, 32 heads over 8 of 128 values (64 rows): 537 MB in 106 us = 5.1 TB/s, products and bytes about even.
+// Eight sequences of 500 - 4095, 48 drafted (192 rows): 12 GF in 38 us; a block has a dozen tiles of keys, and once or twice a beginning
+// and an end that wait for memory.
 template <int ACT, int DP, int GROUPS>
 __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_args a, tree_plan p) {
     typedef tile_shape<DP> SH;
@@ -496,11 +507,15 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
                 if (near && base + KEYS <= part_end) {
                     int64_t place[TILE_BYTES / 4096];
                     table.template places<TILE_BYTES / 4096>(base + wave * (STEP / 4), STEP, place);
+                    auto all_of = [&](auto once) {
 #pragma unroll
-                    for (int j = 0; j < TILE_BYTES / 4096; ++j) {
-                        if (key_at < D) load_lds16<false>(to + j * 4096, k + place[j], key_off);
-                        if (value_at < D) load_lds16<false>(to + TILE_BYTES + j * 4096, v + place[j], value_off);
-                    }
+                        for (int j = 0; j < TILE_BYTES / 4096; ++j) {
+                            if (key_at < D) load_lds16<once.value>(to + j * 4096, k + place[j], key_off);
+                            if (value_at < D) load_lds16<once.value>(to + TILE_BYTES + j * 4096, v + place[j], value_off);
+                        }
+                    };
+                    if (GROUPS == 2 && p.once) all_of(std::true_type());
+                    else all_of(std::false_type());
                 } else {
 #pragma unroll 1
                     for (int j = 0; j < TILE_BYTES / 4096; ++j) {
@@ -614,6 +629,9 @@ tree_plan plan_tree(const fq_tree_args& a) {
     // blocks' worth of units (102 sequences of 223 tokens, 3 units each of 7 tiles: 24.4 -> 18.6 us; one of 250, 2 units of 8: 13.7, whole 18.8).
     const int64_t tiles = (a.table_width * a.cache.page_size + p.tile - 1) / p.tile, units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
     p.whole = tiles <= (units >= 128 ? 8 : 4);
+    // 131 000 tokens, 537 MB: 113.6 -> 103.1 us; 268 MB 49.2 -> 47.1; what the 256 MiB Infinity Cache may still hold from the last call: 16 sequences
+    // of 2000 - 4000, 100 MB, 39.0, past it 41.3.
+    p.once = p.row_tiles == 1 && a.sequences * a.table_width * a.cache.page_size * a.kv_heads * a.head_dim * 4 > (int64_t)256 << 20;
     p.blocks = 2 * fq_cu_count();
     p.factor = a.scale * LOG2E;
     return p;

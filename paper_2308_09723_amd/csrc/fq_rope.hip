@@ -5,7 +5,9 @@
 // consecutive ones where pairs lie side by side; behind it 2 W consecutive ones.  A pair never leaves its lane; the sum of squares
 // goes over a head's lanes (the next power of two of them, those without a unit adding zero).
 //
-// The kernel is bound by memory: what it reads it writes, and computes ten operations a value.
+// The kernel is bound by memory: what it reads it writes, and computes ten operations a value.  One pass, and 16 bytes a lane: 16383
+// tokens of 96 + 96 + 96 heads of 128 values, 2.42 GB in 469 us = 5.2 TB/s (a copy of 2 GiB: 4.9); 2048 tokens of 32 + 32 heads that lie in the
+// Infinity Cache 68 MB in 11.8 us; eight tokens 4.9 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include "fq_internal.h"
