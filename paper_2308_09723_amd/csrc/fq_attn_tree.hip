@@ -30,7 +30,7 @@ struct tree_plan {
     int row_tiles, unit_rows;        // tiles of unit_rows rows that a head's are cut into
     int tile;                        // keys of a tile
     bool whole;                      // units are not cut: each counts as one tile
-    bool once;                       // tiles of 64 rows: keys and values are read past the caches
+    bool once;                       // above 32 rows: keys and values are read past the caches
     int blocks;                      // at most
     int slot_rows;                   // rows of a slot of the workspace
     int D;
@@ -449,9 +449,9 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
 // GROUPS x 32 rows a block; tiles of 64 keys that all waves read, two of them in LDS, as for prompts.  Four groups: every wave takes
 // all keys of a tile.  Two (tiles of 64 rows): two pairs of waves take half a tile each, and join their sums.
 //
-// 131 000 tokens, 16 drafted, 32 heads over 8 of 128 values (64 rows): 537 MB in 106 us = 5.1 TB/s, products and bytes about even.
-// Eight sequences of 500 - 4095, 48 drafted (192 rows): 12 GF in 38 us; a block has a dozen tiles of keys, and once or twice a beginning
-// and an end that wait for memory.
+// 131 000 tokens, 16 drafted, 32 heads over 8 of 128 values (64 rows): 537 MB in 93 us = 5.8 TB/s, bound by what is on its way at once (a tile a
+// block; the matrix units are busy 15 % of the time).  Eight sequences of 500 - 4095, 48 drafted (192 rows): 12 GF in 39 us; a block has a
+// dozen tiles of keys, and once or twice a beginning and an end that wait for memory.
 template <int ACT, int DP, int GROUPS>
 __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_args a, tree_plan p) {
     typedef tile_shape<DP> SH;
@@ -514,7 +514,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
                             if (value_at < D) load_lds16<once.value>(to + TILE_BYTES + j * 4096, v + place[j], value_off);
                         }
                     };
-                    if (GROUPS == 2 && p.once) all_of(std::true_type());
+                    if (p.once) all_of(std::true_type());
                     else all_of(std::false_type());
                 } else {
 #pragma unroll 1
@@ -629,7 +629,7 @@ tree_plan plan_tree(const fq_tree_args& a) {
     // blocks' worth of units (102 sequences of 223 tokens, 3 units each of 7 tiles: 24.4 -> 18.6 us; one of 250, 2 units of 8: 13.7, whole 18.8).
     const int64_t tiles = (a.table_width * a.cache.page_size + p.tile - 1) / p.tile, units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
     p.whole = tiles <= (units >= 128 ? 8 : 4);
-    // 131 000 tokens, 537 MB: 113.6 -> 103.1 us; 268 MB 49.2 -> 47.1; what the 256 MiB Infinity Cache may still hold from the last call: 16 sequences
+    // 131 000 tokens, 537 MB, 64 rows 113.6 -> 103.1 us, 268 MB 49.2 -> 47.1; 100 000, 96 rows 99.6 -> 90.5; what the 256 MiB Infinity Cache may still hold from the last call: 16 sequences
     // of 2000 - 4000, 100 MB, 39.0, past it 41.3.
     p.once = p.row_tiles == 1 && a.sequences * a.table_width * a.cache.page_size * a.kv_heads * a.head_dim * 4 > (int64_t)256 << 20;
     p.blocks = 2 * fq_cu_count();
