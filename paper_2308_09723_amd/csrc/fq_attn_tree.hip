@@ -30,6 +30,7 @@ struct tree_plan {
     int row_tiles, unit_rows;        // tiles of unit_rows rows that a head's are cut into
     int tile;                        // keys of a tile
     bool whole;                      // units are not cut: each counts as one tile
+    bool by_lanes;                   // up to 64 sequences, of fewer than 2^31 tiles
     bool once;                       // above 32 rows: keys and values are read past the caches
     int blocks;                      // at most
     int slot_rows;                   // rows of a slot of the workspace
@@ -81,13 +82,13 @@ struct line {
     int64_t per_block;               // tiles
     int64_t total;
     int units;                       // of a sequence
-    int mine, tiles, upto;           // up to 64 sequences: the lane's length, its tiles, all tiles up to it
+    int mine, tiles, upto;           // by_lanes: the lane's length, its tiles, all tiles up to it
 
     __device__ line(const fq_tree_args& a, const tree_plan& p) : a(a), p(p) {
         const int lane = threadIdx.x & 63;
         units = a.kv_heads / p.heads * p.row_tiles;
         mine = tiles = upto = 0;
-        if (a.sequences <= 64) {
+        if (p.by_lanes) {
             if (lane < a.sequences) {
                 mine = a.context_lens[lane];
                 tiles = tiles_of(a, p, mine);
@@ -101,10 +102,10 @@ struct line {
         }
         per_block = quotient(total + p.blocks - 1, p.blocks);
     }
-    __device__ int context(int b) const { return a.sequences <= 64 ? __builtin_amdgcn_readlane(mine, b) : __builtin_amdgcn_readfirstlane(a.context_lens[b]); }
+    __device__ int context(int b) const { return p.by_lanes ? __builtin_amdgcn_readlane(mine, b) : __builtin_amdgcn_readfirstlane(a.context_lens[b]); }
     // where sequence b's tiles begin
     __device__ int64_t begin(int b) const {
-        if (a.sequences <= 64) return (int64_t)(__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(tiles, b)) * units;
+        if (p.by_lanes) return (int64_t)(__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(tiles, b)) * units;
         int64_t before = 0;
         for (int x = threadIdx.x & 63; x < b; x += 64) before += tiles_of(a, p, a.context_lens[x]);
         return uniform(wave_sum64(before)) * units;
@@ -113,7 +114,7 @@ struct line {
     __device__ void find(int64_t at, int* sequence, int64_t* begin) const {
         const int lane = threadIdx.x & 63;
         const int64_t target = quotient(at, units);        // in tiles of one unit
-        if (a.sequences <= 64) {
+        if (p.by_lanes) {
             const int b = __builtin_popcountll(__ballot(lane < a.sequences && upto <= target));
             *sequence = min(b, (int)a.sequences - 1);
             *begin = this->begin(*sequence);
@@ -629,9 +630,10 @@ tree_plan plan_tree(const fq_tree_args& a) {
     // blocks' worth of units (102 sequences of 223 tokens, 3 units each of 7 tiles: 24.4 -> 18.6 us; one of 250, 2 units of 8: 13.7, whole 18.8).
     const int64_t tiles = (a.table_width * a.cache.page_size + p.tile - 1) / p.tile, units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
     p.whole = tiles <= (units >= 128 ? 8 : 4);
+    p.by_lanes = a.sequences <= 64 && a.sequences * tiles < INT32_MAX;
     // 131 000 tokens, 537 MB, 64 rows 113.6 -> 103.1 us, 268 MB 49.2 -> 47.1; 100 000, 96 rows 99.6 -> 90.5; what the 256 MiB Infinity Cache may still hold from the last call: 16 sequences
     // of 2000 - 4000, 100 MB, 39.0, past it 41.3.
-    p.once = p.row_tiles == 1 && a.sequences * a.table_width * a.cache.page_size * a.kv_heads * a.head_dim * 4 > (int64_t)256 << 20;
+    p.once = p.row_tiles == 1 && (double)a.sequences * a.table_width * a.cache.page_size * a.kv_heads * a.head_dim * 4 > 0x1p28;
     p.blocks = 2 * fq_cu_count();
     p.factor = a.scale * LOG2E;
     return p;
