@@ -539,3 +539,25 @@ def test_tree_many_sequences_find_their_places(count):
     if count < 70:
         _tree_case(lens, 40, 2, 1, 64, 16, F16, "shared", count)
         _tree_case(lens, 70, 2, 1, 64, 16, F16, "shared", count)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("lens,nodes,hq,hk,D", [
+    ([150, 0, 700], 35, 4, 1, 128), ([90, 333], 48, 8, 2, 128), ([200], 43, 3, 1, 104),        # 129 - 192 rows: three tiles of 64
+    ([2100], 40, 4, 1, 128),                                                                   # a unit of many pieces, of few values
+    ([544] * 7, 32, 32, 8, 128),                                                               # nine pieces each, of many values
+])
+def test_tree_rows_in_tiles(dtype, lens, nodes, hq, hk, D):
+    _tree_case(lens, nodes, hq, hk, D, 16, dtype, True, nodes + len(lens))
+
+
+@pytest.mark.parametrize("nodes,hq", [(1, 2), (12, 8), (30, 8), (48, 8)])
+def test_tree_of_a_table_for_long_contexts(nodes, hq):
+    """Tables for more keys than the caches hold, whose sequences are short."""
+    lens, hk, D = [700, 70], 2, 128
+    kc, vc, table, context = _cache(lens, nodes, 16, hk, D, BF16, 21)
+    wide = torch.cat([table, torch.full((2, 9000), 2 ** 31 - 1, dtype=torch.int32)], 1)
+    q = _normal((2, nodes, hq, D), BF16, 22, 1.5)
+    sees = torch.stack([ref.from_parents(_random_tree(nodes, b)) for b in range(2)])
+    got = fq.attention_tree(q.cuda(), kc.cuda(), vc.cuda(), wide.cuda(), context.cuda(), mask=ref.words(sees).cuda())
+    ref.compare(got, *ref.tree(q, kc, vc, table, context, sees), "a wide table")
