@@ -10,7 +10,9 @@
 // Running maximum: numerators are taken relative to a maximum that is renewed only when a score exceeds it by 2^8 (times
 // factor), so that most tiles leave the sums alone.  The numerators are at most 2^8 then, which binary16 holds with the same relative error.
 // bfloat16 numerators may be as large as binary32's: there the maximum of a tile is not even looked for until the numerators' sum
-// has passed 2^60 (8192 tokens: 518 -> 508 us); one that passes 2^128 within a tile shows in the result, and the queries are computed one by one.
+// has passed 2^60 (8192 tokens: 518 -> 508 us).  Sums that large are first made small again (level()): a factor that brings sums of
+// 2^127 down to a larger maximum may lie below binary32's smallest, and nothing would be left of what is half the result.  A sum that passes 2^128
+// within a tile shows in the result, and the queries are computed one by one.
 //
 // What a query does not see has weight zero in the products, and zero times an infinity or a NaN is a NaN: a wave whose
 // results are not finite computes its queries again, one by one and seen keys alone (attend_one).
@@ -193,7 +195,7 @@ struct wave_state {
     u32x4 q[SH::STEPS];
     f32x16 o[SH::TILES];
     bool stale;          // whether the next tile's maximum is looked for (bfloat16)
-    float m, c, l;       // maximum that the numerators are relative to (raw scores), the same times factor (0: none yet), this lane's sum
+    float m, c, l;       // what the numerators are relative to (log2; -infinity: none yet), the same (0: none yet), this lane's sum
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -255,17 +257,38 @@ struct wave_state {
         }
     }
 
+    // Sums of more than 2^30 made relative to as much more: to about 1 by factors that are no smaller than 2^-64.
+    __device__ __forceinline__ void level() {
+        const float most = other_half_max(l);
+        if (!__any(most > 0x1p30f)) return;
+        const float by = m + (float)__builtin_amdgcn_frexp_expf(most) - m;       // (what binary32 makes of it; 0 of a sum that is not finite)
+        const float half = m == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(-0.5f * by);
+        if (m != -__builtin_inff()) c = m += by;
+        l = l * half * half;
+#pragma unroll
+        for (int t = 0; t < SH::TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] = o[t][i] * half * half;
+    }
+
+    // The sum of both halves; sums that others are added to as slots and LDS hold them: no more than 2^30 times the largest numerator.
+    __device__ __forceinline__ void finish(bool joined) {
+        if (ACT == FQ_BF16 && joined) level();
+        l = other_half_sum(l);
+    }
+
     // Numerators of the scores, in the order that accumulate() takes; maximum, sum and results brought along.
     template <int H>
     __device__ __forceinline__ void soften(f32x16 (&s)[H], float factor, u32x4 (&p)[2 * H]) {
         if (ACT == FQ_F16 || stale) {
+            if (ACT == FQ_BF16) level();
             float top = s[0][0];
 #pragma unroll
             for (int i = 1; i < 16 * H; ++i) top = __builtin_fmaxf(top, s[i >> 4][i & 15]);
-            top = other_half_max(top);
-            if (__any(top * factor > m * factor + 8.0f)) {
-                const float now = __builtin_fmaxf(m, top), next = now == -__builtin_inff() ? 0.0f : now * factor;
-                const float again = __builtin_amdgcn_exp2f(m * factor - next);       // (0 where there was none)
+            top = other_half_max(top) * factor;
+            if (__any(top > m + 8.0f)) {
+                const float now = __builtin_fmaxf(m, top), next = now == -__builtin_inff() ? 0.0f : now;
+                const float again = __builtin_amdgcn_exp2f(m - next);       // (0 where there was none)
                 m = now;
                 c = next;
                 l *= again;
@@ -317,7 +340,7 @@ struct wave_state {
     }
 
     // what the sums are relative to (log2), -infinity where there are none
-    __device__ __forceinline__ float top() const { return m == -__builtin_inff() ? m : c; }
+    __device__ __forceinline__ float top() const { return m; }
 
     // whether every sum of the wave's queries is finite
     __device__ __forceinline__ bool finite() const {

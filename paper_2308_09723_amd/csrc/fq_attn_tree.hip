@@ -430,7 +430,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
                 if (more) load(v, base + TILE, mine_at + SH::BYTES, value_off, true);
             }
         }
-        w.l = other_half_sum(w.l);
+        w.finish(PARTS > 1 || slot);
         if constexpr (PARTS == 1) {
             if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
             else if ((lane & 31) < rows.count) w.put(rows.result(row), slot, p.shape(), row);
@@ -545,7 +545,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
                 w.template accumulate<HALVES>(at + TILE_BYTES, x);
             }
         }
-        w.l = other_half_sum(w.l);
+        w.finish(PARTS > 1 || slot);
         if constexpr (PARTS > 1) {
             join_parts<ACT, DP, PARTS>(rows, w, lds, JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
         } else {

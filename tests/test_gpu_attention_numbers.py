@@ -1,0 +1,91 @@
+"""Attention where its arithmetic can go wrong: scores that rise late and far, numerators at the end of a type's range."""
+import pytest
+import torch
+
+from paper_2308_09723_amd import fq
+
+import attention_util as ref
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def _normal(size, dtype, seed, sigma=1.0):
+    return (torch.randn(size, generator=torch.Generator().manual_seed(seed)) * sigma).to(dtype)
+
+
+# Where a row of single keys is attended to, kernel by kernel: (nodes, query heads, key heads), or queries of a prompt.
+# stream: up to 32 rows a key head, one, two and four heads a block; tile64, tile128: rows in tiles of 64 and of 128.
+ROWS = {"stream1": (1, 3, 1), "stream2": (2, 4, 2), "stream4": (1, 16, 4), "tile64": (20, 2, 1), "tile128": (70, 1, 1)}
+
+
+def _scored(name, scores, dtype, D=64, seed=0, v=None):
+    """Attention over keys of the given scores (natural logarithms) -> (result, queries, keys, values, what a row sees); every query's
+    scores are the same, rounded to the type as keys."""
+    n = len(scores)
+    k = torch.zeros((n, D), dtype=dtype)
+    k[:, 0] = torch.tensor(scores, dtype=torch.float64).to(dtype)
+    k[:, 1:] = _normal((n, D - 1), dtype, seed)         # (met by zeros of the queries)
+    v = _normal((n, D), dtype, seed + 1) if v is None else v
+    if name.startswith("prompt"):
+        rows = n if name == "prompt" else 2             # all of the prompt; its last two, whose keys are cut into pieces where they are many
+        q = torch.zeros((rows, 2, D), dtype=dtype)
+        q[..., 0] = 1
+        got = fq.attention_prompt(q.cuda(), k[:, None].contiguous().cuda(), v[:, None].contiguous().cuda(), [0, rows], [0, n], scale=1.0)
+        seen = torch.arange(n)[None] <= torch.arange(rows)[:, None] + n - rows
+        return got.cpu(), q, k, v, seen
+    nodes, hq, hk = ROWS[name]
+    page = 16
+    pages = (n + page - 1) // page
+    q = torch.zeros((1, nodes, hq, D), dtype=dtype)
+    q[..., 0] = 1
+    kc, vc = (torch.zeros((pages * page, hk, D), dtype=dtype) for _ in range(2))
+    kc[:n], vc[:n] = k[:, None], v[:, None]
+    table = torch.arange(pages, dtype=torch.int32)[None]
+    lens = torch.tensor([n - nodes], dtype=torch.int32)
+    got = fq.attention_tree(q.cuda(), kc.view(pages, page, hk, D).cuda(), vc.view(pages, page, hk, D).cuda(), table.cuda(), lens.cuda(), scale=1.0)
+    seen = torch.arange(n)[None] < torch.arange(nodes)[:, None] + n - nodes + 1
+    return got[0].cpu(), q[0], k, v, seen
+
+
+def _check(name, scores, dtype, D=64, seed=0):
+    got, q, k, v, seen = _scored(name, scores, dtype, D, seed)
+    want, tol = ref.attend(q[:, 0], k, v, seen, 1.0)
+    for h in range(q.shape[1]):
+        ref.compare(got[:, h], want, tol, f"{name}, head {h}")
+
+
+ALL = ["prompt", "prompt_end"] + list(ROWS)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("rises", [(87.5, 88.0, 0.0), (88.5, 88.5, 88.5), (87.5, 87.0, 175.0), (43.0, 88.0, 130.0), (86.0, 0.0, 87.5), (60.0, 120.0, 180.0),
+                                   (88.0, 176.0, 264.0), (42.0, 42.0, 42.0), (89.0, 88.0, 87.5), (300.0, 388.0, 300.0)])
+@pytest.mark.parametrize("name", ALL)
+def test_scores_that_rise_late(name, rises, dtype):
+    """Keys of score zero, and three far above them, in neighbouring tiles (of 32, 64 and 128 keys) or some apart: sums relative to the first keys'
+    scores nearly leave binary32 (2^128 is a rise of 88.7), and are brought along to the next."""
+    for n, at in ((300, (70, 100, 140)), (300, (70, 140, 210)), (600, (140, 260, 390)), (4500, (400, 1900, 4300)), (4500, (500, 600, 1000))):
+        scores = [0.0] * n
+        for i, x in zip(at, rises):
+            scores[i] = x
+        if name == "prompt" and n > 600:
+            continue
+        _check(name, scores, dtype, seed=n + at[0])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("name", ["prompt_end"] + list(ROWS))
+def test_a_rise_in_every_piece(name, dtype):
+    """The same rise every 100 keys, in pieces of several tiles: the sums of those that begin with scores of zero are nearly 2^128 of these
+    scores' exponentials, and those of others are not; joined they have their shares."""
+    n = 70000
+    for rise in (87.0, 88.5):
+        scores = [0.0] * n
+        scores[99::100] = [rise] * (n // 100)
+        got, q, k, v, seen = _scored(name, scores, dtype, seed=int(rise))
+        for row in (0, q.shape[0] - 1):
+            want, tol = ref.attend(q[row:row + 1, 0], k, v, seen[row:row + 1], 1.0)
+            for h in range(q.shape[1]):
+                ref.compare(got[row:row + 1, h], want, tol, f"{name}, rise {rise}, row {row}, head {h}")
