@@ -363,7 +363,8 @@ int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_
  * k_offsets[b] .. k_offsets[b+1]-1 of k and v belong to sequence b, whose last query is at its last key:
  *   out[i, h] = sum_j softmax_j(scale * q[i, h] . k[j, h']) v[j, h'],   j <= i + (keys of b) - (queries of b)   (i, j in b)
  * (more keys than queries: a prefix is there already; a query that sees no key gives zeros).  Scores, softmax and sums are
- * binary32; the softmax's numerators are rounded to act_dtype for their product with the values, the result once.  What a
+ * binary32; the softmax's numerators are rounded to act_dtype for their product with the values (FQ_F16: relative to the row's largest
+ * they keep the type's precision down to 2^-21 and are zeros below 2^-32), the result once.  What a
  * query does not see has no part in its result, not by an infinity or a NaN either.
  *
  *   q, k, v        in   device rows of q_heads, kv_heads, kv_heads heads

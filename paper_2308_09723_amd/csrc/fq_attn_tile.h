@@ -8,7 +8,9 @@
 // comes in.  Neither scores nor numerators pass through LDS.
 //
 // Running maximum: numerators are taken relative to a maximum that is renewed only when a score exceeds it by 2^8 (times
-// factor), so that most tiles leave the sums alone.  The numerators are at most 2^8 then, which binary16 holds with the same relative error.
+// factor), so that most tiles leave the sums alone.  binary16 numerators are 2^7 times as large, 2^7 to 2^15 for the largest score: all that
+// lie within 2^-21 of it keep the type's relative error, and only below 2^-32 of it they are zeros for the product while their sum has them (relative
+// to the maximum itself that is 2^-25, and 131071 keys 2^-25 below one other were missing 0.4 % of a result).
 // bfloat16 numerators may be as large as binary32's: there the maximum of a tile is not even looked for until the numerators' sum
 // has passed 2^60 (8192 tokens: 518 -> 508 us).  Sums that large are first made small again (level()): a factor that brings sums of
 // 2^127 down to a larger maximum may lie below binary32's smallest, and nothing would be left of what is half the result.  A sum that passes 2^128
@@ -195,6 +197,7 @@ struct wave_state {
     u32x4 q[SH::STEPS];
     f32x16 o[SH::TILES];
     bool stale;          // whether the next tile's maximum is looked for (bfloat16)
+    static constexpr float LARGER = ACT == FQ_F16 ? 7.0f : 0.0f;       // the first score's numerator, log2
     float m, c, l;       // what the numerators are relative to (log2; -infinity: none yet), the same (0: none yet), this lane's sum
 
     __device__ __forceinline__ void clear() {
@@ -285,7 +288,7 @@ struct wave_state {
             float top = s[0][0];
 #pragma unroll
             for (int i = 1; i < 16 * H; ++i) top = __builtin_fmaxf(top, s[i >> 4][i & 15]);
-            top = other_half_max(top) * factor;
+            top = other_half_max(top) * factor - LARGER;
             if (__any(top > m + 8.0f)) {
                 const float now = __builtin_fmaxf(m, top), next = now == -__builtin_inff() ? 0.0f : now;
                 const float again = __builtin_amdgcn_exp2f(m - next);       // (0 where there was none)

@@ -89,3 +89,38 @@ def test_a_rise_in_every_piece(name, dtype):
             want, tol = ref.attend(q[row:row + 1, 0], k, v, seen[row:row + 1], 1.0)
             for h in range(q.shape[1]):
                 ref.compare(got[row:row + 1, h], want, tol, f"{name}, rise {rise}, row {row}, head {h}")
+
+
+@pytest.mark.parametrize("name", ["prompt"] + list(ROWS))
+def test_many_small_numerators_beside_a_large_one(name):
+    """binary16: one key 17.4 above 131071 others, which together have 0.4 % of the weight, in one piece (as many heads, or sequences that share
+    their pages, as there are blocks).  What is allowed is 2^-32 sum |v| for numerators below the smallest normal binary16, which the largest one
+    exceeds by 2^21 and more (half a unit of subnormal numbers, 2^-25, over the largest numerator, 2^7), in place of attention_util's 2^-25 sum |v|."""
+    n, D = 131072, 64
+    k = torch.zeros((n, D), dtype=F16)
+    k[7, 0] = 17.4
+    v = 1.0 + 0.01 * torch.randn((n, D), generator=torch.Generator().manual_seed(5))
+    v[7] = 0.25
+    v = v.to(F16)
+    blocks = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    if name == "prompt":
+        nodes, hq, hk = 2, blocks, 1
+        q = torch.zeros((nodes, hq, D), dtype=F16, device="cuda")
+        q[..., 0] = 1
+        got = fq.attention_prompt(q, k[:, None].contiguous().cuda(), v[:, None].contiguous().cuda(), [0, 2], [0, n], scale=1.0)[None]
+    else:
+        nodes, hq, hk = ROWS[name]
+        q = torch.zeros((blocks, nodes, hq, D), dtype=F16, device="cuda")
+        q[..., 0] = 1
+        kc, vc = (x[:, None].expand(n, hk, D).contiguous().cuda().view(n // 64, 64, hk, D) for x in (k, v))
+        table = torch.arange(n // 64, dtype=torch.int32, device="cuda")[None].expand(blocks, n // 64).contiguous()
+        lens = torch.full((blocks,), n - nodes, dtype=torch.int32, device="cuda")
+        got = fq.attention_tree(q, kc, vc, table, lens, scale=1.0)
+    one = torch.zeros((1, D), dtype=F16)
+    one[:, 0] = 1
+    for node in (0, nodes - 1):
+        seen = torch.arange(n)[None] < n - nodes + node + 1
+        want, tol = ref.attend(one, k, v, seen, 1.0)
+        total = v[seen[0]].double().abs().sum(0)
+        tol = tol - 2.0 ** -25 * total + 2.0 ** -32 * total
+        ref.compare(got[:, node], want[None], tol[None], f"{name}, node {node}")
