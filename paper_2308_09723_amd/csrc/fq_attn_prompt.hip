@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
     __syncthreads();                         // (nobody reads keys and values any more)
     float* slot = p.splits > 1 ? p.slot(unit, piece) : nullptr;
     w.finish(slot != nullptr);
-    if (!w.finite()) {
+    if (!w.sound()) {
         for (int x = 0; x < 32 && first + x < queries; ++x) {
             const int64_t r = (int64_t)items.q_start[sequence] + first + x;
             const int sees = first + x + 1 + ahead;

@@ -17,7 +17,8 @@
 // within a tile shows in the result, and the queries are computed one by one.
 //
 // What a query does not see has weight zero in the products, and zero times an infinity or a NaN is a NaN: a wave whose
-// results are not finite computes its queries again, one by one and seen keys alone (attend_one).
+// results are not finite, or whose sums say that the largest score's numerator was lost, computes its queries again, one by one and seen
+// keys alone (attend_one).
 #ifndef FQ_ATTN_TILE_H_
 #define FQ_ATTN_TILE_H_
 
@@ -345,9 +346,10 @@ struct wave_state {
     // what the sums are relative to (log2), -infinity where there are none
     __device__ __forceinline__ float top() const { return m; }
 
-    // whether every sum of the wave's queries is finite
-    __device__ __forceinline__ bool finite() const {
-        float x = l * 0.0f;
+    // Whether every sum of the wave's queries is finite, and the largest numerator of each what it should be: a score is taken less the reference
+    // exactly, but the reference is rounded, and from 2^31 on half a unit of it may make all numerators zeros.
+    __device__ __forceinline__ bool sound() const {
+        float x = l >= 0.25f || m == -__builtin_inff() ? l * 0.0f : 1.0f;
 #pragma unroll
         for (int t = 0; t < SH::TILES; ++t)
 #pragma unroll

@@ -276,7 +276,7 @@ __device__ __forceinline__ void join_parts(const unit_rows& rows, const wave_sta
     __syncthreads();                                    // (nobody reads the keys and values that lay here, nor the sums of the piece before)
     if (threadIdx.x == 0) stats[256] = 0.0f;
     __syncthreads();
-    if (!w.finite() && lane == 0) stats[256] = 1.0f;
+    if (!w.sound() && lane == 0) stats[256] = 1.0f;
     if (lane < 32) {
         stats[(wave * 32 + lane) * 2] = w.top();
         stats[(wave * 32 + lane) * 2 + 1] = w.l;
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         }
         w.finish(PARTS > 1 || slot);
         if constexpr (PARTS == 1) {
-            if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
+            if (!w.sound()) rows.one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
             else if ((lane & 31) < rows.count) w.put(rows.result(row), slot, p.shape(), row);
         } else {
             join_parts<ACT, DP, PARTS>(rows, w, lds, WAVE_BYTES, stats, head, HEADS, part_of, 0, key0, key1, slot);
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
         if constexpr (PARTS > 1) {
             join_parts<ACT, DP, PARTS>(rows, w, lds, JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
         } else {
-            if (!w.finite()) rows.one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
+            if (!w.sound()) rows.one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
             else if (r < rows.count) w.put(rows.result(r), slot, p.shape(), r);
         }
         pos += t1 - t0;

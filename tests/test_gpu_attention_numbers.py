@@ -124,3 +124,29 @@ def test_many_small_numerators_beside_a_large_one(name):
         total = v[seen[0]].double().abs().sum(0)
         tol = tol - 2.0 ** -25 * total + 2.0 ** -32 * total
         ref.compare(got[:, node], want[None], tol[None], f"{name}, node {node}")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("nodes,hq,hk", ROWS.values(), ids=list(ROWS))
+def test_one_key_of_any_score(dtype, nodes, hq, hk):
+    """A row that sees one key has its value, however large the score is against binary32's units.  (The numerator and the result are rounded.)"""
+    rows, D = 400, 64
+    gen = torch.Generator().manual_seed(6)
+    size = 2.0 ** (torch.rand(rows, generator=gen) * (15 if dtype == F16 else 40))
+    q, k = torch.zeros((rows, hq, D), dtype=dtype), torch.zeros((rows, hk, D), dtype=dtype)
+    q[..., 0] = size.to(dtype)[:, None]
+    k[..., 0] = (size * (1 + torch.rand(rows, generator=gen)) * (torch.randint(0, 2, (rows,), generator=gen) * 2 - 1) * 0.9).to(dtype)[:, None]
+    v = _normal((rows, hk, D), dtype, 7)
+    want = v[:, torch.arange(hq) // (hq // hk)]
+    got = fq.attention_prompt(q.cuda(), k.cuda(), v.cuda(), list(range(rows + 1)), scale=1.0).cpu()
+    tol = 2 * ref.UNIT[dtype] * want.double().abs() + 2.0 ** -24
+    ref.compare(got, want.double(), tol, "prompts of one token")
+    # over a cache: each sequence's nodes see the node 0 alone
+    kc, vc = (torch.zeros((rows, 128, hk, D), dtype=dtype) for _ in range(2))
+    kc[:, 0], vc[:, 0] = k, v
+    table, lens = torch.arange(rows, dtype=torch.int32, device="cuda")[:, None].contiguous(), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    mask = torch.zeros((nodes, (nodes + 63) // 64), dtype=torch.int64)
+    mask[:, 0] = 1
+    q4 = q[:, None].expand(rows, nodes, hq, D).contiguous()
+    got = fq.attention_tree(q4.cuda(), kc.cuda(), vc.cuda(), table, lens, mask=mask.cuda(), scale=1.0).cpu()
+    ref.compare(got, want.double()[:, None], tol[:, None], "one node")
