@@ -362,10 +362,10 @@ int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_
  * fq_attention_prompt -- causal attention over packed sequences.  Rows q_offsets[b] .. q_offsets[b+1]-1 of q and rows
  * k_offsets[b] .. k_offsets[b+1]-1 of k and v belong to sequence b, whose last query is at its last key:
  *   out[i, h] = sum_j softmax_j(scale * q[i, h] . k[j, h']) v[j, h'],   j <= i + (keys of b) - (queries of b)   (i, j in b)
- * (more keys than queries: a prefix is there already; a query that sees no key gives zeros).  Scores, softmax and sums are
- * binary32; the softmax's numerators are rounded to act_dtype for their product with the values (FQ_F16: relative to the row's largest
- * they keep the type's precision down to 2^-21 and are zeros below 2^-32), the result once.  What a
- * query does not see has no part in its result, not by an infinity or a NaN either.
+ * (more keys than queries: a prefix is there already; a query that sees no key gives zeros, one whose seen scores are all -infinity
+ * gives NaN).  Scores, softmax and sums are binary32; the softmax's numerators are rounded to act_dtype for their product with the
+ * values (FQ_F16: relative to the row's largest they keep the type's precision down to 2^-21 and are zeros below 2^-32), the result
+ * once.  What a query does not see has no part in its result, not by an infinity or a NaN either.
  *
  *   q, k, v        in   device rows of q_heads, kv_heads, kv_heads heads
  *   q_offsets_host in   HOST array [sequences + 1], non-decreasing, q_offsets_host[0] = 0

@@ -127,14 +127,22 @@ __device__ inline void attend_one(const uint16_t* q, const ROWS& rows, const SEE
     *l_out = l;
 }
 
-// Its result, to row `out`.
-template <int ACT>
-__device__ inline void store_one(uint16_t* out, const float* o, float l, int D) {
+// 1 / l for a row's sum of numerators.  0: a row that sees no key, zeros; or one whose keys' scores are all -infinity, whose softmax is no number
+// (sees(): whether the row sees a key, asked for then).
+template <typename SEES>
+__device__ inline float inverse(float l, const SEES& sees) {
+    if (l != 0.0f) return 1.0f / l;
+    return sees() ? __builtin_nanf("") : 0.0f;
+}
+
+// attend_one's result, to row `out`.
+template <int ACT, typename SEES>
+__device__ inline void store_one(uint16_t* out, const float* o, float l, int D, const SEES& sees) {
     typedef typename type16<ACT>::t T;
     typedef T vec2 __attribute__((ext_vector_type(2)));
     const int lane = threadIdx.x & 63;
     if (2 * lane >= D) return;
-    const float r = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
+    const float r = inverse(l, sees);
     vec2 v;
     v[0] = (T)(o[0] * r);
     v[1] = (T)(o[1] * r);

@@ -173,13 +173,14 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
             float o[2], c, sum;
             attend_one<ACT>((const uint16_t*)q.data + r * q.row_stride + h * q.head_stride, rows, sees_first{sees}, t0 * KEYS, min(sees, t1 * KEYS), D,
                             p.factor, o, &c, &sum);
-            put_one<ACT>(out + (r * p.q_heads + h) * D, slot, p.shape(), wave * 32 + x, o, c, sum);
+            put_one<ACT>(out + (r * p.q_heads + h) * D, slot, p.shape(), wave * 32 + x, o, c, sum, [&] { return sees > 0; });
         }
     } else if (slot) {
-        if (i < queries) w.put(nullptr, slot, p.shape(), wave * 32 + (lane & 31));
+        if (i < queries) w.put(nullptr, slot, p.shape(), wave * 32 + (lane & 31), [&] { return end > 0; });
     } else if (first < queries) {
         uint16_t* to = out + (((int64_t)items.q_start[sequence] + first) * p.q_heads + h) * D;
-        w.put_rows(lds + wave * 2 * SH::BYTES, [&](int r) { return to + (int64_t)r * p.q_heads * D; }, queries - first, D);
+        w.put_rows(lds + wave * 2 * SH::BYTES, [&](int r) { return to + (int64_t)r * p.q_heads * D; }, queries - first, D,
+                   [&] { return end > 0; });
     }
 }
 
@@ -198,7 +199,8 @@ __global__ __launch_bounds__(256) void fq_attention_prompt_join_kernel(prompt_pl
         partial_sums all;
         all.clear();
         all.add(0, p.splits, [&](int y) { return p.slot(unit, y); }, p.shape(), r, d);
-        all.template store<ACT>(out + (((int64_t)items.q_start[sequence] + tile * ROWS + r) * p.q_heads + h) * D + d);
+        all.template store<ACT>(out + (((int64_t)items.q_start[sequence] + tile * ROWS + r) * p.q_heads + h) * D + d,
+                                [&] { return tile * ROWS + r + 1 + items.k_len[sequence] - items.q_len[sequence] > 0; });
     }
 }
 

@@ -133,10 +133,10 @@ struct slot_shape {
     }
 };
 // attend_one's result, or its sums to row r of a slot
-template <int ACT>
-__device__ inline void put_one(uint16_t* out, float* slot, const slot_shape& shape, int r, const float* o, float c, float l) {
+template <int ACT, typename SEES>
+__device__ inline void put_one(uint16_t* out, float* slot, const slot_shape& shape, int r, const float* o, float c, float l, const SEES& sees) {
     const int lane = threadIdx.x & 63;
-    if (!slot) return store_one<ACT>(out, o, l, shape.D);
+    if (!slot) return store_one<ACT>(out, o, l, shape.D, sees);
     if (2 * lane < shape.D) {
         float* to = slot + shape.at(r, 2 * lane);
         to[0] = o[0];
@@ -183,9 +183,9 @@ struct partial_sums {
                 if (n + i < end) add(c1[i], l1[i], o1[i]);
         }
     }
-    template <int ACT>
-    __device__ void store(uint16_t* out) const {
-        const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+    template <int ACT, typename SEES>
+    __device__ void store(uint16_t* out, const SEES& sees) const {
+        const float scale = inverse(l, sees);
         const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
         *(u32x2*)out = z;
     }
@@ -357,8 +357,9 @@ struct wave_state {
         return __all(x == 0.0f);
     }
 
-    // The lane's query's result, or its sums to row r of a slot.
-    __device__ __forceinline__ void put(uint16_t* out, float* slot, const slot_shape& shape, int r) const {
+    // The lane's query's result, or its sums to row r of a slot.  sees(): whether the query sees a key.
+    template <typename SEES>
+    __device__ __forceinline__ void put(uint16_t* out, float* slot, const slot_shape& shape, int r, const SEES& sees) const {
         if (slot) {
             float* to = slot + shape.at(r, (threadIdx.x & 32) >> 3);
             const int step = shape.at(0, 8);
@@ -369,7 +370,7 @@ struct wave_state {
             if ((threadIdx.x & 32) == 0) shape.put_stats(slot, r, top(), l);
             return;
         }
-        const float scale = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
+        const float scale = inverse(l, sees);
         quads([&](int d, int i, int t) {
             const u32x2 z = {pack2<ACT>(o[t][i] * scale, o[t][i + 1] * scale), pack2<ACT>(o[t][i + 2] * scale, o[t][i + 3] * scale)};
             if (d < shape.D) *(u32x2*)(out + d) = z;
@@ -378,10 +379,10 @@ struct wave_state {
 
     // The wave's results to rows out(r) (32 of them, `count` there), whole lines at a time: through 32 rows of LDS of its own, where the
     // lanes of a store find neighbouring values (stored as the lanes have them a line takes eight writes).
-    template <typename OUT>
-    __device__ __forceinline__ void put_rows(char* mine, const OUT& out, int count, int D) const {
+    template <typename OUT, typename SEES>
+    __device__ __forceinline__ void put_rows(char* mine, const OUT& out, int count, int D, const SEES& sees) const {
         const int lane = threadIdx.x & 63;
-        const float scale = l == 0.0f ? 0.0f : 1.0f / l;       // (no key seen: zeros)
+        const float scale = inverse(l, sees);
         quads([&](int d, int i, int t) {
             const u32x2 z = {pack2<ACT>(o[t][i] * scale, o[t][i + 1] * scale), pack2<ACT>(o[t][i + 2] * scale, o[t][i + 3] * scale)};
             const int r = lane & 31;

@@ -195,6 +195,15 @@ struct unit_rows {
         }
         return bits & (d < 0 ? low_bits(-d) | drafted << -d : drafted);
     }
+    // whether row r sees any key
+    __device__ bool sees_any(int r) const {
+        if (keys <= 0) return false;
+        if (!a.mask || context > 0) return true;       // (the context; without one, the first drafted token, which the whole chain sees)
+        const uint64_t* w = words(r);
+        for (int n = 0; n < keys; n += 64)
+            if (w[n >> 6] & (keys - n < 64 ? ((uint64_t)1 << (keys - n)) - 1 : ~(uint64_t)0)) return true;
+        return false;
+    }
     // row r over keys begin .. end - 1 by one wave, seen keys alone
     template <int ACT>
     __device__ void one(int r, int begin, int end, float* o, float* c, float* l) const {
@@ -212,7 +221,7 @@ struct unit_rows {
         for (int r = from; r < to; r += step) {
             float o[2], c, l;
             one<ACT>(r, begin, end, o, &c, &l);
-            put_one<ACT>(result(r), slot, p.shape(), r, o, c, l);
+            put_one<ACT>(result(r), slot, p.shape(), r, o, c, l, [&] { return sees_any(r); });
         }
     }
 };
@@ -309,7 +318,7 @@ __device__ __forceinline__ void join_parts(const unit_rows& rows, const wave_sta
                 for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
             }
             if (!slot) {
-                const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+                const float scale = inverse(l, [&] { return rows.sees_any(at); });
                 const u32x2 z = {pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
                 *(u32x2*)(rows.result(at) + d) = z;
             } else {
@@ -433,7 +442,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         w.finish(PARTS > 1 || slot);
         if constexpr (PARTS == 1) {
             if (!w.sound()) rows.one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
-            else if ((lane & 31) < rows.count) w.put(rows.result(row), slot, p.shape(), row);
+            else if ((lane & 31) < rows.count) w.put(rows.result(row), slot, p.shape(), row, [&] { return rows.sees_any(row); });
         } else {
             join_parts<ACT, DP, PARTS>(rows, w, lds, WAVE_BYTES, stats, head, HEADS, part_of, 0, key0, key1, slot);
         }
@@ -550,7 +559,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
             join_parts<ACT, DP, PARTS>(rows, w, lds, JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
         } else {
             if (!w.sound()) rows.one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
-            else if (r < rows.count) w.put(rows.result(r), slot, p.shape(), r);
+            else if (r < rows.count) w.put(rows.result(r), slot, p.shape(), r, [&] { return rows.sees_any(r); });
         }
         pos += t1 - t0;
         t0 = 0;
@@ -607,7 +616,7 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
             if (wave == 0)
                 for (int i = 1; i < waves; ++i) sum.add(stats[i][lane][0], stats[i][lane][1], sums[i][lane]);
         }
-        if (there && (wave == 0 || !many)) sum.template store<ACT>(rows.result(r) + d);
+        if (there && (wave == 0 || !many)) sum.template store<ACT>(rows.result(r) + d, [&] { return rows.sees_any(r); });
     }
 }
 

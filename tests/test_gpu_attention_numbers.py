@@ -1,4 +1,6 @@
 """Attention where its arithmetic can go wrong: scores that rise late and far, numerators at the end of a type's range."""
+import math
+
 import pytest
 import torch
 
@@ -150,3 +152,51 @@ def test_one_key_of_any_score(dtype, nodes, hq, hk):
     q4 = q[:, None].expand(rows, nodes, hq, D).contiguous()
     got = fq.attention_tree(q4.cuda(), kc.cuda(), vc.cuda(), table, lens, mask=mask.cuda(), scale=1.0).cpu()
     ref.compare(got, want.double()[:, None], tol[:, None], "one node")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("name", ["prompt_end"] + list(ROWS))
+@pytest.mark.parametrize("n", [100, 4500])
+def test_scores_of_minus_infinity(name, n, dtype):
+    """The softmax of scores that are all -infinity is no number; of some, it is the others'."""
+    for others in ([], [3], [n // 2], [n - 80, n - 10]):
+        scores = [-math.inf] * n
+        for at in others:
+            scores[at] = 1.0
+        got, q, k, v, seen = _scored(name, scores, dtype)
+        finite = seen & torch.isfinite(k[:, 0].float())
+        some = finite.any(1)
+        assert not others or bool(some.any())
+        want, tol = ref.attend(q[some][:, 0], k, v, finite[some], 1.0)
+        for h in range(q.shape[1]):
+            assert bool(torch.isnan(got[~some][:, h].float()).all()), f"{name}, {others}, head {h}"
+            if others:
+                ref.compare(got[some][:, h], want, tol, f"{name}, {others}, head {h}")
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_scores_of_minus_infinity_and_rows_that_see_nothing(dtype):
+    """Rows before the first key: zeros.  Rows whose keys are all at -infinity: no number.  Rows behind: the keys that are not."""
+    D, rows, keys = 64, 200, 190
+    q, k, v = torch.zeros((rows, 2, D), dtype=dtype), _normal((keys, 1, D), dtype, 8), _normal((keys, 1, D), dtype, 9)
+    q[..., 0] = 1
+    k[:70, :, 0] = -math.inf
+    got = fq.attention_prompt(q.cuda(), k.cuda(), v.cuda(), [0, rows], [0, keys]).cpu()
+    assert int((got[:10] != 0).sum()) == 0 and bool(torch.isnan(got[10:80].float()).all())
+    seen = torch.arange(keys)[None] <= torch.arange(rows)[:, None] - 10
+    seen[:, :70] = False
+    for h in range(2):
+        ref.compare(got[80:, h], *ref.attend(q[80:, h], k[:, 0], v[:, 0], seen[80:], D ** -0.5), "behind")
+    for nodes in (5, 40, 70):      # drafted tokens alone: node 0 sees itself, at -infinity; node 1 nothing; the others themselves
+        kc, vc = _normal((nodes + 15) // 16 * 16 * D, dtype, 10), _normal((nodes + 15) // 16 * 16 * D, dtype, 11)
+        kc, vc = kc.view(-1, 16, 1, D), vc.view(-1, 16, 1, D)
+        kc[0, 0, 0, 0] = -math.inf
+        sees = torch.eye(nodes, dtype=torch.bool)
+        sees[1, 1] = False
+        q = torch.zeros((1, nodes, 1, D), dtype=dtype)
+        q[..., 0] = 1
+        table = torch.arange(kc.shape[0], dtype=torch.int32, device="cuda")[None].contiguous()
+        got = fq.attention_tree(q.cuda(), kc.cuda(), vc.cuda(), table, torch.zeros(1, dtype=torch.int32, device="cuda"), mask=ref.words(sees).cuda()).cpu()[0, :, 0]
+        assert bool(torch.isnan(got[0].float()).all()) and int((got[1] != 0).sum()) == 0
+        want = vc.view(-1, D)[2:nodes].double()
+        ref.compare(got[2:], want, 2 * ref.UNIT[dtype] * want.abs() + 2.0 ** -24, "themselves")
