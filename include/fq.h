@@ -402,8 +402,9 @@ int fq_attention_prompt(const fq_heads* q, const fq_heads* k, const fq_heads* v,
  * Lengths and tables are read on the device when the kernels run, so that a captured call may be replayed with others; calls that
  * share a workspace must be ordered on one stream.  Deterministic; asynchronous on `stream`, no allocation.
  * sequences = 0 or nodes = 0: a valid no-op.
- * Errors: FQ_ERR_INVALID_ARG, FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, 2^20 nodes or 2^24 rows in all, table_width * page_size above
- *         2^31 - 1025, pointers or strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
+ * Errors: FQ_ERR_INVALID_ARG, FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, 2^20 nodes, 2^24 nodes of all sequences or 2^30 rows of a key
+ *         head (nodes * q_heads / kv_heads), 2^24 and more tiles of 128 of these rows over all key heads and sequences (of 64: up to 64 rows, and
+ *         129 - 192 of heads above 96), table_width * page_size above 2^31 - 1025, pointers or strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
  */
 size_t fq_attention_tree_workspace_bytes(int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,
                                          int page_size);

@@ -471,7 +471,7 @@ static int check_tree(int act_dtype, int64_t sequences, int64_t nodes, int q_hea
     a->head_dim = head_dim;
     a->table_width = table_width;
     a->cache.page_size = page_size;
-    return FQ_OK;
+    return fq_tree_fits(*a) ? FQ_OK : FQ_ERR_UNSUPPORTED;
 }
 
 size_t fq_attention_tree_workspace_bytes(int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,

@@ -620,16 +620,19 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
     }
 }
 
+// Rows of a tile, where a key head has `rows` of them.
+// (129 - 192 rows, heads above 96: three tiles of 64 rather than two of 128, a quarter of whose waves had nothing to do: 48 drafted tokens of
+// eight sequences of 500 - 4095, groups of four: 49.8 -> 45.6 us; heads of 96, 160 rows, 32.6, in three 33.4)
+int rows_of_tile(int64_t rows, int head_dim) { return rows <= 64 || (rows > 128 && rows <= 192 && head_dim > 96) ? 64 : ROWS; }
+
 tree_plan plan_tree(const fq_tree_args& a) {
     tree_plan p = {};
     p.group = a.q_heads / a.kv_heads;
-    p.rows = a.nodes * p.group;
+    p.rows = a.nodes * p.group;      // (fq_tree_fits)
     // Few rows: the waves take neighbouring heads, whose rows of a token lie side by side: 4 x 256 bytes come in 10 % faster than
     // 256.  That makes four times as many pieces as waves that share the keys out, of sums that are no longer few from 16 rows on.
     p.heads = p.rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
-    // (129 - 192 rows, heads above 96: three tiles of 64 rather than two of 128, a quarter of whose waves had nothing to do: 48 drafted tokens of
-    // eight sequences of 500 - 4095, groups of four: 49.8 -> 45.6 us; heads of 96, 160 rows, 32.6, in three 33.4)
-    p.unit_rows = p.rows <= 64 || (p.rows > 128 && p.rows <= 192 && a.head_dim > 96) ? 64 : ROWS;
+    p.unit_rows = rows_of_tile(p.rows, a.head_dim);
     p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
     p.slot_rows = p.rows < 32 ? p.rows : ((p.rows < p.unit_rows ? p.rows : p.unit_rows) + 31) / 32 * 32;
     p.D = a.head_dim;
@@ -695,6 +698,12 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
 
 }  // namespace
 
+bool fq_tree_fits(const fq_tree_args& a) {
+    const int64_t rows = (int64_t)a.nodes * (a.q_heads / a.kv_heads), tile = rows_of_tile(rows, a.head_dim);
+    if (rows > 1 << 30) return false;                                            // (they and a tile more are counted in 32 bits)
+    return a.sequences * a.kv_heads * ((rows + tile - 1) / tile) < 1 << 24;      // (2^32 threads)
+}
+
 size_t fq_tree_bytes(const fq_tree_args& a) {
     const tree_plan p = plan_tree(a);
     return p.whole ? 0 : (size_t)p.blocks * 2 * p.heads * p.shape().floats() * sizeof(float);
@@ -703,6 +712,5 @@ size_t fq_tree_bytes(const fq_tree_args& a) {
 int fq_launch_attention_tree(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream) {
     tree_plan p = plan_tree(a);
     p.slots = (float*)workspace;
-    if (a.sequences * a.kv_heads * p.row_tiles >= 1 << 24) return FQ_ERR_UNSUPPORTED;
     return act_dtype == FQ_F16 ? launch<FQ_F16>(a, p, stream) : launch<FQ_BF16>(a, p, stream);
 }

@@ -171,6 +171,7 @@ struct fq_tree_args {
     float scale;
     void* out;
 };
+bool fq_tree_fits(const fq_tree_args& a);        // whether its rows can be counted, and dealt out in one launch
 size_t fq_tree_bytes(const fq_tree_args& a);
 int fq_launch_attention_tree(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream);
 

@@ -1,0 +1,35 @@
+"""Sizes at the attention calls' limits: what is counted there, on the host (no GPU)."""
+import pytest
+
+from paper_2308_09723_amd import fq
+
+P = 1 << 20      # an address that no check follows
+
+
+def _tree(sequences, nodes, hq, hk, D, width, page):
+    """(workspace, status) of a call whose tensors lie far apart; its workspace is refused, so that nothing can be launched."""
+    need = fq.attention_tree_workspace_bytes(sequences, nodes, hq, hk, D, width, page)
+    cache = fq.KvPages(P << 22, P << 23, 1 << 10, page, page * hk * D, hk * D, D)
+    status = fq.attention_tree_raw(fq.Heads(P << 24, hq * D, D), 0, sequences, nodes, hq, hk, D, cache, P, width, P << 1, None, 0, 0.0, P << 26, None, 0)
+    return need, status
+
+
+@pytest.mark.parametrize("nodes,hq,hk", [(1 << 20, 4096, 1), (1 << 19, 4096, 1), (3 << 18, 4096, 1), (1 << 20, 2048, 1), (1 << 20, 4096, 2),
+                                         ((1 << 18) + 1, 4096, 1)])
+@pytest.mark.parametrize("width", [1, 512])
+def test_tree_rows_that_32_bits_do_not_count_are_refused(nodes, hq, hk, width):
+    assert _tree(1, nodes, hq, hk, 8, width, 16) == (0, fq.FQ_ERR_UNSUPPORTED)
+
+
+def test_tree_tiles_beyond_a_launch_are_refused_by_both():
+    """65536 sequences of 256 key heads are 2^24 tiles; one head fewer is not.  (Four heads of 2^30 rows each are 2^25.)"""
+    assert _tree(65536, 1, 256, 256, 8, 512, 16) == (0, fq.FQ_ERR_UNSUPPORTED)
+    assert _tree(1, 1 << 20, 4096, 4, 8, 512, 16) == (0, fq.FQ_ERR_UNSUPPORTED)
+    need, status = _tree(65536, 1, 255, 255, 8, 512, 16)
+    assert 0 < need < 1 << 34 and status == fq.FQ_ERR_WORKSPACE
+
+
+def test_tree_rows_just_within():
+    for nodes, hq, hk in ((1 << 18, 4096, 1), (1 << 20, 1024, 1)):
+        need, status = _tree(1, nodes, hq, hk, 8, 512, 16)
+        assert 0 < need < 1 << 34 and status == fq.FQ_ERR_WORKSPACE
