@@ -13,6 +13,7 @@
 #include <atomic>
 #include <type_traits>
 
+#include "fq_attn_parts.h"
 #include "fq_attn_tile.h"
 #include "fq_lds_limit.h"
 
@@ -247,7 +248,7 @@ struct table_part {
     }
 };
 
-// Brings in the entries of keys begin .. end - 1 (few enough: table_keys()); the caller waits.
+// Brings in the entries of keys begin .. end - 1 (few enough: part_keys()); the caller waits.
 template <int THREADS>
 __device__ inline table_part load_table(const fq_tree_args& a, int b, int begin, int end, int32_t* entries) {
     table_part t;
@@ -264,10 +265,6 @@ __device__ inline table_part load_table(const fq_tree_args& a, int b, int begin,
         entries[i] = page < 0 ? 0 : (int32_t)min((uint32_t)page, (uint32_t)(a.cache.pages - 1));
     }
     return t;
-}
-// How many keys' entries fit, in whole tiles
-__device__ inline int table_keys(const fq_tree_args& a, int entries, int tile) {
-    return (int)min((int64_t)1 << 30, (int64_t)(entries - 1) * a.cache.page_size) / tile * tile;
 }
 // Whether the few neighbouring keys of one load lie in one page and within 32 bits of each other
 __device__ inline bool near_keys(const fq_tree_args& a, int keys) {
@@ -384,9 +381,9 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_stream_kernel(fq_tre
         const int row = min(lane & 31, rows.count - 1);
         w.load_query(rows.query(row), D);
         w.clear();
-        const int most = table_keys(a, TABLE / 4, TILE);
-        for (int part = key0; part < key1; part += most) {
-            const int part_end = min(key1, part + most);
+        const int most = part_keys(TABLE / 4, a.cache.page_size, TILE);
+        for (int part = key0, part_end; part < key1; part = part_end) {
+            part_end = fqa::part_end(part, key1, most);
             const table_part table = load_table<64>(a, b, part, part_end, entries);
             if (D < SH::UNITS * 8) {                    // units that no load fills: zeros
                 const u32x4 zero = {0, 0, 0, 0};
@@ -500,9 +497,9 @@ __global__ __launch_bounds__(256, 2) void fq_attention_tree_tile_kernel(fq_tree_
         const bool busy = group * 32 < rows.count;
         w.load_query(rows.query(row), D);
         w.clear();
-        const int most = table_keys(a, TABLE, KEYS);
-        for (int part = key0; part < key1; part += most) {
-            const int part_end = min(key1, part + most);
+        const int most = part_keys(TABLE, a.cache.page_size, KEYS);
+        for (int part = key0, part_end; part < key1; part = part_end) {
+            part_end = fqa::part_end(part, key1, most);
             __syncthreads();
             const table_part table = load_table<256>(a, b, part, part_end, entries);
             if (D < SH::UNITS * 8) {                    // units that no load fills: zeros

@@ -1,8 +1,13 @@
 """Sizes at the attention calls' limits: what is counted there, on the host (no GPU)."""
+import os
+import shutil
+import subprocess
+
 import pytest
 
 from paper_2308_09723_amd import fq
 
+HERE = os.path.dirname(os.path.abspath(__file__))
 P = 1 << 20      # an address that no check follows
 
 
@@ -33,3 +38,14 @@ def test_tree_rows_just_within():
     for nodes, hq, hk in ((1 << 18, 4096, 1), (1 << 20, 1024, 1)):
         need, status = _tree(1, nodes, hq, hk, 8, 512, 16)
         assert 0 < need < 1 << 34 and status == fq.FQ_ERR_WORKSPACE
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_parts_of_the_longest_contexts(tmp_path):
+    """Keys up to 2^31 - 1025 in parts of up to 2^30, as the kernels go through them (attention_parts_check.cpp)."""
+    exe = str(tmp_path / "parts")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fwrapv", "-o", exe, os.path.join(HERE, "attention_parts_check.cpp")], check=True)
+    out = subprocess.run([exe], capture_output=True, text=True, timeout=100)
+    assert out.returncode == 0, out.stdout[-2000:]
+    walks, wrong = (int(out.stdout.split()[i]) for i in (-4, -2))
+    assert walks > 1000 and wrong == 0
