@@ -200,3 +200,25 @@ def test_scores_of_minus_infinity_and_rows_that_see_nothing(dtype):
         assert bool(torch.isnan(got[0].float()).all()) and int((got[1] != 0).sum()) == 0
         want = vc.view(-1, D)[2:nodes].double()
         ref.compare(got[2:], want, 2 * ref.UNIT[dtype] * want.abs() + 2.0 ** -24, "themselves")
+
+
+@pytest.mark.parametrize("nodes", [1, 40, 70])
+@pytest.mark.parametrize("page", [64, 1 << 22])
+def test_contexts_of_nearly_2_31_keys(page, nodes):
+    """Tables of as many places as are admitted, over a few pages: the first 2^30 places' values are around 1, the others' around 3.  Rows of up
+    to 2^22 keys a block are added up one after the other in binary32: 2^-7 of the values is allowed for that."""
+    D, few = 8, max(1, 4096 // page)
+    places = (2 ** 31 - 1025) // page
+    first = 2 ** 30 // page
+    k, v = (torch.randn((2 * few, page, 1, D), device="cuda", generator=torch.Generator("cuda").manual_seed(i)).to(BF16) for i in (1, 2))
+    v[:few] = v[:few] * 0.25 + 1
+    v[few:] = v[few:] * 0.25 + 3
+    entry = torch.arange(places, device="cuda")
+    table = torch.where(entry < first, entry % few, few + entry % few).to(torch.int32)[None].contiguous()
+    context = places * page - nodes
+    q = _normal((1, nodes, 1, D), BF16, 3)
+    got = fq.attention_tree(q.cuda(), k, v, table, torch.tensor([context], dtype=torch.int32, device="cuda"), scale=0.5)[0, :, 0].cpu()
+    times = torch.bincount(table[0].long(), minlength=2 * few).double()
+    weight = torch.exp(0.5 * (q[0, :, 0].double().cuda() @ k.double().view(-1, D).t().contiguous())) * times.repeat_interleave(page)
+    want = (weight @ v.double().view(-1, D) / weight.sum(1, keepdim=True)).cpu()
+    ref.compare(got, want, 2.0 ** -7 * 3 + 2 * 2.0 ** -8 * want.abs(), f"{context} keys")
