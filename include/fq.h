@@ -350,8 +350,8 @@ typedef struct fq_kv_pages {
  *                         (a negative one: padding) is not written.  Slots that are written are different ones.
  * rot_dim: a multiple of 8, at most head_dim.  q_out, k_out and the cache must not overlap qkv or each other.
  * tokens = 0 is a valid no-op.  Asynchronous on `stream`, one kernel, no scratch.
- * Errors: FQ_ERR_INVALID_ARG (null pointers, sizes, strides that do not hold a row, eps negative or not finite, q_out or k_out over qkv,
- *         neither k_out nor a cache), FQ_ERR_UNSUPPORTED (shape limits, tokens above 2^24, pointers or strides not aligned to 16 bytes), FQ_ERR_HIP.
+ * Errors: FQ_ERR_INVALID_ARG (null pointers, sizes, strides that do not hold a row, eps negative or not finite, q_out or k_out over qkv, k_out
+ *         over q_out, any of them within the cache (from its first key or value to its last), neither k_out nor a cache), FQ_ERR_UNSUPPORTED (shape limits, tokens above 2^24, pointers or strides not aligned to 16 bytes), FQ_ERR_HIP.
  */
 int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_stride, int q_heads, int kv_heads, int head_dim,
                     const void* q_weight, const void* k_weight, float eps, const float* table, int64_t table_rows, int rot_dim,
@@ -397,7 +397,8 @@ int fq_attention_prompt(const fq_heads* q, const fq_heads* k, const fq_heads* v,
  *   context_lens in   [sequences] device.  A negative one: the sequence has no keys, its result is zeros.  Tokens beyond
  *                     table_width pages are not seen
  *   mask         in   device words, node i's at mask + b * mask_stride + i * ((nodes + 63) / 64); mask_stride = 0: one tree for all
- *   scale, out   as fq_attention_prompt; out [sequences, nodes, q_heads, head_dim]
+ *   scale, out   as fq_attention_prompt; out [sequences, nodes, q_heads, head_dim], not over an input nor within the cache (from its first
+ *                key or value to its last)
  *   workspace         device scratch, >= fq_attention_tree_workspace_bytes(...) bytes (may be NULL when that is 0)
  * Lengths and tables are read on the device when the kernels run, so that a captured call may be replayed with others; calls that
  * share a workspace must be ordered on one stream.  Deterministic; asynchronous on `stream`, no allocation.

@@ -356,6 +356,12 @@ static int check_cache(const fq_kv_pages* c, int kv_heads, int head_dim) {
     return c->pages > INT32_MAX / c->page_size ? FQ_ERR_UNSUPPORTED : FQ_OK;
 }
 
+// Whether memory that a call writes lies among the cache's keys or values (from the first of them to the last)
+static bool over_cache(const void* p, size_t bytes, const fq_kv_pages* c, int kv_heads, int head_dim) {
+    const size_t all = (size_t)((c->pages - 1) * c->page_stride + (c->page_size - 1) * c->token_stride + (kv_heads - 1) * c->head_stride + head_dim) * 2;
+    return fq_overlaps(p, bytes, {{c->k, all}, {c->v, all}});
+}
+
 int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_stride, int q_heads, int kv_heads, int head_dim,
                     const void* q_weight, const void* k_weight, float eps, const float* table, int64_t table_rows, int rot_dim,
                     int interleaved, const int32_t* positions, void* q_out, void* k_out, const fq_kv_pages* cache,
@@ -376,8 +382,11 @@ int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_
     if (!qkv || !q_out) return FQ_ERR_INVALID_ARG;
     if (!aligned16(qkv) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_weight) || !aligned16(k_weight)) return FQ_ERR_UNSUPPORTED;
     const size_t read = (size_t)((tokens - 1) * row_stride + row) * 2;
-    if (fq_overlaps(q_out, (size_t)tokens * q_heads * head_dim * 2, {{qkv, read}})) return FQ_ERR_INVALID_ARG;
-    if (k_out && fq_overlaps(k_out, (size_t)tokens * kv_heads * head_dim * 2, {{qkv, read}, {q_out, (size_t)tokens * q_heads * head_dim * 2}}))
+    const size_t q_bytes = (size_t)tokens * q_heads * head_dim * 2, k_bytes = (size_t)tokens * kv_heads * head_dim * 2;
+    if (fq_overlaps(q_out, q_bytes, {{qkv, read}})) return FQ_ERR_INVALID_ARG;
+    if (k_out && fq_overlaps(k_out, k_bytes, {{qkv, read}, {q_out, q_bytes}})) return FQ_ERR_INVALID_ARG;
+    if (cache && (over_cache(qkv, read, cache, kv_heads, head_dim) || over_cache(q_out, q_bytes, cache, kv_heads, head_dim) ||
+                  (k_out && over_cache(k_out, k_bytes, cache, kv_heads, head_dim))))
         return FQ_ERR_INVALID_ARG;
     fq_rope_args a = {qkv, tokens, row_stride, q_heads, kv_heads, head_dim, q_weight, k_weight, eps, table, table_rows, rot_dim, interleaved != 0,
                       positions, q_out, k_out, {}, slots};
@@ -498,7 +507,10 @@ int fq_attention_tree(const fq_heads* q, int act_dtype, int64_t sequences, int64
     if ((st = check_rows(q, sequences * nodes, q_heads)) != FQ_OK) return st;
     if (!aligned16(out) || too_far(sequences, mask_stride)) return FQ_ERR_UNSUPPORTED;
     const size_t bytes = (size_t)(sequences * nodes) * q_heads * head_dim * 2;
-    if (fq_overlaps(out, bytes, {{q->data, (size_t)((sequences * nodes - 1) * q->row_stride + (q_heads - 1) * q->head_stride + head_dim) * 2}}))
+    const size_t words = (size_t)((mask_stride ? (sequences - 1) * mask_stride : 0) + nodes * ((nodes + 63) / 64));
+    if (fq_overlaps(out, bytes, {{q->data, (size_t)((sequences * nodes - 1) * q->row_stride + (q_heads - 1) * q->head_stride + head_dim) * 2},
+                                 {page_table, (size_t)(sequences * table_width) * 4}, {context_lens, (size_t)sequences * 4}, {mask, mask ? words * 8 : 0}}) ||
+        over_cache(out, bytes, cache, kv_heads, head_dim))
         return FQ_ERR_INVALID_ARG;
     const size_t need = fq_tree_bytes(a);
     if (need > 0 && (!workspace || workspace_bytes < need)) return FQ_ERR_WORKSPACE;

@@ -40,6 +40,33 @@ def test_tree_rows_just_within():
         assert 0 < need < 1 << 34 and status == fq.FQ_ERR_WORKSPACE
 
 
+def _overlap(q=P << 24, out=P << 26, table=P, lens=P << 1, mask=None):
+    """fq_attention_tree with a cache of 10 pages of 16 x 2 x 128 values at P << 8 and P << 9, 3 sequences of 5 nodes, 4 heads."""
+    cache = fq.KvPages(P << 8, P << 9, 10, 16, 4096, 256, 128)
+    need = fq.attention_tree_workspace_bytes(3, 5, 4, 2, 128, 64, 16)
+    assert need      # (and is not given: a call that nothing else stops ends there)
+    return fq.attention_tree_raw(fq.Heads(q, 512, 128), 1, 3, 5, 4, 2, 128, cache, table, 64, lens, mask, 0, 0.0, out, None, 0)
+
+
+def test_tree_output_over_an_input():
+    cache_bytes, out_bytes = 10 * 4096 * 2, 3 * 5 * 4 * 128 * 2
+    for first, size in ((P << 8, cache_bytes), (P << 9, cache_bytes), (P, 3 * 64 * 4), (P << 1, 16)):
+        for at in (first, first + size - 16, first - out_bytes + 16):
+            assert _overlap(out=at // 16 * 16) == fq.FQ_ERR_INVALID_ARG, (first, at)
+        for at in (first + (size + 15) // 16 * 16, first - out_bytes):
+            assert _overlap(out=at) == fq.FQ_ERR_WORKSPACE, (first, at)
+    assert _overlap(out=P << 26, mask=(P << 26) + 64) == fq.FQ_ERR_INVALID_ARG
+    assert _overlap(out=P << 26, mask=(P << 26) + out_bytes) == fq.FQ_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("change", [dict(qkv=P << 8), dict(q=P << 8), dict(q=(P << 9) + 10 * 4096 * 2 - 16), dict(k=P << 9), dict(k=(P << 8) + 4096)])
+def test_norm_rope_within_the_cache(change):
+    a = dict(qkv=P << 12, act=0, tokens=4, stride=768, hq=2, hk=2, D=128, qw=None, kw=None, eps=1e-6, table=None, rows=0, rot=0, inter=0, pos=None,
+             q=P << 13, k=P << 14, cache=fq.KvPages(P << 8, P << 9, 10, 16, 4096, 256, 128), slots=P)
+    a.update(change)
+    assert fq.qk_norm_rope_raw(*a.values()) == fq.FQ_ERR_INVALID_ARG
+
+
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
 def test_parts_of_the_longest_contexts(tmp_path):
     """Keys up to 2^31 - 1025 in parts of up to 2^30, as the kernels go through them (attention_parts_check.cpp)."""
