@@ -351,7 +351,7 @@ typedef struct fq_kv_pages {
  * rot_dim: a multiple of 8, at most head_dim.  q_out, k_out and the cache must not overlap qkv or each other.
  * tokens = 0 is a valid no-op.  Asynchronous on `stream`, one kernel, no scratch.
  * Errors: FQ_ERR_INVALID_ARG (null pointers, sizes, strides that do not hold a row, eps negative or not finite, q_out or k_out over qkv, k_out
- *         over q_out, any of them within the cache (from its first key or value to its last), neither k_out nor a cache), FQ_ERR_UNSUPPORTED (shape limits, tokens above 2^24, pointers or strides not aligned to 16 bytes), FQ_ERR_HIP.
+ *         over q_out, any of them within the cache (from its first key or value to its last), neither k_out nor a cache), FQ_ERR_UNSUPPORTED (shape limits, 2^24 tokens and more, pointers or strides not aligned to 16 bytes), FQ_ERR_HIP.
  */
 int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_stride, int q_heads, int kv_heads, int head_dim,
                     const void* q_weight, const void* k_weight, float eps, const float* table, int64_t table_rows, int rot_dim,

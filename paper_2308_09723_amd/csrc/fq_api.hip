@@ -373,7 +373,7 @@ int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_
     if (row_stride < row && tokens > 1) return FQ_ERR_INVALID_ARG;
     if (tokens > 0 && (!cache != !slots || (!k_out && !cache))) return FQ_ERR_INVALID_ARG;
     if (rot_dim > 0 && (table_rows <= 0 || !table || (!positions && tokens > 0))) return FQ_ERR_INVALID_ARG;
-    if (rot_dim % 8 != 0 || tokens > (int64_t)1 << 24 || too_far(tokens, row_stride) || row_stride % 8 != 0) return FQ_ERR_UNSUPPORTED;
+    if (rot_dim % 8 != 0 || tokens >= (int64_t)1 << 24 || too_far(tokens, row_stride) || row_stride % 8 != 0) return FQ_ERR_UNSUPPORTED;
     if (cache) {
         const int cst = check_cache(cache, kv_heads, head_dim);
         if (cst != FQ_OK) return cst;

@@ -67,6 +67,14 @@ def test_norm_rope_within_the_cache(change):
     assert fq.qk_norm_rope_raw(*a.values()) == fq.FQ_ERR_INVALID_ARG
 
 
+def test_norm_rope_of_2_to_24_tokens_is_more_than_a_launch():
+    """(2^32 threads; of one token fewer something else is wrong)"""
+    def call(tokens, q_out=P << 40):
+        return fq.qk_norm_rope_raw(P, 0, tokens, 32, 1, 1, 8, None, None, 0.0, None, 0, 0, 0, None, q_out, P << 41, None, None)
+    assert call(1 << 24) == fq.FQ_ERR_UNSUPPORTED
+    assert call((1 << 24) - 1, q_out=P) == fq.FQ_ERR_INVALID_ARG      # (over qkv)
+
+
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
 def test_parts_of_the_longest_contexts(tmp_path):
     """Keys up to 2^31 - 1025 in parts of up to 2^30, as the kernels go through them (attention_parts_check.cpp)."""
