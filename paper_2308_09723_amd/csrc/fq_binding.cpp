@@ -421,7 +421,9 @@ PyObject* attention_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int act = type16(q.scalar_type());
         require(q.dim() == 4 && q.stride(3) == 1);
         const int64_t B = q.size(0), nodes = q.size(1), hq = q.size(2), D = q.size(3);
-        require((q.stride(0) == nodes * q.stride(1) || B <= 1) && hq <= INT_MAX && D <= INT_MAX);
+        // (of one token, or one sequence, the stride says nothing)
+        const int64_t row = B * nodes <= 1 ? 0 : nodes == 1 ? q.stride(0) : q.stride(1);
+        require((q.stride(0) == nodes * row || B <= 1) && hq <= INT_MAX && D <= INT_MAX);
         const at::Tensor& kc = tensor(a[1]);
         const int64_t hk = kc.dim() == 4 ? kc.size(2) : 0;
         require(hk <= INT_MAX);
@@ -443,7 +445,7 @@ PyObject* attention_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
         size_t size = 0;
         const int64_t width = table.size(1);
         void* ws = scratch_of(a[8], q, lib.attention_tree_workspace_bytes(B, nodes, (int)hq, (int)hk, (int)D, width, cache.page_size), &size, &own);
-        const fq_heads qh = {q.data_ptr(), q.stride(1), q.stride(2)};
+        const fq_heads qh = {q.data_ptr(), row, q.stride(2)};
         const int32_t *tp = (const int32_t*)table.data_ptr(), *lp = (const int32_t*)lens.data_ptr();
         void *op = out.data_ptr(), *s = stream();
         call("fq_attention_tree", [&] {

@@ -723,10 +723,10 @@ def attention_prompt(q, k, v, q_offsets, k_offsets=None, scale=None, out=None, w
 
 
 def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, scale=None, out=None, workspace=None):
-    """Attention of drafted tokens over a paged cache: q cuda [sequences, nodes, heads, head_dim] (float16 or bfloat16), caches
-    [pages, page_size, kv_heads, head_dim], page_table int32 [sequences, width], context_lens int32 [sequences] (tokens in the cache
-    before the drafted ones, whose keys and values lie in the places behind them), mask int64 [nodes, words] or [sequences, nodes, words] (tree_mask;
-    None: a chain) -> [sequences, nodes, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given."""
+    """Attention of drafted tokens over a paged cache: q cuda [sequences, nodes, heads, head_dim] (float16 or bfloat16; the tokens of all
+    sequences evenly apart), caches [pages, page_size, kv_heads, head_dim], page_table int32 [sequences, width], context_lens int32 [sequences]
+    (tokens in the cache before the drafted ones, whose keys and values lie in the places behind them), mask int64 [nodes, words] or
+    [sequences, nodes, words] (tree_mask; None: a chain) -> [sequences, nodes, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given."""
     torch = _torch_mod or _torch()
     done = _native.attention_tree(q, k_cache, v_cache, page_table, context_lens, mask, scale, out, workspace)
     if done is not None:
@@ -735,7 +735,8 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
     act = _act_code(q)
     _require(q.is_cuda and q.dim() == 4 and (q.stride(3) == 1 or q.shape[3] <= 1), where)
     sequences, nodes, heads, D = q.shape
-    _require(q.stride(0) == nodes * q.stride(1) or sequences <= 1, where)
+    row = 0 if sequences * nodes <= 1 else q.stride(0) if nodes == 1 else q.stride(1)      # (of one token, or one sequence, the stride says nothing)
+    _require(q.stride(0) == nodes * row or sequences <= 1, where)
     kv_heads = k_cache.shape[2] if k_cache.dim() == 4 else 0
     cache = _pages(k_cache, v_cache, q, kv_heads, D, where)
     _require(page_table.dim() == 2 and page_table.shape[0] == sequences and context_lens.numel() == sequences, where)
@@ -754,7 +755,7 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
     need = attention_tree_workspace_bytes(sequences, nodes, heads, kv_heads, D, width, page)
     if size < need:
         workspace, size = torch.empty(need, dtype=torch.uint8, device=q.device), need
-    _check(attention_tree_raw(Heads(q.data_ptr(), q.stride(1), q.stride(2)), act, sequences, nodes, heads, kv_heads, D, cache,
+    _check(attention_tree_raw(Heads(q.data_ptr(), row, q.stride(2)), act, sequences, nodes, heads, kv_heads, D, cache,
                               page_table.data_ptr(), width, context_lens.data_ptr(), None if mask is None else mask.data_ptr(), stride,
                               scale or 0.0, o.data_ptr(), workspace.data_ptr() if size else None, size, _stream()), where)
     return o

@@ -1,0 +1,47 @@
+"""The attention calls on torch tensors: layouts that are taken, arguments that are not."""
+import pytest
+import torch
+
+from paper_2308_09723_amd import fq
+
+import attention_util as ref
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+@pytest.fixture(params=["native", "python"])
+def way(request, monkeypatch):
+    """Both ways that a call may go."""
+    fq._stream()
+    if request.param == "python":
+        monkeypatch.setattr(fq, "_native", fq._NoNative())
+    return request.param
+
+
+def _normal(size, dtype, seed):
+    return torch.randn(size, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def _paged(sequences, tokens, hk, D, page=16):
+    pages = (tokens + page - 1) // page
+    kc, vc = (_normal((sequences * pages, page, hk, D), F16, i) for i in (1, 2))
+    return kc, vc, torch.arange(sequences * pages, dtype=torch.int32).view(sequences, pages)
+
+
+def test_one_token_of_each_sequence_where_the_qkv_product_leaves_them(way):
+    """Queries [sequences, 1, heads, head_dim] as views of wider rows: the stride of the one token says nothing."""
+    B, hq, hk, D = 6, 4, 2, 64
+    kc, vc, table = _paged(B, 40, hk, D)
+    rows = _normal((B, (hq + 2 * hk) * D), F16, 3)
+    lens = torch.tensor([39, 5, 0, 17, 22, 30], dtype=torch.int32)
+    q = rows[:, :hq * D].reshape(B, 1, hq, D)
+    want, tol = ref.tree(q, kc, vc, table, lens, ref.chain(B, 1))
+    wide = rows.cuda()
+    args = (kc.cuda(), vc.cuda(), table.cuda(), lens.cuda())
+    for view in (wide[:, :hq * D].view(B, 1, hq, D), wide.view(B, -1, D)[:, :hq].unsqueeze(1), wide.view(B, -1, D)[:, None, :hq]):
+        ref.compare(fq.attention_tree(view, *args), want, tol, str(view.stride()))
+    # one sequence, one token, in a tensor of any strides of these two
+    one = wide[:1, :hq * D].as_strided((1, 1, hq, D), (3, 5, D, 1))
+    ref.compare(fq.attention_tree(one, args[0], args[1], args[2][:1], args[3][:1]), want[:1], tol[:1], "one row")
