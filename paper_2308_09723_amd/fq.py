@@ -650,6 +650,15 @@ def _output(out, shape, like, where):
     return out
 
 
+def _given_scale(scale, where):
+    """A scale that was given, as binary32; 0 for the library's own."""
+    if scale is None:
+        return 0.0
+    scale = ctypes.c_float(scale).value
+    _require(scale > 0.0, where)
+    return scale
+
+
 def qk_norm_rope(qkv, heads, kv_heads, table, positions, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, q_out=None,
                  k_out=None, k_cache=None, v_cache=None, slots=None):
     """qkv: cuda [tokens, (heads + 2 kv_heads) * head_dim] float16/bfloat16, rows of any stride -> (q [tokens, heads, head_dim],
@@ -711,13 +720,13 @@ def attention_prompt(q, k, v, q_offsets, k_offsets=None, scale=None, out=None, w
     _require(len(q_offsets) >= 1 and q_offsets[-1] == rows, where)
     _require(k_offsets is None or len(k_offsets) == len(q_offsets), where)
     _require((q_offsets if k_offsets is None else k_offsets)[-1] == keys, where)
-    _require(scale is None or scale > 0, where)
+    scale = _given_scale(scale, where)
     o = _output(out, (rows, heads, D), q, where)
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     need = attention_prompt_workspace_bytes(heads, kv_heads, D, q_offsets, k_offsets)
     if size < need:
         workspace, size = torch.empty(need, dtype=torch.uint8, device=q.device), need
-    _check(attention_prompt_raw(hq, hk, hv, act, heads, kv_heads, D, q_offsets, k_offsets, scale or 0.0, o.data_ptr(),
+    _check(attention_prompt_raw(hq, hk, hv, act, heads, kv_heads, D, q_offsets, k_offsets, scale, o.data_ptr(),
                                 workspace.data_ptr() if size else None, size, _stream()), where)
     return o
 
@@ -748,7 +757,7 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
         _plain(mask, torch.int64, q.device, where)
         _require(tuple(mask.shape) in ((nodes, words), (sequences, nodes, words)), where)
         stride = nodes * words if mask.dim() == 3 else 0
-    _require(scale is None or scale > 0, where)
+    scale = _given_scale(scale, where)
     o = _output(out, (sequences, nodes, heads, D), q, where)
     width, page = page_table.shape[1], k_cache.shape[1]
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
@@ -757,5 +766,5 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
         workspace, size = torch.empty(need, dtype=torch.uint8, device=q.device), need
     _check(attention_tree_raw(Heads(q.data_ptr(), row, q.stride(2)), act, sequences, nodes, heads, kv_heads, D, cache,
                               page_table.data_ptr(), width, context_lens.data_ptr(), None if mask is None else mask.data_ptr(), stride,
-                              scale or 0.0, o.data_ptr(), workspace.data_ptr() if size else None, size, _stream()), where)
+                              scale, o.data_ptr(), workspace.data_ptr() if size else None, size, _stream()), where)
     return o

@@ -45,3 +45,20 @@ def test_one_token_of_each_sequence_where_the_qkv_product_leaves_them(way):
     # one sequence, one token, in a tensor of any strides of these two
     one = wide[:1, :hq * D].as_strided((1, 1, hq, D), (3, 5, D, 1))
     ref.compare(fq.attention_tree(one, args[0], args[1], args[2][:1], args[3][:1]), want[:1], tol[:1], "one row")
+
+
+def test_a_scale_that_binary32_does_not_hold_is_refused(way):
+    """(1e-50 is zero there, which stands for 1 / sqrt(head_dim))"""
+    kc, vc, table = _paged(1, 40, 2, 64)
+    q = _normal((1, 1, 4, 64), F16, 3).cuda()
+    lens = torch.tensor([20], dtype=torch.int32).cuda()
+    x = _normal((20, 4, 64), F16, 4).cuda()
+    for scale in (1e-50, 1e39, 0.0, -1e-50, float("nan"), float("inf")):
+        with pytest.raises(fq.FqError):
+            fq.attention_tree(q, kc.cuda(), vc.cuda(), table.cuda(), lens, scale=scale)
+        with pytest.raises(fq.FqError):
+            fq.attention_prompt(x, x, x, [0, 20], scale=scale)
+    small = fq.attention_prompt(x, x, x, [0, 20], scale=1e-40)      # (subnormal: all keys weigh the same)
+    v = x.double().cpu()
+    want = v.cumsum(0) / torch.arange(1, 21)[:, None, None]
+    ref.compare(small, want, 2 * ref.UNIT[F16] * v.abs().cumsum(0) / torch.arange(1, 21)[:, None, None] + 2.0 ** -24, "tiny scale")
