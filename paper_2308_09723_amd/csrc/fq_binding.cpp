@@ -374,10 +374,11 @@ float given_scale(PyObject* o) {
     return x;
 }
 
-// a caller's workspace where it is large enough, or a new one of `need` bytes
+// a caller's workspace beside `like` where it is large enough, or a new one of `need` bytes
 void* scratch_of(PyObject* o, const at::Tensor& like, size_t need, size_t* size, at::Tensor* own) {
     if (o != Py_None) {
         const at::Tensor& t = tensor(o);
+        require(t.device() == like.device() && t.is_contiguous());
         *size = (size_t)t.numel() * t.element_size();
         if (*size >= need) return t.data_ptr();
     }

@@ -650,6 +650,18 @@ def _output(out, shape, like, where):
     return out
 
 
+def _scratch(workspace, need, like, where):
+    """A caller's workspace (contiguous, on like's device) where it is large enough, or a new one of `need` bytes; and its size."""
+    torch = _torch_mod or _torch()
+    size = 0
+    if workspace is not None:
+        _require(workspace.device == like.device and workspace.is_contiguous(), where)
+        size = workspace.numel() * workspace.element_size()
+    if size < need:
+        workspace, size = torch.empty(need, dtype=torch.uint8, device=like.device), need
+    return workspace, size
+
+
 def _given_scale(scale, where):
     """A scale that was given, as binary32; 0 for the library's own."""
     if scale is None:
@@ -722,10 +734,7 @@ def attention_prompt(q, k, v, q_offsets, k_offsets=None, scale=None, out=None, w
     _require((q_offsets if k_offsets is None else k_offsets)[-1] == keys, where)
     scale = _given_scale(scale, where)
     o = _output(out, (rows, heads, D), q, where)
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    need = attention_prompt_workspace_bytes(heads, kv_heads, D, q_offsets, k_offsets)
-    if size < need:
-        workspace, size = torch.empty(need, dtype=torch.uint8, device=q.device), need
+    workspace, size = _scratch(workspace, attention_prompt_workspace_bytes(heads, kv_heads, D, q_offsets, k_offsets), q, where)
     _check(attention_prompt_raw(hq, hk, hv, act, heads, kv_heads, D, q_offsets, k_offsets, scale, o.data_ptr(),
                                 workspace.data_ptr() if size else None, size, _stream()), where)
     return o
@@ -760,10 +769,7 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
     scale = _given_scale(scale, where)
     o = _output(out, (sequences, nodes, heads, D), q, where)
     width, page = page_table.shape[1], k_cache.shape[1]
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    need = attention_tree_workspace_bytes(sequences, nodes, heads, kv_heads, D, width, page)
-    if size < need:
-        workspace, size = torch.empty(need, dtype=torch.uint8, device=q.device), need
+    workspace, size = _scratch(workspace, attention_tree_workspace_bytes(sequences, nodes, heads, kv_heads, D, width, page), q, where)
     _check(attention_tree_raw(Heads(q.data_ptr(), row, q.stride(2)), act, sequences, nodes, heads, kv_heads, D, cache,
                               page_table.data_ptr(), width, context_lens.data_ptr(), None if mask is None else mask.data_ptr(), stride,
                               scale, o.data_ptr(), workspace.data_ptr() if size else None, size, _stream()), where)

@@ -62,3 +62,25 @@ def test_a_scale_that_binary32_does_not_hold_is_refused(way):
     v = x.double().cpu()
     want = v.cumsum(0) / torch.arange(1, 21)[:, None, None]
     ref.compare(small, want, 2 * ref.UNIT[F16] * v.abs().cumsum(0) / torch.arange(1, 21)[:, None, None] + 2.0 ** -24, "tiny scale")
+
+
+def test_a_workspace_that_is_not_beside_the_queries_is_refused(way):
+    """(its address would be written to)"""
+    kc, vc, table = _paged(1, 4000, 2, 64)
+    q = _normal((1, 1, 4, 64), F16, 3).cuda()
+    args = (q, kc.cuda(), vc.cuda(), table.cuda(), torch.tensor([3900], dtype=torch.int32).cuda())
+    need = fq.attention_tree_workspace_bytes(1, 1, 4, 2, 64, table.shape[1], 16)
+    rows, keys = _normal((2, 4, 64), F16, 5).cuda(), _normal((3000, 2, 64), F16, 6).cuda()
+    need_prompt = fq.attention_prompt_workspace_bytes(4, 2, 64, [0, 2], [0, 3000])
+    assert need and need_prompt
+    size = max(need, need_prompt)
+    for wrong in (torch.empty(size, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8, device="cuda").expand(size),
+                  torch.empty(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(fq.FqError):
+            fq.attention_tree(*args, workspace=wrong)
+        with pytest.raises(fq.FqError):
+            fq.attention_prompt(rows, keys, keys, [0, 2], [0, 3000], workspace=wrong)
+    good = torch.empty((size + 3) // 4, dtype=torch.float32, device="cuda")
+    assert torch.equal(fq.attention_tree(*args, workspace=good), fq.attention_tree(*args))
+    assert torch.equal(fq.attention_tree(*args, workspace=good[:1]), fq.attention_tree(*args))       # (too small: as if none were given)
+    assert torch.equal(fq.attention_prompt(rows, keys, keys, [0, 2], [0, 3000], workspace=good), fq.attention_prompt(rows, keys, keys, [0, 2], [0, 3000]))
