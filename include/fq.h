@@ -374,8 +374,9 @@ int fq_qk_norm_rope(const void* qkv, int act_dtype, int64_t tokens, int64_t row_
  *   out            out  [q_offsets_host[sequences], q_heads, head_dim], act_dtype; must not overlap an input
  *   workspace           device scratch, >= fq_attention_prompt_workspace_bytes(...) bytes (may be NULL when that is 0)
  * Deterministic; asynchronous on `stream`, no allocation.  No rows, or no sequences: a valid no-op.
- * Errors: FQ_ERR_INVALID_ARG (null pointers, offsets, scale), FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences, 2^31 - 1025 rows or keys, or 2^24
- *         blocks of 128 rows and a head, pointers or strides not aligned to 16 bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
+ * Errors: FQ_ERR_INVALID_ARG (null pointers, offsets, scale), FQ_ERR_UNSUPPORTED (shape limits, more than 65536 sequences or 2^31 - 1025 rows or
+ *         keys, 2^24 and more blocks of 128 rows and a head in 128 sequences from one that 128 divides on, pointers or strides not aligned to 16
+ *         bytes), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
  */
 size_t fq_attention_prompt_workspace_bytes(int q_heads, int kv_heads, int head_dim, const int32_t* q_offsets_host,
                                            const int32_t* k_offsets_host, int sequences);

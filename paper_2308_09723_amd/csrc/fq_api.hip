@@ -422,7 +422,7 @@ static int check_prompt(int act_dtype, int q_heads, int kv_heads, int head_dim, 
     a->q_offsets = q_offsets;
     a->k_offsets = k_offsets;
     a->sequences = sequences;
-    return FQ_OK;
+    return fq_prompt_fits(*a) ? FQ_OK : FQ_ERR_UNSUPPORTED;
 }
 
 // 1 / sqrt(head_dim) for 0; false: not a scale

@@ -243,6 +243,8 @@ struct tile_counts {
     }
 };
 
+constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;       // of a launch (2^32 threads)
+
 // Pieces for the keys of a launch's query tiles, a piece's sums being written and read again and joining them a launch.  Few tiles: as
 // many as bring the blocks up to the number that run at once, of eight key tiles and more (three pieces of prompts behind 4001 keys, 224
 // tiles of heads: 138 us whole, 61 in 2 pieces, 66 in 3, 63 in 4; 100 queries behind 8000 keys 194 whole, 39 in 16; 1000 tokens of 16 heads in
@@ -254,7 +256,7 @@ int plan_splits(const fq_prompt_args& a, const tile_counts& c) {
     if (units == 0) return 1;
     const int64_t even = units * 2 <= room ? std::min<int64_t>(room / units, c.longest / 8)
                                            : std::min<int64_t>((2 * c.longest * room + work) / (2 * work), c.longest / 16);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(64, even));
+    return (int)std::max<int64_t>(1, std::min({(int64_t)64, even, MOST_BLOCKS / units}));
 }
 
 // Heads of a die whose keys and values, of all sequences of a launch, its 4 MiB of cache holds.
@@ -265,6 +267,16 @@ int heads_together(const fq_prompt_args& a, int first, int n) {
 }
 
 }  // namespace
+
+bool fq_prompt_fits(const fq_prompt_args& a) {
+    for (int first = 0; first < a.sequences; first += SEQUENCES) {
+        const int last = std::min(first + SEQUENCES, a.sequences);
+        int64_t tiles = 0;
+        for (int b = first; b < last; ++b) tiles += (a.q_offsets[b + 1] - a.q_offsets[b] + ROWS - 1) / ROWS;
+        if (tiles * a.q_heads > MOST_BLOCKS) return false;
+    }
+    return true;
+}
 
 size_t fq_prompt_bytes(const fq_prompt_args& a) {
     size_t most = 0;
@@ -290,7 +302,6 @@ int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* wor
         p.factor = a.scale * LOG2E;
         p.splits = plan_splits(a, c);
         p.slots = (float*)workspace;
-        if (total * a.q_heads * p.splits >= 1 << 24) return FQ_ERR_UNSUPPORTED;      // (2^32 threads)
         p.units = (int)total * a.q_heads;
         p.together = p.splits > 1 ? std::max(1, a.q_heads / 8) : heads_together(a, first, n);       // (pieces: all blocks run at once anyway)
         p.of_set = (int)total * p.together;

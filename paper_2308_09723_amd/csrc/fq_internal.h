@@ -155,6 +155,7 @@ struct fq_prompt_args {
     float scale;
     void* out;
 };
+bool fq_prompt_fits(const fq_prompt_args& a);      // whether every launch has few enough blocks
 size_t fq_prompt_bytes(const fq_prompt_args& a);
 int fq_launch_attention_prompt(int act_dtype, const fq_prompt_args& a, void* workspace, hipStream_t stream);
 

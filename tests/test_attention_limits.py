@@ -75,6 +75,20 @@ def test_norm_rope_of_2_to_24_tokens_is_more_than_a_launch():
     assert call((1 << 24) - 1, q_out=P) == fq.FQ_ERR_INVALID_ARG      # (over qkv)
 
 
+def test_prompts_of_which_a_later_launch_is_too_large_start_none():
+    """128 sequences a launch: the 129th alone is too much."""
+    def call(last, hq=4096):
+        offsets = list(range(129)) + [128 + last]
+        heads = [fq.Heads(P << 20 + i, hq * 8, 8) for i in range(3)]
+        need = fq.attention_prompt_workspace_bytes(hq, hq, 8, offsets)
+        return need, fq.attention_prompt_raw(*heads, 0, hq, hq, 8, offsets, None, 0.0, P << 24, None, 0)
+    assert call(4096 * 128 - 127) == (0, fq.FQ_ERR_UNSUPPORTED)
+    assert call(4096 * 128) == (0, fq.FQ_ERR_UNSUPPORTED)
+    # one tile fewer is not, nor is it when pieces would make it so: few heads, many keys
+    offsets, keys = [0, 2], [0, 2 ** 31 - 1025]
+    assert fq.attention_prompt_workspace_bytes(4, 4, 8, offsets, keys) > 0
+
+
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
 def test_parts_of_the_longest_contexts(tmp_path):
     """Keys up to 2^31 - 1025 in parts of up to 2^30, as the kernels go through them (attention_parts_check.cpp)."""
