@@ -98,3 +98,29 @@ def test_parts_of_the_longest_contexts(tmp_path):
     assert out.returncode == 0, out.stdout[-2000:]
     walks, wrong = (int(out.stdout.split()[i]) for i in (-4, -2))
     assert walks > 1000 and wrong == 0
+
+
+def _prompt_bytes(rows, behind, hq, hk, D):
+    def offsets(lengths):
+        out = [0]
+        for n in lengths:
+            out.append(out[-1] + n)
+        return out
+    return fq.attention_prompt_workspace_bytes(hq, hk, D, offsets(rows), offsets([r + b for r, b in zip(rows, behind)]))
+
+
+@pytest.mark.parametrize("rows,behind,most", [
+    ([512] * 16 + [256], [0] * 16 + [8000], 0), ([128] * 64 + [256], [0] * 64 + [8000], 0), ([512] * 64 + [256], [0] * 64 + [32000], 0),
+    ([128] * 128, [0] * 127 + [131000], 5),
+])
+def test_one_long_prompt_among_many_short_ones(rows, behind, most):
+    """Every tile's sums are written and read for the long prompt's pieces: fewer of them, or none (times in plan_splits)."""
+    tiles = sum((r + 127) // 128 for r in rows)
+    assert _prompt_bytes(rows, behind, 32, 8, 128) <= most * tiles * 32 * 128 * 130 * 4
+
+
+def test_long_prompts_are_cut():
+    piece = 128 * 66 * 4
+    assert _prompt_bytes([3397], [0], 12, 12, 64) == 27 * 12 * 3 * piece
+    assert _prompt_bytes([3] * 20 + [5], [0] * 20 + [3995], 16, 4, 64) == 21 * 16 * 3 * piece
+    assert _prompt_bytes([100], [7900], 32, 8, 64) == 32 * 15 * piece
