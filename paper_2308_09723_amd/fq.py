@@ -650,6 +650,13 @@ def _output(out, shape, like, where):
     return out
 
 
+def _offsets(offsets, rows, where):
+    """Offsets that end at `rows`, as a list of integers of which none is another in 32 bits."""
+    offsets = [int(x) for x in offsets]
+    _require(len(offsets) >= 1 and offsets[-1] == rows and min(offsets) >= 0 and max(offsets) <= rows, where)
+    return offsets
+
+
 def _scratch(workspace, need, like, where):
     """A caller's workspace (contiguous, on like's device) where it is large enough, or a new one of `need` bytes; and its size."""
     torch = _torch_mod or _torch()
@@ -729,9 +736,9 @@ def attention_prompt(q, k, v, q_offsets, k_offsets=None, scale=None, out=None, w
     (rows, heads, D), (keys, kv_heads, _) = q.shape, k.shape
     for t in (k, v):
         _require(tuple(t.shape) == (keys, kv_heads, D) and t.dtype == q.dtype and t.device == q.device, where)
-    _require(len(q_offsets) >= 1 and q_offsets[-1] == rows, where)
-    _require(k_offsets is None or len(k_offsets) == len(q_offsets), where)
-    _require((q_offsets if k_offsets is None else k_offsets)[-1] == keys, where)
+    q_offsets = _offsets(q_offsets, rows, where)
+    k_offsets = None if k_offsets is None else _offsets(k_offsets, keys, where)
+    _require(len(k_offsets) == len(q_offsets) if k_offsets is not None else keys == rows, where)
     scale = _given_scale(scale, where)
     o = _output(out, (rows, heads, D), q, where)
     workspace, size = _scratch(workspace, attention_prompt_workspace_bytes(heads, kv_heads, D, q_offsets, k_offsets), q, where)

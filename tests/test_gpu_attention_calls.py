@@ -84,3 +84,17 @@ def test_a_workspace_that_is_not_beside_the_queries_is_refused(way):
     assert torch.equal(fq.attention_tree(*args, workspace=good), fq.attention_tree(*args))
     assert torch.equal(fq.attention_tree(*args, workspace=good[:1]), fq.attention_tree(*args))       # (too small: as if none were given)
     assert torch.equal(fq.attention_prompt(rows, keys, keys, [0, 2], [0, 3000], workspace=good), fq.attention_prompt(rows, keys, keys, [0, 2], [0, 3000]))
+
+
+def test_offsets_that_32_bits_do_not_hold_are_refused(way):
+    """(2^32 + 3 is no row, and its lower half is one)"""
+    x = _normal((9, 4, 64), F16, 4).cuda()
+    for wrong in ([0, 2 ** 32 + 3, 9], [0, 2 ** 31, 9], [0, -2 ** 32 + 3, 9]):
+        with pytest.raises(fq.FqError):
+            fq.attention_prompt(x, x, x, wrong)
+        with pytest.raises(fq.FqError):
+            fq.attention_prompt(x, x, x, [0, 3, 9], wrong)
+    want = fq.attention_prompt(x, x, x, [0, 3, 9])
+    for offsets in ((0, 3, 9), torch.tensor([0, 3, 9]), torch.tensor([0, 3, 9], dtype=torch.int32).numpy()):
+        assert torch.equal(fq.attention_prompt(x, x, x, offsets), want)
+        assert torch.equal(fq.attention_prompt(x, x, x, [0, 3, 9], offsets), want)
