@@ -64,9 +64,9 @@ struct prompt_plan {
 // A block: 128 queries of one head, a wave 32 of them (fq_attn_tile.h has the mathematics), and 64 keys and values at a time, twice 32 KiB of LDS
 // for heads of 128 values, so that two blocks fill a compute unit, one's products beside the other's numerators.
 // Bound by the issue of products and numerators, and by power: 8192 tokens, 32 heads over 8 of 128 values in bfloat16, 550 GF in
-// 490 - 530 us = 1.04 - 1.12 PFLOP/s (a library's product of 8192 x 8192 x 8192: 1.21), binary16 542 (540 with maxima looked for as rarely as in
+// 498 - 541 us = 1.02 - 1.10 PFLOP/s (a library's product of 8192 x 8192 x 8192: 1.21), binary16 542 (540 with maxima looked for as rarely as in
 // bfloat16: not theirs).
-// Short prompts by the blocks' beginnings and ends: 24 prompts of 17 - 1500 tokens 101 us = 0.66 PFLOP/s.
+// Short prompts by the blocks' beginnings and ends: 24 prompts of 17 - 1500 tokens 95 - 113 us = 0.59 - 0.70 PFLOP/s.
 template <int ACT, int DP>
 __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q, fq_heads k, fq_heads v, prompt_plan p, uint16_t* out,
                                                                      prompt_items items) {
@@ -252,8 +252,8 @@ constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;       // of a launch (2^32 thread
 // bring those down to a block's even share, of sixteen key tiles and more (15 prompts of 24 - 1018 tokens, 16 heads, 21 whole, 28 in pieces of
 // eight tiles), and of these as many as are through first.  All tiles of a launch are cut into as many, and the sums of many tiles cost more than a long
 // one gains: a key tile takes 1.1 us, and sums are written and read at 4.3 TB/s.  (One prompt of 3397 tokens, 12 heads of 64: 55 us whole, 44 in 3;
-// one of 2324, 32 heads over 8 of 128: 59 whole, 82 in 2; 16 prompts of 512 and 256 queries behind 8000 keys, 32 heads of 128, 187 whole, 443 in 4; 127 of 128 and one behind 131000 2261 whole, 1356 in
-// 4, 2281 in 14.)
+// one of 2324, 32 heads over 8 of 128: 59 whole, 82 in 2; the same heads, 16 prompts of 512 and 256 queries behind 8000 keys 187 whole, 443 in
+// 4; 127 of 128 and one behind 131000 2261 whole, 1356 in 4, 2281 in 14.)
 int plan_splits(const fq_prompt_args& a, const tile_counts& c) {
     const int64_t units = c.total * a.q_heads, work = c.keys * a.q_heads, room = 2 * fq_cu_count();
     if (units == 0) return 1;

