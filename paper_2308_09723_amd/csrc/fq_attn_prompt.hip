@@ -226,9 +226,9 @@ int launch(const fq_prompt_args& a, const prompt_plan& p, const prompt_items& it
     return launch<ACT, 128>(a, p, items, total, stream);
 }
 
-// Of sequences first .. first + n - 1: query tiles, the key tiles of all of them, and the most that one has.
+// Of sequences first .. first + n - 1: rows, query tiles, the key tiles of all of them, and the most that one has.
 struct tile_counts {
-    int64_t total = 0, keys = 0;
+    int64_t rows = 0, total = 0, keys = 0;
     int longest = 0;
     tile_counts(const fq_prompt_args& a, int first, int n) {
         for (int b = first; b < first + n; ++b) {
@@ -236,6 +236,7 @@ struct tile_counts {
             if (queries == 0) continue;
             const int64_t tiles = (queries + ROWS - 1) / ROWS, last = (all + KEYS - 1) / KEYS;
             const int64_t least = std::max<int64_t>(1, std::min(last, (all - queries + ROWS + KEYS - 1) / KEYS));
+            rows += queries;
             total += tiles;
             keys += tiles * (least + std::max<int64_t>(1, last)) / 2;
             longest = std::max(longest, (int)last);
@@ -245,27 +246,27 @@ struct tile_counts {
 
 constexpr int64_t MOST_BLOCKS = (1 << 24) - 1;       // of a launch (2^32 threads)
 
-// Pieces for the keys of a launch's query tiles, a piece's sums being written and read again and joining them a launch.  Few tiles: as
-// many as bring the blocks up to the number that run at once, of eight key tiles and more (three pieces of prompts behind 4001 keys, 224
-// tiles of heads: 138 us whole, 61 in 2 pieces, 66 in 3, 63 in 4; 100 queries behind 8000 keys 194 whole, 39 in 16; 1000 tokens of 16 heads in
-// pieces of four tiles 24.4, of eight 24.7).  More of them, but some of so many keys that the others are done long before: up to as many as
-// bring those down to a block's even share, of sixteen key tiles and more (15 prompts of 24 - 1018 tokens, 16 heads, 21 whole, 28 in pieces of
-// eight tiles), and of these as many as are through first.  All tiles of a launch are cut into as many, and the sums of many tiles cost more than a long
-// one gains: a key tile takes 1.1 us, and sums are written and read at 4.3 TB/s.  (One prompt of 3397 tokens, 12 heads of 64: 55 us whole, 44 in 3;
-// one of 2324, 32 heads over 8 of 128: 59 whole, 82 in 2; the same heads, 16 prompts of 512 and 256 queries behind 8000 keys 187 whole, 443 in
-// 4; 127 of 128 and one behind 131000 2261 whole, 1356 in 4, 2281 in 14.)
+// Pieces for the keys of a launch's query tiles: a piece's sums are written and read again, and joining them is a launch.  At most, where tiles are
+// few, as many as bring the blocks up to the number that run at once, of eight key tiles and more (1000 tokens of 16 heads in pieces of four tiles
+// 24.4 us, of eight 24.7); where they are more, but some of so many keys that the others are done long before, as many as bring those down to a block's
+// even share, of sixteen key tiles and more (15 prompts of 24 - 1018 tokens, 16 heads, 21 us whole, 28 in pieces of eight tiles).
+//
+// Up to there, as many as are through first: a key tile takes 1.1 us, the sums of all rows (all are cut into as many) are written and read at
+// 4.3 TB/s, and joining them takes 4 us more.  us, whole and in pieces: three prompts behind 4001 keys, 224 tiles of heads, 70, 56 in 2; 100 queries
+// behind 8000 keys 134, 36 - 40 in 8 to 16; one prompt of 3397 tokens, 12 heads of 64, 55, 44 in 3; of 1024 tokens, 32 heads over 8 of 128, 25, 32 in 2; of
+// 2324 59, 82 in 2; the same heads, 16 prompts of 512 and 256 queries behind 8000 keys 187, 443 in 4; 127 of 128 and one behind 131000 2261, 1356 in
+// 4, 2281 in 14.
 int plan_splits(const fq_prompt_args& a, const tile_counts& c) {
     const int64_t units = c.total * a.q_heads, work = c.keys * a.q_heads, room = 2 * fq_cu_count();
     if (units == 0) return 1;
     const bool few = units * 2 <= room;
     const int64_t even = few ? room / units : (2 * c.longest * room + work) / (2 * work);
     const int most = (int)std::min({(int64_t)64, even, (int64_t)c.longest / (few ? 8 : 16), MOST_BLOCKS / units});
-    if (most <= 1 || few) return std::max(1, most);
-    const double share = (double)work / room, sums = units * 2.0 * ROWS * (a.head_dim + 2) * sizeof(float) / 4.3e6;      // a piece's of all tiles, us
+    const double share = (double)work / room, sums = 2.0 * c.rows * a.q_heads * (a.head_dim + 2) * sizeof(float) / 4.3e6;      // a piece's of all rows, us
     int best = 1;
     double least = 1.1 * c.longest;
     for (int n = 2; n <= most; ++n) {
-        const double t = 1.1 * std::max((double)c.longest / n, share) + n * sums;
+        const double t = 1.1 * std::max((double)c.longest / n, share) + n * sums + 4;
         if (t < least) best = n, least = t;
     }
     return best;

@@ -119,6 +119,11 @@ def test_one_long_prompt_among_many_short_ones(rows, behind, most):
     assert _prompt_bytes(rows, behind, 32, 8, 128) <= most * tiles * 32 * 128 * 130 * 4
 
 
+@pytest.mark.parametrize("rows,hq,hk,D", [(1024, 32, 8, 128), (1000, 32, 32, 128), (1024, 28, 4, 128), (1024, 24, 4, 96), (2324, 32, 8, 128)])
+def test_one_prompt_that_is_through_sooner_whole(rows, hq, hk, D):
+    assert _prompt_bytes([rows], [0], hq, hk, D) == 0
+
+
 def test_long_prompts_are_cut():
     piece = 128 * 66 * 4
     assert _prompt_bytes([3397], [0], 12, 12, 64) == 27 * 12 * 3 * piece
