@@ -64,9 +64,9 @@ struct prompt_plan {
 // A block: 128 queries of one head, a wave 32 of them (fq_attn_tile.h has the mathematics), and 64 keys and values at a time, twice 32 KiB of LDS
 // for heads of 128 values, so that two blocks fill a compute unit, one's products beside the other's numerators.
 // Bound by the issue of products and numerators, and by power: 8192 tokens, 32 heads over 8 of 128 values in bfloat16, 550 GF in
-// 498 - 541 us = 1.02 - 1.10 PFLOP/s (a library's product of 8192 x 8192 x 8192: 1.21), binary16 542 (540 with maxima looked for as rarely as in
+// 488 - 541 us = 1.02 - 1.13 PFLOP/s (a library's product of 8192 x 8192 x 8192: 1.21), binary16 542 (540 with maxima looked for as rarely as in
 // bfloat16: not theirs).
-// Short prompts by the blocks' beginnings and ends: 24 prompts of 17 - 1500 tokens 95 - 113 us = 0.59 - 0.70 PFLOP/s.
+// Short prompts by the blocks' beginnings and ends: 24 prompts of 17 - 1500 tokens 94 - 113 us = 0.59 - 0.71 PFLOP/s.
 template <int ACT, int DP>
 __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q, fq_heads k, fq_heads v, prompt_plan p, uint16_t* out,
                                                                      prompt_items items) {

@@ -725,7 +725,8 @@ def qk_norm_rope(qkv, heads, kv_heads, table, positions, q_weight=None, k_weight
 def attention_prompt(q, k, v, q_offsets, k_offsets=None, scale=None, out=None, workspace=None):
     """Causal attention over packed sequences: q cuda [rows, heads, head_dim], k and v [keys, kv_heads, head_dim] (float16 or bfloat16,
     any row and head strides), sequence b's rows q_offsets[b] .. q_offsets[b + 1] - 1 (host integers) and keys k_offsets[b] .. (None: the
-    same) -> [rows, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given."""
+    same) -> [rows, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given.  workspace: scratch on the same device, contiguous
+    (attention_prompt_workspace_bytes; a smaller one is as none, for which some is allocated)."""
     torch = _torch_mod or _torch()
     done = _native.attention_prompt(q, k, v, q_offsets, k_offsets, scale, out, workspace)
     if done is not None:
@@ -751,7 +752,8 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
     """Attention of drafted tokens over a paged cache: q cuda [sequences, nodes, heads, head_dim] (float16 or bfloat16; the tokens of all
     sequences evenly apart), caches [pages, page_size, kv_heads, head_dim], page_table int32 [sequences, width], context_lens int32 [sequences]
     (tokens in the cache before the drafted ones, whose keys and values lie in the places behind them), mask int64 [nodes, words] or
-    [sequences, nodes, words] (tree_mask; None: a chain) -> [sequences, nodes, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given."""
+    [sequences, nodes, words] (tree_mask; None: a chain) -> [sequences, nodes, heads, head_dim].  scale: 1 / sqrt(head_dim) unless given.
+    workspace: as attention_prompt's (attention_tree_workspace_bytes)."""
     torch = _torch_mod or _torch()
     done = _native.attention_tree(q, k_cache, v_cache, page_table, context_lens, mask, scale, out, workspace)
     if done is not None:
