@@ -416,6 +416,57 @@ int fq_attention_tree(const fq_heads* q, int act_dtype, int64_t sequences, int64
                       void* stream);
 
 /*
+ * A cache of keys and values held in 4 bits, 4.5 with its scales (16-bit values: 3.6 times as much), by the method's own quantiser: groups of 32
+ * consecutive values w of a head (the last one of a head may be shorter), each with a scale of its own,
+ *   s = the smallest value of act_dtype with at most 8 (FQ_F16) or 5 (FQ_BF16) significant bits and 7.5 s >= max |w|,
+ *   q = clamp(round_half_even(w / s), -7, 7);
+ * what the cache stands for, q s, is a value of act_dtype exactly (3 bits times 8 or 5).  A group that holds an infinity or a NaN stands for NaNs.
+ * Pages are opaque: fq_kv4_page_bytes(page_size, kv_heads, head_dim) bytes of each, page_stride bytes apart, which may be copied
+ * from page to page; every token's bytes in them are its own.  Slot s is place s % page_size of page s / page_size.  A cache is read as the act_dtype that it was
+ * written as.
+ * Shape limits as above, and page_size a multiple of 16; pages * page_size at most 2^31 - 1; data and page_stride aligned to 16 bytes.
+ * (head_dim that is no multiple of 32 takes the room of the next one.)
+ */
+typedef struct fq_kv4_pages {
+    void* data;
+    int64_t pages;
+    int page_size;
+    int64_t page_stride; /* bytes */
+} fq_kv4_pages;
+
+/* Bytes of a page.  0 on invalid arguments. */
+size_t fq_kv4_page_bytes(int page_size, int kv_heads, int head_dim);
+
+/*
+ * fq_kv4_write -- the keys and values of `tokens` tokens into the cache.
+ *   k, v     in   rows of kv_heads heads of head_dim values, act_dtype
+ *   slots    in   [tokens] device; one outside the cache (a negative one: padding) is not written.  Slots that are written are different ones
+ * The cache must not overlap an input.  tokens = 0 is a valid no-op.  Asynchronous on `stream`, one kernel, no scratch.  Nothing else in the
+ * cache is touched, so that calls for different slots may run at the same time.
+ * Errors: FQ_ERR_INVALID_ARG, FQ_ERR_UNSUPPORTED (shape limits, 2^24 tokens and more, pointers or strides not aligned to 16 bytes), FQ_ERR_HIP.
+ */
+int fq_kv4_write(const fq_heads* k, const fq_heads* v, int act_dtype, int64_t tokens, int kv_heads, int head_dim, const fq_kv4_pages* cache,
+                 const int64_t* slots, void* stream);
+
+/*
+ * fq_kv4_read -- the other way: k_out and v_out [tokens, kv_heads, head_dim] get what the cache holds in slots[t] (a prefix, for
+ * fq_attention_prompt); zeros for a slot outside it.  Slots may repeat.  The outputs must not overlap the cache, the slots or each other.
+ */
+int fq_kv4_read(const fq_kv4_pages* cache, int act_dtype, int64_t tokens, int kv_heads, int head_dim, const int64_t* slots, void* k_out,
+                void* v_out, void* stream);
+
+/*
+ * fq_attention_tree_kv4 -- fq_attention_tree over a cache held in 4 bits: the attention of what the cache stands for, with that call's
+ * arguments, limits, numerics and errors (FQ_BF16, up to 32 rows of a key head: numerators are rounded as products with the values' scales).
+ */
+size_t fq_attention_tree_kv4_workspace_bytes(int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,
+                                             int page_size);
+int fq_attention_tree_kv4(const fq_heads* q, int act_dtype, int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim,
+                          const fq_kv4_pages* cache, const int32_t* page_table, int64_t table_width, const int32_t* context_lens,
+                          const uint64_t* mask, int64_t mask_stride, float scale, void* out, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
  * fq_gemm_describe -- writes a short text description of the kernel configuration fq_gemm
  * would use for this problem (kernel family, tile shape, block shape, split-K factor) into
  * buf (HOST memory, at most buf_bytes including the terminating 0).  For logs and benchmark

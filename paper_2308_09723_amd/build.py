@@ -27,6 +27,8 @@ SOURCES = [
     "fq_rope.hip",
     "fq_attn_prompt.hip",
     "fq_attn_tree.hip",
+    "fq_kv4.hip",
+    "fq_attn_kv4.hip",
     "fq_gemm_f16_4.hip",
     "fq_gemm_f16_8.hip",
     "fq_gemm_bf16_4.hip",
@@ -68,7 +70,8 @@ NO_SPILL = [
 # Kernels of which no instantiation may: the streaming kernels of 17 rows and more, of row blocks and of grouped tiles; attention
 # (whose loads into LDS a wait for a reload would drain).
 NO_SPILL_FAMILIES = ["fq_gemm_mid_kernel", "fq_gemm_mid_items_kernel", "fq_w4a8_mid_kernel", "fq_attention_prompt_kernel",
-                     "fq_attention_tree_stream_kernel", "fq_attention_tree_tile_kernel"]
+                     "fq_attention_tree_stream_kernel", "fq_attention_tree_tile_kernel", "fq_attention_kv4_stream_kernel",
+                     "fq_attention_kv4_tile_kernel"]
 
 
 def _run(cmd):

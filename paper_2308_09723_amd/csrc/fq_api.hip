@@ -6,6 +6,7 @@
 #include <stdio.h>
 
 #include "fq_internal.h"
+#include "fq_kv4.h"
 #include "fq_layout.h"
 
 namespace {
@@ -483,6 +484,21 @@ static int check_tree(int act_dtype, int64_t sequences, int64_t nodes, int q_hea
     return fq_tree_fits(*a) ? FQ_OK : FQ_ERR_UNSUPPORTED;
 }
 
+// What fq_attention_tree reads and writes beside the cache, for a call that check_tree() has seen
+static int check_tree_memory(const fq_heads* q, const fq_tree_args& a, const int32_t* page_table, const int32_t* context_lens, const uint64_t* mask,
+                             int64_t mask_stride, const void* out) {
+    const int64_t words = (int64_t)a.nodes * ((a.nodes + 63) / 64), rows = a.sequences * a.nodes;
+    if (mask && mask_stride != 0 && mask_stride < words) return FQ_ERR_INVALID_ARG;
+    const int st = check_rows(q, rows, a.q_heads);
+    if (st != FQ_OK) return st;
+    if (!aligned16(out) || too_far(a.sequences, mask_stride)) return FQ_ERR_UNSUPPORTED;
+    const size_t bytes = (size_t)rows * a.q_heads * a.head_dim * 2, all = (size_t)((mask_stride ? (a.sequences - 1) * mask_stride : 0) + words);
+    if (fq_overlaps(out, bytes, {{q->data, (size_t)((rows - 1) * q->row_stride + (a.q_heads - 1) * q->head_stride + a.head_dim) * 2},
+                                 {page_table, (size_t)(a.sequences * a.table_width) * 4}, {context_lens, (size_t)a.sequences * 4}, {mask, mask ? all * 8 : 0}}))
+        return FQ_ERR_INVALID_ARG;
+    return FQ_OK;
+}
+
 size_t fq_attention_tree_workspace_bytes(int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,
                                          int page_size) {
     fq_tree_args a = {};
@@ -503,15 +519,9 @@ int fq_attention_tree(const fq_heads* q, int act_dtype, int64_t sequences, int64
     if (!effective_scale(&scale, head_dim) || mask_stride < 0) return FQ_ERR_INVALID_ARG;
     if (sequences == 0 || nodes == 0) return FQ_OK;
     if (!q || !out || !context_lens || (!page_table && table_width > 0)) return FQ_ERR_INVALID_ARG;
-    if (mask && mask_stride != 0 && mask_stride < nodes * ((nodes + 63) / 64)) return FQ_ERR_INVALID_ARG;
-    if ((st = check_rows(q, sequences * nodes, q_heads)) != FQ_OK) return st;
-    if (!aligned16(out) || too_far(sequences, mask_stride)) return FQ_ERR_UNSUPPORTED;
+    if ((st = check_tree_memory(q, a, page_table, context_lens, mask, mask_stride, out)) != FQ_OK) return st;
     const size_t bytes = (size_t)(sequences * nodes) * q_heads * head_dim * 2;
-    const size_t words = (size_t)((mask_stride ? (sequences - 1) * mask_stride : 0) + nodes * ((nodes + 63) / 64));
-    if (fq_overlaps(out, bytes, {{q->data, (size_t)((sequences * nodes - 1) * q->row_stride + (q_heads - 1) * q->head_stride + head_dim) * 2},
-                                 {page_table, (size_t)(sequences * table_width) * 4}, {context_lens, (size_t)sequences * 4}, {mask, mask ? words * 8 : 0}}) ||
-        over_cache(out, bytes, cache, kv_heads, head_dim))
-        return FQ_ERR_INVALID_ARG;
+    if (over_cache(out, bytes, cache, kv_heads, head_dim)) return FQ_ERR_INVALID_ARG;
     const size_t need = fq_tree_bytes(a);
     if (need > 0 && (!workspace || workspace_bytes < need)) return FQ_ERR_WORKSPACE;
     a.q = *q;
@@ -523,6 +533,102 @@ int fq_attention_tree(const fq_heads* q, int act_dtype, int64_t sequences, int64
     a.scale = scale;
     a.out = out;
     return fq_launch_attention_tree(act_dtype, a, workspace, (hipStream_t)stream);
+}
+
+// ------------------------------------------------------------------------------------------ a cache held in 4 bits
+size_t fq_kv4_page_bytes(int page_size, int kv_heads, int head_dim) {
+    if (page_size <= 0 || page_size % fqkv::RECORD != 0 || check_heads(FQ_F16, kv_heads, kv_heads, head_dim) != FQ_OK) return 0;
+    return (size_t)fqkv::page_bytes(page_size, kv_heads, head_dim);
+}
+
+static int check_kv4(const fq_kv4_pages* c, int kv_heads, int head_dim) {
+    if (!c->data || c->pages <= 0 || c->page_size <= 0) return FQ_ERR_INVALID_ARG;
+    if (c->page_size % fqkv::RECORD != 0) return FQ_ERR_UNSUPPORTED;
+    if (c->pages > 1 && c->page_stride < fqkv::page_bytes(c->page_size, kv_heads, head_dim)) return FQ_ERR_INVALID_ARG;
+    if (c->page_stride < 0) return FQ_ERR_INVALID_ARG;
+    if (!aligned16(c->data) || c->page_stride % 16 != 0 || too_far(c->pages, c->page_stride)) return FQ_ERR_UNSUPPORTED;
+    return c->pages > INT32_MAX / c->page_size ? FQ_ERR_UNSUPPORTED : FQ_OK;
+}
+
+// The pages as memory (from the first byte to the last)
+static fq_span kv4_span(const fq_kv4_pages* c, int kv_heads, int head_dim) {
+    return {c->data, (size_t)((c->pages - 1) * c->page_stride + fqkv::page_bytes(c->page_size, kv_heads, head_dim))};
+}
+
+static int check_kv4_rows(int act_dtype, int64_t tokens, int kv_heads, int head_dim, const fq_kv4_pages* cache) {
+    if (tokens < 0 || !cache) return FQ_ERR_INVALID_ARG;
+    const int st = check_heads(act_dtype, kv_heads, kv_heads, head_dim);
+    if (st != FQ_OK) return st;
+    if (tokens >= (int64_t)1 << 24) return FQ_ERR_UNSUPPORTED;
+    return check_kv4(cache, kv_heads, head_dim);
+}
+
+int fq_kv4_write(const fq_heads* k, const fq_heads* v, int act_dtype, int64_t tokens, int kv_heads, int head_dim, const fq_kv4_pages* cache,
+                 const int64_t* slots, void* stream) {
+    int st = check_kv4_rows(act_dtype, tokens, kv_heads, head_dim, cache);
+    if (st != FQ_OK) return st;
+    if (tokens == 0) return FQ_OK;
+    if (!k || !v || !slots) return FQ_ERR_INVALID_ARG;
+    if ((st = check_rows(k, tokens, kv_heads)) != FQ_OK || (st = check_rows(v, tokens, kv_heads)) != FQ_OK) return st;
+    const fq_span all = kv4_span(cache, kv_heads, head_dim);
+    auto span = [&](const fq_heads* x) {
+        return fq_span{x->data, (size_t)((tokens - 1) * x->row_stride + (kv_heads - 1) * x->head_stride + head_dim) * 2};
+    };
+    if (fq_overlaps(all.p, all.bytes, {span(k), span(v), {slots, (size_t)tokens * 8}})) return FQ_ERR_INVALID_ARG;
+    const fq_kv4_args a = {*k, *v, nullptr, nullptr, tokens, kv_heads, head_dim, fqkv::groups_of(head_dim), *cache, slots};
+    return fq_launch_kv4_write(act_dtype, a, (hipStream_t)stream);
+}
+
+int fq_kv4_read(const fq_kv4_pages* cache, int act_dtype, int64_t tokens, int kv_heads, int head_dim, const int64_t* slots, void* k_out,
+                void* v_out, void* stream) {
+    const int st = check_kv4_rows(act_dtype, tokens, kv_heads, head_dim, cache);
+    if (st != FQ_OK) return st;
+    if (tokens == 0) return FQ_OK;
+    if (!k_out || !v_out || !slots) return FQ_ERR_INVALID_ARG;
+    if (!aligned16(k_out) || !aligned16(v_out)) return FQ_ERR_UNSUPPORTED;
+    const size_t bytes = (size_t)tokens * kv_heads * head_dim * 2;
+    const fq_span all = kv4_span(cache, kv_heads, head_dim), at = {slots, (size_t)tokens * 8};
+    if (fq_overlaps(k_out, bytes, {all, at, {v_out, bytes}}) || fq_overlaps(v_out, bytes, {all, at})) return FQ_ERR_INVALID_ARG;
+    const fq_kv4_args a = {{}, {}, k_out, v_out, tokens, kv_heads, head_dim, fqkv::groups_of(head_dim), *cache, slots};
+    return fq_launch_kv4_read(act_dtype, a, (hipStream_t)stream);
+}
+
+size_t fq_attention_tree_kv4_workspace_bytes(int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim, int64_t table_width,
+                                             int page_size) {
+    fq_tree_args a = {};
+    if (page_size <= 0 || page_size % fqkv::RECORD != 0) return 0;
+    if (check_tree(FQ_F16, sequences, nodes, q_heads, kv_heads, head_dim, table_width, page_size, &a) != FQ_OK) return 0;
+    if (sequences == 0 || nodes == 0) return 0;
+    return fq_tree_kv4_bytes(a);
+}
+
+int fq_attention_tree_kv4(const fq_heads* q, int act_dtype, int64_t sequences, int64_t nodes, int q_heads, int kv_heads, int head_dim,
+                          const fq_kv4_pages* cache, const int32_t* page_table, int64_t table_width, const int32_t* context_lens,
+                          const uint64_t* mask, int64_t mask_stride, float scale, void* out, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+    if (!cache) return FQ_ERR_INVALID_ARG;
+    fq_tree_args a = {};
+    int st = check_tree(act_dtype, sequences, nodes, q_heads, kv_heads, head_dim, table_width, cache->page_size, &a);
+    if (st != FQ_OK) return st;
+    if ((st = check_kv4(cache, kv_heads, head_dim)) != FQ_OK) return st;
+    if (!effective_scale(&scale, head_dim) || mask_stride < 0) return FQ_ERR_INVALID_ARG;
+    if (sequences == 0 || nodes == 0) return FQ_OK;
+    if (!q || !out || !context_lens || (!page_table && table_width > 0)) return FQ_ERR_INVALID_ARG;
+    if ((st = check_tree_memory(q, a, page_table, context_lens, mask, mask_stride, out)) != FQ_OK) return st;
+    const size_t bytes = (size_t)(sequences * nodes) * q_heads * head_dim * 2;
+    if (fq_overlaps(out, bytes, {kv4_span(cache, kv_heads, head_dim)})) return FQ_ERR_INVALID_ARG;
+    const size_t need = fq_tree_kv4_bytes(a);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return FQ_ERR_WORKSPACE;
+    a.q = *q;
+    const int64_t head_bytes = (int64_t)(cache->page_size / fqkv::RECORD) * fqkv::record_bytes(fqkv::groups_of(head_dim));
+    a.cache = {cache->data, cache->data, cache->pages, cache->page_size, cache->page_stride, 0, head_bytes};
+    a.page_table = page_table;
+    a.context_lens = context_lens;
+    a.mask = mask;
+    a.mask_stride = mask_stride;
+    a.scale = scale;
+    a.out = out;
+    return fq_launch_attention_tree_kv4(act_dtype, a, workspace, (hipStream_t)stream);
 }
 
 int fq_gemm_describe(int64_t M, int64_t N, int64_t K, int bits, int group_size, char* buf,

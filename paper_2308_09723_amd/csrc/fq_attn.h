@@ -27,15 +27,43 @@ struct divisor {
     __device__ int quotient(int n) const { return m == 0 ? n : (int)(__umulhi((uint32_t)n, m) >> shift); }
 };
 
+// Keys and values of 16 bits, one at a time: ROWS says where they lie.
+template <typename ROWS>
+struct rows16 {
+    // q . k of key j
+    template <int ACT>
+    __device__ float dot(const uint16_t* q, int j, int D) const {
+        typedef typename type16<ACT>::t T;
+        typedef T vec8 __attribute__((ext_vector_type(8)));
+        const T* k = (const T*)((const ROWS*)this)->key(j);
+        float sum = 0.0f;
+        for (int c = 0; c < D; c += 8) {
+            const vec8 x = *(const vec8*)((const T*)q + c), y = *(const vec8*)(k + c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)x[i], (float)y[i], sum);
+        }
+        return sum;
+    }
+    // values d and d + 1 of key j (d even)
+    template <int ACT>
+    __device__ void two(int j, int d, float* v) const {
+        typedef typename type16<ACT>::t T;
+        typedef T vec2 __attribute__((ext_vector_type(2)));
+        const vec2 x = *(const vec2*)((const T*)((const ROWS*)this)->value(j) + d);
+        v[0] = (float)x[0];
+        v[1] = (float)x[1];
+    }
+};
+
 // One key head's keys and values of a sequence, packed: rows a stride apart.
-struct packed_rows {
+struct packed_rows : rows16<packed_rows> {
     const uint16_t *k, *v;
     int64_t k_stride, v_stride;
     __device__ const uint16_t* key(int j) const { return k + j * k_stride; }
     __device__ const uint16_t* value(int j) const { return v + j * v_stride; }
 };
 // The same in the pages of a cache.
-struct paged_rows {
+struct paged_rows : rows16<paged_rows> {
     const uint16_t *k, *v;
     int64_t page_stride, token_stride;
     const int32_t* table;       // the sequence's row of the page table
@@ -47,6 +75,19 @@ struct paged_rows {
     }
     __device__ const uint16_t* key(int j) const { return k + place(j); }
     __device__ const uint16_t* value(int j) const { return v + place(j); }
+
+    // of sequence b and key head `head`
+    __device__ static paged_rows of(const fq_tree_args& a, int b, int head) {
+        paged_rows x;
+        x.k = (const uint16_t*)a.cache.k + head * a.cache.head_stride;
+        x.v = (const uint16_t*)a.cache.v + head * a.cache.head_stride;
+        x.page_stride = a.cache.page_stride;
+        x.token_stride = a.cache.token_stride;
+        x.table = a.page_table + b * a.table_width;
+        x.page_size = (uint32_t)a.cache.page_size;
+        x.last_page = (uint32_t)(a.cache.pages - 1);
+        return x;
+    }
 };
 
 // The query sees keys 0 .. end - 1.
@@ -82,9 +123,6 @@ __device__ inline float wave_sum(float x) {
 template <int ACT, typename ROWS, typename SEES>
 __device__ inline void attend_one(const uint16_t* q, const ROWS& rows, const SEES& sees, int begin, int end, int D, float factor,
                                   float* o, float* m_out, float* l_out) {
-    typedef typename type16<ACT>::t T;
-    typedef T vec8 __attribute__((ext_vector_type(8)));
-    typedef T vec2 __attribute__((ext_vector_type(2)));
     const int lane = threadIdx.x & 63;
     float m = -__builtin_inff(), l = 0.0f;
     o[0] = o[1] = 0.0f;
@@ -92,16 +130,7 @@ __device__ inline void attend_one(const uint16_t* q, const ROWS& rows, const SEE
         const int j = base + lane;
         const bool seen = j < end && sees(j);
         float s = -__builtin_inff();
-        if (seen) {
-            const T* k = (const T*)rows.key(j);
-            float sum = 0.0f;
-            for (int c = 0; c < D; c += 8) {
-                const vec8 x = *(const vec8*)((const T*)q + c), y = *(const vec8*)(k + c);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum = __builtin_fmaf((float)x[i], (float)y[i], sum);
-            }
-            s = sum * factor;
-        }
+        if (seen) s = rows.template dot<ACT>(q, j, D) * factor;
         uint64_t left = __ballot(seen);
         if (left == 0) continue;
         // (a score that is a NaN makes its numerator one; the maximum passes it by)
@@ -117,9 +146,10 @@ __device__ inline void attend_one(const uint16_t* q, const ROWS& rows, const SEE
             left &= left - 1;
             const float w = __shfl(p, i);
             if (2 * lane < D) {
-                const vec2 v = *(const vec2*)((const T*)rows.value(base + i) + 2 * lane);
-                o[0] = __builtin_fmaf(w, (float)v[0], o[0]);
-                o[1] = __builtin_fmaf(w, (float)v[1], o[1]);
+                float v[2];
+                rows.template two<ACT>(base + i, 2 * lane, v);
+                o[0] = __builtin_fmaf(w, v[0], o[0]);
+                o[1] = __builtin_fmaf(w, v[1], o[1]);
             }
         }
     }

@@ -1,0 +1,695 @@
+// Attention of drafted tokens over a cache held in 4 bits (fq_attention_tree_kv4; what the cache holds: fq_kv4.h).
+//
+// Work is dealt out as over a cache of 16 bits (fq_attn_units.h).  A key and its value are 1.125 D bytes, and taking their codes to 16 bits
+// is 2 D / 8 times 9 instructions, beside 4 D operations for each row on the matrix cores: with few rows the cache's bytes and
+// the conversions bind it about equally.
+//
+// Up to 32 rows (fq_attention_kv4_stream_kernel) every wave brings 32 keys at a time into LDS of its own, as they lie in the cache: a
+// record of 16 tokens is what one product of 16 x 16 x 32 takes, lane by lane.  S^T = K Q^T goes over the keys' codes, group by group, and
+// a group's products are multiplied by its scales in binary32.  The numerators leave S^T in the order in which O^T = V^T P^T takes them.
+// binary16 values are code times scale, exactly; bfloat16 has no packed multiplication, and there the numerators are multiplied by the
+// values' scales instead, before they are rounded, once, as they are anyway.
+//
+// Above 32 rows (fq_attention_kv4_tile_kernel) four waves take 64 keys' codes to 16 bits once, each a record, into tiles that all of them read: keys as over a
+// cache of 16 bits, values turned over (a lane has four tokens of a value).
+#include <hip/hip_runtime.h>
+#include <atomic>
+
+#include "fq_attn_units.h"
+#include "fq_kv4.h"
+#include "fq_lds_limit.h"
+
+namespace {
+
+using namespace fqa;
+using namespace fqkv;
+
+// One key head's keys and values of a sequence, one at a time.
+struct kv4_rows {
+    const char* head;
+    int64_t page_stride;
+    const int32_t* table;
+    uint32_t page_size, last_page;
+    int S;
+
+    // (cache.k: the pages; strides of a page and of a head in bytes)
+    __device__ static kv4_rows of(const fq_tree_args& a, int b, int head) {
+        kv4_rows x;
+        x.head = (const char*)a.cache.k + head * a.cache.head_stride;
+        x.page_stride = a.cache.page_stride;
+        x.table = a.page_table + b * a.table_width;
+        x.page_size = (uint32_t)a.cache.page_size;
+        x.last_page = (uint32_t)(a.cache.pages - 1);
+        x.S = groups_of(a.head_dim);
+        return x;
+    }
+    __device__ const char* record(int j) const {
+        const uint32_t n = (uint32_t)j / page_size, at = (uint32_t)j - n * page_size;
+        const int32_t page = table[n];
+        return head + (int64_t)(page < 0 ? 0u : min((uint32_t)page, last_page)) * page_stride + (int64_t)(at / RECORD) * record_bytes(S);
+    }
+    template <int ACT>
+    __device__ float dot(const uint16_t* q, int j, int D) const {
+        typedef typename type16<ACT>::t T;
+        const char* from = record(j);
+        const int token = j % RECORD;             // (pages are whole records)
+        float sum = 0.0f;
+        for (int c = 0; c < D; c += 8) {
+            const float s = (float)*(const T*)(from + scale_at(S, token, c / 32));
+            const uint32_t x = *(const uint32_t*)(from + key_at(S, token, c / 32, c / 8 % 4)), first = firsts(x), second = seconds(x);
+            for (int i = 0; i < 4; ++i) {
+                sum = __builtin_fmaf((float)((const T*)q)[c + i], decoded(first >> 8 * i & 0xffu) * s, sum);
+                sum = __builtin_fmaf((float)((const T*)q)[c + 4 + i], decoded(second >> 8 * i & 0xffu) * s, sum);
+            }
+        }
+        return sum;
+    }
+    template <int ACT>
+    __device__ void two(int j, int d, float* v) const {
+        typedef typename type16<ACT>::t T;
+        const char* from = record(j);
+        const int token = j % RECORD;
+        const float s = (float)*(const T*)(from + 32 * S + scale_at(S, token, d / 32));
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t x = *(const uint8_t*)(from + value_at(S, token, d / 32, d % 16 + i));
+            v[i] = decoded(d % 32 < 16 ? x & 0x87u : from_second(x)) * s;
+        }
+    }
+};
+
+template <int ACT>
+__device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, const f32x4& c) {
+    if constexpr (ACT == FQ_F16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// The four lanes that hold a row (16 apart)
+__device__ __forceinline__ float row_max(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return other_half_max(__builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float row_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return other_half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// Two 16-bit numbers
+template <int ACT, int HIGH>
+__device__ __forceinline__ float half_of(uint32_t x) {
+    if constexpr (ACT == FQ_F16) {
+        typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
+        return (float)__builtin_bit_cast(vec2, x)[HIGH];
+    } else {
+        return __uint_as_float(HIGH ? x & 0xffff0000u : x << 16);
+    }
+}
+__device__ __forceinline__ uint32_t times16(uint32_t a, uint32_t b) {
+    typedef _Float16 vec2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(vec2, a) * __builtin_bit_cast(vec2, b));
+}
+
+// Of four neighbouring tokens' scales (two words) those of the first `count`: what lies behind the last key may be anything.
+__device__ __forceinline__ uint32_t first_mask(int count) { return count >= 2 ? ~0u : count == 1 ? 0xffffu : 0u; }
+
+// N words in LDS from a place that is aligned to 4 (N odd), 8 or 16 bytes
+template <int N>
+__device__ __forceinline__ void read_words(const char* p, uint32_t (&x)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const u32x4 v = *(const u32x4*)(p + 4 * i);
+            x[i] = v[0], x[i + 1] = v[1], x[i + 2] = v[2], x[i + 3] = v[3];
+        }
+    } else if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const u32x2 v = *(const u32x2*)(p + 4 * i);
+            x[i] = v[0], x[i + 1] = v[1];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = ((const uint32_t*)p)[i];
+    }
+}
+
+// Where a part's records lie: the entries of the page table that the wave has in LDS.
+struct record_places {
+    const int32_t* entries;
+    uint32_t first;                  // entry 0's place in the table
+    divisor by_records;              // of a page
+    int records;
+    const char* head;
+    int64_t page_stride;
+
+    // record r (keys 16 r .. 16 r + 15), the same for all lanes
+    template <int BYTES>
+    __device__ __forceinline__ const void* place(int r) const {
+        const int n = by_records.quotient(r);
+        return uniform(head + entries[(uint32_t)n - first] * page_stride + (int64_t)(r - n * records) * BYTES);
+    }
+};
+
+// Loads of a record: 36 S units of 16 bytes
+template <int S>
+struct record_loads {
+    static constexpr int COUNT = (36 * S + 63) / 64;
+    __device__ static __forceinline__ void issue(uint32_t to, const void* from) {
+        const uint32_t lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+            if (i * 64 + (int)lane < 36 * S) load_lds16<true>(to + i * 1024, (const char*)from + i * 1024, lane * 16);
+    }
+};
+
+// ------------------------------------------------------------------------------------------ up to 32 rows
+// One wave's NT x 16 rows (lane 16 h + x: row x of each 16; of a record's keys 4 h .. 4 h + 3)
+template <int ACT, int S, int NT>
+struct few_rows {
+    static constexpr float LARGER = ACT == FQ_F16 ? 7.0f : 0.0f;       // the first score's numerator, log2
+    u32x4 q[NT][S];
+    f32x4 o[NT][2 * S];              // values 16 i + 4 h .. + 3 of the lane's row
+    float m[NT], c[NT], l[NT];       // as wave_state's
+    bool stale;
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 2 * S; ++i) o[n][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            m[n] = -__builtin_inff();
+            c[n] = l[n] = 0.0f;
+        }
+        stale = true;
+    }
+    __device__ __forceinline__ void load_query(int n, const uint16_t* row, int D) {
+        const int h = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            const int d = 32 * t + 8 * h;
+            q[n][t] = d < D ? *(const u32x4*)(row + d) : u32x4{0, 0, 0, 0};
+        }
+    }
+    // (waits for the queries here: see wave_state)
+    __device__ __forceinline__ void query_is_here() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < S; ++t) asm volatile("" : "+v"(q[n][t]));
+    }
+
+    // S^T of a record: score r belongs to key 4 h + r
+    __device__ __forceinline__ void scores(const char* record, f32x4 (&s)[NT]) const {
+        const int lane = threadIdx.x & 63, h = lane >> 4;
+        uint32_t k[S], scale[2 * S];
+        read_words(record + lane * 4 * S, k);
+        read_words(record + 512 * S + h * 8 * S, scale);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            const uint32_t first = firsts(k[t]), second = seconds(k[t]);
+            const u32x4 x = {codes16<ACT, false>(first), codes16<ACT, true>(first), codes16<ACT, false>(second), codes16<ACT, true>(second)};
+            const float by[4] = {half_of<ACT, 0>(scale[2 * t]), half_of<ACT, 1>(scale[2 * t]), half_of<ACT, 0>(scale[2 * t + 1]), half_of<ACT, 1>(scale[2 * t + 1])};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const f32x4 y = mfma16<ACT>(x, q[n][t], f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[n][r] = __builtin_fmaf(y[r], by[r], s[n][r]);
+            }
+        }
+    }
+
+    // Sums of more than 2^30 made relative to as much more (see wave_state)
+    __device__ __forceinline__ void level(int n) {
+        const float most = row_max(l[n]);
+        if (!__any(most > 0x1p30f)) return;
+        const float by = m[n] + (float)__builtin_amdgcn_frexp_expf(most) - m[n];
+        const float half = m[n] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(-0.5f * by);
+        if (m[n] != -__builtin_inff()) c[n] = m[n] += by;
+        l[n] = l[n] * half * half;
+#pragma unroll
+        for (int i = 0; i < 2 * S; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[n][i][r] = o[n][i][r] * half * half;
+    }
+
+    // Numerators of the scores of two records in place; maximum, sum and results brought along (see wave_state)
+    __device__ __forceinline__ void soften(f32x4 (&s)[2][NT], float factor) {
+        bool large = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (ACT == FQ_F16 || stale) {
+                if (ACT == FQ_BF16) level(n);
+                float top = s[0][n][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = __builtin_fmaxf(top, s[i >> 2][n][i & 3]);
+                top = row_max(top) * factor - LARGER;
+                if (__any(top > m[n] + 8.0f)) {
+                    const float now = __builtin_fmaxf(m[n], top), next = now == -__builtin_inff() ? 0.0f : now;
+                    const float again = __builtin_amdgcn_exp2f(m[n] - next);
+                    m[n] = now;
+                    c[n] = next;
+                    l[n] *= again;
+#pragma unroll
+                    for (int i = 0; i < 2 * S; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[n][i][r] *= again;
+                }
+            }
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][n][i & 3], factor, -c[n]));
+                s[i >> 2][n][i & 3] = x;
+                sum += x;
+            }
+            l[n] += sum;
+            large = large || sum > 0x1p58f || m[n] == -__builtin_inff();
+        }
+        if (ACT == FQ_BF16) stale = __any(large);
+    }
+
+    // O^T += V^T P^T over two records, of whose values the first `there` are keys
+    __device__ __forceinline__ void accumulate(const char* record0, const char* record1, const f32x4 (&p)[2][NT], bool tail, int there) {
+        const int lane = threadIdx.x & 63, h = lane >> 4;
+        const char* record[2] = {record0, record1};
+        uint32_t v[2][S], scale[2][2 * S];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            read_words(record[u] + 256 * S + lane * 4 * S, v[u]);
+            read_words(record[u] + 544 * S + h * 8 * S, scale[u]);
+        }
+        if (tail) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int count = there - 16 * u - 4 * h;
+#pragma unroll
+                for (int g = 0; g < S; ++g) {
+                    scale[u][2 * g] &= first_mask(count);
+                    scale[u][2 * g + 1] &= first_mask(count - 2);
+                }
+            }
+        }
+        u32x4 x[NT];
+        auto pack = [&](int g) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float a = p[u][n][2 * i], b = p[u][n][2 * i + 1];
+                        if constexpr (ACT == FQ_BF16) {
+                            a *= half_of<ACT, 0>(scale[u][2 * g + i]);
+                            b *= half_of<ACT, 1>(scale[u][2 * g + i]);
+                        }
+                        x[n][2 * u + i] = pack2<ACT>(a, b);
+                    }
+        };
+        if (ACT == FQ_F16) pack(0);
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+            if (ACT == FQ_BF16) pack(j);
+            u32x4 first, second;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t f = firsts(v[u][j]), g = seconds(v[u][j]);
+                first[2 * u] = codes16<ACT, false>(f);
+                first[2 * u + 1] = codes16<ACT, true>(f);
+                second[2 * u] = codes16<ACT, false>(g);
+                second[2 * u + 1] = codes16<ACT, true>(g);
+                if constexpr (ACT == FQ_F16) {
+                    first[2 * u] = times16(first[2 * u], scale[u][2 * j]);
+                    first[2 * u + 1] = times16(first[2 * u + 1], scale[u][2 * j + 1]);
+                    second[2 * u] = times16(second[2 * u], scale[u][2 * j]);
+                    second[2 * u + 1] = times16(second[2 * u + 1], scale[u][2 * j + 1]);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                o[n][2 * j] = mfma16<ACT>(first, x[n], o[n][2 * j]);
+                o[n][2 * j + 1] = mfma16<ACT>(second, x[n], o[n][2 * j + 1]);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void finish() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (ACT == FQ_BF16) level(n);
+            l[n] = row_sum(l[n]);
+        }
+    }
+    __device__ __forceinline__ bool sound() const {
+        float x = 0.0f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            x = __builtin_fmaf(l[n], 0.0f, x);
+            if (!(l[n] >= 0.25f || m[n] == -__builtin_inff())) x = 1.0f;
+#pragma unroll
+            for (int i = 0; i < 2 * S; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x = __builtin_fmaf(o[n][i][r], 0.0f, x);
+        }
+        return __all(x == 0.0f);
+    }
+};
+
+// Four waves of a block share a unit's keys out, 32 at a time, and join their sums through LDS at the end of a piece.  A wave's ring has RING times
+// two records, all but one of them on their way while that one is used.
+template <int ACT, int S, int NT>
+__global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree_args a, tree_plan p, divisor by_records) {
+    constexpr int BYTES = record_bytes(S), RING = 4, STEP = 2 * BYTES, WAVE_BYTES = RING * STEP;
+    constexpr int LOADS = 2 * record_loads<S>::COUNT;
+    constexpr int TILE = 128, QUADS = 8 * S;             // keys of the block; fours of a row's values
+    constexpr int TURN = QUADS == 24 || QUADS == 8 ? 7 : 15;
+    static_assert(NT * 16 * QUADS * 16 <= WAVE_BYTES, "the sums of a wave fit its ring");
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4;
+    int32_t* entries = (int32_t*)(lds + 4 * WAVE_BYTES) + wave * (TABLE / 4);
+    float* stats = (float*)(lds + 4 * WAVE_BYTES + TABLE * 4);       // [4][32][2], and a flag
+    const int D = a.head_dim;
+    char* mine = lds + wave * WAVE_BYTES;
+    const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+
+    const line all(a, p);
+    const int64_t begin = blockIdx.x * all.per_block, stop = min(all.total, begin + all.per_block);
+    if (begin >= stop) return;
+    int b;
+    int64_t at_b;
+    all.find(begin, &b, &at_b);
+    int context = all.context(b), tiles = tiles_of(a, p, context);
+    int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
+    few_rows<ACT, S, NT> w;
+
+    for (int64_t pos = begin; pos < stop;) {
+        const unit_rows<kv4_rows> rows(a, p, b, u, 0, context);
+        const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, 0);
+        const int key0 = t0 * TILE, key1 = p.whole ? rows.keys : min(rows.keys, t1 * TILE);
+        int row[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            row[n] = min(16 * n + (lane & 15), rows.count - 1);
+            w.load_query(n, rows.query(row[n]), D);
+        }
+        w.clear();
+        const int most = part_keys(TABLE / 4, a.cache.page_size, TILE);
+        for (int part = key0, part_end; part < key1; part = part_end) {
+            part_end = fqa::part_end(part, key1, most);
+            const table_part table = load_table<64>(a, b, part, part_end, entries);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the wave's own: no barrier)
+            w.query_is_here();                          // (with the table)
+            const record_places places = {entries, table.first, by_records, a.cache.page_size / RECORD,
+                                          (const char*)a.cache.k + rows.head * a.cache.head_stride, a.cache.page_stride};
+            const int last = (part_end - 1) / RECORD;
+            const int base0 = part + wave * 32, steps = base0 < part_end ? (part_end - base0 + TILE - 1) / TILE : 0;
+            auto load = [&](int i) {
+                const int r = (base0 + i * TILE) / RECORD;
+                const uint32_t to = mine_at + (uint32_t)(i % RING) * STEP;
+                record_loads<S>::issue(to, places.template place<BYTES>(r));
+                record_loads<S>::issue(to + BYTES, places.template place<BYTES>(min(r + 1, last)));       // (no record behind the last)
+            };
+            for (int i = 0; i < min(steps, RING - 1); ++i) load(i);
+            for (int i = 0; i < steps; ++i) {
+                const int base = base0 + i * TILE;
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (what was read from the records that these loads replace is here)
+                if (i + RING - 1 < steps) {
+                    load(i + RING - 1);
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * LOADS) : "memory");
+                } else {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                }
+                const char* at = mine + (i % RING) * STEP;
+                f32x4 s[2][NT];
+                w.scores(at, s[0]);
+                w.scores(at + BYTES, s[1]);
+                if (base + 32 > min(rows.context, part_end)) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint32_t seen = rows.seen(row[n], base) >> 4 * h;
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) s[x >> 2][n][x & 3] = seen >> (16 * (x >> 2) + (x & 3)) & 1 ? s[x >> 2][n][x & 3] : -__builtin_inff();
+                    }
+                }
+                w.soften(s, p.factor);
+                w.accumulate(at, at + BYTES, s, base + 32 > part_end, part_end - base);
+            }
+        }
+        w.finish();
+        // the waves' sums, joined
+        __syncthreads();
+        if (threadIdx.x == 0) stats[256] = 0.0f;
+        __syncthreads();
+        if (!w.sound() && lane == 0) stats[256] = 1.0f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = 16 * n + (lane & 15);
+            if (h == 0) {
+                stats[(wave * 32 + r) * 2] = w.m[n];
+                stats[(wave * 32 + r) * 2 + 1] = w.l[n];
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * S; ++i) *(f32x4*)((float*)mine + r * 4 * QUADS + ((4 * i + h) ^ (r & TURN)) * 4) = w.o[n][i];
+        }
+        __syncthreads();
+        if (stats[256] != 0.0f) {
+            rows.template one_by_one<ACT>(key0, key1, slot, wave, rows.count, 4);
+        } else {
+            for (int x = threadIdx.x; x < rows.count * QUADS; x += 256) {
+                const int r = x / QUADS, quad = x % QUADS, d = quad * 4;
+                if (d >= D) continue;
+                float c = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) c = __builtin_fmaxf(c, stats[(y * 32 + r) * 2]);
+                const float from = c == -__builtin_inff() ? 0.0f : c;
+                f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const float weight = __builtin_amdgcn_exp2f(stats[(y * 32 + r) * 2] - from);
+                    const f32x4 z = *(const f32x4*)((const float*)(lds + y * WAVE_BYTES) + r * 4 * QUADS + (quad ^ (r & TURN)) * 4);
+                    l += weight * stats[(y * 32 + r) * 2 + 1];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
+                }
+                if (!slot) {
+                    const float scale = inverse(l, [&] { return rows.sees_any(r); });
+                    *(u32x2*)(rows.result(r) + d) = u32x2{pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+                } else {
+                    *(f32x4*)(slot + p.shape().at(r, d)) = o;
+                    if (d == 0) p.shape().put_stats(slot, r, c, l);
+                }
+            }
+        }
+        __syncthreads();
+        pos += t1 - t0;
+        t0 = 0;
+        if (++u == all.units) {
+            u = 0;
+            if (++b < a.sequences) context = all.context(b), tiles = tiles_of(a, p, context);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ above 32 rows
+// A word's eight codes times scales, exactly: first codes of bytes 0, 1 and 2, 3, second codes of the same (low, high: the scales of bytes 0, 1
+// and 2, 3)
+template <int ACT>
+__device__ __forceinline__ u32x4 words16(uint32_t x, uint32_t low, uint32_t high) {
+    const uint32_t f = firsts(x), g = seconds(x);
+    u32x4 y = {codes16<ACT, false>(f), codes16<ACT, true>(f), codes16<ACT, false>(g), codes16<ACT, true>(g)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t scale = i & 1 ? high : low;
+        if constexpr (ACT == FQ_F16) y[i] = times16(y[i], scale);
+        else y[i] = pack2<ACT>(half_of<ACT, 0>(y[i]) * half_of<ACT, 0>(scale), half_of<ACT, 1>(y[i]) * half_of<ACT, 1>(scale));
+    }
+    return y;
+}
+
+// O^T += V^T P^T over H half-tiles of values that lie as [value][key]
+template <int H, int PITCH, int ACT, int DP>
+__device__ __forceinline__ void accumulate(wave_state<ACT, DP>& w, const char* values, const u32x4 (&p)[2 * H]) {
+    const int lane = threadIdx.x & 63;
+    const char* mine = values + (lane & 31) * PITCH + (lane >> 5) * 8;
+#pragma unroll
+    for (int k = 0; k < 2 * H; ++k)
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) {
+            const char* at = mine + 32 * t * PITCH + 32 * k;
+            const u32x2 x = *(const u32x2*)at, y = *(const u32x2*)(at + 16);
+            w.o[t] = mfma32<ACT>(u32x4{x[0], x[1], y[0], y[1]}, p[k], w.o[t]);
+        }
+}
+
+// GROUPS x 32 rows a block, as over a cache of 16 bits.  Every wave brings in one record of the four of a tile, RING of them on their way, and
+// takes it to 16 bits.  Keys lie as wave_state takes them; values as [value][key], rows 8 bytes longer than 64 keys so that a read's
+// 32 rows fall on different banks.
+template <int ACT, int S, int GROUPS>
+__global__ __launch_bounds__(256, 2) void fq_attention_kv4_tile_kernel(fq_tree_args a, tree_plan p, divisor by_records) {
+    constexpr int DP = S < 2 ? 64 : 32 * S, BYTES = record_bytes(S), RING = 3, LOADS = record_loads<S>::COUNT;
+    typedef tile_shape<DP> SH;
+    constexpr int KEY_BYTES = 2 * SH::BYTES, PITCH = 2 * KEYS + 8, VALUE_BYTES = DP * PITCH;
+    constexpr int JOIN = 32 * DP * 4, PARTS = 4 / GROUPS, HALVES = 2 / PARTS;
+    constexpr int ALL = KEY_BYTES + VALUE_BYTES + 4 * RING * BYTES, ROOM = PARTS > 1 && 4 * JOIN > ALL ? 4 * JOIN : ALL;
+    extern __shared__ __align__(16) char lds[];
+    int32_t* entries = (int32_t*)(lds + ROOM);
+    float* stats = (float*)(entries + TABLE);           // [4][32][2], and a flag
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4, x16 = lane & 15;
+    const int group = wave % GROUPS, part_of = wave / GROUPS;
+    const int D = a.head_dim;
+    char *keys = lds, *values = lds + KEY_BYTES, *mine = lds + KEY_BYTES + VALUE_BYTES + wave * RING * BYTES;
+    const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+
+    const line all(a, p);
+    const int64_t block = p.in_line(blockIdx.x), begin = block * all.per_block, stop = min(all.total, begin + all.per_block);
+    if (begin >= stop) return;
+    int b;
+    int64_t at_b;
+    all.find(begin, &b, &at_b);
+    int context = all.context(b), tiles = tiles_of(a, p, context);
+    int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
+    wave_state<ACT, DP> w;
+
+    for (int64_t pos = begin; pos < stop;) {
+        const unit_rows<kv4_rows> rows(a, p, b, u, 0, context);
+        const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(block, pos == begin, 0);
+        const int key0 = t0 * KEYS, key1 = p.whole ? rows.keys : min(rows.keys, t1 * KEYS);
+        const int r = group * 32 + (lane & 31), row = min(r, rows.count - 1);
+        const bool busy = group * 32 < rows.count;
+        w.load_query(rows.query(row), D);
+        w.clear();
+        const int most = part_keys(TABLE, a.cache.page_size, KEYS);
+        for (int part = key0, part_end; part < key1; part = part_end) {
+            part_end = fqa::part_end(part, key1, most);
+            __syncthreads();
+            const table_part table = load_table<256>(a, b, part, part_end, entries);
+            if (32 * S < DP) {                          // values that no record has: zeros
+                const u32x4 zero = {0, 0, 0, 0};
+                for (int x = threadIdx.x; x < (KEY_BYTES + VALUE_BYTES) / 16; x += 256) ((u32x4*)lds)[x] = zero;
+            }
+            __syncthreads();
+            w.query_is_here();                          // (with the table)
+            const record_places places = {entries, table.first, by_records, a.cache.page_size / RECORD,
+                                          (const char*)a.cache.k + rows.head * a.cache.head_stride, a.cache.page_stride};
+            const int last = (part_end - 1) / RECORD, steps = (part_end - part + KEYS - 1) / KEYS;
+            auto load = [&](int i) {
+                record_loads<S>::issue(mine_at + (uint32_t)(i % RING) * BYTES, places.template place<BYTES>(min((part + i * KEYS) / RECORD + wave, last)));
+            };
+            for (int i = 0; i < min(steps, RING); ++i) load(i);
+            for (int i = 0; i < steps; ++i) {
+                const int base = part + i * KEYS;
+                if (i + RING - 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * LOADS) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                const char* from = mine + (i % RING) * BYTES;
+                uint32_t k[S], v[S], key_scale[S], value_scale[2 * S];
+                read_words(from + lane * 4 * S, k);
+                read_words(from + 256 * S + lane * 4 * S, v);
+                read_words(from + 544 * S + h * 8 * S, value_scale);
+#pragma unroll
+                for (int t = 0; t < S; ++t) key_scale[t] = *(const uint16_t*)(from + scale_at(S, x16, t));
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (i + RING < steps) load(i + RING);
+                if (base + KEYS > part_end) {           // what lies behind the last key may be anything
+                    const int count = part_end - base - 16 * wave - 4 * h;
+#pragma unroll
+                    for (int g = 0; g < S; ++g) {
+                        value_scale[2 * g] &= first_mask(count);
+                        value_scale[2 * g + 1] &= first_mask(count - 2);
+                    }
+                }
+                __syncthreads();                        // (the tile before has been read)
+                const int key = 16 * (wave & 1) + x16;
+#pragma unroll
+                for (int t = 0; t < S; ++t) {
+                    const uint32_t both = key_scale[t] * 0x10001u;
+                    u32x4 x = words16<ACT>(k[t], both, both);
+                    *(u32x4*)(keys + (wave >> 1) * SH::BYTES + key * SH::PITCH + key_unit<SH::UNITS>(key, 4 * t + h) * 16) = x;
+                    x = words16<ACT>(v[t], value_scale[2 * t], value_scale[2 * t + 1]);
+                    char* to = values + (32 * t + x16) * PITCH + (16 * wave + 4 * h) * 2;
+                    *(u32x2*)to = u32x2{x[0], x[1]};
+                    *(u32x2*)(to + 16 * PITCH) = u32x2{x[2], x[3]};
+                }
+                __syncthreads();
+                if (!busy) continue;
+                const int first = base + part_of * HALF;
+                f32x16 s[HALVES];
+                u32x4 x[2 * HALVES];
+                w.template scores<HALVES>(keys + part_of * SH::BYTES, s);
+                if (first + HALVES * HALF > min(rows.context, part_end)) {
+#pragma unroll
+                    for (int y = 0; y < HALVES; ++y) keep_seen(s[y], rows.seen(row, first + y * HALF));
+                }
+                w.template soften<HALVES>(s, p.factor, x);
+                accumulate<HALVES, PITCH>(w, values + part_of * HALF * 2, x);
+            }
+        }
+        w.finish(PARTS > 1 || slot);
+        if constexpr (PARTS > 1) {
+            join_parts<ACT, DP, PARTS>(rows, w, lds, JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
+        } else {
+            if (!w.sound()) rows.template one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
+            else if (r < rows.count) w.put(rows.result(r), slot, p.shape(), r, [&] { return rows.sees_any(r); });
+        }
+        pos += t1 - t0;
+        t0 = 0;
+        if (++u == all.units) {
+            u = 0;
+            if (++b < a.sequences) context = all.context(b), tiles = tiles_of(a, p, context);
+        }
+    }
+}
+
+template <int ACT, int S, int NT>
+int launch_stream(const fq_tree_args& a, const tree_plan& p, const divisor& by_records, hipStream_t stream) {
+    static std::atomic<uint64_t> raised{0};
+    const int st = fqd::raise_lds_limit((const void*)fq_attention_kv4_stream_kernel<ACT, S, NT>, raised);
+    if (st != FQ_OK) return st;
+    fq_attention_kv4_stream_kernel<ACT, S, NT><<<(unsigned)p.blocks, 256, 32 * record_bytes(S) + TABLE * 4 + 257 * 4, stream>>>(a, p, by_records);
+    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
+template <int ACT, int S, int GROUPS>
+int launch_tiles(const fq_tree_args& a, const tree_plan& p, const divisor& by_records, hipStream_t stream) {
+    constexpr int DP = S < 2 ? 64 : 32 * S, ALL = 2 * tile_shape<DP>::BYTES + DP * (2 * KEYS + 8) + 12 * record_bytes(S), JOIN = 4 * 32 * DP * 4;
+    static std::atomic<uint64_t> raised{0};
+    const int st = fqd::raise_lds_limit((const void*)fq_attention_kv4_tile_kernel<ACT, S, GROUPS>, raised);
+    if (st != FQ_OK) return st;
+    const int room = GROUPS < 4 && JOIN > ALL ? JOIN : ALL;
+    fq_attention_kv4_tile_kernel<ACT, S, GROUPS><<<(unsigned)p.blocks, 256, room + TABLE * 4 + 257 * 4, stream>>>(a, p, by_records);
+    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+}
+
+template <int ACT, int S>
+int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
+    const divisor by_records = divisor::of((uint32_t)(a.cache.page_size / RECORD));
+    const int st = p.unit_rows > 64 ? launch_tiles<ACT, S, 4>(a, p, by_records, stream)
+                   : p.rows > 32    ? launch_tiles<ACT, S, 2>(a, p, by_records, stream)
+                   : p.rows > 16    ? launch_stream<ACT, S, 2>(a, p, by_records, stream)
+                                    : launch_stream<ACT, S, 1>(a, p, by_records, stream);
+    if (st != FQ_OK || p.whole) return st;
+    return launch_join<ACT, kv4_rows>(a, p, stream);
+}
+
+template <int ACT>
+int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
+    switch (groups_of(a.head_dim)) {
+        case 1: return launch<ACT, 1>(a, p, stream);
+        case 2: return launch<ACT, 2>(a, p, stream);
+        case 3: return launch<ACT, 3>(a, p, stream);
+        default: return launch<ACT, 4>(a, p, stream);
+    }
+}
+
+}  // namespace
+
+size_t fq_tree_kv4_bytes(const fq_tree_args& a) { return slots_bytes(plan_units(a, 1)); }
+
+int fq_launch_attention_tree_kv4(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream) {
+    tree_plan p = plan_units(a, 1);
+    p.slots = (float*)workspace;
+    return act_dtype == FQ_F16 ? launch<FQ_F16>(a, p, stream) : launch<FQ_BF16>(a, p, stream);
+}

@@ -176,4 +176,19 @@ bool fq_tree_fits(const fq_tree_args& a);        // whether its rows can be coun
 size_t fq_tree_bytes(const fq_tree_args& a);
 int fq_launch_attention_tree(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream);
 
+// a cache held in 4 bits (fq_kv4.h)
+struct fq_kv4_args {
+    fq_heads k, v;                   // written from
+    void *k_out, *v_out;             // read to
+    int64_t tokens;
+    int kv_heads, head_dim, groups;  // groups: ceil(head_dim / 32)
+    fq_kv4_pages cache;
+    const int64_t* slots;
+};
+int fq_launch_kv4_write(int act_dtype, const fq_kv4_args& a, hipStream_t stream);
+int fq_launch_kv4_read(int act_dtype, const fq_kv4_args& a, hipStream_t stream);
+// (a.cache: k the pages, page_stride and head_stride in bytes)
+size_t fq_tree_kv4_bytes(const fq_tree_args& a);
+int fq_launch_attention_tree_kv4(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream);
+
 #endif  // FQ_INTERNAL_H_

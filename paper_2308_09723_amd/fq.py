@@ -39,6 +39,11 @@ class KvPages(ctypes.Structure):
                 ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
+class Kv4Pages(ctypes.Structure):
+    """fq_kv4_pages: a cache held in 4 bits, page_stride in bytes."""
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int), ("page_stride", ctypes.c_int64)]
+
+
 class FqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -104,6 +109,12 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "fq_attention_tree_workspace_bytes": (sz, [i64, i64, i32, i32, i32, i64, i32]),
         "fq_attention_tree": (i32, [ctypes.POINTER(Heads), i32, i64, i64, i32, i32, i32, ctypes.POINTER(KvPages), vp, i64, vp, vp,
                                     i64, f32, vp, vp, sz, vp]),
+        "fq_kv4_page_bytes": (sz, [i32, i32, i32]),
+        "fq_kv4_write": (i32, [ctypes.POINTER(Heads), ctypes.POINTER(Heads), i32, i64, i32, i32, ctypes.POINTER(Kv4Pages), vp, vp]),
+        "fq_kv4_read": (i32, [ctypes.POINTER(Kv4Pages), i32, i64, i32, i32, vp, vp, vp, vp]),
+        "fq_attention_tree_kv4_workspace_bytes": (sz, [i64, i64, i32, i32, i32, i64, i32]),
+        "fq_attention_tree_kv4": (i32, [ctypes.POINTER(Heads), i32, i64, i64, i32, i32, i32, ctypes.POINTER(Kv4Pages), vp, i64, vp, vp,
+                                        i64, f32, vp, vp, sz, vp]),
         "fq_status_string": (ctypes.c_char_p, [i32]),
         "fq_version": (ctypes.c_char_p, []),
     }
@@ -125,7 +136,8 @@ EXPORTED = [
     "fq_mfma_rate_probe_operand_bytes", "fq_mfma_rate_probe_sink_bytes", "fq_mfma_rate_probe_flops", "fq_mfma_rate_probe",
     "fq_zscale_bytes", "fq_unpack_w4a8", "fq_quantize_w4a8", "fq_quantize_act_i8", "fq_gemm_w4a8_workspace_bytes", "fq_gemm_w4a8",
     "fq_qk_norm_rope", "fq_attention_prompt_workspace_bytes", "fq_attention_prompt", "fq_attention_tree_workspace_bytes",
-    "fq_attention_tree",
+    "fq_attention_tree", "fq_kv4_page_bytes", "fq_kv4_write", "fq_kv4_read", "fq_attention_tree_kv4_workspace_bytes",
+    "fq_attention_tree_kv4",
 ]
 
 
@@ -343,6 +355,31 @@ def attention_tree_raw(q, act_dtype, sequences, nodes, q_heads, kv_heads, head_d
     return int(load().fq_attention_tree(q, act_dtype, sequences, nodes, q_heads, kv_heads, head_dim, cache, page_table_ptr,
                                         table_width, context_lens_ptr, mask_ptr, mask_stride, scale, out_ptr, ws_ptr, ws_bytes,
                                         stream))
+
+
+def kv4_page_bytes(page_size, kv_heads, head_dim):
+    return int(load().fq_kv4_page_bytes(page_size, kv_heads, head_dim))
+
+
+def kv4_write_raw(k, v, act_dtype, tokens, kv_heads, head_dim, cache, slots_ptr, stream=0):
+    """k, v: Heads; cache: Kv4Pages."""
+    return int(load().fq_kv4_write(k, v, act_dtype, tokens, kv_heads, head_dim, cache, slots_ptr, stream))
+
+
+def kv4_read_raw(cache, act_dtype, tokens, kv_heads, head_dim, slots_ptr, k_out_ptr, v_out_ptr, stream=0):
+    return int(load().fq_kv4_read(cache, act_dtype, tokens, kv_heads, head_dim, slots_ptr, k_out_ptr, v_out_ptr, stream))
+
+
+def attention_tree_kv4_workspace_bytes(sequences, nodes, q_heads, kv_heads, head_dim, table_width, page_size):
+    return int(load().fq_attention_tree_kv4_workspace_bytes(sequences, nodes, q_heads, kv_heads, head_dim, table_width, page_size))
+
+
+def attention_tree_kv4_raw(q, act_dtype, sequences, nodes, q_heads, kv_heads, head_dim, cache, page_table_ptr, table_width,
+                           context_lens_ptr, mask_ptr, mask_stride, scale, out_ptr, ws_ptr=None, ws_bytes=0, stream=0):
+    """q: Heads; cache: Kv4Pages."""
+    return int(load().fq_attention_tree_kv4(q, act_dtype, sequences, nodes, q_heads, kv_heads, head_dim, cache, page_table_ptr,
+                                            table_width, context_lens_ptr, mask_ptr, mask_stride, scale, out_ptr, ws_ptr, ws_bytes,
+                                            stream))
 
 
 # ------------------------------------------------------------------ torch-tensor conveniences
@@ -748,6 +785,31 @@ def attention_prompt(q, k, v, q_offsets, k_offsets=None, scale=None, out=None, w
     return o
 
 
+def _drafted(q, where):
+    """Type, sizes and row stride of the drafted tokens' queries [sequences, nodes, heads, head_dim]."""
+    act = _act_code(q)
+    _require(q.is_cuda and q.dim() == 4 and (q.stride(3) == 1 or q.shape[3] <= 1), where)
+    sequences, nodes, heads, D = q.shape
+    row = 0 if sequences * nodes <= 1 else q.stride(0) if nodes == 1 else q.stride(1)      # (of one token, or one sequence, the stride says nothing)
+    _require(q.stride(0) == nodes * row or sequences <= 1, where)
+    return act, sequences, nodes, heads, D, row
+
+
+def _tree_of(q, page_table, context_lens, mask, where):
+    """The stride of the sequences' masks, having looked at tables, lengths and masks."""
+    torch = _torch_mod or _torch()
+    sequences, nodes = q.shape[:2]
+    _require(page_table.dim() == 2 and page_table.shape[0] == sequences and context_lens.numel() == sequences, where)
+    _plain(page_table, torch.int32, q.device, where)
+    _plain(context_lens, torch.int32, q.device, where)
+    if mask is None:
+        return 0
+    words = (nodes + 63) // 64
+    _plain(mask, torch.int64, q.device, where)
+    _require(tuple(mask.shape) in ((nodes, words), (sequences, nodes, words)), where)
+    return nodes * words if mask.dim() == 3 else 0
+
+
 def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, scale=None, out=None, workspace=None):
     """Attention of drafted tokens over a paged cache: q cuda [sequences, nodes, heads, head_dim] (float16 or bfloat16; the tokens of all
     sequences evenly apart), caches [pages, page_size, kv_heads, head_dim], page_table int32 [sequences, width], context_lens int32 [sequences]
@@ -759,22 +821,10 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
     if done is not None:
         return done
     where = "fq_attention_tree"
-    act = _act_code(q)
-    _require(q.is_cuda and q.dim() == 4 and (q.stride(3) == 1 or q.shape[3] <= 1), where)
-    sequences, nodes, heads, D = q.shape
-    row = 0 if sequences * nodes <= 1 else q.stride(0) if nodes == 1 else q.stride(1)      # (of one token, or one sequence, the stride says nothing)
-    _require(q.stride(0) == nodes * row or sequences <= 1, where)
+    act, sequences, nodes, heads, D, row = _drafted(q, where)
     kv_heads = k_cache.shape[2] if k_cache.dim() == 4 else 0
     cache = _pages(k_cache, v_cache, q, kv_heads, D, where)
-    _require(page_table.dim() == 2 and page_table.shape[0] == sequences and context_lens.numel() == sequences, where)
-    _plain(page_table, torch.int32, q.device, where)
-    _plain(context_lens, torch.int32, q.device, where)
-    stride = 0
-    if mask is not None:
-        words = (nodes + 63) // 64
-        _plain(mask, torch.int64, q.device, where)
-        _require(tuple(mask.shape) in ((nodes, words), (sequences, nodes, words)), where)
-        stride = nodes * words if mask.dim() == 3 else 0
+    stride = _tree_of(q, page_table, context_lens, mask, where)
     scale = _given_scale(scale, where)
     o = _output(out, (sequences, nodes, heads, D), q, where)
     width, page = page_table.shape[1], k_cache.shape[1]
@@ -782,4 +832,75 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
     _check(attention_tree_raw(Heads(q.data_ptr(), row, q.stride(2)), act, sequences, nodes, heads, kv_heads, D, cache,
                               page_table.data_ptr(), width, context_lens.data_ptr(), None if mask is None else mask.data_ptr(), stride,
                               scale, o.data_ptr(), workspace.data_ptr() if size else None, size, _stream()), where)
+    return o
+
+
+# ------------------------------------------------------------------ a cache held in 4 bits
+def kv4_cache(pages, page_size, kv_heads, head_dim, device="cuda"):
+    """Pages of a cache held in 4 bits: uint8 [pages, kv4_page_bytes(...)], zeros (which stand for zeros)."""
+    torch = _torch_mod or _torch()
+    size = kv4_page_bytes(page_size, kv_heads, head_dim)
+    if size == 0:
+        raise FqError(FQ_ERR_UNSUPPORTED, "fq_kv4_page_bytes")
+    return torch.zeros((pages, size), dtype=torch.uint8, device=device)
+
+
+def _kv4_pages(cache, page_size, kv_heads, head_dim, device, where):
+    """Kv4Pages of a tensor [pages, bytes] whose pages are whole."""
+    torch = _torch_mod or _torch()
+    _require(cache.is_cuda and cache.dim() == 2 and cache.dtype == torch.uint8 and cache.device == device and cache.stride(1) == 1, where)
+    size = kv4_page_bytes(page_size, kv_heads, head_dim)
+    if size == 0:
+        raise FqError(FQ_ERR_UNSUPPORTED, where)
+    _require(cache.shape[1] == size, where)
+    return Kv4Pages(cache.data_ptr(), cache.shape[0], page_size, cache.stride(0))
+
+
+def kv4_write(k, v, cache, page_size, slots):
+    """Keys and values into a cache held in 4 bits: k, v cuda [tokens, kv_heads, head_dim] (float16 or bfloat16, any row and head strides), cache
+    uint8 [pages, kv4_page_bytes(page_size, kv_heads, head_dim)] (kv4_cache), slots int64 [tokens] (slot s: place s % page_size of page
+    s // page_size; one outside the cache is not written)."""
+    torch = _torch_mod or _torch()
+    where = "fq_kv4_write"
+    act = _act_code(k)
+    hk, hv = _heads(k, where), _heads(v, where)
+    _require(v.shape == k.shape and v.dtype == k.dtype and v.device == k.device, where)
+    tokens, kv_heads, D = k.shape
+    pages = _kv4_pages(cache, page_size, kv_heads, D, k.device, where)
+    _require(slots.numel() == tokens, where)
+    _plain(slots, torch.int64, k.device, where)
+    _check(kv4_write_raw(hk, hv, act, tokens, kv_heads, D, pages, slots.data_ptr(), _stream()), where)
+
+
+def kv4_read(cache, page_size, kv_heads, head_dim, slots, dtype, k_out=None, v_out=None):
+    """What a cache held in 4 bits has in slots (int64 [tokens]; zeros for one outside it): (k, v), each [tokens, kv_heads, head_dim] of dtype, the
+    type that was written."""
+    torch = _torch_mod or _torch()
+    where = "fq_kv4_read"
+    pages = _kv4_pages(cache, page_size, kv_heads, head_dim, slots.device, where)
+    _plain(slots, torch.int64, cache.device, where)
+    like = torch.empty(0, dtype=dtype, device=cache.device) if k_out is None else k_out
+    act = _act_code(like)
+    _require(like.dtype == dtype and like.device == cache.device, where)
+    shape = (slots.numel(), kv_heads, head_dim)
+    k, v = _output(k_out, shape, like, where), _output(v_out, shape, like, where)
+    _check(kv4_read_raw(pages, act, shape[0], kv_heads, head_dim, slots.data_ptr(), k.data_ptr(), v.data_ptr(), _stream()), where)
+    return k, v
+
+
+def attention_tree_kv4(q, cache, page_size, kv_heads, page_table, context_lens, mask=None, scale=None, out=None, workspace=None):
+    """attention_tree over a cache held in 4 bits (kv4_cache, written by kv4_write as q's type): its arguments and result, with the cache's pages, their
+    size and their heads in the place of the caches.  workspace: attention_tree_kv4_workspace_bytes."""
+    where = "fq_attention_tree_kv4"
+    act, sequences, nodes, heads, D, row = _drafted(q, where)
+    pages = _kv4_pages(cache, page_size, kv_heads, D, q.device, where)
+    stride = _tree_of(q, page_table, context_lens, mask, where)
+    scale = _given_scale(scale, where)
+    o = _output(out, (sequences, nodes, heads, D), q, where)
+    width = page_table.shape[1]
+    need = attention_tree_kv4_workspace_bytes(sequences, nodes, heads, kv_heads, D, width, page_size)
+    workspace, size = _scratch(workspace, need, q, where)
+    _check(attention_tree_kv4_raw(Heads(q.data_ptr(), row, q.stride(2)), act, sequences, nodes, heads, kv_heads, D, pages,
+                                  page_table.data_ptr(), width, context_lens.data_ptr(), None if mask is None else mask.data_ptr(), stride,
+                                  scale, o.data_ptr(), workspace.data_ptr() if size else None, size, _stream()), where)
     return o
