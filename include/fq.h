@@ -467,6 +467,95 @@ int fq_attention_tree_kv4(const fq_heads* q, int act_dtype, int64_t sequences, i
                           void* stream);
 
 /*
+ * Pages that sequences share.  A pool of `pages` pages: refs[p] (device) is the number of rows that hold page p, a page with none (0 or less) is free; whoever keeps
+ * a page for something else sets its refs to 1.  A row of `table` [rows, width] (device) holds the pages of one sequence, its first
+ * ceil(lens[r] / page_size) entries (as many as width has; entries that are no page of the pool are kept and not counted).  Only a sequence's last page, where it is not full, is ever written
+ * to, so that full pages may be several rows'.  What the pages hold lies in buffers: any number of tensors with room for all pages each (layers;
+ * keys and values of fq_kv_pages, whose pages are contiguous; fq_kv4_pages).
+ * All of it happens on the device, so that a captured step may be replayed; free pages are taken in their order, the lowest first, so that results are the same
+ * every time.  Calls on one pool must be ordered on one stream.  Asynchronous, no allocation.
+ * Limits of the five: up to 8192 rows (and children, and rows to free), width up to 2^17, pages up to 2^31 - 1; refs, tables and lengths aligned to 4 bytes and not overlapping each other;
+ * buffers aligned to 16 bytes, with their strides and bytes of a page.
+ */
+typedef struct fq_page_buffer {
+    void* data;
+    int64_t count;       /* tensors, */
+    int64_t stride;      /* so many bytes apart */
+    int64_t page_stride; /* bytes from a page to the next one of a tensor */
+    int64_t page_bytes;  /* of a page, copied as they are */
+} fq_page_buffer;
+
+/*
+ * fq_pages_copy -- page from[m] (device) to page to[m] (device) of every tensor, for m below moves.  Pairs of which either is outside the pool (a negative one:
+ * nothing to do), or both are the same page, are left out.  No page that is written is named twice, nor read by another pair.
+ * Errors of these calls: FQ_ERR_INVALID_ARG, FQ_ERR_UNSUPPORTED (limits), FQ_ERR_WORKSPACE, FQ_ERR_HIP.
+ */
+int fq_pages_copy(const fq_page_buffer* buffers_host, int buffers, int64_t pages, const int32_t* from, const int32_t* to, int64_t moves,
+                  void* stream);
+
+/*
+ * fq_pages_take -- free pages for rows that are to grow from lens[r] to wanted[r] tokens: they go into the row's next entries and lens[r]
+ * becomes wanted[r].  Rows that want no more than they have, or more than width holds, or whose length is negative stay as they are.  Rows are served in
+ * their order: one that there are too few pages for, and all after it that need any, stay as they are, too (lens tells).
+ */
+int fq_pages_take(int32_t* refs, int64_t pages, int page_size, int32_t* table, int64_t rows, int64_t width, int32_t* lens, const int32_t* wanted,
+                  void* stream);
+
+/*
+ * fq_pages_fork -- `children` new rows, each a continuation of row parents[i] (device; one outside 0 .. rows - 1: an empty row): it shares its parent's
+ * full pages and gets a page of its own, a copy, in the place of one that is not full.  Entries behind a row's pages become -1, lens_out[i] its
+ * parent's length.  Children are served in their order; one that there is no page for, and all after it that need any, get length -1 and nothing.
+ * release != 0: the old rows are given up (beams go on as continuations of some of themselves): the first child of a row takes its last page over, without a
+ * copy, and pages that no row holds any more are free, for the children as well.
+ *   table, lens           in   [rows, width], [rows]; stay as they are (with release they hold pages no longer)
+ *   table_out, lens_out   out  [children, width], [children]; not over the inputs
+ *   buffers_host          what is copied in (none: nothing)
+ *   workspace             device scratch, >= fq_pages_fork_workspace_bytes(rows, children) bytes
+ */
+size_t fq_pages_fork_workspace_bytes(int64_t rows, int64_t children);
+int fq_pages_fork(int32_t* refs, int64_t pages, int page_size, const int32_t* table, int64_t rows, int64_t width, const int32_t* lens,
+                  const int32_t* parents, int64_t children, int release, int32_t* table_out, int32_t* lens_out,
+                  const fq_page_buffer* buffers_host, int buffers, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * fq_pages_free -- rows which[0 .. count - 1] (device; NULL: all rows) give their pages up: entries become -1, lengths 0.  A row that is named twice is freed
+ * once, one outside 0 .. rows - 1 not at all.
+ */
+int fq_pages_free(int32_t* refs, int64_t pages, int page_size, int32_t* table, int64_t rows, int64_t width, int32_t* lens, const int32_t* which,
+                  int64_t count, void* stream);
+
+/*
+ * fq_pages_compact -- gathers the pool's U used pages in pages 0 .. U - 1: those behind go into free ones before, both in their order; refs and the table's entries
+ * follow, and what the pages hold.  (A pool's rows must all be in the table.  What lay in the pages that become free stays there.)
+ *   workspace   device scratch, >= fq_pages_compact_workspace_bytes(pages) bytes
+ */
+size_t fq_pages_compact_workspace_bytes(int64_t pages);
+int fq_pages_compact(int32_t* refs, int64_t pages, int page_size, int32_t* table, int64_t rows, int64_t width, const int32_t* lens,
+                     const fq_page_buffer* buffers_host, int buffers, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * fq_adapters -- low-rank adapters of many requests, added to a product that they share (fq_gemm's): for every row m with adapter id = ids[m]
+ *   out[m, n] += scales[id] * sum_r (sum_k x[m, k] A[id, r, k]) B[id, n, r],
+ * sums in binary32; the inner ones enter the outer with 16 bits of precision (FQ_BF16) or 22 (FQ_F16: relative to the row's largest), the
+ * result is rounded once more.  Rows without an adapter (an id outside 0 .. adapters - 1, -1 say) stay as they are, and a row's result
+ * does not depend on other rows' adapters, not by an infinity or a NaN either.
+ *   x        in      [rows, K] act_dtype, rows x_stride elements apart
+ *   A, B     in      [adapters, rank, K] and [adapters, N, rank], act_dtype
+ *   ids      in      [rows] device.  Any order; rows of a request side by side are cheaper
+ *   scales   in      [adapters] device (NULL: 1)
+ *   out      in/out  [rows, N] act_dtype, rows out_stride elements apart; not over an input
+ *   workspace        device scratch, >= fq_adapters_workspace_bytes(rows, adapters, rank, N, K) bytes
+ * Limits: rank a multiple of 8 up to 128, N and K multiples of 8 up to 2^24, rows and adapters up to 2^20; pointers and strides aligned to
+ * 16 bytes.  rows = 0 or adapters = 0: a valid no-op.  Deterministic; asynchronous on `stream`, no allocation; ids and scales are read on the device when the
+ * kernels run.  Calls that share a workspace must be ordered on one stream.
+ * Errors: FQ_ERR_INVALID_ARG, FQ_ERR_UNSUPPORTED, FQ_ERR_WORKSPACE, FQ_ERR_HIP.
+ */
+size_t fq_adapters_workspace_bytes(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K);
+int fq_adapters(const void* x, int64_t x_stride, int act_dtype, int64_t rows, int64_t N, int64_t K, const void* A, const void* B, int64_t adapters,
+                int rank, const int32_t* ids, const float* scales, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                void* stream);
+
+/*
  * fq_gemm_describe -- writes a short text description of the kernel configuration fq_gemm
  * would use for this problem (kernel family, tile shape, block shape, split-K factor) into
  * buf (HOST memory, at most buf_bytes including the terminating 0).  For logs and benchmark

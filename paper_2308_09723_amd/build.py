@@ -29,6 +29,8 @@ SOURCES = [
     "fq_attn_tree.hip",
     "fq_kv4.hip",
     "fq_attn_kv4.hip",
+    "fq_pages.hip",
+    "fq_adapters.hip",
     "fq_gemm_f16_4.hip",
     "fq_gemm_f16_8.hip",
     "fq_gemm_bf16_4.hip",
@@ -71,7 +73,7 @@ NO_SPILL = [
 # (whose loads into LDS a wait for a reload would drain).
 NO_SPILL_FAMILIES = ["fq_gemm_mid_kernel", "fq_gemm_mid_items_kernel", "fq_w4a8_mid_kernel", "fq_attention_prompt_kernel",
                      "fq_attention_tree_stream_kernel", "fq_attention_tree_tile_kernel", "fq_attention_kv4_stream_kernel",
-                     "fq_attention_kv4_tile_kernel"]
+                     "fq_attention_kv4_tile_kernel", "fq_adapter_down_kernel", "fq_adapter_up_kernel"]
 
 
 def _run(cmd):

@@ -631,6 +631,191 @@ int fq_attention_tree_kv4(const fq_heads* q, int act_dtype, int64_t sequences, i
     return fq_launch_attention_tree_kv4(act_dtype, a, workspace, (hipStream_t)stream);
 }
 
+// ------------------------------------------------------------------------------------------ pages that sequences share
+static int check_buffers(const fq_page_buffer* b, int buffers, int64_t pages) {
+    if (buffers < 0 || (buffers > 0 && !b)) return FQ_ERR_INVALID_ARG;
+    for (int i = 0; i < buffers; ++i) {
+        if (!b[i].data || b[i].count < 0 || b[i].page_bytes <= 0 || b[i].stride < 0 || b[i].page_stride < 0) return FQ_ERR_INVALID_ARG;
+        if (pages > 1 && b[i].page_stride < b[i].page_bytes) return FQ_ERR_INVALID_ARG;
+        if (!aligned16(b[i].data) || b[i].page_bytes % 16 != 0 || b[i].page_stride % 16 != 0 || b[i].stride % 16 != 0) return FQ_ERR_UNSUPPORTED;
+        if (too_far(b[i].count, b[i].stride) || too_far(pages, b[i].page_stride) || b[i].count > 1 << 20 || b[i].page_bytes > (int64_t)1 << 32) return FQ_ERR_UNSUPPORTED;
+    }
+    return buffers > 1 << 16 ? FQ_ERR_UNSUPPORTED : FQ_OK;
+}
+
+// Whether memory that a call writes lies within the buffers (from their first byte to their last)
+static bool over_buffers(const void* p, size_t bytes, const fq_page_buffer* b, int buffers, int64_t pages) {
+    for (int i = 0; i < buffers; ++i)
+        if (b[i].count > 0 && pages > 0 &&
+            fq_overlaps(p, bytes, {{b[i].data, (size_t)((b[i].count - 1) * b[i].stride + (pages - 1) * b[i].page_stride + b[i].page_bytes)}}))
+            return true;
+    return false;
+}
+
+static bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+
+int fq_pages_copy(const fq_page_buffer* buffers_host, int buffers, int64_t pages, const int32_t* from, const int32_t* to, int64_t moves,
+                  void* stream) {
+    if (pages < 0 || moves < 0) return FQ_ERR_INVALID_ARG;
+    const int st = check_buffers(buffers_host, buffers, pages);
+    if (st != FQ_OK) return st;
+    if (pages > INT32_MAX || moves > INT32_MAX) return FQ_ERR_UNSUPPORTED;
+    if (moves == 0 || buffers == 0) return FQ_OK;
+    if (!from || !to) return FQ_ERR_INVALID_ARG;
+    if (!aligned4(from) || !aligned4(to)) return FQ_ERR_UNSUPPORTED;
+    if (over_buffers(from, (size_t)moves * 4, buffers_host, buffers, pages) || over_buffers(to, (size_t)moves * 4, buffers_host, buffers, pages))
+        return FQ_ERR_INVALID_ARG;
+    fq_copy_args a = {};
+    a.from = from;
+    a.to = to;
+    a.moves = moves;
+    a.pages = pages;
+    return fq_launch_pages_copy(buffers_host, buffers, a, (hipStream_t)stream);
+}
+
+// A pool of pages and a table of rows that hold them
+static int check_pool(const int32_t* refs, int64_t pages, int page_size, const int32_t* table, int64_t rows, int64_t width, const int32_t* lens) {
+    if (pages < 0 || page_size <= 0 || rows < 0 || width < 0) return FQ_ERR_INVALID_ARG;
+    if (pages > INT32_MAX || rows > FQ_MOST_PAGE_ROWS || width > 1 << 17) return FQ_ERR_UNSUPPORTED;
+    if ((pages > 0 && !refs) || (rows > 0 && (!lens || (width > 0 && !table)))) return FQ_ERR_INVALID_ARG;
+    if (!aligned4(refs) || !aligned4(table) || !aligned4(lens)) return FQ_ERR_UNSUPPORTED;
+    const size_t t = (size_t)(rows * width) * 4, l = (size_t)rows * 4;
+    if (fq_overlaps(refs, (size_t)pages * 4, {{table, t}, {lens, l}}) || fq_overlaps(table, t, {{lens, l}})) return FQ_ERR_INVALID_ARG;
+    return FQ_OK;
+}
+
+int fq_pages_take(int32_t* refs, int64_t pages, int page_size, int32_t* table, int64_t rows, int64_t width, int32_t* lens, const int32_t* wanted,
+                  void* stream) {
+    const int st = check_pool(refs, pages, page_size, table, rows, width, lens);
+    if (st != FQ_OK) return st;
+    if (rows == 0) return FQ_OK;
+    if (!wanted) return FQ_ERR_INVALID_ARG;
+    if (!aligned4(wanted)) return FQ_ERR_UNSUPPORTED;
+    const fq_span read = {wanted, (size_t)rows * 4};
+    if (fq_overlaps(refs, (size_t)pages * 4, {read}) || fq_overlaps(table, (size_t)(rows * width) * 4, {read}) || fq_overlaps(lens, (size_t)rows * 4, {read}))
+        return FQ_ERR_INVALID_ARG;
+    const fq_take_args a = {refs, pages, page_size, table, lens, wanted, (int)rows, width};
+    return fq_launch_pages_take(a, (hipStream_t)stream);
+}
+
+size_t fq_pages_fork_workspace_bytes(int64_t rows, int64_t children) {
+    if (rows < 0 || children < 0 || rows > FQ_MOST_PAGE_ROWS || children > FQ_MOST_PAGE_ROWS) return 0;
+    return (size_t)(rows + 2 * children + 1) * 4;
+}
+
+int fq_pages_fork(int32_t* refs, int64_t pages, int page_size, const int32_t* table, int64_t rows, int64_t width, const int32_t* lens,
+                  const int32_t* parents, int64_t children, int release, int32_t* table_out, int32_t* lens_out,
+                  const fq_page_buffer* buffers_host, int buffers, void* workspace, size_t workspace_bytes, void* stream) {
+    int st = check_pool(refs, pages, page_size, table, rows, width, lens);
+    if (st != FQ_OK) return st;
+    if (children < 0) return FQ_ERR_INVALID_ARG;
+    if (children > FQ_MOST_PAGE_ROWS) return FQ_ERR_UNSUPPORTED;
+    if ((st = check_buffers(buffers_host, buffers, pages)) != FQ_OK) return st;
+    if (children == 0 && (!release || rows == 0)) return FQ_OK;
+    if (children > 0 && (!parents || !lens_out || (width > 0 && !table_out))) return FQ_ERR_INVALID_ARG;
+    if (!aligned4(parents) || !aligned4(table_out) || !aligned4(lens_out)) return FQ_ERR_UNSUPPORTED;
+    const size_t need = fq_pages_fork_workspace_bytes(rows, children), p = (size_t)pages * 4, t = (size_t)(rows * width) * 4, l = (size_t)rows * 4,
+                 to = (size_t)(children * width) * 4, lo = (size_t)children * 4;
+    const fq_span read[] = {{table, t}, {lens, l}, {parents, lo}};
+    for (const fq_span& x : read) {
+        if (fq_overlaps(refs, p, {x}) || (children > 0 && (fq_overlaps(table_out, to, {x}) || fq_overlaps(lens_out, lo, {x})))) return FQ_ERR_INVALID_ARG;
+        if (workspace && fq_overlaps(workspace, need, {x})) return FQ_ERR_INVALID_ARG;
+        if (over_buffers(x.p, x.bytes, buffers_host, buffers, pages)) return FQ_ERR_INVALID_ARG;
+    }
+    if (children > 0 && (fq_overlaps(table_out, to, {{refs, p}, {lens_out, lo}}) || fq_overlaps(lens_out, lo, {{refs, p}}))) return FQ_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < need) return FQ_ERR_WORKSPACE;
+    if (!aligned4(workspace)) return FQ_ERR_UNSUPPORTED;
+    if (fq_overlaps(workspace, need, {{refs, p}, {table_out, children > 0 ? to : 0}, {lens_out, children > 0 ? lo : 0}})) return FQ_ERR_INVALID_ARG;
+    int32_t* w = (int32_t*)workspace;
+    const fq_fork_args a = {refs, pages, page_size, table, lens, parents, (int)rows, width, (int)children, release != 0, table_out, lens_out,
+                            w, w + rows, w + rows + children, w + rows + 2 * children};
+    st = fq_launch_pages_fork(a, (hipStream_t)stream);
+    if (st != FQ_OK || buffers == 0 || children == 0) return st;
+    fq_copy_args c = {};
+    c.from = a.from;
+    c.to = a.to;
+    c.moves = children;
+    c.count = a.moves;
+    c.pages = pages;
+    return fq_launch_pages_copy(buffers_host, buffers, c, (hipStream_t)stream);
+}
+
+int fq_pages_free(int32_t* refs, int64_t pages, int page_size, int32_t* table, int64_t rows, int64_t width, int32_t* lens, const int32_t* which,
+                  int64_t count, void* stream) {
+    const int st = check_pool(refs, pages, page_size, table, rows, width, lens);
+    if (st != FQ_OK) return st;
+    if (count < 0) return FQ_ERR_INVALID_ARG;
+    if (which && count > FQ_MOST_PAGE_ROWS) return FQ_ERR_UNSUPPORTED;
+    if (!which) count = rows;
+    if (count == 0 || rows == 0) return FQ_OK;
+    if (!aligned4(which)) return FQ_ERR_UNSUPPORTED;
+    const fq_span read = {which, which ? (size_t)count * 4 : 0};
+    if (fq_overlaps(refs, (size_t)pages * 4, {read}) || fq_overlaps(table, (size_t)(rows * width) * 4, {read}) || fq_overlaps(lens, (size_t)rows * 4, {read}))
+        return FQ_ERR_INVALID_ARG;
+    const fq_free_args a = {refs, pages, page_size, table, lens, which, (int)rows, width};
+    return fq_launch_pages_free(a, (int)count, (hipStream_t)stream);
+}
+
+size_t fq_pages_compact_workspace_bytes(int64_t pages) { return pages < 0 || pages > INT32_MAX ? 0 : (size_t)(2 * (pages / 2) + pages + 2) * 4; }
+
+int fq_pages_compact(int32_t* refs, int64_t pages, int page_size, int32_t* table, int64_t rows, int64_t width, const int32_t* lens,
+                     const fq_page_buffer* buffers_host, int buffers, void* workspace, size_t workspace_bytes, void* stream) {
+    int st = check_pool(refs, pages, page_size, table, rows, width, lens);
+    if (st != FQ_OK) return st;
+    if ((st = check_buffers(buffers_host, buffers, pages)) != FQ_OK) return st;
+    if (pages == 0) return FQ_OK;
+    const size_t need = fq_pages_compact_workspace_bytes(pages), p = (size_t)pages * 4, t = (size_t)(rows * width) * 4, l = (size_t)rows * 4;
+    if (over_buffers(refs, p, buffers_host, buffers, pages) || (t > 0 && over_buffers(table, t, buffers_host, buffers, pages))) return FQ_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < need) return FQ_ERR_WORKSPACE;
+    if (!aligned4(workspace)) return FQ_ERR_UNSUPPORTED;
+    if (fq_overlaps(workspace, need, {{refs, p}, {table, t}, {lens, l}}) || over_buffers(workspace, need, buffers_host, buffers, pages)) return FQ_ERR_INVALID_ARG;
+    int32_t* w = (int32_t*)workspace;
+    const int64_t half = pages / 2;
+    const fq_compact_args a = {refs, pages, page_size, table, lens, (int)rows, width, w, w + half, w + 2 * half, w + 2 * half + pages};
+    st = fq_launch_pages_compact(a, (hipStream_t)stream);
+    if (st != FQ_OK || buffers == 0 || half == 0) return st;
+    fq_copy_args c = {};
+    c.from = a.from;
+    c.to = a.to;
+    c.moves = half;
+    c.count = a.moves;
+    c.pages = pages;
+    return fq_launch_pages_copy(buffers_host, buffers, c, (hipStream_t)stream);
+}
+
+// ------------------------------------------------------------------------------------------ low-rank adapters
+static int check_adapters(int act_dtype, int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K) {
+    if ((act_dtype != FQ_F16 && act_dtype != FQ_BF16) || rows < 0 || adapters < 0 || rank <= 0 || N <= 0 || K <= 0) return FQ_ERR_INVALID_ARG;
+    if (rank % 8 != 0 || rank > 128 || N % 8 != 0 || K % 8 != 0) return FQ_ERR_UNSUPPORTED;
+    return N > 1 << 24 || K > 1 << 24 || rows > 1 << 20 || adapters > 1 << 20 ? FQ_ERR_UNSUPPORTED : FQ_OK;
+}
+
+size_t fq_adapters_workspace_bytes(int64_t rows, int64_t adapters, int rank, int64_t N, int64_t K) {
+    if (check_adapters(FQ_F16, rows, adapters, rank, N, K) != FQ_OK || rows == 0 || adapters == 0) return 0;
+    return fq_adapter_bytes(rows, (int)adapters, rank, N, K);
+}
+
+int fq_adapters(const void* x, int64_t x_stride, int act_dtype, int64_t rows, int64_t N, int64_t K, const void* A, const void* B, int64_t adapters,
+                int rank, const int32_t* ids, const float* scales, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                void* stream) {
+    const int st = check_adapters(act_dtype, rows, adapters, rank, N, K);
+    if (st != FQ_OK) return st;
+    if (rows > 1 && (x_stride < K || out_stride < N)) return FQ_ERR_INVALID_ARG;
+    if (rows == 0 || adapters == 0) return FQ_OK;
+    if (!x || !A || !B || !ids || !out) return FQ_ERR_INVALID_ARG;
+    if (rows > 1 && (x_stride % 8 != 0 || out_stride % 8 != 0 || too_far(rows, x_stride) || too_far(rows, out_stride))) return FQ_ERR_UNSUPPORTED;
+    if (!aligned16(x) || !aligned16(A) || !aligned16(B) || !aligned16(out) || !aligned16(workspace) || !aligned4(ids) || !aligned4(scales)) return FQ_ERR_UNSUPPORTED;
+    const size_t need = fq_adapter_bytes(rows, (int)adapters, rank, N, K), written = (size_t)((rows - 1) * (rows > 1 ? out_stride : 0) + N) * 2;
+    const fq_span read[] = {{x, (size_t)((rows - 1) * (rows > 1 ? x_stride : 0) + K) * 2}, {A, (size_t)(adapters * rank * K) * 2}, {B, (size_t)(adapters * rank * N) * 2},
+                            {ids, (size_t)rows * 4}, {scales, scales ? (size_t)adapters * 4 : 0}};
+    for (const fq_span& s : read)
+        if (fq_overlaps(out, written, {s}) || (workspace && fq_overlaps(workspace, need, {s}))) return FQ_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < need) return FQ_ERR_WORKSPACE;
+    if (fq_overlaps(workspace, need, {{out, written}})) return FQ_ERR_INVALID_ARG;
+    const fq_adapter_args a = {x, A, B, rows, rows > 1 ? x_stride : K, (int)adapters, rank, (int)N, (int)K, ids, scales, out, rows > 1 ? out_stride : N, (float*)workspace};
+    return fq_launch_adapters(act_dtype, a, (hipStream_t)stream);
+}
+
 int fq_gemm_describe(int64_t M, int64_t N, int64_t K, int bits, int group_size, char* buf,
                      size_t buf_bytes) {
     if (!buf || buf_bytes == 0 || M < 0) return FQ_ERR_INVALID_ARG;

@@ -191,4 +191,77 @@ int fq_launch_kv4_read(int act_dtype, const fq_kv4_args& a, hipStream_t stream);
 size_t fq_tree_kv4_bytes(const fq_tree_args& a);
 int fq_launch_attention_tree_kv4(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream);
 
+// pages that sequences share (device pointers but where it says host)
+#define FQ_MOST_PAGE_ROWS 8192       // rows of a table, or children
+#define FQ_COPY_BUFFERS 32           // of one launch
+struct fq_copy_args {
+    const int32_t *from, *to;
+    int64_t moves;                   // at most
+    const int32_t* count;            // how many of them, or null
+    int64_t pages;
+    int buffers;
+    int64_t pieces;                  // of a page, in all buffers
+    fq_page_buffer buffer[FQ_COPY_BUFFERS];
+    int64_t first[FQ_COPY_BUFFERS];  // a buffer's first piece
+};
+// buffers: host
+int fq_launch_pages_copy(const fq_page_buffer* buffers, int count, fq_copy_args a, hipStream_t stream);
+struct fq_fork_args {
+    int32_t* refs;
+    int64_t pages;
+    int page_size;
+    const int32_t *table, *lens, *parents;
+    int rows;
+    int64_t width;
+    int children, release;
+    int32_t *table_out, *lens_out;
+    int32_t *first, *from, *to, *moves;        // workspace
+};
+int fq_launch_pages_fork(const fq_fork_args& a, hipStream_t stream);
+struct fq_take_args {
+    int32_t* refs;
+    int64_t pages;
+    int page_size;
+    int32_t *table, *lens;
+    const int32_t* wanted;
+    int rows;
+    int64_t width;
+};
+int fq_launch_pages_take(const fq_take_args& a, hipStream_t stream);
+struct fq_free_args {
+    int32_t* refs;
+    int64_t pages;
+    int page_size;
+    int32_t *table, *lens;
+    const int32_t* which;
+    int rows;
+    int64_t width;
+};
+int fq_launch_pages_free(const fq_free_args& a, int count, hipStream_t stream);
+struct fq_compact_args {
+    int32_t* refs;
+    int64_t pages;
+    int page_size;
+    int32_t* table;
+    const int32_t* lens;
+    int rows;
+    int64_t width;
+    int32_t *from, *to, *place, *moves;        // workspace
+};
+int fq_launch_pages_compact(const fq_compact_args& a, hipStream_t stream);
+
+// low-rank adapters
+struct fq_adapter_args {
+    const void *x, *a, *b;
+    int64_t rows, x_stride;
+    int adapters, rank, N, K;
+    const int32_t* ids;
+    const float* scales;             // or null
+    void* out;
+    int64_t out_stride;
+    float* partial;                  // workspace
+};
+size_t fq_adapter_bytes(int64_t rows, int adapters, int rank, int64_t N, int64_t K);
+int fq_launch_adapters(int act_dtype, const fq_adapter_args& a, hipStream_t stream);
+
 #endif  // FQ_INTERNAL_H_

@@ -44,6 +44,12 @@ class Kv4Pages(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_size", ctypes.c_int), ("page_stride", ctypes.c_int64)]
 
 
+class PageBuffer(ctypes.Structure):
+    """fq_page_buffer: `count` tensors with room for all pages each, strides in bytes."""
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_int64), ("stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("page_bytes", ctypes.c_int64)]
+
+
 class FqError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -115,6 +121,15 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "fq_attention_tree_kv4_workspace_bytes": (sz, [i64, i64, i32, i32, i32, i64, i32]),
         "fq_attention_tree_kv4": (i32, [ctypes.POINTER(Heads), i32, i64, i64, i32, i32, i32, ctypes.POINTER(Kv4Pages), vp, i64, vp, vp,
                                         i64, f32, vp, vp, sz, vp]),
+        "fq_pages_copy": (i32, [ctypes.POINTER(PageBuffer), i32, i64, vp, vp, i64, vp]),
+        "fq_pages_take": (i32, [vp, i64, i32, vp, i64, i64, vp, vp, vp]),
+        "fq_pages_fork_workspace_bytes": (sz, [i64, i64]),
+        "fq_pages_fork": (i32, [vp, i64, i32, vp, i64, i64, vp, vp, i64, i32, vp, vp, ctypes.POINTER(PageBuffer), i32, vp, sz, vp]),
+        "fq_pages_free": (i32, [vp, i64, i32, vp, i64, i64, vp, vp, i64, vp]),
+        "fq_pages_compact_workspace_bytes": (sz, [i64]),
+        "fq_pages_compact": (i32, [vp, i64, i32, vp, i64, i64, vp, ctypes.POINTER(PageBuffer), i32, vp, sz, vp]),
+        "fq_adapters_workspace_bytes": (sz, [i64, i64, i32, i64, i64]),
+        "fq_adapters": (i32, [vp, i64, i32, i64, i64, i64, vp, vp, i64, i32, vp, vp, vp, i64, vp, sz, vp]),
         "fq_status_string": (ctypes.c_char_p, [i32]),
         "fq_version": (ctypes.c_char_p, []),
     }
@@ -137,7 +152,8 @@ EXPORTED = [
     "fq_zscale_bytes", "fq_unpack_w4a8", "fq_quantize_w4a8", "fq_quantize_act_i8", "fq_gemm_w4a8_workspace_bytes", "fq_gemm_w4a8",
     "fq_qk_norm_rope", "fq_attention_prompt_workspace_bytes", "fq_attention_prompt", "fq_attention_tree_workspace_bytes",
     "fq_attention_tree", "fq_kv4_page_bytes", "fq_kv4_write", "fq_kv4_read", "fq_attention_tree_kv4_workspace_bytes",
-    "fq_attention_tree_kv4",
+    "fq_attention_tree_kv4", "fq_pages_copy", "fq_pages_take", "fq_pages_fork_workspace_bytes", "fq_pages_fork", "fq_pages_free",
+    "fq_pages_compact_workspace_bytes", "fq_pages_compact", "fq_adapters_workspace_bytes", "fq_adapters",
 ]
 
 
@@ -380,6 +396,48 @@ def attention_tree_kv4_raw(q, act_dtype, sequences, nodes, q_heads, kv_heads, he
     return int(load().fq_attention_tree_kv4(q, act_dtype, sequences, nodes, q_heads, kv_heads, head_dim, cache, page_table_ptr,
                                             table_width, context_lens_ptr, mask_ptr, mask_stride, scale, out_ptr, ws_ptr, ws_bytes,
                                             stream))
+
+
+def pages_copy_raw(buffers, pages, from_ptr, to_ptr, moves, stream=0):
+    """buffers: an array of PageBuffer."""
+    return int(load().fq_pages_copy(buffers, len(buffers), pages, from_ptr, to_ptr, moves, stream))
+
+
+def pages_take_raw(refs_ptr, pages, page_size, table_ptr, rows, width, lens_ptr, wanted_ptr, stream=0):
+    return int(load().fq_pages_take(refs_ptr, pages, page_size, table_ptr, rows, width, lens_ptr, wanted_ptr, stream))
+
+
+def pages_fork_workspace_bytes(rows, children):
+    return int(load().fq_pages_fork_workspace_bytes(rows, children))
+
+
+def pages_fork_raw(refs_ptr, pages, page_size, table_ptr, rows, width, lens_ptr, parents_ptr, children, release, table_out_ptr, lens_out_ptr,
+                   buffers, ws_ptr, ws_bytes, stream=0):
+    return int(load().fq_pages_fork(refs_ptr, pages, page_size, table_ptr, rows, width, lens_ptr, parents_ptr, children, release, table_out_ptr,
+                                    lens_out_ptr, buffers, len(buffers), ws_ptr, ws_bytes, stream))
+
+
+def pages_free_raw(refs_ptr, pages, page_size, table_ptr, rows, width, lens_ptr, which_ptr, count, stream=0):
+    return int(load().fq_pages_free(refs_ptr, pages, page_size, table_ptr, rows, width, lens_ptr, which_ptr, count, stream))
+
+
+def pages_compact_workspace_bytes(pages):
+    return int(load().fq_pages_compact_workspace_bytes(pages))
+
+
+def pages_compact_raw(refs_ptr, pages, page_size, table_ptr, rows, width, lens_ptr, buffers, ws_ptr, ws_bytes, stream=0):
+    return int(load().fq_pages_compact(refs_ptr, pages, page_size, table_ptr, rows, width, lens_ptr, buffers, len(buffers), ws_ptr, ws_bytes,
+                                       stream))
+
+
+def adapters_workspace_bytes(rows, adapters, rank, N, K):
+    return int(load().fq_adapters_workspace_bytes(rows, adapters, rank, N, K))
+
+
+def adapters_raw(x_ptr, x_stride, act_dtype, rows, N, K, a_ptr, b_ptr, adapters, rank, ids_ptr, scales_ptr, out_ptr, out_stride, ws_ptr, ws_bytes,
+                 stream=0):
+    return int(load().fq_adapters(x_ptr, x_stride, act_dtype, rows, N, K, a_ptr, b_ptr, adapters, rank, ids_ptr, scales_ptr, out_ptr, out_stride,
+                                  ws_ptr, ws_bytes, stream))
 
 
 # ------------------------------------------------------------------ torch-tensor conveniences
@@ -904,3 +962,124 @@ def attention_tree_kv4(q, cache, page_size, kv_heads, page_table, context_lens, 
                                   page_table.data_ptr(), width, context_lens.data_ptr(), None if mask is None else mask.data_ptr(), stride,
                                   scale, o.data_ptr(), workspace.data_ptr() if size else None, size, _stream()), where)
     return o
+
+
+# ------------------------------------------------------------------ pages that sequences share
+def _page_buffers(buffers, pages, device, where):
+    """PageBuffers of one tensor [tensors, pages, ...] or of a list of tensors [pages, ...], whose pages are contiguous."""
+    torch = _torch_mod or _torch()
+    whole = isinstance(buffers, torch.Tensor)
+    tensors = [buffers] if whole else list(buffers)
+    array_of = (PageBuffer * len(tensors))()
+    for i, t in enumerate(tensors):
+        dims = 2 if whole else 1
+        _require(t.is_cuda and t.device == device and t.dim() > dims and t.shape[dims - 1] == pages, where)
+        size, expected = t.element_size(), 1
+        for d in range(t.dim() - 1, dims - 1, -1):       # a page's values lie side by side
+            _require(t.shape[d] == 1 or t.stride(d) == expected, where)
+            expected *= t.shape[d]
+        array_of[i] = PageBuffer(t.data_ptr(), t.shape[0] if whole else 1, t.stride(0) * size if whole else 0, t.stride(dims - 1) * size,
+                                 expected * size)
+    return array_of
+
+
+def _pool(refs, page_table, lens, where):
+    """Number of pages, rows and width of a pool and a table, having looked at them."""
+    torch = _torch_mod or _torch()
+    _require(refs.is_cuda and refs.dim() == 1 and page_table.dim() == 2 and lens.numel() == page_table.shape[0], where)
+    for t in (refs, page_table, lens):
+        _plain(t, torch.int32, refs.device, where)
+    return refs.shape[0], page_table.shape[0], page_table.shape[1]
+
+
+def pages_copy(buffers, from_pages, to_pages):
+    """Copies pages from_pages[m] to to_pages[m] (int32, on the device) of buffers: one tensor [tensors, pages, ...] or a list of tensors [pages, ...],
+    contiguous within a page.  A pair with a page outside the pool (-1) is left out."""
+    torch = _torch_mod or _torch()
+    where = "fq_pages_copy"
+    _require(from_pages.numel() == to_pages.numel(), where)
+    for t in (from_pages, to_pages):
+        _plain(t, torch.int32, from_pages.device, where)
+    whole = isinstance(buffers, torch.Tensor)
+    if not whole and len(buffers) == 0:
+        return
+    pages = buffers.shape[1] if whole and buffers.dim() > 1 else buffers[0].shape[0]
+    table = _page_buffers(buffers, pages, from_pages.device, where)
+    _check(pages_copy_raw(table, pages, from_pages.data_ptr(), to_pages.data_ptr(), from_pages.numel(), _stream()), where)
+
+
+def pages_take(refs, page_size, page_table, lens, wanted):
+    """Free pages for rows of page_table (int32 [rows, width]) that are to grow from lens to wanted tokens (int32 [rows]); refs int32 [pages]: the rows that
+    hold each page.  All are changed in place; lens tells which rows got what they wanted."""
+    torch = _torch_mod or _torch()
+    where = "fq_pages_take"
+    pages, rows, width = _pool(refs, page_table, lens, where)
+    _require(wanted.numel() == rows, where)
+    _plain(wanted, torch.int32, refs.device, where)
+    _check(pages_take_raw(refs.data_ptr(), pages, page_size, page_table.data_ptr(), rows, width, lens.data_ptr(), wanted.data_ptr(), _stream()), where)
+
+
+def pages_fork(refs, page_size, page_table, lens, parents, buffers=(), release=False, table_out=None, lens_out=None, workspace=None):
+    """Rows that go on as continuations of rows parents (int32 [children]): -> (page table [children, width], lens [children]).  Full pages are shared (refs is
+    changed in place), one that is not full is copied in the buffers (as pages_copy's).  release: the old rows are given up, and the first child of each takes
+    its last page over.  A child that there is no page for has length -1.  workspace: pages_fork_workspace_bytes."""
+    torch = _torch_mod or _torch()
+    where = "fq_pages_fork"
+    pages, rows, width = _pool(refs, page_table, lens, where)
+    _plain(parents, torch.int32, refs.device, where)
+    children = parents.numel()
+    array_of = _page_buffers(buffers, pages, refs.device, where)
+    table, out = _output(table_out, (children, width), page_table, where), _output(lens_out, (children,), lens, where)
+    workspace, size = _scratch(workspace, pages_fork_workspace_bytes(rows, children), refs, where)
+    _check(pages_fork_raw(refs.data_ptr(), pages, page_size, page_table.data_ptr(), rows, width, lens.data_ptr(), parents.data_ptr(), children,
+                          int(release), table.data_ptr(), out.data_ptr(), array_of, workspace.data_ptr() if size else None, size, _stream()), where)
+    return table, out
+
+
+def pages_free(refs, page_size, page_table, lens, rows=None):
+    """Rows (int32; None: all) of page_table give their pages up: refs, entries (-1) and lens (0) are changed in place."""
+    torch = _torch_mod or _torch()
+    where = "fq_pages_free"
+    pages, count, width = _pool(refs, page_table, lens, where)
+    if rows is not None:
+        _plain(rows, torch.int32, refs.device, where)
+        if rows.numel() == 0:
+            return
+    _check(pages_free_raw(refs.data_ptr(), pages, page_size, page_table.data_ptr(), count, width, lens.data_ptr(),
+                          None if rows is None else rows.data_ptr(), 0 if rows is None else rows.numel(), _stream()), where)
+
+
+def pages_compact(refs, page_size, page_table, lens, buffers=(), workspace=None):
+    """Gathers the pool's used pages at its beginning: refs and page_table (all rows that hold pages) are changed in place, pages copied in the buffers (as
+    pages_copy's).  workspace: pages_compact_workspace_bytes."""
+    where = "fq_pages_compact"
+    pages, rows, width = _pool(refs, page_table, lens, where)
+    array_of = _page_buffers(buffers, pages, refs.device, where)
+    workspace, size = _scratch(workspace, pages_compact_workspace_bytes(pages), refs, where)
+    _check(pages_compact_raw(refs.data_ptr(), pages, page_size, page_table.data_ptr(), rows, width, lens.data_ptr(), array_of,
+                             workspace.data_ptr() if size else None, size, _stream()), where)
+
+
+# ------------------------------------------------------------------ low-rank adapters
+def adapters(x, a, b, ids, out, scales=None, workspace=None):
+    """Adds each row's low-rank adapter to a product: out[m] += scales[ids[m]] * (x[m] @ a[ids[m]].T) @ b[ids[m]].T, in place; returns out.  x cuda [rows, K]
+    (float16 or bfloat16, rows any stride apart), a [adapters, rank, K], b [adapters, N, rank], ids int32 [rows] (-1: none), out [rows, N] (rows any stride
+    apart), scales float32 [adapters] (None: 1).  workspace: adapters_workspace_bytes."""
+    torch = _torch_mod or _torch()
+    where = "fq_adapters"
+    act = _act_code(x)
+    _require(x.is_cuda and x.dim() == 2 and out.dim() == 2 and a.dim() == 3 and b.dim() == 3, where)
+    (rows, K), (count, rank, _), N = x.shape, a.shape, b.shape[1]
+    _require((x.stride(1) == 1 or K <= 1) and (out.stride(1) == 1 or N <= 1) and out.dtype == x.dtype and out.device == x.device, where)
+    _require(tuple(a.shape) == (count, rank, K) and tuple(b.shape) == (count, N, rank) and tuple(out.shape) == (rows, N) and ids.numel() == rows, where)
+    for t in (a, b):
+        _plain(t, x.dtype, x.device, where)
+    _plain(ids, torch.int32, x.device, where)
+    if scales is not None:
+        _require(scales.numel() == count, where)
+        _plain(scales, torch.float32, x.device, where)
+    workspace, size = _scratch(workspace, adapters_workspace_bytes(rows, count, rank, N, K), x, where)
+    _check(adapters_raw(x.data_ptr(), x.stride(0), act, rows, N, K, a.data_ptr(), b.data_ptr(), count, rank, ids.data_ptr(),
+                        None if scales is None else scales.data_ptr(), out.data_ptr(), out.stride(0), workspace.data_ptr() if size else None, size,
+                        _stream()), where)
+    return out
