@@ -165,8 +165,9 @@ struct record_loads {
 
 // ------------------------------------------------------------------------------------------ up to 32 rows
 // One wave's NT x 16 rows (lane 16 h + x: row x of each 16; of a record's keys 4 h .. 4 h + 3)
-template <int ACT, int S, int NT>
+template <int ACT, int S, int TILES>
 struct few_rows {
+    static constexpr int NT = TILES, RECORDS = 2, RING = 4;             // records of a step; steps that a wave's ring has room for
     static constexpr float LARGER = ACT == FQ_F16 ? 7.0f : 0.0f;       // the first score's numerator, log2
     u32x4 q[NT][S];
     f32x4 o[NT][2 * S];              // values 16 i + 4 h .. + 3 of the lane's row
@@ -335,6 +336,28 @@ struct few_rows {
         }
     }
 
+    // The rows that a lane has scores of: row 16 n + its own
+    __device__ __forceinline__ static int own_row() { return threadIdx.x & 15; }
+
+    // A step's records, of which the first `there` keys are keys; those of the row that are seen: seen(row, key)
+    template <typename SEEN>
+    __device__ __forceinline__ void step(char* at, float factor, bool masked, int there, const SEEN& seen) {
+        const int h = (threadIdx.x & 63) >> 4;
+        f32x4 s[2][NT];
+        scores(at, s[0]);
+        scores(at + record_bytes(S), s[1]);
+        if (masked) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t bits = seen(n, 0) >> 4 * h;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) s[x >> 2][n][x & 3] = bits >> (16 * (x >> 2) + (x & 3)) & 1 ? s[x >> 2][n][x & 3] : -__builtin_inff();
+            }
+        }
+        soften(s, factor);
+        accumulate(at, at + record_bytes(S), s, there < 32, there);
+    }
+
     __device__ __forceinline__ void finish() {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -357,20 +380,243 @@ struct few_rows {
     }
 };
 
-// Four waves of a block share a unit's keys out, 32 at a time, and join their sums through LDS at the end of a piece.  A wave's ring has RING times
-// two records, all but one of them on their way while that one is used.
-template <int ACT, int S, int NT>
+// Four rows: S^T by products of 4 x 4 x 4, sixteen at once, so that no column is a row that is not there (lane 4 b + j: row j; keys 4 b .. 4 b + 3 of
+// a step of 64, of whose values the lane converts its own key's).  Scores, scales and numerators are a quarter of the instructions then.  The
+// numerators go through LDS (where the keys' codes lay) into the order of the 16 x 16 x 32 products for O^T, whose columns are the four rows, four times.
+template <int ACT>
+__device__ __forceinline__ f32x4 mfma4(const u32x2& a, const u32x2& b, const f32x4& c) {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    if constexpr (ACT == FQ_F16)
+        return __builtin_amdgcn_mfma_f32_4x4x4f16(__builtin_bit_cast(f16x4, a), __builtin_bit_cast(f16x4, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), c, 0, 0, 0);
+}
+
+template <int ACT, int S>
+struct four_rows {
+    static constexpr int NT = 1, RECORDS = 4, RING = 2;
+    static constexpr float LARGER = ACT == FQ_F16 ? 7.0f : 0.0f;
+    static constexpr int BYTES = record_bytes(S);
+    u32x2 q[S][4][2];                // [t][a][half]: values 32 t + 8 a + 4 half .. + 3 of row j
+    f32x4 o[1][2 * S];               // values 16 i + 4 h .. + 3 of row (lane % 16) % 4
+    float m[1], c[1], l[1];
+    bool stale;
+
+    __device__ __forceinline__ static int own_row() { return threadIdx.x & 3; }
+    __device__ __forceinline__ static float rows_max(float x) {      // over the lanes of a row
+        x = __builtin_fmaxf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x124, 0xf, 0xf, true)));       // 4 lanes on in the row of 16
+        x = __builtin_fmaxf(x, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x128, 0xf, 0xf, true)));       // 8
+        return row_max(x);
+    }
+    __device__ __forceinline__ static float rows_sum(float x) {
+        x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x124, 0xf, 0xf, true));
+        x += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x128, 0xf, 0xf, true));
+        return row_sum(x);
+    }
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 2 * S; ++i) o[0][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        m[0] = -__builtin_inff();
+        c[0] = l[0] = 0.0f;
+        stale = true;
+    }
+    __device__ __forceinline__ void load_query(int, const uint16_t* row, int D) {
+#pragma unroll
+        for (int t = 0; t < S; ++t)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const int d = 32 * t + 8 * a;
+                const u32x4 x = d < D ? *(const u32x4*)(row + d) : u32x4{0, 0, 0, 0};
+                q[t][a][0] = u32x2{x[0], x[1]};
+                q[t][a][1] = u32x2{x[2], x[3]};
+            }
+    }
+    __device__ __forceinline__ void query_is_here() {
+#pragma unroll
+        for (int t = 0; t < S; ++t)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) asm volatile("" : "+v"(q[t][a][0]), "+v"(q[t][a][1]));
+    }
+    __device__ __forceinline__ void again(float by) {
+#pragma unroll
+        for (int i = 0; i < 2 * S; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[0][i][r] *= by;
+    }
+    __device__ __forceinline__ void level() {
+        const float most = rows_max(l[0]);
+        if (!__any(most > 0x1p30f)) return;
+        const float by = m[0] + (float)__builtin_amdgcn_frexp_expf(most) - m[0];
+        const float half = m[0] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(-0.5f * by);
+        if (m[0] != -__builtin_inff()) c[0] = m[0] += by;
+        l[0] = l[0] * half * half;
+        again(half);
+        again(half);
+    }
+
+    template <typename SEEN>
+    __device__ __forceinline__ void step(char* at, float factor, bool masked, int there, const SEEN& seen) {
+        const int lane = threadIdx.x & 63, b = lane >> 2, x16 = lane & 15, h = lane >> 4;
+        // scores of keys 4 b + i; the lane brings in key `lane`
+        f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+        char* own = at + (b >> 2) * BYTES;             // the record of the lane's scores
+        {
+            const char* from = at + h * BYTES + x16 * 4 * S;
+            uint32_t k[4][S], scale[2 * S];
+#pragma unroll
+            for (int a = 0; a < 4; ++a) read_words(from + a * 64 * S, k[a]);
+            read_words(own + 512 * S + (b & 3) * 8 * S, scale);
+            f32x4 y[S];
+#pragma unroll
+            for (int t = 0; t < S; ++t) y[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+#pragma unroll
+                for (int t = 0; t < S; ++t) {
+                    const uint32_t first = firsts(k[a][t]), second = seconds(k[a][t]);
+                    y[t] = mfma4<ACT>(u32x2{codes16<ACT, false>(first), codes16<ACT, true>(first)}, q[t][a][0], y[t]);
+                    y[t] = mfma4<ACT>(u32x2{codes16<ACT, false>(second), codes16<ACT, true>(second)}, q[t][a][1], y[t]);
+                }
+#pragma unroll
+            for (int t = 0; t < S; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    s[i] = __builtin_fmaf(y[t][i], i & 1 ? half_of<ACT, 1>(scale[2 * t + i / 2]) : half_of<ACT, 0>(scale[2 * t + i / 2]), s[i]);
+        }
+        if (masked) {
+            const uint32_t first = seen(0, 0), last = seen(0, 32), bits = (b < 8 ? first : last) >> (4 * b & 31);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] = bits >> i & 1 ? s[i] : -__builtin_inff();
+        }
+        // numerators (see wave_state)
+        if (ACT == FQ_F16 || stale) {
+            if (ACT == FQ_BF16) level();
+            const float top = rows_max(__builtin_fmaxf(__builtin_fmaxf(s[0], s[1]), __builtin_fmaxf(s[2], s[3]))) * factor - LARGER;
+            if (__any(top > m[0] + 8.0f)) {
+                const float now = __builtin_fmaxf(m[0], top), next = now == -__builtin_inff() ? 0.0f : now;
+                const float by = __builtin_amdgcn_exp2f(m[0] - next);
+                m[0] = now;
+                c[0] = next;
+                l[0] *= by;
+                again(by);
+            }
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], factor, -c[0]));
+            sum += s[i];
+        }
+        l[0] += sum;
+        if (ACT == FQ_BF16) stale = __any(sum > 0x1p58f || m[0] == -__builtin_inff());
+        // to LDS, as products with the values' scales in bfloat16: [record][group][token / 4][row]
+        constexpr int GROUPS = ACT == FQ_BF16 ? S : 1;
+        {
+            uint32_t scale[2 * S];
+            if constexpr (ACT == FQ_BF16) {
+                read_words(own + 544 * S + (b & 3) * 8 * S, scale);
+                if (there < 64) {                      // what lies behind the last key may be anything
+#pragma unroll
+                    for (int g = 0; g < S; ++g) {
+                        scale[2 * g] &= first_mask(there - 4 * b);
+                        scale[2 * g + 1] &= first_mask(there - 4 * b - 2);
+                    }
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                u32x2 p;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float x = s[2 * i], y = s[2 * i + 1];
+                    if constexpr (ACT == FQ_BF16) {
+                        x *= half_of<ACT, 0>(scale[2 * g + i]);
+                        y *= half_of<ACT, 1>(scale[2 * g + i]);
+                    }
+                    p[i] = pack2<ACT>(x, y);
+                }
+                *(u32x2*)(own + g * 128 + (lane & 15) * 8) = p;        // (lane % 16: 4 (b % 4) + j)
+            }
+        }
+        // O^T += V^T P^T, two records at a time
+#pragma unroll
+        for (int pair = 0; pair < 2; ++pair) {
+            const char* record[2] = {at + 2 * pair * BYTES, at + (2 * pair + 1) * BYTES};
+            uint32_t v[2][S], scale[2][2 * S];
+            u32x2 p[GROUPS][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                read_words(record[u] + 256 * S + lane * 4 * S, v[u]);
+                if constexpr (ACT == FQ_F16) {
+                    read_words(record[u] + 544 * S + h * 8 * S, scale[u]);
+                    if (there < 64) {
+                        const int count = there - 32 * pair - 16 * u - 4 * h;
+#pragma unroll
+                        for (int g = 0; g < S; ++g) {
+                            scale[u][2 * g] &= first_mask(count);
+                            scale[u][2 * g + 1] &= first_mask(count - 2);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) p[g][u] = *(const u32x2*)(record[u] + g * 128 + (4 * h + (x16 & 3)) * 8);
+            }
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
+                u32x4 first, second;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t f = firsts(v[u][j]), g = seconds(v[u][j]);
+                    first[2 * u] = codes16<ACT, false>(f);
+                    first[2 * u + 1] = codes16<ACT, true>(f);
+                    second[2 * u] = codes16<ACT, false>(g);
+                    second[2 * u + 1] = codes16<ACT, true>(g);
+                    if constexpr (ACT == FQ_F16) {
+                        first[2 * u] = times16(first[2 * u], scale[u][2 * j]);
+                        first[2 * u + 1] = times16(first[2 * u + 1], scale[u][2 * j + 1]);
+                        second[2 * u] = times16(second[2 * u], scale[u][2 * j]);
+                        second[2 * u + 1] = times16(second[2 * u + 1], scale[u][2 * j + 1]);
+                    }
+                }
+                const int g = ACT == FQ_BF16 ? j : 0;
+                const u32x4 x = {p[g][0][0], p[g][0][1], p[g][1][0], p[g][1][1]};
+                o[0][2 * j] = mfma16<ACT>(first, x, o[0][2 * j]);
+                o[0][2 * j + 1] = mfma16<ACT>(second, x, o[0][2 * j + 1]);
+            }
+        }
+    }
+
+    __device__ __forceinline__ void finish() {
+        if (ACT == FQ_BF16) level();
+        l[0] = rows_sum(l[0]);
+    }
+    __device__ __forceinline__ bool sound() const {
+        float x = l[0] >= 0.25f || m[0] == -__builtin_inff() ? l[0] * 0.0f : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 2 * S; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x = __builtin_fmaf(o[0][i][r], 0.0f, x);
+        return __all(x == 0.0f);
+    }
+};
+
+// A block's four waves are HEADS key heads x PARTS parts of a tile of 32 PARTS keys; where they share the keys out, they join their sums through
+// LDS at the end of a piece.  A wave's ring has RING times two records, all but one of them on their way while that one is used.
+template <int ACT, int S, typename STATE, int HEADS>
 __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree_args a, tree_plan p, divisor by_records) {
-    constexpr int BYTES = record_bytes(S), RING = 4, STEP = 2 * BYTES, WAVE_BYTES = RING * STEP;
-    constexpr int LOADS = 2 * record_loads<S>::COUNT;
-    constexpr int TILE = 128, QUADS = 8 * S;             // keys of the block; fours of a row's values
+    constexpr int NT = STATE::NT, RECORDS = STATE::RECORDS, BYTES = record_bytes(S), RING = STATE::RING, STEP = RECORDS * BYTES, WAVE_BYTES = RING * STEP;
+    constexpr int APART = RECORDS * record_loads<S>::COUNT, TOGETHER = record_loads<RECORDS * S>::COUNT;       // loads of a step
+    constexpr int WIDE = RECORD * RECORDS, PARTS = 4 / HEADS, TILE = WIDE * PARTS, QUADS = 8 * S;              // QUADS: fours of a row's values
     constexpr int TURN = QUADS == 24 || QUADS == 8 ? 7 : 15;
     static_assert(NT * 16 * QUADS * 16 <= WAVE_BYTES, "the sums of a wave fit its ring");
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4;
+    const int head = wave % HEADS, part_of = wave / HEADS;
     int32_t* entries = (int32_t*)(lds + 4 * WAVE_BYTES) + wave * (TABLE / 4);
     float* stats = (float*)(lds + 4 * WAVE_BYTES + TABLE * 4);       // [4][32][2], and a flag
     const int D = a.head_dim;
+    const bool together = a.cache.page_size % WIDE == 0;         // a step's records lie one behind the other
     char* mine = lds + wave * WAVE_BYTES;
     const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
 
@@ -382,17 +628,17 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree
     all.find(begin, &b, &at_b);
     int context = all.context(b), tiles = tiles_of(a, p, context);
     int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
-    few_rows<ACT, S, NT> w;
+    STATE w;
 
     for (int64_t pos = begin; pos < stop;) {
-        const unit_rows<kv4_rows> rows(a, p, b, u, 0, context);
+        const unit_rows<kv4_rows> rows(a, p, b, u, head, context);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
-        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, 0);
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, head);
         const int key0 = t0 * TILE, key1 = p.whole ? rows.keys : min(rows.keys, t1 * TILE);
         int row[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            row[n] = min(16 * n + (lane & 15), rows.count - 1);
+            row[n] = min(16 * n + STATE::own_row(), rows.count - 1);
             w.load_query(n, rows.query(row[n]), D);
         }
         w.clear();
@@ -405,12 +651,17 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree
             const record_places places = {entries, table.first, by_records, a.cache.page_size / RECORD,
                                           (const char*)a.cache.k + rows.head * a.cache.head_stride, a.cache.page_stride};
             const int last = (part_end - 1) / RECORD;
-            const int base0 = part + wave * 32, steps = base0 < part_end ? (part_end - base0 + TILE - 1) / TILE : 0;
+            const int base0 = part + part_of * WIDE, steps = base0 < part_end ? (part_end - base0 + TILE - 1) / TILE : 0;
             auto load = [&](int i) {
                 const int r = (base0 + i * TILE) / RECORD;
                 const uint32_t to = mine_at + (uint32_t)(i % RING) * STEP;
-                record_loads<S>::issue(to, places.template place<BYTES>(r));
-                record_loads<S>::issue(to + BYTES, places.template place<BYTES>(min(r + 1, last)));       // (no record behind the last)
+                if (together) {
+                    record_loads<RECORDS * S>::issue(to, places.template place<BYTES>(r));
+                } else {
+#pragma unroll
+                    for (int u = 0; u < RECORDS; ++u)                // (no record behind the last)
+                        record_loads<S>::issue(to + u * BYTES, places.template place<BYTES>(min(r + u, last)));
+                }
             };
             for (int i = 0; i < min(steps, RING - 1); ++i) load(i);
             for (int i = 0; i < steps; ++i) {
@@ -418,72 +669,84 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (what was read from the records that these loads replace is here)
                 if (i + RING - 1 < steps) {
                     load(i + RING - 1);
-                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * LOADS) : "memory");
+                    if (together) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * TOGETHER) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * APART) : "memory");
                 } else {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 }
-                const char* at = mine + (i % RING) * STEP;
-                f32x4 s[2][NT];
-                w.scores(at, s[0]);
-                w.scores(at + BYTES, s[1]);
-                if (base + 32 > min(rows.context, part_end)) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const uint32_t seen = rows.seen(row[n], base) >> 4 * h;
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) s[x >> 2][n][x & 3] = seen >> (16 * (x >> 2) + (x & 3)) & 1 ? s[x >> 2][n][x & 3] : -__builtin_inff();
-                    }
-                }
-                w.soften(s, p.factor);
-                w.accumulate(at, at + BYTES, s, base + 32 > part_end, part_end - base);
+                w.step(mine + (i % RING) * STEP, p.factor, base + WIDE > min(rows.context, part_end), part_end - base,
+                       [&](int n, int on) { return rows.seen(row[n], base + on); });
             }
         }
         w.finish();
-        // the waves' sums, joined
-        __syncthreads();
-        if (threadIdx.x == 0) stats[256] = 0.0f;
-        __syncthreads();
-        if (!w.sound() && lane == 0) stats[256] = 1.0f;
+        if constexpr (PARTS == 1) {
+            if (!w.sound()) {
+                rows.template one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
+            } else {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int r = 16 * n + (lane & 15);
-            if (h == 0) {
-                stats[(wave * 32 + r) * 2] = w.m[n];
-                stats[(wave * 32 + r) * 2 + 1] = w.l[n];
+                for (int n = 0; n < NT; ++n) {
+                    const int r = 16 * n + (lane & 15);
+                    if (r >= rows.count) continue;
+                    const float scale = slot ? 1.0f : inverse(w.l[n], [&] { return rows.sees_any(r); });
+#pragma unroll
+                    for (int i = 0; i < 2 * S; ++i) {
+                        const int d = 16 * i + 4 * h;
+                        if (d >= D) continue;
+                        const f32x4 o = w.o[n][i] * scale;
+                        if (slot) *(f32x4*)(slot + p.shape().at(r, d)) = o;
+                        else *(u32x2*)(rows.result(r) + d) = u32x2{pack2<ACT>(o[0], o[1]), pack2<ACT>(o[2], o[3])};
+                    }
+                    if (slot && h == 0) p.shape().put_stats(slot, r, w.m[n], w.l[n]);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < 2 * S; ++i) *(f32x4*)((float*)mine + r * 4 * QUADS + ((4 * i + h) ^ (r & TURN)) * 4) = w.o[n][i];
-        }
-        __syncthreads();
-        if (stats[256] != 0.0f) {
-            rows.template one_by_one<ACT>(key0, key1, slot, wave, rows.count, 4);
         } else {
-            for (int x = threadIdx.x; x < rows.count * QUADS; x += 256) {
-                const int r = x / QUADS, quad = x % QUADS, d = quad * 4;
-                if (d >= D) continue;
-                float c = -__builtin_inff(), l = 0.0f;
+            // the waves' sums, joined
+            __syncthreads();
+            if (threadIdx.x == 0) stats[256] = 0.0f;
+            __syncthreads();
+            if (!w.sound() && lane == 0) stats[256] = 1.0f;
 #pragma unroll
-                for (int y = 0; y < 4; ++y) c = __builtin_fmaxf(c, stats[(y * 32 + r) * 2]);
-                const float from = c == -__builtin_inff() ? 0.0f : c;
-                f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const float weight = __builtin_amdgcn_exp2f(stats[(y * 32 + r) * 2] - from);
-                    const f32x4 z = *(const f32x4*)((const float*)(lds + y * WAVE_BYTES) + r * 4 * QUADS + (quad ^ (r & TURN)) * 4);
-                    l += weight * stats[(y * 32 + r) * 2 + 1];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
+            for (int n = 0; n < NT; ++n) {
+                const int r = 16 * n + (lane & 15);
+                if (h == 0) {
+                    stats[(wave * 32 + r) * 2] = w.m[n];
+                    stats[(wave * 32 + r) * 2 + 1] = w.l[n];
                 }
-                if (!slot) {
-                    const float scale = inverse(l, [&] { return rows.sees_any(r); });
-                    *(u32x2*)(rows.result(r) + d) = u32x2{pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
-                } else {
-                    *(f32x4*)(slot + p.shape().at(r, d)) = o;
-                    if (d == 0) p.shape().put_stats(slot, r, c, l);
+#pragma unroll
+                for (int i = 0; i < 2 * S; ++i) *(f32x4*)((float*)mine + r * 4 * QUADS + ((4 * i + h) ^ (r & TURN)) * 4) = w.o[n][i];
+            }
+            __syncthreads();
+            if (stats[256] != 0.0f) {
+                rows.template one_by_one<ACT>(key0, key1, slot, part_of, rows.count, PARTS);
+            } else {
+                for (int x = part_of * 64 + lane; x < rows.count * QUADS; x += 64 * PARTS) {
+                    const int r = x / QUADS, quad = x % QUADS, d = quad * 4;
+                    if (d >= D) continue;
+                    float c = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+                    for (int y = 0; y < PARTS; ++y) c = __builtin_fmaxf(c, stats[((head + y * HEADS) * 32 + r) * 2]);
+                    const float from = c == -__builtin_inff() ? 0.0f : c;
+                    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int y = 0; y < PARTS; ++y) {
+                        const int other = head + y * HEADS;
+                        const float weight = __builtin_amdgcn_exp2f(stats[(other * 32 + r) * 2] - from);
+                        const f32x4 z = *(const f32x4*)((const float*)(lds + other * WAVE_BYTES) + r * 4 * QUADS + (quad ^ (r & TURN)) * 4);
+                        l += weight * stats[(other * 32 + r) * 2 + 1];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[i] += weight * z[i];
+                    }
+                    if (!slot) {
+                        const float scale = inverse(l, [&] { return rows.sees_any(r); });
+                        *(u32x2*)(rows.result(r) + d) = u32x2{pack2<ACT>(o[0] * scale, o[1] * scale), pack2<ACT>(o[2] * scale, o[3] * scale)};
+                    } else {
+                        *(f32x4*)(slot + p.shape().at(r, d)) = o;
+                        if (d == 0) p.shape().put_stats(slot, r, c, l);
+                    }
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();
         pos += t1 - t0;
         t0 = 0;
         if (++u == all.units) {
@@ -643,12 +906,12 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_tile_kernel(fq_tree_a
     }
 }
 
-template <int ACT, int S, int NT>
+template <int ACT, int S, typename STATE, int HEADS>
 int launch_stream(const fq_tree_args& a, const tree_plan& p, const divisor& by_records, hipStream_t stream) {
     static std::atomic<uint64_t> raised{0};
-    const int st = fqd::raise_lds_limit((const void*)fq_attention_kv4_stream_kernel<ACT, S, NT>, raised);
+    const int st = fqd::raise_lds_limit((const void*)fq_attention_kv4_stream_kernel<ACT, S, STATE, HEADS>, raised);
     if (st != FQ_OK) return st;
-    fq_attention_kv4_stream_kernel<ACT, S, NT><<<(unsigned)p.blocks, 256, 32 * record_bytes(S) + TABLE * 4 + 257 * 4, stream>>>(a, p, by_records);
+    fq_attention_kv4_stream_kernel<ACT, S, STATE, HEADS><<<(unsigned)p.blocks, 256, 4 * STATE::RING * STATE::RECORDS * record_bytes(S) + TABLE * 4 + 257 * 4, stream>>>(a, p, by_records);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
@@ -663,13 +926,21 @@ int launch_tiles(const fq_tree_args& a, const tree_plan& p, const divisor& by_re
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
+template <int ACT, int S, typename STATE>
+int launch_few(const fq_tree_args& a, const tree_plan& p, const divisor& by_records, hipStream_t stream) {
+    return p.heads == 4   ? launch_stream<ACT, S, STATE, 4>(a, p, by_records, stream)
+           : p.heads == 2 ? launch_stream<ACT, S, STATE, 2>(a, p, by_records, stream)
+                          : launch_stream<ACT, S, STATE, 1>(a, p, by_records, stream);
+}
+
 template <int ACT, int S>
 int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
     const divisor by_records = divisor::of((uint32_t)(a.cache.page_size / RECORD));
     const int st = p.unit_rows > 64 ? launch_tiles<ACT, S, 4>(a, p, by_records, stream)
                    : p.rows > 32    ? launch_tiles<ACT, S, 2>(a, p, by_records, stream)
-                   : p.rows > 16    ? launch_stream<ACT, S, 2>(a, p, by_records, stream)
-                                    : launch_stream<ACT, S, 1>(a, p, by_records, stream);
+                   : p.rows > 16    ? launch_stream<ACT, S, few_rows<ACT, S, 2>, 1>(a, p, by_records, stream)
+                   : p.rows > 4     ? launch_few<ACT, S, few_rows<ACT, S, 1>>(a, p, by_records, stream)
+                                    : launch_few<ACT, S, four_rows<ACT, S>>(a, p, by_records, stream);
     if (st != FQ_OK || p.whole) return st;
     return launch_join<ACT, kv4_rows>(a, p, stream);
 }
@@ -686,10 +957,17 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
 
 }  // namespace
 
-size_t fq_tree_kv4_bytes(const fq_tree_args& a) { return slots_bytes(plan_units(a, 1)); }
+// The waves of few rows take heads of their own where there are enough: pieces are four times as long, and few are joined in LDS.
+static tree_plan plan_kv4(const fq_tree_args& a) {
+    const int rows = a.nodes * (a.q_heads / a.kv_heads);
+    const int heads = rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
+    return plan_units(a, heads, rows > 32 ? KEYS : (rows > 4 ? 128 : 256) / heads);
+}
+
+size_t fq_tree_kv4_bytes(const fq_tree_args& a) { return slots_bytes(plan_kv4(a)); }
 
 int fq_launch_attention_tree_kv4(int act_dtype, const fq_tree_args& a, void* workspace, hipStream_t stream) {
-    tree_plan p = plan_units(a, 1);
+    tree_plan p = plan_kv4(a);
     p.slots = (float*)workspace;
     return act_dtype == FQ_F16 ? launch<FQ_F16>(a, p, stream) : launch<FQ_BF16>(a, p, stream);
 }

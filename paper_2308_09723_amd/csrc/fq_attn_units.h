@@ -363,8 +363,8 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
 // eight sequences of 500 - 4095, groups of four: 49.8 -> 45.6 us; heads of 96, 160 rows, 32.6, in three 33.4)
 inline int rows_of_tile(int64_t rows, int head_dim) { return rows <= 64 || (rows > 128 && rows <= 192 && head_dim > 96) ? 64 : ROWS; }
 
-// The plan of a call whose blocks take `heads` key heads together (up to 32 rows a head; above, one).
-inline tree_plan plan_units(const fq_tree_args& a, int heads) {
+// The plan of a call whose blocks take `heads` key heads together (up to 32 rows a head; above, one), `tile` keys at a time.
+inline tree_plan plan_units(const fq_tree_args& a, int heads, int tile) {
     tree_plan p = {};
     p.group = a.q_heads / a.kv_heads;
     p.rows = a.nodes * p.group;      // (fq_tree_fits)
@@ -376,7 +376,7 @@ inline tree_plan plan_units(const fq_tree_args& a, int heads) {
     p.by_group = divisor::of((uint32_t)p.group);
     p.by_quads = divisor::of((uint32_t)a.head_dim / 4);
     p.by_side = divisor::of((uint32_t)(p.rows < 32 ? p.rows : 32));
-    p.tile = p.rows > 32 ? KEYS : 128 / p.heads;
+    p.tile = tile;
     // Units of few tiles are left whole: a block is through with four tiles as soon as with one and the join, and with eight where there are
     // blocks' worth of units (102 sequences of 223 tokens, 3 units each of 7 tiles: 24.4 -> 18.6 us; one of 250, 2 units of 8: 13.7, whole 18.8).
     const int64_t tiles = (a.table_width * a.cache.page_size + p.tile - 1) / p.tile, units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
