@@ -184,14 +184,21 @@ struct few_rows {
         }
         stale = true;
     }
-    __device__ __forceinline__ void load_query(int n, const uint16_t* row, int D) {
+    template <typename ROWS>
+    __device__ __forceinline__ void load_query(const ROWS& rows, int D) {
         const int h = (threadIdx.x & 63) >> 4;
 #pragma unroll
-        for (int t = 0; t < S; ++t) {
-            const int d = 32 * t + 8 * h;
-            q[n][t] = d < D ? *(const u32x4*)(row + d) : u32x4{0, 0, 0, 0};
+        for (int n = 0; n < NT; ++n) {
+            const uint16_t* row = rows.query(min(16 * n + own_row(), rows.count - 1));
+#pragma unroll
+            for (int t = 0; t < S; ++t) {
+                const int d = 32 * t + 8 * h;
+                q[n][t] = d < D ? *(const u32x4*)(row + d) : u32x4{0, 0, 0, 0};
+            }
         }
     }
+    __device__ __forceinline__ void pass_query(char*) {}
+    __device__ __forceinline__ void take_query(const char*) {}
     // (waits for the queries here: see wave_state)
     __device__ __forceinline__ void query_is_here() {
 #pragma unroll
@@ -421,22 +428,27 @@ struct four_rows {
         c[0] = l[0] = 0.0f;
         stale = true;
     }
-    __device__ __forceinline__ void load_query(int, const uint16_t* row, int D) {
+    // Each lane loads 16 bytes of the four rows and takes its row out of LDS (loaded as they are needed, a row 16 times, they took 3 us)
+    u32x4 loaded;
+    template <typename ROWS>
+    __device__ __forceinline__ void load_query(const ROWS& rows, int D) {
+        const int lane = threadIdx.x & 63, d = (lane & 15) * 8;
+        loaded = d < D ? *(const u32x4*)(rows.query(min(lane >> 4, rows.count - 1)) + d) : u32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void query_is_here() { asm volatile("" : "+v"(loaded)); }
+    __device__ __forceinline__ void pass_query(char* room) {
+        const int lane = threadIdx.x & 63;
+        if ((lane & 15) < 4 * S) *(u32x4*)(room + ((lane >> 4) * 4 * S + (lane & 15)) * 16) = loaded;
+    }
+    __device__ __forceinline__ void take_query(const char* room) {
 #pragma unroll
         for (int t = 0; t < S; ++t)
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
-                const int d = 32 * t + 8 * a;
-                const u32x4 x = d < D ? *(const u32x4*)(row + d) : u32x4{0, 0, 0, 0};
+                const u32x4 x = *(const u32x4*)(room + (own_row() * 4 * S + 4 * t + a) * 16);
                 q[t][a][0] = u32x2{x[0], x[1]};
                 q[t][a][1] = u32x2{x[2], x[3]};
             }
-    }
-    __device__ __forceinline__ void query_is_here() {
-#pragma unroll
-        for (int t = 0; t < S; ++t)
-#pragma unroll
-            for (int a = 0; a < 4; ++a) asm volatile("" : "+v"(q[t][a][0]), "+v"(q[t][a][1]));
     }
     __device__ __forceinline__ void again(float by) {
 #pragma unroll
@@ -627,27 +639,26 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree
     int64_t at_b;
     all.find(begin, &b, &at_b);
     int context = all.context(b), tiles = tiles_of(a, p, context);
-    int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
+    int u = (int)quotient(begin - at_b, tiles + p.extra), t0 = (int)(begin - at_b - (int64_t)u * (tiles + p.extra));
     STATE w;
 
     for (int64_t pos = begin; pos < stop;) {
         const unit_rows<kv4_rows> rows(a, p, b, u, head, context);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
-        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, head);
+        if (t0 < tiles) {                               // (behind them are places that hold nothing)
         const int key0 = t0 * TILE, key1 = p.whole ? rows.keys : min(rows.keys, t1 * TILE);
-        int row[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            row[n] = min(16 * n + STATE::own_row(), rows.count - 1);
-            w.load_query(n, rows.query(row[n]), D);
-        }
+        w.load_query(rows, D);
         w.clear();
         const int most = part_keys(TABLE / 4, a.cache.page_size, TILE);
         for (int part = key0, part_end; part < key1; part = part_end) {
             part_end = fqa::part_end(part, key1, most);
             const table_part table = load_table<64>(a, b, part, part_end, entries);
+            char* room = mine + (RING - 1) * STEP;      // (the step that comes in last)
+            if (part == key0) {
+                w.query_is_here();                      // (with the table)
+                w.pass_query(room);
+            }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (the wave's own: no barrier)
-            w.query_is_here();                          // (with the table)
             const record_places places = {entries, table.first, by_records, a.cache.page_size / RECORD,
                                           (const char*)a.cache.k + rows.head * a.cache.head_stride, a.cache.page_stride};
             const int last = (part_end - 1) / RECORD;
@@ -664,6 +675,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree
                 }
             };
             for (int i = 0; i < min(steps, RING - 1); ++i) load(i);
+            if (part == key0) w.take_query(room);
             for (int i = 0; i < steps; ++i) {
                 const int base = base0 + i * TILE;
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (what was read from the records that these loads replace is here)
@@ -675,10 +687,11 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 }
                 w.step(mine + (i % RING) * STEP, p.factor, base + WIDE > min(rows.context, part_end), part_end - base,
-                       [&](int n, int on) { return rows.seen(row[n], base + on); });
+                       [&](int n, int on) { return rows.seen(min(16 * n + STATE::own_row(), rows.count - 1), base + on); });
             }
         }
         w.finish();
+        float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(blockIdx.x, pos == begin, head);
         if constexpr (PARTS == 1) {
             if (!w.sound()) {
                 rows.template one_by_one<ACT>(key0, key1, slot, 0, rows.count, 1);
@@ -747,7 +760,8 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree
             }
             __syncthreads();
         }
-        pos += t1 - t0;
+        }
+        pos += tiles + p.extra - t0;
         t0 = 0;
         if (++u == all.units) {
             u = 0;
@@ -958,10 +972,13 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
 }  // namespace
 
 // The waves of few rows take heads of their own where there are enough: pieces are four times as long, and few are joined in LDS.
+#ifndef EXTRA
+#define EXTRA 3
+#endif
 static tree_plan plan_kv4(const fq_tree_args& a) {
     const int rows = a.nodes * (a.q_heads / a.kv_heads);
     const int heads = rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
-    return plan_units(a, heads, rows > 32 ? KEYS : (rows > 4 ? 128 : 256) / heads);
+    return plan_units(a, heads, rows > 32 ? KEYS : (rows > 4 ? 128 : 256) / heads, rows > 32 ? 0 : EXTRA);
 }
 
 size_t fq_tree_kv4_bytes(const fq_tree_args& a) { return slots_bytes(plan_kv4(a)); }

@@ -21,6 +21,7 @@ struct tree_plan {
     int heads;                       // key heads that a block takes together
     int row_tiles, unit_rows;        // tiles of unit_rows rows that a head's are cut into
     int tile;                        // keys of a tile
+    int extra;                       // tiles' worth of time that a unit's beginning and end take: so many places in the line that hold nothing
     bool whole;                      // units are not cut: each counts as one tile
     bool by_lanes;                   // up to 64 sequences, of fewer than 2^31 tiles
     bool once;                       // above 32 rows: keys and values are read past the caches
@@ -83,13 +84,13 @@ struct line {
         if (p.by_lanes) {
             if (lane < a.sequences) {
                 mine = a.context_lens[lane];
-                tiles = tiles_of(a, p, mine);
+                tiles = tiles_of(a, p, mine) + p.extra;
             }
             upto = sum_upto(tiles);
             total = (int64_t)__builtin_amdgcn_readlane(upto, 63) * units;
         } else {
             int64_t sum = 0;
-            for (int b = lane; b < a.sequences; b += 64) sum += tiles_of(a, p, a.context_lens[b]);
+            for (int b = lane; b < a.sequences; b += 64) sum += tiles_of(a, p, a.context_lens[b]) + p.extra;
             total = uniform(wave_sum64(sum)) * units;
         }
         per_block = quotient(total + p.blocks - 1, p.blocks);
@@ -99,7 +100,7 @@ struct line {
     __device__ int64_t begin(int b) const {
         if (p.by_lanes) return (int64_t)(__builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(tiles, b)) * units;
         int64_t before = 0;
-        for (int x = threadIdx.x & 63; x < b; x += 64) before += tiles_of(a, p, a.context_lens[x]);
+        for (int x = threadIdx.x & 63; x < b; x += 64) before += tiles_of(a, p, a.context_lens[x]) + p.extra;
         return uniform(wave_sum64(before)) * units;
     }
     // the sequence whose tiles the line has at `at`, and where they begin
@@ -114,7 +115,7 @@ struct line {
         }
         int64_t before = 0;
         for (int first = 0;; first += 64) {
-            const int b = first + lane, n = b < a.sequences ? tiles_of(a, p, a.context_lens[b]) : 0;
+            const int b = first + lane, n = b < a.sequences ? tiles_of(a, p, a.context_lens[b]) + p.extra : 0;
             int64_t upto = n;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
@@ -320,7 +321,7 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
     const line all(a, p);
     const int b = (int)(blockIdx.x / (unsigned)all.units), u = (int)blockIdx.x - b * all.units;
     const int context = all.context(b), tiles = tiles_of(a, p, context);
-    const int64_t begin = all.begin(b) + (int64_t)u * tiles, end = begin + tiles;
+    const int64_t begin = all.begin(b) + (int64_t)u * (tiles + p.extra), end = begin + tiles;
     const int64_t from = quotient(begin, all.per_block), to = quotient(end - 1, all.per_block);        // blocks that have pieces of it
     if (from == to) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.head_dim;
@@ -363,8 +364,8 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
 // eight sequences of 500 - 4095, groups of four: 49.8 -> 45.6 us; heads of 96, 160 rows, 32.6, in three 33.4)
 inline int rows_of_tile(int64_t rows, int head_dim) { return rows <= 64 || (rows > 128 && rows <= 192 && head_dim > 96) ? 64 : ROWS; }
 
-// The plan of a call whose blocks take `heads` key heads together (up to 32 rows a head; above, one), `tile` keys at a time.
-inline tree_plan plan_units(const fq_tree_args& a, int heads, int tile) {
+// The plan of a call whose blocks take `heads` key heads together (up to 32 rows a head; above, one), `tile` keys at a time; extra: see tree_plan.
+inline tree_plan plan_units(const fq_tree_args& a, int heads, int tile, int extra) {
     tree_plan p = {};
     p.group = a.q_heads / a.kv_heads;
     p.rows = a.nodes * p.group;      // (fq_tree_fits)
@@ -381,7 +382,8 @@ inline tree_plan plan_units(const fq_tree_args& a, int heads, int tile) {
     // blocks' worth of units (102 sequences of 223 tokens, 3 units each of 7 tiles: 24.4 -> 18.6 us; one of 250, 2 units of 8: 13.7, whole 18.8).
     const int64_t tiles = (a.table_width * a.cache.page_size + p.tile - 1) / p.tile, units = a.sequences * (a.kv_heads / p.heads) * p.row_tiles;
     p.whole = tiles <= (units >= 128 ? 8 : 4);
-    p.by_lanes = a.sequences <= 64 && a.sequences * tiles < INT32_MAX;
+    p.extra = p.whole ? 0 : extra;
+    p.by_lanes = a.sequences <= 64 && a.sequences * (tiles + p.extra) < INT32_MAX;
     p.blocks = 2 * fq_cu_count();
     p.factor = a.scale * LOG2E;
     return p;
