@@ -45,6 +45,19 @@ struct {
     decltype(&fq_attention_prompt_workspace_bytes) attention_prompt_workspace_bytes;
     decltype(&fq_attention_tree) attention_tree;
     decltype(&fq_attention_tree_workspace_bytes) attention_tree_workspace_bytes;
+    decltype(&fq_kv4_page_bytes) kv4_page_bytes;
+    decltype(&fq_kv4_write) kv4_write;
+    decltype(&fq_kv4_read) kv4_read;
+    decltype(&fq_attention_tree_kv4) attention_tree_kv4;
+    decltype(&fq_attention_tree_kv4_workspace_bytes) attention_tree_kv4_workspace_bytes;
+    decltype(&fq_pages_take) pages_take;
+    decltype(&fq_pages_fork) pages_fork;
+    decltype(&fq_pages_fork_workspace_bytes) pages_fork_workspace_bytes;
+    decltype(&fq_pages_free) pages_free;
+    decltype(&fq_pages_compact) pages_compact;
+    decltype(&fq_pages_compact_workspace_bytes) pages_compact_workspace_bytes;
+    decltype(&fq_adapters) adapters;
+    decltype(&fq_adapters_workspace_bytes) adapters_workspace_bytes;
 } lib;
 
 PyObject* fq_error;       // fq.FqError
@@ -414,45 +427,292 @@ PyObject* attention_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// the row stride of drafted tokens' queries [sequences, nodes, heads, head_dim] (of one token, or one sequence, the tensor's says nothing)
+int64_t drafted_rows(const at::Tensor& q) {
+    require(q.dim() == 4 && q.stride(3) == 1);
+    const int64_t B = q.size(0), nodes = q.size(1), row = B * nodes <= 1 ? 0 : nodes == 1 ? q.stride(0) : q.stride(1);
+    require((q.stride(0) == nodes * row || B <= 1) && q.size(2) <= INT_MAX && q.size(3) <= INT_MAX);
+    return row;
+}
+
+// page table, lengths and masks of them
+struct tree_inputs {
+    const int32_t *table, *lens;
+    int64_t width, stride = 0;
+    const uint64_t* mask = nullptr;
+    tree_inputs(PyObject* to, PyObject* lo, PyObject* mo, const at::Tensor& q) {
+        const at::Tensor &t = plain(to, at::kInt, q), &l = plain(lo, at::kInt, q);
+        const int64_t B = q.size(0), nodes = q.size(1), words = (nodes + 63) / 64;
+        require(t.dim() == 2 && t.size(0) == B && l.numel() == B);
+        table = (const int32_t*)t.data_ptr();
+        lens = (const int32_t*)l.data_ptr();
+        width = t.size(1);
+        if (mo == Py_None) return;
+        const at::Tensor& m = plain(mo, at::kLong, q);
+        const bool shared = m.dim() == 2;
+        require(shared ? m.size(0) == nodes && m.size(1) == words : m.dim() == 3 && m.size(0) == B && m.size(1) == nodes && m.size(2) == words);
+        mask = (const uint64_t*)m.data_ptr();
+        stride = shared ? 0 : nodes * words;
+    }
+};
+
 // attention_tree(q, k_cache, v_cache, page_table, context_lens, mask, scale, out, workspace)
 PyObject* attention_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         arguments(n, 9);
         const at::Tensor& q = tensor(a[0]);
         const int act = type16(q.scalar_type());
-        require(q.dim() == 4 && q.stride(3) == 1);
-        const int64_t B = q.size(0), nodes = q.size(1), hq = q.size(2), D = q.size(3);
-        // (of one token, or one sequence, the stride says nothing)
-        const int64_t row = B * nodes <= 1 ? 0 : nodes == 1 ? q.stride(0) : q.stride(1);
-        require((q.stride(0) == nodes * row || B <= 1) && hq <= INT_MAX && D <= INT_MAX);
+        const int64_t row = drafted_rows(q), B = q.size(0), nodes = q.size(1), hq = q.size(2), D = q.size(3);
         const at::Tensor& kc = tensor(a[1]);
         const int64_t hk = kc.dim() == 4 ? kc.size(2) : 0;
         require(hk <= INT_MAX);
         const fq_kv_pages cache = pages(a[1], a[2], q, hk, D);
-        const at::Tensor &table = plain(a[3], at::kInt, q), &lens = plain(a[4], at::kInt, q);
-        require(table.dim() == 2 && table.size(0) == B && lens.numel() == B);
-        const uint64_t* mask = nullptr;
-        int64_t stride = 0;
-        if (a[5] != Py_None) {
-            const at::Tensor& m = plain(a[5], at::kLong, q);
-            const int64_t words = (nodes + 63) / 64;
-            const bool shared = m.dim() == 2;
-            require(shared ? m.size(0) == nodes && m.size(1) == words : m.dim() == 3 && m.size(0) == B && m.size(1) == nodes && m.size(2) == words);
-            mask = (const uint64_t*)m.data_ptr();
-            stride = shared ? 0 : nodes * words;
-        }
+        const tree_inputs in(a[3], a[4], a[5], q);
         const float scale = given_scale(a[6]);
         at::Tensor out = output(a[7], q.sizes(), q), own;
         size_t size = 0;
-        const int64_t width = table.size(1);
-        void* ws = scratch_of(a[8], q, lib.attention_tree_workspace_bytes(B, nodes, (int)hq, (int)hk, (int)D, width, cache.page_size), &size, &own);
+        void* ws = scratch_of(a[8], q, lib.attention_tree_workspace_bytes(B, nodes, (int)hq, (int)hk, (int)D, in.width, cache.page_size), &size, &own);
         const fq_heads qh = {q.data_ptr(), row, q.stride(2)};
-        const int32_t *tp = (const int32_t*)table.data_ptr(), *lp = (const int32_t*)lens.data_ptr();
         void *op = out.data_ptr(), *s = stream();
         call("fq_attention_tree", [&] {
-            return lib.attention_tree(&qh, act, B, nodes, (int)hq, (int)hk, (int)D, &cache, tp, width, lp, mask, stride, scale, op, ws, size, s);
+            return lib.attention_tree(&qh, act, B, nodes, (int)hq, (int)hk, (int)D, &cache, in.table, in.width, in.lens, in.mask, in.stride, scale, op, ws, size, s);
         });
         return result(a[7], std::move(out));
+    });
+}
+
+// Whether a call's tensors lie on the device whose stream it goes to
+void here(const at::Tensor& t) { require(t.device().index() == c10::hip::current_device()); }
+
+// ------------------------------------------------------------------------------------------ a cache held in 4 bits
+fq_kv4_pages kv4_pages(PyObject* o, int page_size, int64_t kv_heads, int64_t head_dim, const at::Device& device) {
+    const at::Tensor& t = tensor(o);
+    require(t.dim() == 2 && t.scalar_type() == at::kByte && t.device() == device && t.stride(1) == 1 && kv_heads <= INT_MAX && head_dim <= INT_MAX);
+    const size_t bytes = lib.kv4_page_bytes(page_size, (int)kv_heads, (int)head_dim);
+    require(bytes > 0 && t.size(1) == (int64_t)bytes);
+    return {t.data_ptr(), t.size(0), page_size, t.stride(0)};
+}
+
+// kv4_write(k, v, cache, page_size, slots)
+PyObject* kv4_write(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 5);
+        const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]);
+        const int act = type16(k.scalar_type());
+        const fq_heads kh = heads(k), vh = heads(v);
+        require(v.sizes() == k.sizes() && v.scalar_type() == k.scalar_type() && v.device() == k.device() && k.size(0) > 0);
+        here(k);
+        const fq_kv4_pages cache = kv4_pages(a[2], integer(a[3]), k.size(1), k.size(2), k.device());
+        const at::Tensor& slots = plain(a[4], at::kLong, k);
+        require(slots.numel() == k.size(0));
+        const int64_t* at = (const int64_t*)slots.data_ptr();
+        const int64_t tokens = k.size(0);
+        const int hk = (int)k.size(1), D = (int)k.size(2);
+        void* s = stream();
+        call("fq_kv4_write", [&] { return lib.kv4_write(&kh, &vh, act, tokens, hk, D, &cache, at, s); });
+        Py_RETURN_TRUE;
+    });
+}
+
+// kv4_read(cache, page_size, kv_heads, head_dim, slots, dtype, k_out, v_out)
+PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 8);
+        const at::Tensor& slots = tensor(a[4]);
+        here(slots);
+        const int hk = integer(a[2]), D = integer(a[3]), act = scalar16(a[5]);
+        const fq_kv4_pages cache = kv4_pages(a[0], integer(a[1]), hk, D, slots.device());
+        require(slots.scalar_type() == at::kLong && slots.is_contiguous() && slots.numel() > 0);
+        const at::ScalarType type = act == 0 ? at::kHalf : at::kBFloat16;
+        const int64_t tokens = slots.numel();
+        at::Tensor out[2];
+        void* p[2];
+        for (int i = 0; i < 2; ++i) {
+            out[i] = a[6 + i] != Py_None ? plain(a[6 + i], type, slots) : empty({tokens, hk, D}, type, slots);
+            require(out[i].dim() == 3 && out[i].size(0) == tokens && out[i].size(1) == hk && out[i].size(2) == D);
+            p[i] = out[i].data_ptr();
+        }
+        const int64_t* at = (const int64_t*)slots.data_ptr();
+        void* s = stream();
+        call("fq_kv4_read", [&] { return lib.kv4_read(&cache, act, tokens, hk, D, at, p[0], p[1], s); });
+        PyObject* first = result(a[6], std::move(out[0]));
+        return Py_BuildValue("(NN)", first, result(a[7], std::move(out[1])));
+    });
+}
+
+// attention_tree_kv4(q, cache, page_size, kv_heads, page_table, context_lens, mask, scale, out, workspace)
+PyObject* attention_tree_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 10);
+        const at::Tensor& q = tensor(a[0]);
+        here(q);
+        const int act = type16(q.scalar_type()), hk = integer(a[3]);
+        const int64_t row = drafted_rows(q), B = q.size(0), nodes = q.size(1), hq = q.size(2), D = q.size(3);
+        const fq_kv4_pages cache = kv4_pages(a[1], integer(a[2]), hk, D, q.device());
+        const tree_inputs in(a[4], a[5], a[6], q);
+        const float scale = given_scale(a[7]);
+        at::Tensor out = output(a[8], q.sizes(), q), own;
+        size_t size = 0;
+        void* ws = scratch_of(a[9], q, lib.attention_tree_kv4_workspace_bytes(B, nodes, (int)hq, hk, (int)D, in.width, cache.page_size), &size, &own);
+        const fq_heads qh = {q.data_ptr(), row, q.stride(2)};
+        void *op = out.data_ptr(), *s = stream();
+        call("fq_attention_tree_kv4", [&] {
+            return lib.attention_tree_kv4(&qh, act, B, nodes, (int)hq, hk, (int)D, &cache, in.table, in.width, in.lens, in.mask, in.stride, scale, op, ws, size, s);
+        });
+        return result(a[8], std::move(out));
+    });
+}
+
+// ------------------------------------------------------------------------------------------ pages that sequences share
+// refs, table and lengths of a pool
+struct pool {
+    int32_t *refs, *table, *lens;
+    int64_t pages, rows, width;
+    at::Tensor like;
+    pool(PyObject* ro, PyObject* to, PyObject* lo) {
+        const at::Tensor& r = tensor(ro);
+        here(r);
+        const at::Tensor &t = plain(to, at::kInt, r), &l = plain(lo, at::kInt, r);
+        require(r.scalar_type() == at::kInt && r.is_contiguous() && r.dim() == 1 && t.dim() == 2 && l.numel() == t.size(0));
+        refs = (int32_t*)r.data_ptr();
+        table = (int32_t*)t.data_ptr();
+        lens = (int32_t*)l.data_ptr();
+        pages = r.size(0);
+        rows = t.size(0);
+        width = t.size(1);
+        like = r;
+    }
+};
+
+// one tensor [tensors, pages, ...], or a list or tuple of up to 256 tensors [pages, ...]
+struct page_buffers {
+    fq_page_buffer at[256];
+    int count = 0;
+    void add(const at::Tensor& t, int dims, const pool& p) {
+        require(t.dim() > dims && t.size(dims - 1) == p.pages && t.device() == p.like.device());
+        const int64_t size = t.element_size();
+        int64_t expected = 1;
+        for (int64_t d = t.dim() - 1; d >= dims; --d) {
+            require(t.size(d) == 1 || t.stride(d) == expected);
+            expected *= t.size(d);
+        }
+        at[count++] = {t.data_ptr(), dims == 2 ? t.size(0) : 1, dims == 2 ? t.stride(0) * size : 0, t.stride(dims - 1) * size, expected * size};
+    }
+    page_buffers(PyObject* o, const pool& p) {
+        if (PyList_CheckExact(o) || PyTuple_CheckExact(o)) {
+            const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+            require(n <= 256);
+            for (Py_ssize_t i = 0; i < n; ++i) add(tensor(PySequence_Fast_GET_ITEM(o, i)), 1, p);
+        } else {
+            add(tensor(o), 2, p);
+        }
+    }
+};
+
+// pages_take(refs, page_size, page_table, lens, wanted)
+PyObject* pages_take(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 5);
+        const pool p(a[0], a[2], a[3]);
+        const int page = integer(a[1]);
+        const at::Tensor& wanted = plain(a[4], at::kInt, p.like);
+        require(wanted.numel() == p.rows);
+        const int32_t* w = (const int32_t*)wanted.data_ptr();
+        void* s = stream();
+        call("fq_pages_take", [&] { return lib.pages_take(p.refs, p.pages, page, p.table, p.rows, p.width, p.lens, w, s); });
+        Py_RETURN_TRUE;
+    });
+}
+
+// pages_fork(refs, page_size, page_table, lens, parents, buffers, release, table_out, lens_out, workspace)
+PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 10);
+        const pool p(a[0], a[2], a[3]);
+        const int page = integer(a[1]), release = truth(a[6]);
+        const at::Tensor& parents = plain(a[4], at::kInt, p.like);
+        const page_buffers buffers(a[5], p);
+        const int64_t children = parents.numel();
+        at::Tensor table = output(a[7], {children, p.width}, p.like), lens = output(a[8], {children}, p.like), own;
+        size_t size = 0;
+        void* ws = scratch_of(a[9], p.like, lib.pages_fork_workspace_bytes(p.rows, children), &size, &own);
+        const int32_t* from = (const int32_t*)parents.data_ptr();
+        int32_t *t = (int32_t*)table.data_ptr(), *l = (int32_t*)lens.data_ptr();
+        void* s = stream();
+        call("fq_pages_fork", [&] {
+            return lib.pages_fork(p.refs, p.pages, page, p.table, p.rows, p.width, p.lens, from, children, release, t, l, buffers.at, buffers.count, ws, size, s);
+        });
+        PyObject* first = result(a[7], std::move(table));
+        return Py_BuildValue("(NN)", first, result(a[8], std::move(lens)));
+    });
+}
+
+// pages_free(refs, page_size, page_table, lens, rows)
+PyObject* pages_free(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 5);
+        const pool p(a[0], a[2], a[3]);
+        const int page = integer(a[1]);
+        const int32_t* which = nullptr;
+        int64_t count = 0;
+        if (a[4] != Py_None) {
+            const at::Tensor& w = plain(a[4], at::kInt, p.like);
+            count = w.numel();
+            require(count > 0);
+            which = (const int32_t*)w.data_ptr();
+        }
+        void* s = stream();
+        call("fq_pages_free", [&] { return lib.pages_free(p.refs, p.pages, page, p.table, p.rows, p.width, p.lens, which, count, s); });
+        Py_RETURN_TRUE;
+    });
+}
+
+// pages_compact(refs, page_size, page_table, lens, buffers, workspace)
+PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 6);
+        const pool p(a[0], a[2], a[3]);
+        const int page = integer(a[1]);
+        const page_buffers buffers(a[4], p);
+        at::Tensor own;
+        size_t size = 0;
+        void* ws = scratch_of(a[5], p.like, lib.pages_compact_workspace_bytes(p.pages), &size, &own);
+        void* s = stream();
+        call("fq_pages_compact",
+             [&] { return lib.pages_compact(p.refs, p.pages, page, p.table, p.rows, p.width, p.lens, buffers.at, buffers.count, ws, size, s); });
+        Py_RETURN_TRUE;
+    });
+}
+
+// ------------------------------------------------------------------------------------------ low-rank adapters
+// adapters(x, a, b, ids, out, scales, workspace)
+PyObject* adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 7);
+        const at::Tensor &x = tensor(a[0]), &out = tensor(a[4]);
+        here(x);
+        const int act = type16(x.scalar_type());
+        const at::Tensor &A = plain(a[1], x.scalar_type(), x), &B = plain(a[2], x.scalar_type(), x), &ids = plain(a[3], at::kInt, x);
+        require(x.dim() == 2 && out.dim() == 2 && A.dim() == 3 && B.dim() == 3 && x.stride(1) == 1 && out.stride(1) == 1);
+        const int64_t rows = x.size(0), K = x.size(1), count = A.size(0), rank = A.size(1), N = B.size(1);
+        require(out.scalar_type() == x.scalar_type() && out.device() == x.device() && A.size(2) == K && B.size(0) == count && B.size(2) == rank &&
+                out.size(0) == rows && out.size(1) == N && ids.numel() == rows && rank <= INT_MAX);
+        const float* scales = nullptr;
+        if (a[5] != Py_None) {
+            const at::Tensor& t = plain(a[5], at::kFloat, x);
+            require(t.numel() == count);
+            scales = (const float*)t.data_ptr();
+        }
+        at::Tensor own;
+        size_t size = 0;
+        void* ws = scratch_of(a[6], x, lib.adapters_workspace_bytes(rows, count, (int)rank, N, K), &size, &own);
+        const void *xp = x.data_ptr(), *ap = A.data_ptr(), *bp = B.data_ptr();
+        const int32_t* ip = (const int32_t*)ids.data_ptr();
+        const int64_t xs = x.stride(0), os = out.stride(0);
+        void *op = out.data_ptr(), *s = stream();
+        call("fq_adapters", [&] { return lib.adapters(xp, xs, act, rows, N, K, ap, bp, count, (int)rank, ip, scales, op, os, ws, size, s); });
+        Py_INCREF(a[4]);
+        return a[4];
     });
 }
 
@@ -480,7 +740,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FQ_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FQ_METHOD(gemm),     FQ_METHOD(gemm_grouped),  FQ_METHOD(quantize_act_i8), FQ_METHOD(gemm_w4a8),
                          FQ_METHOD(quantize), FQ_METHOD(quantize_w4a8), FQ_METHOD(qk_norm_rope),    FQ_METHOD(attention_prompt),
-                         FQ_METHOD(attention_tree), FQ_METHOD(bind),    {nullptr, nullptr, 0, nullptr}};
+                         FQ_METHOD(attention_tree), FQ_METHOD(kv4_write),     FQ_METHOD(kv4_read),        FQ_METHOD(attention_tree_kv4),
+                         FQ_METHOD(pages_take), FQ_METHOD(pages_fork),   FQ_METHOD(pages_free),      FQ_METHOD(pages_compact),
+                         FQ_METHOD(adapters), FQ_METHOD(bind),           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fqcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -59,13 +59,15 @@ __device__ __forceinline__ uint32_t codes16(uint32_t x) {
     else
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 512.0f, HIGH));
 }
-// code (-7 .. 7) as sign and magnitude in bits 7, 2 .. 0
-__device__ __forceinline__ uint32_t coded(float q) {
-    const uint32_t m = (uint32_t)__builtin_fabsf(q);
-    return m | (q < 0.0f ? 0x80u : 0u);
+// Four codes (-7 .. 7) as bytes, sign and magnitude in bits 7, 2 .. 0 (the sign of a zero is anything)
+__device__ __forceinline__ uint32_t coded(const float* q) {
+    uint32_t x = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_cvt_pk_u8_f32(__builtin_fabsf(q[i]), i, x);
+    const uint32_t low = __builtin_amdgcn_perm(__float_as_uint(q[1]), __float_as_uint(q[0]), 0x0c0c0703u),
+                   high = __builtin_amdgcn_perm(__float_as_uint(q[3]), __float_as_uint(q[2]), 0x07030c0cu);       // their top bytes
+    return x | ((low | high) & 0x80808080u);
 }
-// its place as second code of the byte
-__device__ __forceinline__ uint32_t as_second(uint32_t c) { return (c & 7u) << 3 | (c & 0x80u) >> 1; }
 // the code (of bits 7, 2 .. 0) as a number
 __device__ __forceinline__ float decoded(uint32_t c) {
     const float m = (float)(c & 7u);
@@ -89,11 +91,14 @@ struct group_scale {
         return s;
     }
     __device__ float value() const { return __builtin_amdgcn_ldexpf(n, k); }
-    // the code of w, |w| <= m: the nearest number, halves to even, and 7 for 7.5
-    __device__ float code(float w) const {
-        if (n == 0.0f) return 0.0f;
-        const float q = __builtin_rintf(__builtin_amdgcn_ldexpf(w, -k) / n);
-        return __builtin_fminf(__builtin_fmaxf(q, -7.0f), 7.0f);
+    // What code() multiplies values times 2^-k with
+    __device__ float inverse() const { return n == 0.0f ? 0.0f : 1.0f / n; }
+    // The code of w, |w| <= m: the nearest number to w / s, halves to even, and 7 for 7.5.  w 2^-k times 1 / n is off by less than 2^-19.  The
+    // quotient is a half exactly or 2^-12 away from one (values have 11 bits, n 8), so that the addition, which leaves multiples of 2^-16,
+    // makes halves exact and takes nothing else to the other side of one.
+    __device__ float code(float w, float inverse) const {
+        const float x = __builtin_amdgcn_ldexpf(w, -k) * inverse + 128.0f;
+        return __builtin_amdgcn_fmed3f(__builtin_rintf(x - 128.0f), -7.0f, 7.0f);
     }
 };
 #endif

@@ -85,17 +85,16 @@ __global__ __launch_bounds__(256) void fq_kv4_write_kernel(fq_kv4_args a) {
         m = __builtin_fmaxf(m, __shfl_xor(m, 8));
         const bool sound = m < __builtin_inff();
         const group_scale s = group_scale::of<ACT>(sound ? m : 0.0f);
-        uint32_t c[8];
+        const float inverse = s.inverse();
+        float q[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = coded(sound ? s.code(w[i]) : 0.0f);
+        for (int i = 0; i < 8; ++i) q[i] = sound ? s.code(w[i], inverse) : 0.0f;
         char* to = f.record + head * head_bytes;
         const bool put = in && f.there;
         if (part == 0 && put) *(T*)(to + (values ? 32 * S : 0) + scale_at(S, f.at, g)) = (T)(sound ? s.value() : __builtin_nanf(""));
         // Keys: the lane's codes are a word.  Values: first codes are half the lanes', second codes the other half's, of the same places; each
         // lane of such two makes four bytes of them.
-        uint32_t low = 0, high = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) low |= c[i] << 8 * i, high |= c[4 + i] << 8 * i;
+        const uint32_t low = coded(q), high = coded(q + 4);
         const uint32_t other = __shfl_xor(part < 2 ? high : low, 8);
         const uint32_t one = values ? (part < 2 ? low : other) : low, two = values ? (part < 2 ? other : high) : high;
         const uint32_t word = one | (two & 0x07070707u) << 3 | (two & 0x80808080u) >> 1;

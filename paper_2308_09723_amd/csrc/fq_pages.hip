@@ -8,6 +8,7 @@
 // all of a fork's bookkeeping in one kernel; the copies are a second one, since they want the whole card.
 #include <hip/hip_runtime.h>
 
+#include "fq_attn.h"
 #include "fq_internal.h"
 
 namespace {
@@ -127,8 +128,8 @@ __device__ inline void fork_entries(const fq_fork_args& a, int64_t at, int64_t s
     }
 }
 
-// Pages for the children whose last one is not whole and not their parent's own
-__device__ inline void fork_last(const fq_fork_args& a, int* sums) {
+// Children whose last page is not whole and not their parent's own: listed in from[], in their order
+__device__ inline int fork_wanted(const fq_fork_args& a, int* sums) {
     int wanted = 0;
     for (int base = 0; base < a.children; base += THREADS) {
         const int i = base + threadIdx.x;
@@ -143,6 +144,10 @@ __device__ inline void fork_last(const fq_fork_args& a, int* sums) {
         wanted += all;
     }
     __syncthreads();
+    return wanted;
+}
+// Pages for them
+__device__ inline void fork_last(const fq_fork_args& a, int* sums, int wanted) {
     const int found = each_free(a.refs, a.pages, wanted, sums, [&](int k, int64_t p) {
         const int i = a.from[k];
         const child_of c(a, i);
@@ -164,14 +169,80 @@ __device__ inline void fork_last(const fq_fork_args& a, int* sums) {
     if (threadIdx.x == 0) *a.moves = found;
 }
 
-// All of it by one block: 4 beams of 49 pages 6 us, 256 rows of 32 pages
-__global__ __launch_bounds__(THREADS) void fq_pages_fork_kernel(fq_fork_args a) {
+// All of it by one block, up to SMALL children and rows: what becomes of each is worked out once, and the entries' reads do not wait for each other.
+constexpr int SMALL = 1024;
+__global__ __launch_bounds__(THREADS) void fq_pages_fork_kernel(fq_fork_args a, fqa::divisor by_width) {
     __shared__ int sums[THREADS / 64 + 1];
-    fork_first(a);
+    __shared__ int first[SMALL];                    // child of each row
+    __shared__ int whole[SMALL], source[SMALL];     // of a child: full pages; its parent, -1 - its parent where the last page passes to it, INT32_MIN: none
+    constexpr int EACH = 8;
+    const int t = threadIdx.x, width = (int)a.width, used_by = t < a.rows ? pages_of(a.lens[t], a.page_size) : 0;
+    first[t] = INT32_MAX;
     __syncthreads();
-    fork_entries(a, threadIdx.x, THREADS);
+    bool wants = false;
+    if (t < a.children) {
+        const child_of c(a, t);
+        const bool there = c.parent >= 0 && c.parent < a.rows;
+        if (there) atomicMin(&first[c.parent], t);
+        whole[t] = c.whole;
+        a.lens_out[t] = c.len;
+        source[t] = there ? c.parent : INT32_MIN;
+        wants = c.part;
+    }
     __syncthreads();
-    fork_last(a, sums);
+    if (wants && a.release && first[source[t]] == t) {
+        source[t] = -1 - source[t];
+        wants = false;
+    }
+    const int passed = t < a.rows && first[t] != INT32_MAX ? 1 : 0;
+    // pages of old rows that are given up: all but one that is not full and has passed
+    __syncthreads();
+    const int entries = a.children * width;
+    for (int e0 = t; e0 < entries; e0 += THREADS * EACH) {
+        int32_t page[EACH];
+#pragma unroll
+        for (int y = 0; y < EACH; ++y) {
+            const int e = e0 + y * THREADS;
+            page[y] = -1;
+            if (e >= entries) continue;
+            const int i = by_width.quotient(e), j = e - i * width, from = source[i];
+            if (from != INT32_MIN && (j < whole[i] || (from < 0 && j == whole[i]))) page[y] = a.table[(from < 0 ? -1 - from : from) * width + j];
+        }
+#pragma unroll
+        for (int y = 0; y < EACH; ++y) {
+            const int e = e0 + y * THREADS;
+            if (e >= entries) continue;
+            const int i = by_width.quotient(e), j = e - i * width;
+            if (j < whole[i]) refer(a.refs, a.pages, page[y], 1);
+            a.table_out[e] = page[y];
+        }
+    }
+    if (a.release) {
+        __syncthreads();                            // (whole has been read)
+        const int len = t < a.rows ? a.lens[t] : 0;
+        if (t < a.rows) whole[t] = passed && len > 0 && len % a.page_size != 0 ? used_by - 1 : used_by;
+        __syncthreads();
+        const int old = a.rows * width;
+        for (int e0 = t; e0 < old; e0 += THREADS * EACH) {
+            int32_t page[EACH];
+#pragma unroll
+            for (int y = 0; y < EACH; ++y) {
+                const int e = e0 + y * THREADS;
+                page[y] = -1;
+                if (e >= old) continue;
+                const int r = by_width.quotient(e);
+                if (e - r * width < whole[r]) page[y] = a.table[e];
+            }
+#pragma unroll
+            for (int y = 0; y < EACH; ++y) refer(a.refs, a.pages, page[y], -1);
+        }
+    }
+    __syncthreads();
+    int wanted;
+    const int k = sum_before(wants, sums, &wanted);
+    if (wants) a.from[k] = t;                       // (for now: who wants a page)
+    __syncthreads();
+    fork_last(a, sums, wanted);
 }
 __global__ __launch_bounds__(THREADS) void fq_pages_fork_first_kernel(fq_fork_args a) { fork_first(a); }
 __global__ __launch_bounds__(256) void fq_pages_fork_entries_kernel(fq_fork_args a) {
@@ -179,7 +250,7 @@ __global__ __launch_bounds__(256) void fq_pages_fork_entries_kernel(fq_fork_args
 }
 __global__ __launch_bounds__(THREADS) void fq_pages_fork_last_kernel(fq_fork_args a) {
     __shared__ int sums[THREADS / 64 + 1];
-    fork_last(a, sums);
+    fork_last(a, sums, fork_wanted(a, sums));
 }
 
 // ------------------------------------------------------------------------------------------ taking and freeing
@@ -357,8 +428,8 @@ int fq_launch_pages_copy(const fq_page_buffer* buffers, int count, fq_copy_args 
 
 int fq_launch_pages_fork(const fq_fork_args& a, hipStream_t stream) {
     const int64_t entries = ((int64_t)a.children + (a.release ? a.rows : 0)) * a.width;
-    if (entries <= 32 * THREADS) {
-        fq_pages_fork_kernel<<<1, THREADS, 0, stream>>>(a);
+    if (entries <= 64 * THREADS && a.children <= SMALL && a.rows <= SMALL && a.width > 0) {
+        fq_pages_fork_kernel<<<1, THREADS, 0, stream>>>(a, fqa::divisor::of((uint32_t)a.width));
         return status();
     }
     fq_pages_fork_first_kernel<<<1, THREADS, 0, stream>>>(a);

@@ -469,7 +469,9 @@ NATIVE_PATH = os.path.join(_HERE, "_fqcall.so")
 _NATIVE_FUNCTIONS = ("fq_gemm_sf", "fq_gemm_workspace_bytes", "fq_gemm_grouped_sf", "fq_gemm_w4a8", "fq_gemm_w4a8_workspace_bytes",
                      "fq_quantize_act_i8", "fq_quantize_sf", "fq_quantize_w4a8", "fq_codes_bytes", "fq_scales_bytes", "fq_zscale_bytes",
                      "fq_qk_norm_rope", "fq_attention_prompt", "fq_attention_prompt_workspace_bytes", "fq_attention_tree",
-                     "fq_attention_tree_workspace_bytes")
+                     "fq_attention_tree_workspace_bytes", "fq_kv4_page_bytes", "fq_kv4_write", "fq_kv4_read", "fq_attention_tree_kv4",
+                     "fq_attention_tree_kv4_workspace_bytes", "fq_pages_take", "fq_pages_fork", "fq_pages_fork_workspace_bytes", "fq_pages_free",
+                     "fq_pages_compact", "fq_pages_compact_workspace_bytes", "fq_adapters", "fq_adapters_workspace_bytes")
 _native = None
 
 
@@ -893,6 +895,11 @@ def attention_tree(q, k_cache, v_cache, page_table, context_lens, mask=None, sca
     return o
 
 
+def _here(t, where):
+    """The call goes to the current device's stream: its tensors have to lie there."""
+    _require(t.is_cuda and t.device.index == _device(), where)
+
+
 # ------------------------------------------------------------------ a cache held in 4 bits
 def kv4_cache(pages, page_size, kv_heads, head_dim, device="cuda"):
     """Pages of a cache held in 4 bits: uint8 [pages, kv4_page_bytes(...)], zeros (which stand for zeros)."""
@@ -919,8 +926,11 @@ def kv4_write(k, v, cache, page_size, slots):
     uint8 [pages, kv4_page_bytes(page_size, kv_heads, head_dim)] (kv4_cache), slots int64 [tokens] (slot s: place s % page_size of page
     s // page_size; one outside the cache is not written)."""
     torch = _torch_mod or _torch()
+    if _native.kv4_write(k, v, cache, page_size, slots):
+        return
     where = "fq_kv4_write"
     act = _act_code(k)
+    _here(k, where)
     hk, hv = _heads(k, where), _heads(v, where)
     _require(v.shape == k.shape and v.dtype == k.dtype and v.device == k.device, where)
     tokens, kv_heads, D = k.shape
@@ -934,7 +944,11 @@ def kv4_read(cache, page_size, kv_heads, head_dim, slots, dtype, k_out=None, v_o
     """What a cache held in 4 bits has in slots (int64 [tokens]; zeros for one outside it): (k, v), each [tokens, kv_heads, head_dim] of dtype, the
     type that was written."""
     torch = _torch_mod or _torch()
+    done = _native.kv4_read(cache, page_size, kv_heads, head_dim, slots, dtype, k_out, v_out)
+    if done is not None:
+        return done
     where = "fq_kv4_read"
+    _here(slots, where)
     pages = _kv4_pages(cache, page_size, kv_heads, head_dim, slots.device, where)
     _plain(slots, torch.int64, cache.device, where)
     like = torch.empty(0, dtype=dtype, device=cache.device) if k_out is None else k_out
@@ -949,8 +963,14 @@ def kv4_read(cache, page_size, kv_heads, head_dim, slots, dtype, k_out=None, v_o
 def attention_tree_kv4(q, cache, page_size, kv_heads, page_table, context_lens, mask=None, scale=None, out=None, workspace=None):
     """attention_tree over a cache held in 4 bits (kv4_cache, written by kv4_write as q's type): its arguments and result, with the cache's pages, their
     size and their heads in the place of the caches.  workspace: attention_tree_kv4_workspace_bytes."""
+    if _torch_mod is None:
+        _torch()
+    done = _native.attention_tree_kv4(q, cache, page_size, kv_heads, page_table, context_lens, mask, scale, out, workspace)
+    if done is not None:
+        return done
     where = "fq_attention_tree_kv4"
     act, sequences, nodes, heads, D, row = _drafted(q, where)
+    _here(q, where)
     pages = _kv4_pages(cache, page_size, kv_heads, D, q.device, where)
     stride = _tree_of(q, page_table, context_lens, mask, where)
     scale = _given_scale(scale, where)
@@ -986,7 +1006,8 @@ def _page_buffers(buffers, pages, device, where):
 def _pool(refs, page_table, lens, where):
     """Number of pages, rows and width of a pool and a table, having looked at them."""
     torch = _torch_mod or _torch()
-    _require(refs.is_cuda and refs.dim() == 1 and page_table.dim() == 2 and lens.numel() == page_table.shape[0], where)
+    _here(refs, where)
+    _require(refs.dim() == 1 and page_table.dim() == 2 and lens.numel() == page_table.shape[0], where)
     for t in (refs, page_table, lens):
         _plain(t, torch.int32, refs.device, where)
     return refs.shape[0], page_table.shape[0], page_table.shape[1]
@@ -997,6 +1018,7 @@ def pages_copy(buffers, from_pages, to_pages):
     contiguous within a page.  A pair with a page outside the pool (-1) is left out."""
     torch = _torch_mod or _torch()
     where = "fq_pages_copy"
+    _here(from_pages, where)
     _require(from_pages.numel() == to_pages.numel(), where)
     for t in (from_pages, to_pages):
         _plain(t, torch.int32, from_pages.device, where)
@@ -1012,6 +1034,8 @@ def pages_take(refs, page_size, page_table, lens, wanted):
     """Free pages for rows of page_table (int32 [rows, width]) that are to grow from lens to wanted tokens (int32 [rows]); refs int32 [pages]: the rows that
     hold each page.  All are changed in place; lens tells which rows got what they wanted."""
     torch = _torch_mod or _torch()
+    if _native.pages_take(refs, page_size, page_table, lens, wanted):
+        return
     where = "fq_pages_take"
     pages, rows, width = _pool(refs, page_table, lens, where)
     _require(wanted.numel() == rows, where)
@@ -1024,6 +1048,9 @@ def pages_fork(refs, page_size, page_table, lens, parents, buffers=(), release=F
     changed in place), one that is not full is copied in the buffers (as pages_copy's).  release: the old rows are given up, and the first child of each takes
     its last page over.  A child that there is no page for has length -1.  workspace: pages_fork_workspace_bytes."""
     torch = _torch_mod or _torch()
+    done = _native.pages_fork(refs, page_size, page_table, lens, parents, buffers, release, table_out, lens_out, workspace)
+    if done is not None:
+        return done
     where = "fq_pages_fork"
     pages, rows, width = _pool(refs, page_table, lens, where)
     _plain(parents, torch.int32, refs.device, where)
@@ -1039,6 +1066,8 @@ def pages_fork(refs, page_size, page_table, lens, parents, buffers=(), release=F
 def pages_free(refs, page_size, page_table, lens, rows=None):
     """Rows (int32; None: all) of page_table give their pages up: refs, entries (-1) and lens (0) are changed in place."""
     torch = _torch_mod or _torch()
+    if _native.pages_free(refs, page_size, page_table, lens, rows):
+        return
     where = "fq_pages_free"
     pages, count, width = _pool(refs, page_table, lens, where)
     if rows is not None:
@@ -1052,6 +1081,10 @@ def pages_free(refs, page_size, page_table, lens, rows=None):
 def pages_compact(refs, page_size, page_table, lens, buffers=(), workspace=None):
     """Gathers the pool's used pages at its beginning: refs and page_table (all rows that hold pages) are changed in place, pages copied in the buffers (as
     pages_copy's).  workspace: pages_compact_workspace_bytes."""
+    if _torch_mod is None:
+        _torch()
+    if _native.pages_compact(refs, page_size, page_table, lens, buffers, workspace):
+        return
     where = "fq_pages_compact"
     pages, rows, width = _pool(refs, page_table, lens, where)
     array_of = _page_buffers(buffers, pages, refs.device, where)
@@ -1066,9 +1099,13 @@ def adapters(x, a, b, ids, out, scales=None, workspace=None):
     (float16 or bfloat16, rows any stride apart), a [adapters, rank, K], b [adapters, N, rank], ids int32 [rows] (-1: none), out [rows, N] (rows any stride
     apart), scales float32 [adapters] (None: 1).  workspace: adapters_workspace_bytes."""
     torch = _torch_mod or _torch()
+    done = _native.adapters(x, a, b, ids, out, scales, workspace)
+    if done is not None:
+        return done
     where = "fq_adapters"
     act = _act_code(x)
-    _require(x.is_cuda and x.dim() == 2 and out.dim() == 2 and a.dim() == 3 and b.dim() == 3, where)
+    _here(x, where)
+    _require(x.dim() == 2 and out.dim() == 2 and a.dim() == 3 and b.dim() == 3, where)
     (rows, K), (count, rank, _), N = x.shape, a.shape, b.shape[1]
     _require((x.stride(1) == 1 or K <= 1) and (out.stride(1) == 1 or N <= 1) and out.dtype == x.dtype and out.device == x.device, where)
     _require(tuple(a.shape) == (count, rank, K) and tuple(b.shape) == (count, N, rank) and tuple(out.shape) == (rows, N) and ids.numel() == rows, where)
