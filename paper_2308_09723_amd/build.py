@@ -73,7 +73,7 @@ NO_SPILL = [
 # (whose loads into LDS a wait for a reload would drain).
 NO_SPILL_FAMILIES = ["fq_gemm_mid_kernel", "fq_gemm_mid_items_kernel", "fq_w4a8_mid_kernel", "fq_attention_prompt_kernel",
                      "fq_attention_tree_stream_kernel", "fq_attention_tree_tile_kernel", "fq_attention_kv4_stream_kernel",
-                     "fq_attention_kv4_tile_kernel", "fq_adapter_down_kernel", "fq_adapter_up_kernel"]
+                     "fq_attention_kv4_tile_kernel", "fq_adapter_down_few_kernel", "fq_adapter_down_kernel", "fq_adapter_up_kernel"]
 
 
 def _run(cmd):

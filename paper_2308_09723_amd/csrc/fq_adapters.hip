@@ -1,43 +1,40 @@
 // Low-rank adapters of many requests beside a shared product (fq_adapters): out[m] += scale[id] (x[m] A[id]^T) B[id]^T for the adapter id of each row.
 //
-// Two kernels: t = x A^T in binary32, K split over blocks (each leaves partial sums), then out += scale t B^T.  Both take 16 rows at a time as the
-// columns of 16 x 16 x 32 products, so that a lane's results are all one row's and a row takes those of its own adapter, whatever
-// others hold: for each of a tile's different adapters the products are made for all rows.  (Requests' rows lie side by side, so that a tile
-// of a prompt has one or two; single tokens have one each, and their adapters' bytes bind them, not the products.)
+// t = x A^T in binary32, K split over blocks (each leaves partial sums), then out += scale t B^T.  Products are made for each of a tile's different
+// adapters and all its rows, and a row takes those of its own adapter, whatever others hold.  (Requests' rows lie side by side, so that
+// a tile of a prompt has one or two.)
 //
-// t goes into the second product as the sum of two 16-bit numbers (16 bits and more of it), in binary16 after a division by a power of
-// two that brings the row's largest to about one: nothing is lost that the result's rounding would keep.
+// Up to FEW rows each is likely to have an adapter of its own, whose bytes bind it: the first kernel takes 16 rows as the columns of products of
+// 16 x 16 x 32, the second makes dot products, eight ranks a lane.
+// More rows: 64 a block, everything through LDS, in pieces that neighbouring lanes read side by side (a load of 64 rows' 16 bytes takes the
+// address unit four times as long as one of four rows' 256).  t goes into the second product as the sum of two 16-bit numbers (16 bits and
+// more of it), in binary16 after a division by a power of two that brings the row's largest to about one.
 //
 // Bound by memory: A and B of each adapter, x once, the output twice.
 #include <hip/hip_runtime.h>
+#include <atomic>
 
+#include "fq_attn_tile.h"
 #include "fq_internal.h"
+#include "fq_lds_limit.h"
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+using fqa::f32x4;
+using fqa::load_lds16;
+using fqa::pack2;
+using fqa::type16;
+using fqa::u32x2;
+using fqa::u32x4;
 
-template <int ACT> struct type16;
-template <> struct type16<FQ_F16> { typedef _Float16 t; };
-template <> struct type16<FQ_BF16> { typedef __bf16 t; };
+constexpr int FEW = 64;              // rows
 
 template <int ACT>
 __device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, const f32x4& c) {
     if constexpr (ACT == FQ_F16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fqa::f16x8, a), __builtin_bit_cast(fqa::f16x8, b), c, 0, 0, 0);
     else
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-template <int ACT>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-    typedef typename type16<ACT>::t T;
-    typedef T vec2 __attribute__((ext_vector_type(2)));
-    const f32x2 x = {a, b};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, vec2));
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(fqa::bf16x8, a), __builtin_bit_cast(fqa::bf16x8, b), c, 0, 0, 0);
 }
 template <int ACT, int HIGH>
 __device__ __forceinline__ float half_of(uint32_t x) {
@@ -70,37 +67,35 @@ __device__ __forceinline__ int id_of(const fq_adapter_args& a, int64_t row) {
     return id >= 0 && id < a.adapters ? id : -1;
 }
 
-// ------------------------------------------------------------------------------------------ t = x A^T
-// MT x 16 rows, RT x 16 values of t, one of blockIdx.y's turns of the tile's adapters, one of gridDim.x parts of K, which the block's four waves share out
+// ------------------------------------------------------------------------------------------ t = x A^T, few rows
+// 16 rows, RT x 16 values of t, one of blockIdx.y's turns of the tile's adapters, one of gridDim.x parts of K, which the block's four waves share out
 // step by step of 32.  Results: partial[part][row][rank, rounded up to 16].
 // (Two waves a SIMD at least, here and below: with them the compiler keeps the sums in ordinary registers.  Where they went to accumulation registers it
 // read the first of them behind the loop without waiting for the last product.)
-template <int ACT, int MT, int RT>
-__global__ __launch_bounds__(256, 2) void fq_adapter_down_kernel(fq_adapter_args a) {
+template <int ACT, int RT>
+__global__ __launch_bounds__(256, 2) void fq_adapter_down_few_kernel(fq_adapter_args a) {
     constexpr int WAVES = 4, AHEAD = 4;
-    __shared__ f32x4 sums[WAVES - 1][MT * RT][64];
+    __shared__ f32x4 sums[WAVES - 1][RT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4, x16 = lane & 15;
-    const int64_t row0 = (int64_t)blockIdx.z * (16 * MT);
+    const int64_t row = (int64_t)blockIdx.z * 16 + x16;
     const int ranks = (a.rank + 15) / 16 * 16, steps = (a.K + 31) / 32;
     const int part = blockIdx.x, each = (steps + (int)gridDim.x - 1) / (int)gridDim.x, begin = part * each, end = min(steps, begin + each);
-    distinct tile(id_of(a, lane < 16 * MT ? row0 + lane : a.rows));
-    const int mine[4] = {__shfl(tile.id, x16), __shfl(tile.id, (16 + x16) & 63), __shfl(tile.id, (32 + x16) & 63), __shfl(tile.id, (48 + x16) & 63)};
+    distinct tile(id_of(a, lane < 16 ? row : a.rows));
+    const int mine = __shfl(tile.id, x16);
+    const uint16_t* x = (const uint16_t*)a.x + min(row, a.rows - 1) * a.x_stride + 8 * h;
     int turn = 0;
     for (int id = tile.next(); id >= 0; id = tile.next(), ++turn) {
         if (turn % (int)gridDim.y != (int)blockIdx.y) continue;
         for (int r0 = 0; r0 < ranks; r0 += 16 * RT) {
-            const uint16_t *x[MT], *w[RT];
+            const uint16_t* w[RT];
+            f32x4 t[RT];
 #pragma unroll
-            for (int m = 0; m < MT; ++m) x[m] = (const uint16_t*)a.x + min(row0 + 16 * m + x16, a.rows - 1) * a.x_stride + 8 * h;
-#pragma unroll
-            for (int r = 0; r < RT; ++r) w[r] = (const uint16_t*)a.a + ((int64_t)id * a.rank + min(r0 + 16 * r + x16, a.rank - 1)) * a.K + 8 * h;
-            f32x4 t[MT][RT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int r = 0; r < RT; ++r) t[m][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int r = 0; r < RT; ++r) {
+                w[r] = (const uint16_t*)a.a + ((int64_t)id * a.rank + min(r0 + 16 * r + x16, a.rank - 1)) * a.K + 8 * h;
+                t[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            }
             for (int s = begin + wave; s < end; s += WAVES * AHEAD) {
-                u32x4 xs[AHEAD][MT], ws[AHEAD][RT];
+                u32x4 xs[AHEAD], ws[AHEAD][RT];
                 const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) {
@@ -108,199 +103,407 @@ __global__ __launch_bounds__(256, 2) void fq_adapter_down_kernel(fq_adapter_args
                     const bool in = s + i * WAVES < end && k + 8 * h < a.K;
 #pragma unroll
                     for (int r = 0; r < RT; ++r) ws[i][r] = in ? *(const u32x4*)(w[r] + k) : zero;
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) xs[i][m] = in ? *(const u32x4*)(x[m] + k) : zero;
+                    xs[i] = in ? *(const u32x4*)(x + k) : zero;
                 }
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-                    for (int m = 0; m < MT; ++m)
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) t[m][r] = mfma16<ACT>(ws[i][r], xs[i][m], t[m][r]);
+                    for (int r = 0; r < RT; ++r) t[r] = mfma16<ACT>(ws[i][r], xs[i], t[r]);
             }
             __syncthreads();                      // (the sums of the turn before have been read)
             if (wave > 0)
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) sums[wave - 1][m * RT + r][lane] = t[m][r];
+                for (int r = 0; r < RT; ++r) sums[wave - 1][r][lane] = t[r];
             __syncthreads();
             if (wave > 0) continue;
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const int64_t row = row0 + 16 * m + x16;
+            for (int r = 0; r < RT; ++r) {
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-#pragma unroll
-                    for (int y = 0; y < WAVES - 1; ++y) t[m][r] += sums[y][m * RT + r][lane];
-                    const int at = r0 + 16 * r + 4 * h;
-                    if (mine[m] == id && at < a.rank) *(f32x4*)(a.partial + ((int64_t)part * a.rows + row) * ranks + at) = t[m][r];
-                }
+                for (int y = 0; y < WAVES - 1; ++y) t[r] += sums[y][r][lane];
+                const int at = r0 + 16 * r + 4 * h;
+                if (mine == id && at < a.rank) *(f32x4*)(a.partial + ((int64_t)part * a.rows + row) * ranks + at) = t[r];
             }
         }
     }
 }
 
-// ------------------------------------------------------------------------------------------ out += scale t B^T
-// MT x 16 rows and NJ x 16 columns a wave at a time, `turns` of them one after the other.  Column 4 i + c of product j is column (4 NJ) i + 4 j + c of
-// the wave's, so that a lane has 4 NJ neighbouring ones of its row.  RS: steps of 32 ranks.
-template <int ACT, int MT, int NJ, int RS>
-__global__ __launch_bounds__(256, 2) void fq_adapter_up_kernel(fq_adapter_args a, int parts, int turns) {
+// ------------------------------------------------------------------------------------------ out += scale t B^T, few rows
+// A wave has one row at a time and a column for each LANES lanes (a power of two: eight ranks each), 64 / LANES columns a step, whose weights lie one
+// behind the other.
+template <int ACT, int LANES>
+__global__ __launch_bounds__(256) void fq_adapter_up_few_kernel(fq_adapter_args a, int parts, int steps) {
+    typedef typename type16<ACT>::t T;
+    constexpr int COLUMNS = 64 / LANES, AHEAD = 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, u = lane % LANES, ranks = (a.rank + 15) / 16 * 16;
+    const int64_t row = blockIdx.y;
+    const int id = id_of(a, row);
+    if (id < 0) return;
+    const bool in = 8 * u < a.rank;
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = 0.0f;
+    if (in) {
+        const float scale = a.scales ? a.scales[id] : 1.0f;
+        f32x4 x[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll 4
+        for (int p = 0; p < parts; ++p) {
+            const float* from = a.partial + ((int64_t)p * a.rows + row) * ranks + 8 * u;
+            x[0] += *(const f32x4*)from;
+            x[1] += *(const f32x4*)(from + 4);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = x[i >> 2][i & 3] * scale;
+    }
+    const uint16_t* weights = (const uint16_t*)a.b + (int64_t)id * a.N * a.rank + 8 * u;
+    T* out = (T*)a.out + row * a.out_stride;
+    const int first = ((int)blockIdx.x * 4 + wave) * steps * COLUMNS + lane / LANES;
+    for (int s = 0; s < steps; s += AHEAD) {
+        u32x4 w[AHEAD];
+        float o[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int n = first + (s + i) * COLUMNS;
+            const bool there = s + i < steps && n < a.N;
+            w[i] = there && in ? *(const u32x4*)(weights + (int64_t)n * a.rank) : u32x4{0, 0, 0, 0};
+            o[i] = there && u == 0 ? (float)out[n] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int n = first + (s + i) * COLUMNS;
+            float sum = 0.0f;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                sum = __builtin_fmaf(half_of<ACT, 0>(w[i][y]), t[2 * y], sum);
+                sum = __builtin_fmaf(half_of<ACT, 1>(w[i][y]), t[2 * y + 1], sum);
+            }
+#pragma unroll
+            for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
+            if (u == 0 && s + i < steps && n < a.N) out[n] = (T)(o[i] + sum);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ t = x A^T, 64 rows a block
+// RT x 16 ranks, one of gridDim.x parts of K in chunks of 128.  A wave has 16 of the rows.  A chunk's rows of x and A lie in LDS as 16 units of 16
+// bytes, moved about within the row so that 16 rows' same unit falls on different banks; the next chunk is on its way beside the present one.
+template <int ACT, int RT>
+__global__ __launch_bounds__(256, 2) void fq_adapter_down_kernel(fq_adapter_args a) {
+    constexpr int ROWS = 64 + 16 * RT, BYTES = ROWS * 256, LOADS = ROWS / 16;       // LOADS: of a wave, four rows each
+    extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4, x16 = lane & 15;
-    const int64_t row0 = (int64_t)blockIdx.y * (16 * MT);
-    const int ranks = (a.rank + 15) / 16 * 16;
-    const u32x4 zero = {0, 0, 0, 0};
-    distinct tile(id_of(a, lane < 16 * MT ? row0 + lane : a.rows));
-    if (tile.left == 0) return;
-    const int ids[4] = {__shfl(tile.id, x16), __shfl(tile.id, (16 + x16) & 63), __shfl(tile.id, (32 + x16) & 63), __shfl(tile.id, (48 + x16) & 63)};
-    // the rows' t: values 32 s + 8 h .. + 7 of row 16 m + x16
-    u32x4 high[MT][RS], low[MT][RS];
-    float back[MT];
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    const int64_t row0 = (int64_t)blockIdx.y * 64;
+    const int ranks = (a.rank + 15) / 16 * 16, chunks = (a.K + 127) / 128;
+    const int part = blockIdx.x, each = (chunks + (int)gridDim.x - 1) / (int)gridDim.x, begin = part * each, end = min(chunks, begin + each);
+    distinct tile(id_of(a, row0 + lane));
+    const int mine = __shfl(tile.id, 16 * wave + x16);
+    for (int id = tile.next(); id >= 0; id = tile.next()) {
+        const bool busy = __any(mine == id);
+        for (int r0 = 0; r0 < ranks; r0 += 16 * RT) {
+            f32x4 t[RT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int64_t row = row0 + 16 * m + x16;
-        float t[RS][8], most = 0.0f;
-        const float scale = ids[m] < 0 ? 0.0f : a.scales ? a.scales[ids[m]] : 1.0f;
+            for (int r = 0; r < RT; ++r) t[r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            auto load = [&](int c) {
+                const uint32_t to = at + (uint32_t)(c & 1) * BYTES;
 #pragma unroll
-        for (int s = 0; s < RS; ++s) {
-            f32x4 sum[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-            if (ids[m] >= 0 && 32 * s + 8 * h < a.rank) {
-                const float* from = a.partial + row * ranks + 32 * s + 8 * h;
-                for (int p = 0; p < parts; ++p) {
-                    sum[0] += *(const f32x4*)(from + (int64_t)p * a.rows * ranks);
-                    sum[1] += *(const f32x4*)(from + (int64_t)p * a.rows * ranks + 4);
+                for (int i = 0; i < LOADS; ++i) {
+                    const int y = (i * 4 + wave) * 4 + h;          // row of the chunk: 64 of x, then A's
+                    const int unit = x16 ^ (y & 15), k = 128 * c + 8 * unit;
+                    const uint16_t* from = y < 64 ? (const uint16_t*)a.x + min(row0 + y, a.rows - 1) * a.x_stride
+                                                  : (const uint16_t*)a.a + ((int64_t)id * a.rank + min(r0 + y - 64, a.rank - 1)) * a.K;
+                    if (k < a.K) load_lds16(to + (uint32_t)(i * 4 + wave) * 1024, from + k);
+                    else *(u32x4*)(lds + (c & 1) * BYTES + (i * 4 + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+                }
+            };
+            __syncthreads();                      // (the chunks of the turn before have been read)
+            if (begin < end) load(begin);
+            for (int c = begin; c < end; ++c) {
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                __syncthreads();
+                if (c + 1 < end) load(c + 1);
+                if (!busy) continue;
+                const char* from = lds + (c & 1) * BYTES;
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int unit = (4 * s + h) ^ x16;
+                    const u32x4 x = *(const u32x4*)(from + (16 * wave + x16) * 256 + unit * 16);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) t[r] = mfma16<ACT>(*(const u32x4*)(from + (64 + 16 * r + x16) * 256 + unit * 16), x, t[r]);
                 }
             }
+            const int64_t row = row0 + 16 * wave + x16;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                t[s][i] = sum[i >> 2][i & 3] * scale;
-                most = __builtin_fmaxf(most, __builtin_fabsf(t[s][i]));
+            for (int r = 0; r < RT; ++r) {
+                const int rank = r0 + 16 * r + 4 * h;
+                if (mine == id && rank < a.rank) *(f32x4*)(a.partial + ((int64_t)part * a.rows + row) * ranks + rank) = t[r];
             }
         }
-        int e = 0;
-        if (ACT == FQ_F16) {
-            most = __builtin_fmaxf(most, __shfl_xor(most, 16));
-            most = __builtin_fmaxf(most, __shfl_xor(most, 32));
-            e = __builtin_amdgcn_frexp_expf(most);              // (0 for an infinity)
+    }
+}
+
+// ------------------------------------------------------------------------------------------ t as two 16-bit numbers
+// Eight values of a row's t, over 2^e: e of the row (binary16) is asked for by exponent().
+template <int ACT>
+struct split8 {
+    float t[8];
+    // the parts' sums, times the scale
+    __device__ __forceinline__ void sum(const fq_adapter_args& a, int64_t row, int rank0, int ranks, int parts, float scale) {
+        f32x4 x[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+        if (rank0 < a.rank) {
+            const float* from = a.partial + row * ranks + rank0;
+            for (int p = 0; p < parts; ++p) {
+                x[0] += *(const f32x4*)(from + (int64_t)p * a.rows * ranks);
+                x[1] += *(const f32x4*)(from + (int64_t)p * a.rows * ranks + 4);
+            }
         }
-        back[m] = (float)e;
 #pragma unroll
-        for (int s = 0; s < RS; ++s)
+        for (int i = 0; i < 8; ++i) t[i] = x[i >> 2][i & 3] * scale;
+    }
+    __device__ __forceinline__ float most() const {
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = __builtin_fmaxf(m, __builtin_fabsf(t[i]));
+        return m;
+    }
+    __device__ __forceinline__ void split(int e, u32x4* high, u32x4* low) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float u = t[2 * i], v = t[2 * i + 1];
+            if (ACT == FQ_F16) u = __builtin_amdgcn_ldexpf(u, -e), v = __builtin_amdgcn_ldexpf(v, -e);
+            (*high)[i] = pack2<ACT>(u, v);
+            const float du = u - half_of<ACT, 0>((*high)[i]), dv = v - half_of<ACT, 1>((*high)[i]);
+            (*low)[i] = pack2<ACT>(du == du ? du : 0.0f, dv == dv ? dv : 0.0f);        // (of an infinity: nothing)
+        }
+    }
+};
+
+// For many rows, once rather than by each block that needs them: [row][ranks, rounded up to 32] high, the same low, then the rows' exponents.
+template <int ACT>
+__global__ __launch_bounds__(256) void fq_adapter_fold_kernel(fq_adapter_args a, int parts, uint32_t* folded) {
+    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int rank0 = threadIdx.x % 16 * 8, ranks = (a.rank + 15) / 16 * 16, wide = (a.rank + 31) / 32 * 32;
+    const int id = id_of(a, row);
+    split8<ACT> s;
+    if (id >= 0) s.sum(a, row, rank0, ranks, parts, a.scales ? a.scales[id] : 1.0f);
+    float most = id >= 0 ? s.most() : 0.0f;
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, d));
+    const int e = ACT == FQ_F16 ? __builtin_amdgcn_frexp_expf(most) : 0;       // (0 for an infinity)
+    if (id < 0 || rank0 >= wide) return;
+    u32x4 high, low;
+    s.split(e, &high, &low);
+    uint16_t* to = (uint16_t*)folded + row * wide + rank0;
+    *(u32x4*)to = high;
+    *(u32x4*)(to + a.rows * wide) = low;
+    if (rank0 == 0) ((int32_t*)folded)[a.rows * wide + row] = e;
+}
+
+// ------------------------------------------------------------------------------------------ out += scale t B^T, 64 rows a block
+// 128 columns at a time, `turns` of them one after the other; a wave has 16 of the rows.  Column 8 x + j is column x of product j, so that a lane has
+// eight neighbouring columns of four rows, and 16 lanes 256 bytes of each.  Weights come through registers into LDS, the next turn's on their
+// way beside the present one: eight columns' together, and 16 bytes to the next eight, so that the columns of a product fall on different banks.
+template <int ACT, int RS>
+__global__ __launch_bounds__(256, 2) void fq_adapter_up_kernel(fq_adapter_args a, int turns, const uint32_t* folded) {
+    constexpr int UNITS = RS * 4 * 128 / 256;         // 16-byte units of a turn's weights that a thread brings in, at most
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4, x16 = lane & 15;
+    const int64_t row0 = (int64_t)blockIdx.y * 64;
+    const int wide = (a.rank + 31) / 32 * 32, units = a.rank / 8, group = 8 * 16 * units + 16, bytes = 16 * group;
+    const u32x4 zero = {0, 0, 0, 0};
+    const distinct tile(id_of(a, row0 + lane));
+    if (tile.left == 0) return;
+    // the rows' t as products take it: values 32 s + 8 h .. + 7 of row x16; and what becomes of the results: rows 4 h + i
+    const int64_t mine = row0 + 16 * wave + x16, first = row0 + 16 * wave + 4 * h;
+    const int id_x = __shfl(tile.id, 16 * wave + x16);
+    u32x4 high[RS], low[RS];
+#pragma unroll
+    for (int s = 0; s < RS; ++s) {
+        const uint16_t* from = (const uint16_t*)folded + mine * wide + 8 * h + 32 * s;
+        const bool in = id_x >= 0 && 32 * s < wide;
+        high[s] = in ? *(const u32x4*)from : zero;
+        low[s] = in ? *(const u32x4*)(from + a.rows * wide) : zero;
+    }
+    int id[4], back[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        id[i] = __shfl(tile.id, 16 * wave + 4 * h + i);
+        back[i] = ACT == FQ_F16 && id[i] >= 0 ? ((const int32_t*)folded)[a.rows * wide + first + i] : 0;
+    }
+    u32x4 coming[UNITS];
+    auto load = [&](int n0, int which) {
+        const uint16_t* from = (const uint16_t*)a.b + ((int64_t)which * a.N + n0) * a.rank;
+        const int count = min(128, a.N - n0) * units;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i)
+            if (i * 256 + (int)threadIdx.x < count) coming[i] = *(const u32x4*)(from + (int64_t)(i * 256 + threadIdx.x) * 8);
+    };
+    auto arrive = [&](char* to, int n0) {
+        const int count = min(128, a.N - n0) * units;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int y = i * 256 + threadIdx.x, eight = y / (8 * units);
+            if (y < count) *(u32x4*)(to + eight * 16 + y * 16) = coming[i];
+        }
+    };
+    const int n_first = (int)blockIdx.x * turns * 128, n_end = min(a.N, n_first + turns * 128);
+    // (turn, adapter) after (turn, adapter)
+    distinct next = tile;
+    int next_id = next.next(), next_n = n_first, buffer = 0;
+    load(next_n, next_id);
+    u32x4 o[4];
+    f32x4 sum[8];
+    bool begun = false;
+    while (next_n < n_end) {
+        const int now = next_id, n0 = next_n;
+        if (!begun) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float u = t[s][2 * i], v = t[s][2 * i + 1];
-                if (ACT == FQ_F16) u = __builtin_amdgcn_ldexpf(u, -e), v = __builtin_amdgcn_ldexpf(v, -e);
-                high[m][s][i] = pack2<ACT>(u, v);
-                const float du = u - half_of<ACT, 0>(high[m][s][i]), dv = v - half_of<ACT, 1>(high[m][s][i]);
-                low[m][s][i] = pack2<ACT>(du == du ? du : 0.0f, dv == dv ? dv : 0.0f);
-            }
-    }
-    for (int turn = 0; turn < turns; ++turn) {
-        const int n0 = (((int)blockIdx.x * turns + turn) * 4 + wave) * (16 * NJ);
-        if (n0 >= a.N) return;
-        f32x4 sum[MT][NJ];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) sum[m][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        distinct each = tile;
-        for (int id = each.next(); id >= 0; id = each.next()) {
-            u32x4 w[NJ][RS];
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const int n = min(n0 + 4 * NJ * (x16 >> 2) + 4 * j + (x16 & 3), a.N - 1);
-                const uint16_t* from = (const uint16_t*)a.b + ((int64_t)id * a.N + n) * a.rank + 8 * h;
-#pragma unroll
-                for (int s = 0; s < RS; ++s) w[j][s] = 32 * s + 8 * h < a.rank ? *(const u32x4*)(from + 32 * s) : zero;
+                const bool in = id[i] >= 0 && n0 + 8 * x16 < a.N;
+                o[i] = in ? __builtin_nontemporal_load((const u32x4*)((const uint16_t*)a.out + (first + i) * a.out_stride + n0 + 8 * x16)) : zero;
             }
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int s = 0; s < RS; ++s) {
-                        y = mfma16<ACT>(w[j][s], low[m][s], y);
-                        y = mfma16<ACT>(w[j][s], high[m][s], y);
-                    }
-                    if (ids[m] == id) sum[m][j] = y;
-                }
+            for (int j = 0; j < 8; ++j) sum[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            begun = true;
         }
+        char* weights = lds + buffer * bytes;
+        arrive(weights, n0);
+        next_id = next.next();
+        if (next_id < 0) {
+            next = tile;
+            next_id = next.next();
+            next_n += 128;
+            begun = false;
+        }
+        if (next_n < n_end) load(next_n, next_id);
+        __syncthreads();
+        if (__any(id_x == now)) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int64_t row = row0 + 16 * m + x16;
-            if (ids[m] < 0) continue;
-            uint16_t* out = (uint16_t*)a.out + row * a.out_stride;
+            for (int j = 0; j < 8; ++j) {
+                f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < NJ; j += 2) {
-                const int n = n0 + 4 * NJ * h + 4 * j;             // eight neighbouring columns
-                if (n >= a.N) continue;
-                u32x4 o = *(const u32x4*)(out + n);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float u = sum[m][j + i / 2][2 * i % 4], v = sum[m][j + i / 2][2 * i % 4 + 1];
-                    if (ACT == FQ_F16) u = __builtin_amdgcn_ldexpf(u, (int)back[m]), v = __builtin_amdgcn_ldexpf(v, (int)back[m]);
-                    o[i] = pack2<ACT>(half_of<ACT, 0>(o[i]) + u, half_of<ACT, 1>(o[i]) + v);
+                for (int s = 0; s < RS; ++s) {
+                    // (columns behind the last: what lies there goes into results that nobody takes)
+                    const u32x4 w = 4 * s + h < units ? *(const u32x4*)(weights + x16 * group + (j * units + 4 * s + h) * 16) : zero;
+                    y = mfma16<ACT>(low[s], w, y);
+                    y = mfma16<ACT>(high[s], w, y);
                 }
-                *(u32x4*)(out + n) = o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[j][i] = id[i] == now ? y[i] : sum[j][i];
+            }
+        }
+        buffer ^= 1;
+        if (!begun && n0 + 8 * x16 < a.N) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (id[i] < 0) continue;
+                u32x4 z;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float u = sum[2 * j][i], v = sum[2 * j + 1][i];
+                    if (ACT == FQ_F16) u = __builtin_amdgcn_ldexpf(u, back[i]), v = __builtin_amdgcn_ldexpf(v, back[i]);
+                    z[j] = pack2<ACT>(half_of<ACT, 0>(o[i][j]) + u, half_of<ACT, 1>(o[i][j]) + v);
+                }
+                *(u32x4*)((uint16_t*)a.out + (first + i) * a.out_stride + n0 + 8 * x16) = z;
             }
         }
     }
 }
 
 struct adapter_plan {
-    int tall;                 // 16-row tiles of a block
+    bool few;
     int slots, parts;         // of the first kernel: blocks that take a tile's adapters in turn, parts of K
-    int wide, turns;          // of the second: 16-column products of a wave, and how often
+    int turns;                // of the second: steps of a wave, or turns of a block
+    int64_t folded;           // where the folded t begins in the workspace, in floats
 };
 
 adapter_plan plan(int64_t rows, int adapters, int rank, int64_t N, int64_t K) {
     adapter_plan p;
-    p.tall = rows > 256 ? 4 : 1;
-    const int64_t tiles = (rows + 16 * p.tall - 1) / (16 * p.tall), steps = (K + 31) / 32;
-    const int64_t most = rows < 16 ? rows : 16;
-    p.slots = p.tall > 1 ? (adapters < 2 ? 1 : 2) : (int)(adapters < most ? adapters : most);
-    const int64_t wanted = 512 / (tiles * p.slots), fit = (steps + 15) / 16;
+    p.few = rows <= FEW;
+    const int64_t tiles = (rows + (p.few ? 15 : 63)) / (p.few ? 16 : 64), most = rows < 16 ? rows : 16;
+    p.slots = p.few ? (int)(adapters < most ? adapters : most) : 1;
+    const int64_t pieces = p.few ? (K + 31) / 32 : (K + 127) / 128, least = p.few ? 16 : 4;        // pieces of K; of a block, at least
+    const int64_t wanted = 512 / (tiles * p.slots), fit = (pieces + least - 1) / least;
     p.parts = (int)(wanted < 1 ? 1 : wanted < fit ? wanted : fit);
-    const int64_t each = (steps + p.parts - 1) / p.parts;
-    p.parts = (int)((steps + each - 1) / each);
-    p.wide = p.tall > 1 && rank <= 64 ? 4 : 2;
-    const int64_t groups = (N + 64 * p.wide - 1) / (64 * p.wide);
-    int64_t turns = tiles * groups / 768;
-    p.turns = (int)(turns < 1 ? 1 : turns < 8 ? turns : 8);
+    const int64_t each = (pieces + p.parts - 1) / p.parts;
+    p.parts = (int)((pieces + each - 1) / each);
+    int64_t turns;
+    if (p.few) {
+        int lanes = 1;
+        while (8 * lanes < rank) lanes *= 2;
+        const int64_t steps = (N * lanes + 63) / 64;           // of a row, all columns
+        turns = (rows * steps + 4095) / 4096;                  // (two waves a SIMD and more)
+        turns = turns < 4 ? 4 : turns > 32 ? 32 : turns;
+    } else {
+        const int64_t all = tiles * ((N + 127) / 128);
+        turns = all / 2048;
+        turns = turns < 1 ? 1 : turns > 8 ? 8 : turns;
+    }
+    p.turns = (int)turns;
+    p.folded = (int64_t)p.parts * rows * ((rank + 15) / 16 * 16);
     return p;
 }
 
-template <int ACT, int MT>
-int down(const fq_adapter_args& a, const adapter_plan& p, hipStream_t stream) {
-    const dim3 grid((unsigned)p.parts, (unsigned)p.slots, (unsigned)((a.rows + 16 * MT - 1) / (16 * MT)));
-    if (a.rank <= 16) fq_adapter_down_kernel<ACT, MT, 1><<<grid, 256, 0, stream>>>(a);
-    else if (a.rank <= 32) fq_adapter_down_kernel<ACT, MT, 2><<<grid, 256, 0, stream>>>(a);
-    else fq_adapter_down_kernel<ACT, MT, 4><<<grid, 256, 0, stream>>>(a);
-    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+int status() { return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP; }
+
+template <int ACT, int LANES>
+void up_few(const fq_adapter_args& a, const adapter_plan& p, hipStream_t stream) {
+    const int64_t each = (int64_t)4 * p.turns * (64 / LANES);
+    fq_adapter_up_few_kernel<ACT, LANES><<<dim3((unsigned)((a.N + each - 1) / each), (unsigned)a.rows), 256, 0, stream>>>(a, p.parts, p.turns);
 }
 
-template <int ACT, int MT, int NJ>
-int up(const fq_adapter_args& a, const adapter_plan& p, hipStream_t stream) {
-    const int64_t groups = (a.N + 64 * NJ - 1) / (64 * NJ);
-    const dim3 grid((unsigned)((groups + p.turns - 1) / p.turns), (unsigned)((a.rows + 16 * MT - 1) / (16 * MT)));
-    if (a.rank <= 32) fq_adapter_up_kernel<ACT, MT, NJ, 1><<<grid, 256, 0, stream>>>(a, p.parts, p.turns);
-    else if (a.rank <= 64) fq_adapter_up_kernel<ACT, MT, NJ, 2><<<grid, 256, 0, stream>>>(a, p.parts, p.turns);
-    else fq_adapter_up_kernel<ACT, MT, 2, 4><<<grid, 256, 0, stream>>>(a, p.parts, p.turns);        // (p.wide is 2)
-    return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
+template <int ACT>
+int launch_few(const fq_adapter_args& a, const adapter_plan& p, hipStream_t stream) {
+    const dim3 grid((unsigned)p.parts, (unsigned)p.slots, (unsigned)((a.rows + 15) / 16));
+    if (a.rank <= 16) fq_adapter_down_few_kernel<ACT, 1><<<grid, 256, 0, stream>>>(a);
+    else if (a.rank <= 32) fq_adapter_down_few_kernel<ACT, 2><<<grid, 256, 0, stream>>>(a);
+    else fq_adapter_down_few_kernel<ACT, 4><<<grid, 256, 0, stream>>>(a);
+    const int st = status();
+    if (st != FQ_OK) return st;
+    if (a.rank <= 8) up_few<ACT, 1>(a, p, stream);
+    else if (a.rank <= 16) up_few<ACT, 2>(a, p, stream);
+    else if (a.rank <= 32) up_few<ACT, 4>(a, p, stream);
+    else if (a.rank <= 64) up_few<ACT, 8>(a, p, stream);
+    else up_few<ACT, 16>(a, p, stream);
+    return status();
+}
+
+template <int ACT, int RT>
+int down(const fq_adapter_args& a, const adapter_plan& p, hipStream_t stream) {
+    static std::atomic<uint64_t> raised{0};
+    const int st = fqd::raise_lds_limit((const void*)fq_adapter_down_kernel<ACT, RT>, raised);
+    if (st != FQ_OK) return st;
+    const dim3 grid((unsigned)p.parts, (unsigned)((a.rows + 63) / 64));
+    fq_adapter_down_kernel<ACT, RT><<<grid, 256, 2 * (64 + 16 * RT) * 256, stream>>>(a);
+    return status();
+}
+
+template <int ACT, int RS>
+int up(const fq_adapter_args& a, const adapter_plan& p, const uint32_t* folded, hipStream_t stream) {
+    static std::atomic<uint64_t> raised{0};
+    const int st = fqd::raise_lds_limit((const void*)fq_adapter_up_kernel<ACT, RS>, raised);
+    if (st != FQ_OK) return st;
+    const int64_t groups = (a.N + 127) / 128;
+    const dim3 grid((unsigned)((groups + p.turns - 1) / p.turns), (unsigned)((a.rows + 63) / 64));
+    fq_adapter_up_kernel<ACT, RS><<<grid, 256, 2 * 16 * (16 * a.rank + 16), stream>>>(a, p.turns, folded);
+    return status();
 }
 
 template <int ACT>
 int launch(const fq_adapter_args& a, const adapter_plan& p, hipStream_t stream) {
-    const int st = p.tall > 1 ? down<ACT, 4>(a, p, stream) : down<ACT, 1>(a, p, stream);
+    if (p.few) return launch_few<ACT>(a, p, stream);
+    int st = a.rank <= 16 ? down<ACT, 1>(a, p, stream) : a.rank <= 32 ? down<ACT, 2>(a, p, stream) : down<ACT, 4>(a, p, stream);
     if (st != FQ_OK) return st;
-    return p.tall == 1 ? up<ACT, 1, 2>(a, p, stream) : p.wide == 4 ? up<ACT, 4, 4>(a, p, stream) : up<ACT, 4, 2>(a, p, stream);
+    uint32_t* folded = (uint32_t*)(a.partial + p.folded);
+    fq_adapter_fold_kernel<ACT><<<(unsigned)((a.rows + 15) / 16), 256, 0, stream>>>(a, p.parts, folded);
+    if ((st = status()) != FQ_OK) return st;
+    return a.rank <= 32 ? up<ACT, 1>(a, p, folded, stream) : a.rank <= 64 ? up<ACT, 2>(a, p, folded, stream) : up<ACT, 4>(a, p, folded, stream);
 }
 
 }  // namespace
 
 size_t fq_adapter_bytes(int64_t rows, int adapters, int rank, int64_t N, int64_t K) {
-    return (size_t)plan(rows, adapters, rank, N, K).parts * rows * ((rank + 15) / 16 * 16) * sizeof(float);
+    const adapter_plan p = plan(rows, adapters, rank, N, K);
+    return ((size_t)p.folded + (p.few ? 0 : (size_t)rows * ((rank + 31) / 32 * 32 + 1))) * sizeof(float);
 }
 
 int fq_launch_adapters(int act_dtype, const fq_adapter_args& a, hipStream_t stream) {
