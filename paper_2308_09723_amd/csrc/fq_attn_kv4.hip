@@ -772,18 +772,20 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_stream_kernel(fq_tree
 
 // ------------------------------------------------------------------------------------------ above 32 rows
 // A word's eight codes times scales, exactly: first codes of bytes 0, 1 and 2, 3, second codes of the same (low, high: the scales of bytes 0, 1
-// and 2, 3)
+// and 2, 3).  bfloat16 has no packed multiplication: through binary32.
 template <int ACT>
 __device__ __forceinline__ u32x4 words16(uint32_t x, uint32_t low, uint32_t high) {
     const uint32_t f = firsts(x), g = seconds(x);
-    u32x4 y = {codes16<ACT, false>(f), codes16<ACT, true>(f), codes16<ACT, false>(g), codes16<ACT, true>(g)};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t scale = i & 1 ? high : low;
-        if constexpr (ACT == FQ_F16) y[i] = times16(y[i], scale);
-        else y[i] = pack2<ACT>(half_of<ACT, 0>(y[i]) * half_of<ACT, 0>(scale), half_of<ACT, 1>(y[i]) * half_of<ACT, 1>(scale));
+    if constexpr (ACT == FQ_F16) {
+        return u32x4{times16(codes16<ACT, false>(f), low), times16(codes16<ACT, true>(f), high), times16(codes16<ACT, false>(g), low),
+                     times16(codes16<ACT, true>(g), high)};
+    } else {
+        const float s[4] = {half_of<ACT, 0>(low), half_of<ACT, 1>(low), half_of<ACT, 0>(high), half_of<ACT, 1>(high)};
+        const auto f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(f, 512.0f, false), f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(f, 512.0f, true);
+        const auto g0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(g, 512.0f, false), g1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(g, 512.0f, true);
+        return u32x4{pack2<ACT>(f0[0] * s[0], f0[1] * s[1]), pack2<ACT>(f1[0] * s[2], f1[1] * s[3]), pack2<ACT>(g0[0] * s[0], g0[1] * s[1]),
+                     pack2<ACT>(g1[0] * s[2], g1[1] * s[3])};
     }
-    return y;
 }
 
 // O^T += V^T P^T over H half-tiles of values that lie as [value][key]
@@ -827,12 +829,13 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_tile_kernel(fq_tree_a
     int64_t at_b;
     all.find(begin, &b, &at_b);
     int context = all.context(b), tiles = tiles_of(a, p, context);
-    int u = (int)quotient(begin - at_b, tiles), t0 = (int)(begin - at_b - (int64_t)u * tiles);
+    int u = (int)quotient(begin - at_b, tiles + p.extra), t0 = (int)(begin - at_b - (int64_t)u * (tiles + p.extra));
     wave_state<ACT, DP> w;
 
     for (int64_t pos = begin; pos < stop;) {
         const unit_rows<kv4_rows> rows(a, p, b, u, 0, context);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
+        if (t0 < tiles) {                               // (behind them are places that hold nothing)
         float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(block, pos == begin, 0);
         const int key0 = t0 * KEYS, key1 = p.whole ? rows.keys : min(rows.keys, t1 * KEYS);
         const int r = group * 32 + (lane & 31), row = min(r, rows.count - 1);
@@ -911,7 +914,8 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_tile_kernel(fq_tree_a
             if (!w.sound()) rows.template one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
             else if (r < rows.count) w.put(rows.result(r), slot, p.shape(), r, [&] { return rows.sees_any(r); });
         }
-        pos += t1 - t0;
+        }
+        pos += tiles + p.extra - t0;
         t0 = 0;
         if (++u == all.units) {
             u = 0;
@@ -978,7 +982,7 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
 static tree_plan plan_kv4(const fq_tree_args& a) {
     const int rows = a.nodes * (a.q_heads / a.kv_heads);
     const int heads = rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
-    return plan_units(a, heads, rows > 32 ? KEYS : (rows > 4 ? 128 : 256) / heads, rows > 32 ? 0 : EXTRA);
+    return plan_units(a, heads, rows > 32 ? KEYS : (rows > 4 ? 128 : 256) / heads, EXTRA);
 }
 
 size_t fq_tree_kv4_bytes(const fq_tree_args& a) { return slots_bytes(plan_kv4(a)); }
