@@ -720,12 +720,15 @@ int fq_pages_fork(int32_t* refs, int64_t pages, int page_size, const int32_t* ta
     for (const fq_span& x : read) {
         if (fq_overlaps(refs, p, {x}) || (children > 0 && (fq_overlaps(table_out, to, {x}) || fq_overlaps(lens_out, lo, {x})))) return FQ_ERR_INVALID_ARG;
         if (workspace && fq_overlaps(workspace, need, {x})) return FQ_ERR_INVALID_ARG;
-        if (over_buffers(x.p, x.bytes, buffers_host, buffers, pages)) return FQ_ERR_INVALID_ARG;
+        if (x.bytes > 0 && over_buffers(x.p, x.bytes, buffers_host, buffers, pages)) return FQ_ERR_INVALID_ARG;
     }
     if (children > 0 && (fq_overlaps(table_out, to, {{refs, p}, {lens_out, lo}}) || fq_overlaps(lens_out, lo, {{refs, p}}))) return FQ_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < need) return FQ_ERR_WORKSPACE;
     if (!aligned4(workspace)) return FQ_ERR_UNSUPPORTED;
     if (fq_overlaps(workspace, need, {{refs, p}, {table_out, children > 0 ? to : 0}, {lens_out, children > 0 ? lo : 0}})) return FQ_ERR_INVALID_ARG;
+    const fq_span written[] = {{refs, p}, {workspace, need}, {table_out, children > 0 ? to : 0}, {lens_out, children > 0 ? lo : 0}};
+    for (const fq_span& x : written)
+        if (x.bytes > 0 && over_buffers(x.p, x.bytes, buffers_host, buffers, pages)) return FQ_ERR_INVALID_ARG;
     int32_t* w = (int32_t*)workspace;
     const fq_fork_args a = {refs, pages, page_size, table, lens, parents, (int)rows, width, (int)children, release != 0, table_out, lens_out,
                             w, w + rows, w + rows + children, w + rows + 2 * children};
@@ -765,7 +768,8 @@ int fq_pages_compact(int32_t* refs, int64_t pages, int page_size, int32_t* table
     if ((st = check_buffers(buffers_host, buffers, pages)) != FQ_OK) return st;
     if (pages == 0) return FQ_OK;
     const size_t need = fq_pages_compact_workspace_bytes(pages), p = (size_t)pages * 4, t = (size_t)(rows * width) * 4, l = (size_t)rows * 4;
-    if (over_buffers(refs, p, buffers_host, buffers, pages) || (t > 0 && over_buffers(table, t, buffers_host, buffers, pages))) return FQ_ERR_INVALID_ARG;
+    for (const fq_span& x : {fq_span{refs, p}, fq_span{table, t}, fq_span{lens, l}})
+        if (x.bytes > 0 && over_buffers(x.p, x.bytes, buffers_host, buffers, pages)) return FQ_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < need) return FQ_ERR_WORKSPACE;
     if (!aligned4(workspace)) return FQ_ERR_UNSUPPORTED;
     if (fq_overlaps(workspace, need, {{refs, p}, {table, t}, {lens, l}}) || over_buffers(workspace, need, buffers_host, buffers, pages)) return FQ_ERR_INVALID_ARG;

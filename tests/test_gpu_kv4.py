@@ -164,3 +164,158 @@ CASES = [  # lengths, nodes, heads, key heads, D, page
 @pytest.mark.parametrize("lens,nodes,hq,hk,D,page", CASES)
 def test_attention(lens, nodes, hq, hk, D, page, dtype):
     _check(lens, nodes, hq, hk, D, page, dtype, len(lens) + nodes + D)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("nodes,hq,hk,D,page", [(3, 4, 4, 64, 16), (7, 4, 2, 128, 32), (12, 8, 4, 96, 16), (24, 2, 2, 80, 16), (40, 8, 2, 128, 48), (70, 2, 1, 128, 64), (130, 4, 4, 32, 16)])
+def test_trees(nodes, hq, hk, D, page, dtype):
+    """Masks of each sequence, and one for all; some nodes see nothing but the context, and without a context nothing."""
+    gen = torch.Generator().manual_seed(nodes)
+    lens = [0, 50, 333]
+    sees = torch.rand((3, nodes, nodes), generator=gen) < 0.4
+    sees[:, nodes // 2] = False
+    sees[:, 0] = False
+    mask = attention.words(sees).cuda()
+    _check(lens, nodes, hq, hk, D, page, dtype, nodes, sees=sees, mask=mask)
+    shared = sees[1:2].expand(3, nodes, nodes)
+    _check(lens, nodes, hq, hk, D, page, dtype, nodes + 1, sees=shared, mask=mask[1].contiguous())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("lens,nodes,hq,hk,D", [([20000], 1, 4, 1, 128), ([9000, 3, 17000], 2, 8, 4, 64), ([12000, 100], 10, 2, 2, 128), ([9000], 30, 2, 2, 96), ([7000, 5000], 50, 4, 4, 128),
+                                                ([30000], 1, 2, 2, 80)])
+def test_long_contexts_in_pieces(lens, nodes, hq, hk, D, dtype):
+    """Cut into pieces, and joined; with a workspace of the caller's, and one that is too small."""
+    got, (device, table, q) = _check(lens, nodes, hq, hk, D, 16 if nodes < 10 else 64, dtype, nodes + D)
+    page = 16 if nodes < 10 else 64
+    need = fq.attention_tree_kv4_workspace_bytes(len(lens), nodes, hq, hk, D, table.shape[1], page)
+    assert need > 0
+    at = torch.tensor(lens, dtype=torch.int32).cuda()
+    for size in (need, 16):
+        ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        assert torch.equal(fq.attention_tree_kv4(q.cuda(), device, page, hk, table.cuda(), at, workspace=ws), got)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("nodes,hq,hk", [(1, 4, 1), (1, 12, 1), (6, 4, 1), (20, 4, 2)])
+def test_uneven_sizes(nodes, hq, hk, dtype):
+    """Keys and values whose tokens are up to some hundred times as large as others; scores that rise late; large and small scales."""
+    _check([700, 65], nodes, hq, hk, 128, 32, dtype, nodes, spread=6.0)
+    _check([700, 65], nodes, hq, hk, 64, 16, dtype, nodes + 1, sigma=20.0)
+    _check([300, 1], nodes, hq, hk, 128, 16, dtype, nodes + 2, scale=2.0)
+    _check([300, 1], nodes, hq, hk, 40, 16, dtype, nodes + 3, scale=1e-6)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("nodes,hq,hk,D", [(8, 2, 2, 128), (8, 4, 1, 64), (24, 1, 1, 96), (48, 2, 1, 128)])
+def test_broken_values_that_nobody_sees(nodes, hq, hk, D, dtype):
+    """A drafted token with a NaN: a part of the results of those that see it, and of no other."""
+    lens, page = [100, 37], 16
+    device, table, k, v = _context(lens, nodes, hk, D, page, dtype, 5)
+    bad = 3
+    slots = torch.stack([table[b].long()[(c + bad) // page] * page + (c + bad) % page for b, c in enumerate(lens)])
+    rows = _normal((2, hk, D), dtype, 6)
+    values = rows.clone()
+    values[:, 0, 2] = math.nan
+    fq.kv4_write(rows.cuda(), values.cuda(), device, page, slots.cuda())
+    k.view(-1, hk, D)[slots], v.view(-1, hk, D)[slots] = ref.quantise(rows)[2].to(dtype), ref.quantise(values)[2].to(dtype)
+    sees = torch.ones((nodes, nodes), dtype=torch.bool).tril()
+    sees[:, bad] = False
+    sees[5, bad] = True
+    sees = sees[None].expand(2, nodes, nodes)
+    q = _normal((2, nodes, hq, D), dtype, 7)
+    got = fq.attention_tree_kv4(q.cuda(), device, page, hk, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), mask=attention.words(sees[0]).cuda()).cpu()
+    want, tol = attention.tree(q, k, v, table.clamp_max(k.shape[0] - 1), lens, sees)
+    group = hq // hk
+    assert bool(got[:, 5, :group, :min(32, D)].isnan().all()) and bool(want[:, 5, :group, :min(32, D)].isnan().all())
+    fine = want.isfinite()
+    assert torch.equal(got.isfinite(), fine)
+    assert bool(((got.double() - want).abs() <= tol)[fine].all())
+
+
+@pytest.mark.parametrize("nodes", [1, 5, 40])
+def test_strides_outputs_and_streams(nodes):
+    """Queries within the rows of a product, an output of the caller's, pages with room between them, another stream."""
+    lens, hq, hk, D, page = [70, 300], 8, 2, 128, 32
+    device, table, k, v = _context(lens, nodes, hk, D, page, BF16, 9)
+    wide = torch.zeros((device.shape[0], device.shape[1] + 4096), dtype=torch.uint8, device="cuda")
+    wide[:, :device.shape[1]] = device
+    pages = wide[:, :device.shape[1]]
+    rows = _normal((2 * nodes, (hq + 2 * hk) * D), BF16, 10)
+    q = rows.cuda().view(2, nodes, hq + 2 * hk, D)[:, :, :hq]
+    out = torch.full((2, nodes, hq, D), 9.0, dtype=BF16, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = fq.attention_tree_kv4(q, pages, page, hk, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), out=out)
+    side.synchronize()
+    assert got is out
+    want, tol = attention.tree(q.cpu(), k, v, table.clamp_max(k.shape[0] - 1), lens, attention.chain(2, nodes))
+    attention.compare(out, want, tol, "strided")
+    # writes into them leave the room between pages alone
+    fq.kv4_write(_normal((3, hk, D), BF16, 1).cuda(), _normal((3, hk, D), BF16, 2).cuda(), pages, page, torch.tensor([1, 40, 66]).cuda())
+    assert not bool(wide[:, device.shape[1]:].any())
+
+
+def test_pages_beyond_four_gigabytes():
+    hk, D, page = 8, 128, 256
+    size = fq.kv4_page_bytes(page, hk, D)
+    pages = (5 << 30) // size
+    cache = torch.empty((pages, size), dtype=torch.uint8, device="cuda")
+    k, v = _normal((300, hk, D), F16, 1), _normal((300, hk, D), F16, 2)
+    at = torch.arange(300)
+    table = torch.tensor([[pages - 1, 0], [pages - 3, pages - 2]], dtype=torch.int32)
+    slots = table[0].long()[at // page] * page + at % page
+    fq.kv4_write(k.cuda(), v.cuda(), cache, page, slots.cuda())
+    back, _ = fq.kv4_read(cache, page, hk, D, slots.cuda(), F16)
+    kept = ref.quantise(k)[2], ref.quantise(v)[2]
+    assert torch.equal(back.cpu().double(), kept[0])
+    q = _normal((1, 1, 32, D), F16, 3)
+    got = fq.attention_tree_kv4(q.cuda(), cache, page, hk, table[:1].cuda(), torch.tensor([299], dtype=torch.int32).cuda())
+    for h in range(0, 32, 5):
+        want, tol = attention.attend(q[0, :, h], kept[0][:, h // 4], kept[1][:, h // 4], torch.ones((1, 300), dtype=torch.bool), D ** -0.5)
+        attention.compare(got[0, :, h], want, tol, "far pages")
+
+
+@pytest.mark.parametrize("nodes", [1, 4, 12, 40])
+def test_captured_with_other_lengths(nodes):
+    """Writes and attention, captured once and replayed with other tokens, slots, tables and lengths; eager calls in between share the workspace."""
+    hq, hk, D, page, B, width = 8, 2, 128, 16, 3, 40
+    pages = B * width + 1
+    cache = fq.kv4_cache(pages, page, hk, D)
+    gen = torch.Generator().manual_seed(1)
+    every = torch.arange(pages * page)
+    all_k, all_v = _normal((pages * page, hk, D), BF16, 2), _normal((pages * page, hk, D), BF16, 3)
+    fq.kv4_write(all_k.cuda(), all_v.cuda(), cache, page, every.cuda())
+    new_k, new_v = torch.zeros((B * nodes, hk, D), dtype=BF16, device="cuda"), torch.zeros((B * nodes, hk, D), dtype=BF16, device="cuda")
+    slots, table, lens = torch.full((B * nodes,), -1, device="cuda"), torch.zeros((B, width), dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    q, out = torch.zeros((B, nodes, hq, D), dtype=BF16, device="cuda"), torch.zeros((B, nodes, hq, D), dtype=BF16, device="cuda")
+    ws = torch.empty(fq.attention_tree_kv4_workspace_bytes(B, nodes, hq, hk, D, width, page) + 16, dtype=torch.uint8, device="cuda")
+
+    def step():
+        fq.kv4_write(new_k, new_v, cache, page, slots)
+        return fq.attention_tree_kv4(q, cache, page, hk, table, lens, out=out, workspace=ws)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        order = torch.randperm(pages, generator=gen)[:B * width].view(B, width)
+        contexts = torch.randint(0, width * page - nodes, (B,), generator=gen)
+        at = contexts[:, None] + torch.arange(nodes)
+        table.copy_(order)
+        lens.copy_(contexts)
+        slots.copy_((order.gather(1, at // page) * page + at % page).flatten())
+        for x, seed in ((new_k, 0), (new_v, 1), (q, 2)):
+            x.copy_(_normal(x.shape, BF16, 10 * i + seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(step(), got)
+        k, v = fq.kv4_read(cache, page, hk, D, every.cuda(), BF16)
+        want, tol = attention.tree(q.cpu(), k.cpu().view(pages, page, hk, D), v.cpu().view(pages, page, hk, D), order, contexts.tolist(), attention.chain(B, nodes))
+        attention.compare(got, want, tol, f"replay {i}")

@@ -65,6 +65,7 @@ def _fork(**kw):
     (dict(parents=None), BAD), (dict(children=-1), BAD), (dict(table_out=None), BAD), (dict(lens_out=None), BAD), (dict(table_out=P << 1), BAD), (dict(lens_out=P << 2), BAD),
     (dict(lens_out=P << 3), BAD), (dict(table_out=P), BAD), (dict(lens_out=P << 4), BAD), (dict(ws=P), BAD), (dict(ws=P << 4), BAD), (dict(ws=(P << 6) + 2), NOT_HERE),
     (dict(children=8193), NOT_HERE), (dict(ws=None), SCRATCH), (dict(less=1), SCRATCH), (dict(table=P << 10), BAD),
+    (dict(refs=P << 10), BAD), (dict(table_out=P << 10), BAD), (dict(lens_out=(P << 10) + 40), BAD), (dict(ws=P << 10), BAD), (dict(parents=P << 10), BAD),
 ])
 def test_fork_refuses(change, status):
     assert _fork(**change) == status
@@ -90,7 +91,7 @@ def _compact(**kw):
 
 @pytest.mark.parametrize("change,status", POOL + [(dict(buffers=b), s) for b, s in BUFFERS] + [
     (dict(ws=None), SCRATCH), (dict(less=1), SCRATCH), (dict(ws=P), BAD), (dict(ws=P << 10), BAD), (dict(refs=P << 10), BAD), (dict(table=P << 10), BAD),
-    (dict(ws=(P << 6) + 2), NOT_HERE),
+    (dict(lens=P << 10), BAD), (dict(ws=(P << 6) + 2), NOT_HERE),
 ])
 def test_compact_refuses(change, status):
     assert _compact(**change) == status
