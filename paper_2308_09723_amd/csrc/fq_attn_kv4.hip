@@ -10,8 +10,9 @@
 // binary16 values are code times scale, exactly; bfloat16 has no packed multiplication, and there the numerators are multiplied by the
 // values' scales instead, before they are rounded, once, as they are anyway.
 //
-// Above 32 rows (fq_attention_kv4_tile_kernel) four waves take 64 keys' codes to 16 bits once, each a record, into tiles that all of them read: keys as over a
-// cache of 16 bits, values turned over (a lane has four tokens of a value).
+// Above 32 rows (fq_attention_kv4_tile_kernel) the waves of a block take a tile's codes to 16 bits once, each a record, into tiles that all of them read: keys
+// as over a cache of 16 bits, values turned over (a lane has four tokens of a value).  Bound by instructions: for 32 rows and 64 keys a wave has 32 products, 170
+// instructions' time for the numerators and, of four waves, 200 for the codes, of eight 100.
 #include <hip/hip_runtime.h>
 #include <atomic>
 
@@ -803,24 +804,73 @@ __device__ __forceinline__ void accumulate(wave_state<ACT, DP>& w, const char* v
         }
 }
 
-// GROUPS x 32 rows a block, as over a cache of 16 bits.  Every wave brings in one record of the four of a tile, RING of them on their way, and
-// takes it to 16 bits.  Keys lie as wave_state takes them; values as [value][key], rows 8 bytes longer than 64 keys so that a read's
-// 32 rows fall on different banks.
-template <int ACT, int S, int GROUPS>
-__global__ __launch_bounds__(256, 2) void fq_attention_kv4_tile_kernel(fq_tree_args a, tree_plan p, divisor by_records) {
-    constexpr int DP = S < 2 ? 64 : 32 * S, BYTES = record_bytes(S), RING = 3, LOADS = record_loads<S>::COUNT;
+// A record on its way to 16 bits: keys' words 4 h .. of token x16 (64 lanes: the codes back to back), values' words, scales.
+template <int ACT, int S>
+struct record_words {
+    uint32_t k[S], v[S], key_scale[S], value_scale[2 * S];
+
+    __device__ __forceinline__ void fetch(const void* record) {
+        const int lane = threadIdx.x & 63, h = lane >> 4, x16 = lane & 15;
+        const char* from = (const char*)record;
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            k[t] = *(const uint32_t*)(from + lane * 4 * S + 4 * t);
+            v[t] = *(const uint32_t*)(from + 256 * S + lane * 4 * S + 4 * t);
+            value_scale[2 * t] = *(const uint32_t*)(from + 544 * S + h * 8 * S + 8 * t);
+            value_scale[2 * t + 1] = *(const uint32_t*)(from + 544 * S + h * 8 * S + 8 * t + 4);
+            key_scale[t] = *(const uint16_t*)(from + scale_at(S, x16, t));
+        }
+    }
+    // what lies behind the last of `there` keys may be anything
+    __device__ __forceinline__ void cut(int there) {
+        const int count = there - 4 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+        for (int g = 0; g < S; ++g) {
+            value_scale[2 * g] &= first_mask(count);
+            value_scale[2 * g + 1] &= first_mask(count - 2);
+        }
+    }
+    // as record r of a tile: keys as wave_state takes them, values as [value][key]
+    template <int PITCH, int DP>
+    __device__ __forceinline__ void put(char* keys, char* values, int r) const {
+        typedef tile_shape<DP> SH;
+        const int lane = threadIdx.x & 63, h = lane >> 4, x16 = lane & 15, key = 16 * (r & 1) + x16;
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            const uint32_t both = __builtin_amdgcn_perm(key_scale[t], key_scale[t], 0x01000100u);
+            u32x4 x = words16<ACT>(k[t], both, both);
+            *(u32x4*)(keys + (r >> 1) * SH::BYTES + key * SH::PITCH + key_unit<SH::UNITS>(key, 4 * t + h) * 16) = x;
+            x = words16<ACT>(v[t], value_scale[2 * t], value_scale[2 * t + 1]);
+            char* to = values + (32 * t + x16) * PITCH + (16 * r + 4 * h) * 2;
+            *(u32x2*)to = u32x2{x[0], x[1]};
+            *(u32x2*)(to + 16 * PITCH) = u32x2{x[2], x[3]};
+        }
+    }
+};
+
+// GROUPS x 32 rows a block, as over a cache of 16 bits, its waves a record of a tile each: the next tile's are taken to 16 bits beside the products of the
+// present one, the one's after it are on their way.  Values lie as [value][key], rows 8 bytes longer than a tile's keys so that a read's 32 rows
+// fall on different banks.
+template <int S, int WAVES>
+struct tile_room {
+    static constexpr int DP = S < 2 ? 64 : 32 * S, TILE = RECORD * WAVES, PITCH = 2 * TILE + 8;
+    static constexpr int KEY_BYTES = TILE / 32 * tile_shape<DP>::BYTES, BYTES = KEY_BYTES + DP * PITCH;
+    static constexpr int JOIN = 32 * DP * 4;
+    template <int GROUPS>
+    static constexpr int all() { return GROUPS < WAVES && WAVES * JOIN > 2 * BYTES ? WAVES * JOIN : 2 * BYTES; }
+};
+template <int ACT, int S, int GROUPS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void fq_attention_kv4_tile_kernel(fq_tree_args a, tree_plan p, divisor by_records) {
+    typedef tile_room<S, WAVES> room;
+    constexpr int DP = room::DP, TILE = room::TILE, PITCH = room::PITCH;
     typedef tile_shape<DP> SH;
-    constexpr int KEY_BYTES = 2 * SH::BYTES, PITCH = 2 * KEYS + 8, VALUE_BYTES = DP * PITCH;
-    constexpr int JOIN = 32 * DP * 4, PARTS = 4 / GROUPS, HALVES = 2 / PARTS;
-    constexpr int ALL = KEY_BYTES + VALUE_BYTES + 4 * RING * BYTES, ROOM = PARTS > 1 && 4 * JOIN > ALL ? 4 * JOIN : ALL;
+    constexpr int PARTS = WAVES / GROUPS, OWN = TILE / 32 / PARTS, HALVES = OWN < 2 ? OWN : 2;       // OWN: half-tiles of 32 keys that a wave takes
     extern __shared__ __align__(16) char lds[];
-    int32_t* entries = (int32_t*)(lds + ROOM);
+    int32_t* entries = (int32_t*)(lds + room::template all<GROUPS>());
     float* stats = (float*)(entries + TABLE);           // [4][32][2], and a flag
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4, x16 = lane & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = wave % GROUPS, part_of = wave / GROUPS;
     const int D = a.head_dim;
-    char *keys = lds, *values = lds + KEY_BYTES, *mine = lds + KEY_BYTES + VALUE_BYTES + wave * RING * BYTES;
-    const uint32_t mine_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
 
     const line all(a, p);
     const int64_t block = p.in_line(blockIdx.x), begin = block * all.per_block, stop = min(all.total, begin + all.per_block);
@@ -831,85 +881,68 @@ __global__ __launch_bounds__(256, 2) void fq_attention_kv4_tile_kernel(fq_tree_a
     int context = all.context(b), tiles = tiles_of(a, p, context);
     int u = (int)quotient(begin - at_b, tiles + p.extra), t0 = (int)(begin - at_b - (int64_t)u * (tiles + p.extra));
     wave_state<ACT, DP> w;
+    record_words<ACT, S> words;
 
     for (int64_t pos = begin; pos < stop;) {
         const unit_rows<kv4_rows> rows(a, p, b, u, 0, context);
         const int t1 = (int)min((int64_t)tiles, t0 + stop - pos);
         if (t0 < tiles) {                               // (behind them are places that hold nothing)
         float* slot = t0 == 0 && t1 == tiles ? nullptr : p.slot(block, pos == begin, 0);
-        const int key0 = t0 * KEYS, key1 = p.whole ? rows.keys : min(rows.keys, t1 * KEYS);
+        const int key0 = t0 * TILE, key1 = p.whole ? rows.keys : min(rows.keys, t1 * TILE);
         const int r = group * 32 + (lane & 31), row = min(r, rows.count - 1);
         const bool busy = group * 32 < rows.count;
         w.load_query(rows.query(row), D);
         w.clear();
-        const int most = part_keys(TABLE, a.cache.page_size, KEYS);
+        const int most = part_keys(TABLE, a.cache.page_size, TILE);
         for (int part = key0, part_end; part < key1; part = part_end) {
             part_end = fqa::part_end(part, key1, most);
             __syncthreads();
-            const table_part table = load_table<256>(a, b, part, part_end, entries);
+            const table_part table = load_table<64 * WAVES>(a, b, part, part_end, entries);
             if (32 * S < DP) {                          // values that no record has: zeros
                 const u32x4 zero = {0, 0, 0, 0};
-                for (int x = threadIdx.x; x < (KEY_BYTES + VALUE_BYTES) / 16; x += 256) ((u32x4*)lds)[x] = zero;
+                for (int x = threadIdx.x; x < 2 * room::BYTES / 16; x += 64 * WAVES) ((u32x4*)lds)[x] = zero;
             }
             __syncthreads();
             w.query_is_here();                          // (with the table)
             const record_places places = {entries, table.first, by_records, a.cache.page_size / RECORD,
                                           (const char*)a.cache.k + rows.head * a.cache.head_stride, a.cache.page_stride};
-            const int last = (part_end - 1) / RECORD, steps = (part_end - part + KEYS - 1) / KEYS;
-            auto load = [&](int i) {
-                record_loads<S>::issue(mine_at + (uint32_t)(i % RING) * BYTES, places.template place<BYTES>(min((part + i * KEYS) / RECORD + wave, last)));
+            const int last = (part_end - 1) / RECORD, steps = (part_end - part + TILE - 1) / TILE;
+            auto fetch = [&](int i) { words.fetch(places.template place<record_bytes(S)>(min((part + i * TILE) / RECORD + wave, last))); };
+            auto put = [&](int i) {
+                if (part + (i + 1) * TILE > part_end) words.cut(part_end - part - i * TILE - RECORD * wave);
+                char* to = lds + (i & 1) * room::BYTES;
+                words.template put<PITCH, DP>(to, to + room::KEY_BYTES, wave);
+                if (i + 1 < steps) fetch(i + 1);
             };
-            for (int i = 0; i < min(steps, RING); ++i) load(i);
+            fetch(0);
+            put(0);
+            __syncthreads();
             for (int i = 0; i < steps; ++i) {
-                const int base = part + i * KEYS;
-                if (i + RING - 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * LOADS) : "memory");
-                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                const char* from = mine + (i % RING) * BYTES;
-                uint32_t k[S], v[S], key_scale[S], value_scale[2 * S];
-                read_words(from + lane * 4 * S, k);
-                read_words(from + 256 * S + lane * 4 * S, v);
-                read_words(from + 544 * S + h * 8 * S, value_scale);
+                const int base = part + i * TILE;
+                const char* tile = lds + (i & 1) * room::BYTES;
+                if (i + 1 < steps) put(i + 1);
+                if (busy) {
+#pragma unroll 1
+                    for (int y = 0; y < OWN; y += HALVES) {
+                        const int first = base + (part_of * OWN + y) * HALF;
+                        if (OWN > HALVES && first >= part_end) break;
+                        f32x16 s[HALVES];
+                        u32x4 x[2 * HALVES];
+                        w.template scores<HALVES, 6>(tile + (part_of * OWN + y) * SH::BYTES, s);
+                        if (first + HALVES * HALF > min(rows.context, part_end)) {
 #pragma unroll
-                for (int t = 0; t < S; ++t) key_scale[t] = *(const uint16_t*)(from + scale_at(S, x16, t));
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (i + RING < steps) load(i + RING);
-                if (base + KEYS > part_end) {           // what lies behind the last key may be anything
-                    const int count = part_end - base - 16 * wave - 4 * h;
-#pragma unroll
-                    for (int g = 0; g < S; ++g) {
-                        value_scale[2 * g] &= first_mask(count);
-                        value_scale[2 * g + 1] &= first_mask(count - 2);
+                            for (int z = 0; z < HALVES; ++z) keep_seen(s[z], rows.seen(row, first + z * HALF));
+                        }
+                        w.template soften<HALVES>(s, p.factor, x);
+                        accumulate<HALVES, PITCH>(w, tile + room::KEY_BYTES + (part_of * OWN + y) * HALF * 2, x);
                     }
                 }
-                __syncthreads();                        // (the tile before has been read)
-                const int key = 16 * (wave & 1) + x16;
-#pragma unroll
-                for (int t = 0; t < S; ++t) {
-                    const uint32_t both = key_scale[t] * 0x10001u;
-                    u32x4 x = words16<ACT>(k[t], both, both);
-                    *(u32x4*)(keys + (wave >> 1) * SH::BYTES + key * SH::PITCH + key_unit<SH::UNITS>(key, 4 * t + h) * 16) = x;
-                    x = words16<ACT>(v[t], value_scale[2 * t], value_scale[2 * t + 1]);
-                    char* to = values + (32 * t + x16) * PITCH + (16 * wave + 4 * h) * 2;
-                    *(u32x2*)to = u32x2{x[0], x[1]};
-                    *(u32x2*)(to + 16 * PITCH) = u32x2{x[2], x[3]};
-                }
                 __syncthreads();
-                if (!busy) continue;
-                const int first = base + part_of * HALF;
-                f32x16 s[HALVES];
-                u32x4 x[2 * HALVES];
-                w.template scores<HALVES>(keys + part_of * SH::BYTES, s);
-                if (first + HALVES * HALF > min(rows.context, part_end)) {
-#pragma unroll
-                    for (int y = 0; y < HALVES; ++y) keep_seen(s[y], rows.seen(row, first + y * HALF));
-                }
-                w.template soften<HALVES>(s, p.factor, x);
-                accumulate<HALVES, PITCH>(w, values + part_of * HALF * 2, x);
             }
         }
         w.finish(PARTS > 1 || slot);
         if constexpr (PARTS > 1) {
-            join_parts<ACT, DP, PARTS>(rows, w, lds, JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
+            join_parts<ACT, DP, PARTS>(rows, w, lds, room::JOIN, stats, group, GROUPS, part_of, group, key0, key1, slot);
         } else {
             if (!w.sound()) rows.template one_by_one<ACT>(key0, key1, slot, group * 32, min(group * 32 + 32, rows.count), 1);
             else if (r < rows.count) w.put(rows.result(r), slot, p.shape(), r, [&] { return rows.sees_any(r); });
@@ -933,14 +966,14 @@ int launch_stream(const fq_tree_args& a, const tree_plan& p, const divisor& by_r
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
-template <int ACT, int S, int GROUPS>
+template <int ACT, int S, int GROUPS, int WAVES>
 int launch_tiles(const fq_tree_args& a, const tree_plan& p, const divisor& by_records, hipStream_t stream) {
-    constexpr int DP = S < 2 ? 64 : 32 * S, ALL = 2 * tile_shape<DP>::BYTES + DP * (2 * KEYS + 8) + 12 * record_bytes(S), JOIN = 4 * 32 * DP * 4;
+    typedef tile_room<S, WAVES> room;
     static std::atomic<uint64_t> raised{0};
-    const int st = fqd::raise_lds_limit((const void*)fq_attention_kv4_tile_kernel<ACT, S, GROUPS>, raised);
+    const int st = fqd::raise_lds_limit((const void*)fq_attention_kv4_tile_kernel<ACT, S, GROUPS, WAVES>, raised);
     if (st != FQ_OK) return st;
-    const int room = GROUPS < 4 && JOIN > ALL ? JOIN : ALL;
-    fq_attention_kv4_tile_kernel<ACT, S, GROUPS><<<(unsigned)p.blocks, 256, room + TABLE * 4 + 257 * 4, stream>>>(a, p, by_records);
+    const int bytes = room::template all<GROUPS>() + TABLE * 4 + (GROUPS < WAVES ? 257 * 4 : 0);
+    fq_attention_kv4_tile_kernel<ACT, S, GROUPS, WAVES><<<(unsigned)p.blocks, 64 * WAVES, bytes, stream>>>(a, p, by_records);
     return hipGetLastError() == hipSuccess ? FQ_OK : FQ_ERR_HIP;
 }
 
@@ -954,8 +987,9 @@ int launch_few(const fq_tree_args& a, const tree_plan& p, const divisor& by_reco
 template <int ACT, int S>
 int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
     const divisor by_records = divisor::of((uint32_t)(a.cache.page_size / RECORD));
-    const int st = p.unit_rows > 64 ? launch_tiles<ACT, S, 4>(a, p, by_records, stream)
-                   : p.rows > 32    ? launch_tiles<ACT, S, 2>(a, p, by_records, stream)
+    const int st = p.unit_rows > 128  ? launch_tiles<ACT, S, 8, 8>(a, p, by_records, stream)
+                   : p.unit_rows > 64 ? launch_tiles<ACT, S, 4, 4>(a, p, by_records, stream)
+                   : p.rows > 32      ? launch_tiles<ACT, S, 2, 4>(a, p, by_records, stream)
                    : p.rows > 16    ? launch_stream<ACT, S, few_rows<ACT, S, 2>, 1>(a, p, by_records, stream)
                    : p.rows > 4     ? launch_few<ACT, S, few_rows<ACT, S, 1>>(a, p, by_records, stream)
                                     : launch_few<ACT, S, four_rows<ACT, S>>(a, p, by_records, stream);
@@ -975,14 +1009,24 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
 
 }  // namespace
 
-// The waves of few rows take heads of their own where there are enough: pieces are four times as long, and few are joined in LDS.
-#ifndef EXTRA
-#define EXTRA 3
-#endif
+// Above 128 rows blocks of 256, which take a key to 16 bits half as often as blocks of 128, where there are six tiles for each of them or more (a block begins
+// with 5 us in which it multiplies nothing).  us, 256 rows and 128: two sequences of 2500 - 3900 tokens, 2800 rows of eight heads 108, 121; eight of 500 - 4095, 192 rows
+// 39.3, 46.5; one of 20 000, 192 rows, which has five, 46.6, 42.1; one of 8000, eight heads of 64, 200 rows, two, 29.1, 23.2.
+static bool wide(const fq_tree_args& a, int64_t rows) {
+    const int64_t tiles = (a.table_width * a.cache.page_size + 127) / 128, units = a.sequences * a.kv_heads * ((rows + 255) / 256);
+    return rows > 128 && tiles * units >= 6 * (int64_t)fq_cu_count();
+}
+
+// Few rows: waves take heads of their own where there are enough, so that pieces are four times as long, and few are joined in LDS.
+// The beginning and end of a unit count as three tiles, one of 128 keys (a token each of 64 sequences of 100 - 8191: 40.8 us where they count as none, 29.1 so; two
+// sequences' pieces as above, none 108.8, one 108.4, two 107.6, eight sequences' trees 42.6, 39.3, 42.1).
 static tree_plan plan_kv4(const fq_tree_args& a) {
-    const int rows = a.nodes * (a.q_heads / a.kv_heads);
+    const int64_t rows = (int64_t)a.nodes * (a.q_heads / a.kv_heads);
     const int heads = rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
-    return plan_units(a, heads, rows > 32 ? KEYS : (rows > 4 ? 128 : 256) / heads, EXTRA);
+    if (!wide(a, rows)) return plan_units(a, heads, rows <= 64 ? 64 : 128, rows > 32 ? KEYS : (rows > 4 ? 128 : 256) / heads, 3);
+    tree_plan p = plan_units(a, 1, 256, 128, 1);
+    p.blocks /= 2;                       // (one has a compute unit's LDS for itself)
+    return p;
 }
 
 size_t fq_tree_kv4_bytes(const fq_tree_args& a) { return slots_bytes(plan_kv4(a)); }

@@ -236,7 +236,7 @@ struct wave_state {
     }
 
     // S^T of H half-tiles of keys in LDS.  Score i of half-tile t belongs to key 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4.
-    template <int H>
+    template <int H, int MOST = 8>
     __device__ __forceinline__ void scores(const char* keys, f32x16 (&s)[H]) const {
         const int lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31;
 #pragma unroll
@@ -245,7 +245,7 @@ struct wave_state {
             for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
         // keys are read AHEAD products before they are multiplied (left to itself the compiler reads them one product ahead, which
         // has every product wait for LDS)
-        constexpr int N = SH::STEPS * H, AHEAD = N < 8 ? N : 8;
+        constexpr int N = SH::STEPS * H, AHEAD = N < MOST ? N : MOST;
         u32x4 k[AHEAD];
         auto read = [&](int n) {
             const int t = n % H, step = n / H;

@@ -265,7 +265,7 @@ tree_plan plan_tree(const fq_tree_args& a) {
     // 256.  That makes four times as many pieces as waves that share the keys out, of sums that are no longer few from 16 rows on.
     const int rows = a.nodes * (a.q_heads / a.kv_heads);
     const int heads = rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
-    tree_plan p = plan_units(a, heads, rows > 32 ? KEYS : 128 / heads, 0);
+    tree_plan p = plan_units(a, heads, rows_of_tile(rows, a.head_dim), rows > 32 ? KEYS : 128 / heads, 0);
     // 131 000 tokens, 537 MB, 64 rows 113.6 -> 103.1 us, 268 MB 49.2 -> 47.1; 100 000, 96 rows 99.6 -> 90.5; what the 256 MiB Infinity Cache may still hold from the last call: 16 sequences
     // of 2000 - 4000, 100 MB, 39.0, past it 41.3.
     p.once = p.row_tiles == 1 && (double)a.sequences * a.table_width * a.cache.page_size * a.kv_heads * a.head_dim * 4 > 0x1p28;

@@ -364,13 +364,14 @@ __global__ __launch_bounds__(1024) void fq_attention_tree_join_kernel(fq_tree_ar
 // eight sequences of 500 - 4095, groups of four: 49.8 -> 45.6 us; heads of 96, 160 rows, 32.6, in three 33.4)
 inline int rows_of_tile(int64_t rows, int head_dim) { return rows <= 64 || (rows > 128 && rows <= 192 && head_dim > 96) ? 64 : ROWS; }
 
-// The plan of a call whose blocks take `heads` key heads together (up to 32 rows a head; above, one), `tile` keys at a time; extra: see tree_plan.
-inline tree_plan plan_units(const fq_tree_args& a, int heads, int tile, int extra) {
+// The plan of a call whose blocks take `heads` key heads together (up to 32 rows a head; above, one) and unit_rows rows of each, `tile` keys at a time; extra:
+// see tree_plan.
+inline tree_plan plan_units(const fq_tree_args& a, int heads, int unit_rows, int tile, int extra) {
     tree_plan p = {};
     p.group = a.q_heads / a.kv_heads;
     p.rows = a.nodes * p.group;      // (fq_tree_fits)
     p.heads = heads;
-    p.unit_rows = rows_of_tile(p.rows, a.head_dim);
+    p.unit_rows = unit_rows;
     p.row_tiles = (p.rows + p.unit_rows - 1) / p.unit_rows;
     p.slot_rows = p.rows < 32 ? p.rows : ((p.rows < p.unit_rows ? p.rows : p.unit_rows) + 31) / 32 * 32;
     p.D = a.head_dim;
