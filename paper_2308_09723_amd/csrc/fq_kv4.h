@@ -59,11 +59,11 @@ __device__ __forceinline__ uint32_t codes16(uint32_t x) {
     else
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 512.0f, HIGH));
 }
-// Four codes (-7 .. 7) as bytes, sign and magnitude in bits 7, 2 .. 0 (the sign of a zero is anything)
+// Four quotients as codes, the nearest numbers (halves to even, 7 for 7.5), sign and magnitude in bits 7, 2 .. 0 of a byte (the sign of a zero is anything)
 __device__ __forceinline__ uint32_t coded(const float* q) {
     uint32_t x = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_cvt_pk_u8_f32(__builtin_fabsf(q[i]), i, x);
+    for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_cvt_pk_u8_f32(__builtin_fminf(__builtin_fabsf(q[i]), 7.0f), i, x);
     const uint32_t low = __builtin_amdgcn_perm(__float_as_uint(q[1]), __float_as_uint(q[0]), 0x0c0c0703u),
                    high = __builtin_amdgcn_perm(__float_as_uint(q[3]), __float_as_uint(q[2]), 0x07030c0cu);       // their top bytes
     return x | ((low | high) & 0x80808080u);
@@ -82,7 +82,8 @@ struct group_scale {
     template <int ACT>
     __device__ static group_scale of(float m) {
         constexpr int BITS = ACT == FQ_F16 ? 8 : 5, LEAST = ACT == FQ_F16 ? -24 : -133;
-        const float x = m / 7.5f;             // (its error never passes a whole number: those are exact)
+        // m / 7.5, too large by less than 2^-23 of it.  m 2^-k is a multiple of 1 / 8, a quotient that is not whole at least 1 / 60 away from one.
+        const float x = m * 0x1.111112p-3f;
         const int e = m > 0.0f ? __builtin_amdgcn_frexp_expf(x) : LEAST;
         group_scale s;
         s.k = e - BITS > LEAST ? e - BITS : LEAST;
@@ -91,14 +92,18 @@ struct group_scale {
         return s;
     }
     __device__ float value() const { return __builtin_amdgcn_ldexpf(n, k); }
-    // What code() multiplies values times 2^-k with
-    __device__ float inverse() const { return n == 0.0f ? 0.0f : 1.0f / n; }
-    // The code of w, |w| <= m: the nearest number to w / s, halves to even, and 7 for 7.5.  w 2^-k times 1 / n is off by less than 2^-19.  The
-    // quotient is a half exactly or 2^-12 away from one (values have 11 bits, n 8), so that the addition, which leaves multiples of 2^-16,
-    // makes halves exact and takes nothing else to the other side of one.
-    __device__ float code(float w, float inverse) const {
-        const float x = __builtin_amdgcn_ldexpf(w, -k) * inverse + 128.0f;
-        return __builtin_amdgcn_fmed3f(__builtin_rintf(x - 128.0f), -7.0f, 7.0f);
+    // What quotient() multiplies values with (bfloat16: values times 2^-k, whose product with it may be too large for one)
+    template <int ACT>
+    __device__ float inverse() const {
+        const float x = n == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(n);
+        return ACT == FQ_F16 ? __builtin_amdgcn_ldexpf(x, -k) : x;
+    }
+    // w / s for |w| <= m, halves exactly.  The product with the inverse (whose last bit may be wrong) is off by less than 2^-20.  The quotient is a half
+    // exactly or 2^-12 away from one (values have 11 bits, n 8), so that the addition, which leaves multiples of 2^-16, makes halves exact and takes
+    // nothing else to the other side of one.
+    template <int ACT>
+    __device__ float quotient(float w, float inverse) const {
+        return __builtin_fmaf(ACT == FQ_F16 ? w : __builtin_amdgcn_ldexpf(w, -k), inverse, 128.0f) - 128.0f;
     }
 };
 #endif

@@ -107,6 +107,30 @@ def test_large_small_and_broken_values(dtype):
     assert int(want.isnan().sum()) == 3 * 32
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_every_largest_value(dtype):
+    """Groups whose largest magnitude is each finite number of the type, with random values, halves of scales and their neighbours beside it."""
+    top = torch.arange(1, 0x7c00 if dtype == F16 else 0x7f80).to(torch.int16).view(dtype)
+    n = len(top)
+    gen = torch.Generator().manual_seed(5)
+    x = (torch.rand((n, 32), generator=gen, dtype=torch.float64) * 2 - 1) * top.double()[:, None]
+    scales = torch.tensor([ref.scale_of(m, dtype) for m in top.double().tolist()], dtype=torch.float64)
+    x[:, :15] = scales[:, None] * (torch.arange(15) - 7 + 0.5 * (torch.rand((n, 15), generator=gen) < 0.8)).clamp(-7, 7)
+    x = x.to(dtype)
+    x[:, 15:20] = (x[:, :5].view(torch.int16) + 1).view(dtype)
+    x[:, 20:25] = (x[:, 9:14].view(torch.int16) - 1).view(dtype)
+    x = torch.where(x.double().abs() <= top.double()[:, None], x, 0)
+    x[torch.arange(n), torch.randint(0, 32, (n,), generator=gen)] = top * torch.where(torch.rand(n, generator=gen) < 0.5, -1.0, 1.0).to(dtype)
+    pages = (n + 63) // 64
+    cache = torch.zeros((pages, fq.kv4_page_bytes(64, 1, 32)), dtype=torch.uint8, device="cuda")
+    slots = torch.arange(n).cuda()
+    k = x.view(n, 1, 32).cuda()
+    fq.kv4_write(k, -k, cache, 64, slots)
+    want = torch.round(x.double() / scales[:, None]).clamp(-7, 7) * scales[:, None]
+    for back, sign in zip(fq.kv4_read(cache, 64, 1, 32, slots, dtype), (1, -1)):
+        assert torch.equal(back.cpu().double().view(n, 32) * sign, want)
+
+
 def test_read_takes_slots_twice_and_outside():
     k, v = _normal((4, 2, 64), F16, 1), _normal((4, 2, 64), F16, 2)
     device, _ = _stored(k.cuda(), v.cuda(), 16, 3, torch.tensor([0, 17, 18, 40]))
