@@ -184,7 +184,7 @@ __global__ __launch_bounds__(256) void fq_adapter_up_few_kernel(fq_adapter_args 
 }
 
 // ------------------------------------------------------------------------------------------ t = x A^T, 64 rows a block
-// RT x 16 ranks, one of gridDim.x parts of K in chunks of 128.  A wave has 16 of the rows.  A chunk's rows of x and A lie in LDS as 16 units of 16
+// RT x 16 ranks, one of gridDim.x parts of K in chunks of 128, one of gridDim.z's turns of the tile's adapters.  A wave has 16 of the rows.  A chunk's rows of x and A lie in LDS as 16 units of 16
 // bytes, moved about within the row so that 16 rows' same unit falls on different banks; the next chunk is on its way beside the present one.
 template <int ACT, int RT>
 __global__ __launch_bounds__(256, 2) void fq_adapter_down_kernel(fq_adapter_args a) {
@@ -197,7 +197,9 @@ __global__ __launch_bounds__(256, 2) void fq_adapter_down_kernel(fq_adapter_args
     const int part = blockIdx.x, each = (chunks + (int)gridDim.x - 1) / (int)gridDim.x, begin = part * each, end = min(chunks, begin + each);
     distinct tile(id_of(a, row0 + lane));
     const int mine = __shfl(tile.id, 16 * wave + x16);
-    for (int id = tile.next(); id >= 0; id = tile.next()) {
+    int turn = 0;
+    for (int id = tile.next(); id >= 0; id = tile.next(), ++turn) {
+        if (turn % (int)gridDim.z != (int)blockIdx.z) continue;
         const bool busy = __any(mine == id);
         for (int r0 = 0; r0 < ranks; r0 += 16 * RT) {
             f32x4 t[RT];
@@ -420,10 +422,13 @@ adapter_plan plan(int64_t rows, int adapters, int rank, int64_t N, int64_t K) {
     adapter_plan p;
     p.few = rows <= FEW;
     const int64_t tiles = (rows + (p.few ? 15 : 63)) / (p.few ? 16 : 64), most = rows < 16 ? rows : 16;
-    p.slots = p.few ? (int)(adapters < most ? adapters : most) : 1;
+    // More rows: of a prompt's tiles most have one adapter, some two, whose second turn is another block's (rows of 5 requests, as below: 43.7 us by the same, 29.0).
+    p.slots = p.few ? (int)(adapters < most ? adapters : most) : adapters < 4 ? adapters : 4;
     const int64_t pieces = p.few ? (K + 31) / 32 : (K + 127) / 128, least = p.few ? 16 : 4;        // pieces of K; of a block, at least
-    const int64_t wanted = 512 / (tiles * p.slots), fit = (pieces + least - 1) / least;
+    const int64_t wanted = p.few ? 512 / (tiles * p.slots) : 464 / tiles, fit = (pieces + least - 1) / least;
     p.parts = (int)(wanted < 1 ? 1 : wanted < fit ? wanted : fit);
+    // (blocks go to the eight dies in turn: a part's columns of A stay in one die's cache; eight parts 29.0 us, ten 35.6, sixteen 31.7)
+    if (p.parts > 8) p.parts = p.parts / 8 * 8;
     const int64_t each = (pieces + p.parts - 1) / p.parts;
     p.parts = (int)((pieces + each - 1) / each);
     int64_t turns;
@@ -472,7 +477,7 @@ int down(const fq_adapter_args& a, const adapter_plan& p, hipStream_t stream) {
     static std::atomic<uint64_t> raised{0};
     const int st = fqd::raise_lds_limit((const void*)fq_adapter_down_kernel<ACT, RT>, raised);
     if (st != FQ_OK) return st;
-    const dim3 grid((unsigned)p.parts, (unsigned)((a.rows + 63) / 64));
+    const dim3 grid((unsigned)p.parts, (unsigned)((a.rows + 63) / 64), (unsigned)p.slots);
     fq_adapter_down_kernel<ACT, RT><<<grid, 256, 2 * (64 + 16 * RT) * 256, stream>>>(a);
     return status();
 }
