@@ -10,7 +10,9 @@
 // address unit four times as long as one of four rows' 256).  t goes into the second product as the sum of two 16-bit numbers (16 bits and
 // more of it), in binary16 after a division by a power of two that brings the row's largest to about one.
 //
-// Bound by memory: A and B of each adapter, x once, the output twice.
+// Bound by memory: A and B of each adapter, x once, the output twice.  One row, K and N 1024, rank 8: 2.8 + 3.2 us, launches; 64 rows of 64 adapters, K 4096, N 6144,
+// rank 16, 20 MB: 6.2 + 6.2; 2900 rows of 5 requests, K 12288, N 36864, rank 64: 28.4 for the inner sums (71 MB of x: 2.5 TB/s), 5.2 to fold them, 105 for the output (428 MB
+// read and written: 4.1 TB/s).
 #include <hip/hip_runtime.h>
 #include <atomic>
 
@@ -27,7 +29,8 @@ using fqa::type16;
 using fqa::u32x2;
 using fqa::u32x4;
 
-constexpr int FEW = 64;              // rows
+// Rows up to which each is taken to have an adapter of its own (a tile of 64 rows is where the kernels for more begin to have one block's work)
+constexpr int FEW = 64;
 
 template <int ACT>
 __device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, const f32x4& c) {
