@@ -4,7 +4,7 @@
 // adapters and all its rows, and a row takes those of its own adapter, whatever others hold.  (Requests' rows lie side by side, so that
 // a tile of a prompt has one or two.)
 //
-// Up to FEW rows each is likely to have an adapter of its own, whose bytes bind it: the first kernel takes 16 rows as the columns of products of
+// Where rows are few each is likely to have an adapter of its own, whose bytes bind it: the first kernel takes 16 rows as the columns of products of
 // 16 x 16 x 32, the second makes dot products, eight ranks a lane.
 // More rows: 64 a block, everything through LDS, in pieces that neighbouring lanes read side by side (a load of 64 rows' 16 bytes takes the
 // address unit four times as long as one of four rows' 256).  t goes into the second product as the sum of two 16-bit numbers (16 bits and
@@ -29,8 +29,10 @@ using fqa::type16;
 using fqa::u32x2;
 using fqa::u32x4;
 
-// Rows up to which each is taken to have an adapter of its own (a tile of 64 rows is where the kernels for more begin to have one block's work)
-constexpr int FEW = 64;
+// Rows that are taken to have adapters of their own: where that costs little if they have not, and up to 256 where there are many adapters.  us, K 4096 and N 6144, so and with
+// 64 rows a block: 64 rows of rank 64, 64 adapters in turn 21.5, 149, three requests' 14.1, 16.4; 256 of rank 16, 19.7, 88.6 and 12.0, 13.2; 256 of rank 64, 42.5, 150 and 25.1,
+// 15.9; 512 of rank 16, 31.8, 97.3 and 17.3, 14.1.
+inline bool few_rows(int64_t rows, int64_t adapters, int rank) { return rows * rank <= 4096 || (adapters > 8 && rows <= 256); }
 
 template <int ACT>
 __device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, const f32x4& c) {
@@ -423,7 +425,7 @@ struct adapter_plan {
 
 adapter_plan plan(int64_t rows, int adapters, int rank, int64_t N, int64_t K) {
     adapter_plan p;
-    p.few = rows <= FEW;
+    p.few = few_rows(rows, adapters, rank);
     const int64_t tiles = (rows + (p.few ? 15 : 63)) / (p.few ? 16 : 64), most = rows < 16 ? rows : 16;
     // More rows: of a prompt's tiles most have one adapter, some two, whose second turn is another block's (rows of 5 requests, as below: 43.7 us by the same, 29.0).
     p.slots = p.few ? (int)(adapters < most ? adapters : most) : adapters < 4 ? adapters : 4;
@@ -439,10 +441,12 @@ adapter_plan plan(int64_t rows, int adapters, int rank, int64_t N, int64_t K) {
         int lanes = 1;
         while (8 * lanes < rank) lanes *= 2;
         const int64_t steps = (N * lanes + 63) / 64;           // of a row, all columns
-        turns = (rows * steps + 4095) / 4096;                  // (two waves a SIMD and more)
+        // (four waves a SIMD: 64 rows, N 6144, rank 16, 10.2 us; sixteen 12.2; rank 64, N and K 12288, 37.7 and 40.1)
+        turns = (rows * steps + 4095) / 4096;
         turns = turns < 4 ? 4 : turns > 32 ? 32 : turns;
     } else {
         const int64_t all = tiles * ((N + 127) / 128);
+        // (eight blocks a compute unit: 2900 rows, N 36864, rank 64, 127.5 us in all; two 137.8, a turn each 138.4)
         turns = all / 2048;
         turns = turns < 1 ? 1 : turns > 8 ? 8 : turns;
     }

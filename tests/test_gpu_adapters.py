@@ -74,6 +74,7 @@ CASES = [  # rows, N, K, adapters, rank, ids
     (1, 8, 8, 1, 8, "first"), (1, 1024, 1024, 4, 8, "first"), (3, 776, 520, 2, 24, "turns"), (16, 64, 4096, 16, 16, "turns"), (17, 200, 64, 3, 32, "some"),
     (64, 1536, 2048, 64, 16, "turns"), (64, 96, 40, 5, 128, "any"), (65, 136, 72, 4, 8, "runs"), (63, 256, 264, 3, 72, "some"), (100, 328, 1032, 7, 64, "runs"), (256, 128, 256, 2, 40, "runs"), (257, 264, 512, 5, 16, "runs"),
     (300, 136, 328, 40, 72, "any"), (700, 72, 96, 3, 64, "runs"), (1000, 520, 64, 9, 128, "runs"), (600, 24, 4104, 1, 32, "first"),
+    (256, 72, 264, 20, 48, "any"), (512, 64, 128, 3, 8, "runs"), (130, 200, 72, 9, 128, "turns"), (100, 328, 1032, 9, 64, "any"), (255, 1032, 16, 300, 16, "turns"),
 ]
 
 
