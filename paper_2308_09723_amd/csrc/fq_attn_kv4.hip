@@ -13,8 +13,8 @@
 //
 // Above 32 rows (fq_attention_kv4_tile_kernel) the waves of a block take a tile's codes to 16 bits once, each a record, into tiles that all of them read: keys
 // as over a cache of 16 bits, values turned over (a lane has four tokens of a value).  Bound by instructions: for 32 rows and 64 keys a wave has 32 products, 170
-// instructions' time for the numerators and, of four waves, 200 for the codes, of eight 100.  Pieces of 700 tokens over 2500 - 3900, two sequences, 32 heads over 8: 118 us (0.81
-// PFLOP/s) and 17 to join.
+// instructions' time for the numerators and, of four waves, 200 for the codes, of eight 100.  Pieces of 700 tokens over 2500 - 3900, two sequences, 32 heads over 8: 134 us with
+// the join, 0.72 PFLOP/s; over 16 bits 151.
 #include <hip/hip_runtime.h>
 #include <atomic>
 
