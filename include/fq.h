@@ -470,7 +470,7 @@ int fq_attention_tree_kv4(const fq_heads* q, int act_dtype, int64_t sequences, i
  * Pages that sequences share.  A pool of `pages` pages: refs[p] (device) is the number of rows that hold page p, a page with none (0 or less) is free; whoever keeps
  * a page for something else sets its refs to 1.  A row of `table` [rows, width] (device) holds the pages of one sequence, its first
  * ceil(lens[r] / page_size) entries (as many as width has; entries that are no page of the pool are kept and not counted).  Only a sequence's last page, where it is not full, is ever written
- * to, so that full pages may be several rows'.  What the pages hold lies in buffers: any number of tensors with room for all pages each (layers;
+ * to, so that full pages may be several rows' (a row is not shortened into one).  What the pages hold lies in buffers: any number of tensors with room for all pages each (layers;
  * keys and values of fq_kv_pages, whose pages are contiguous; fq_kv4_pages).
  * All of it happens on the device, so that a captured step may be replayed; free pages are taken in their order, the lowest first, so that results are the same
  * every time.  Calls on one pool must be ordered on one stream.  Asynchronous, no allocation.

@@ -146,3 +146,29 @@ def test_captured_with_other_adapters():
         assert torch.equal(out, eager)
         want, tol = _reference(x.cpu(), a.cpu(), b.cpu(), ids.cpu(), before.cpu(), scales.cpu())
         assert bool(((eager.cpu().double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("rows", [3, 300])
+def test_adapters_beyond_four_gigabytes(rows):
+    N, rank, count = 1 << 18, 128, 70
+    b = torch.empty((count, N, rank), dtype=F16, device="cuda")
+    for i in range(count):
+        b[i].fill_(0.0)
+    x, a = _normal((rows, 16), F16, 1), _normal((count, rank, 16), F16, 2)
+    at = torch.randint(0, N, (40,), generator=torch.Generator().manual_seed(3))
+    at[0], at[1] = 0, N - 1
+    used = [0, 66, 69]       # (66 * 2^18 * 128 values of two bytes)
+    part = _normal((3, 40, rank), F16, 4)
+    for i, id in enumerate(used):
+        b[id, at.cuda()] = part[i].cuda()
+        part[i] = b[id, at.cuda()].cpu()
+    ids = torch.tensor([used[i % 3] for i in range(rows)], dtype=torch.int32)
+    out = torch.zeros((rows, N), dtype=F16, device="cuda")
+    fq.adapters(x.cuda(), a.cuda(), b, ids.cuda(), out)
+    small = torch.zeros((count, 40, rank), dtype=F16)
+    small[used] = part
+    want, tol = _reference(x, a, small, ids, torch.zeros((rows, 40), dtype=F16), None)
+    assert bool(((out[:, at.cuda()].cpu().double() - want).abs() <= tol).all())
+    other = torch.ones(N, dtype=torch.bool, device="cuda")
+    other[at.cuda()] = False
+    assert not bool((out * other).any())

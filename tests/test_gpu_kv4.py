@@ -343,3 +343,75 @@ def test_captured_with_other_lengths(nodes):
         k, v = fq.kv4_read(cache, page, hk, D, every.cuda(), BF16)
         want, tol = attention.tree(q.cpu(), k.cpu().view(pages, page, hk, D), v.cpu().view(pages, page, hk, D), order, contexts.tolist(), attention.chain(B, nodes))
         attention.compare(got, want, tol, f"replay {i}")
+
+
+@pytest.mark.parametrize("nodes", [1, 3, 7, 20, 40, 150])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_ends_of_the_table(nodes, dtype):
+    """Lengths that a table has no room for (what lies behind it does not exist), tables of no entries, entries that are no pages (brought into the cache)."""
+    hk, D, page, pages = 2, 64, 16, 5
+    every = torch.arange(pages * page)
+    k, v = _normal((pages * page, hk, D), dtype, 1), _normal((pages * page, hk, D), dtype, 2)
+    device, _ = _stored(k.cuda(), v.cuda(), page, pages, every)
+    k, v = (ref.quantise(x)[2].to(dtype).view(pages, page, hk, D) for x in (k, v))
+    table = torch.tensor([[3, 1], [0, -7], [1 << 30, 2], [4, 4]], dtype=torch.int32)
+    lens = [20, 1000, 31, 2 ** 31 - 1 - nodes]
+    q = _normal((4, nodes, 4, D), dtype, nodes, 1.5)
+    want, tol = attention.tree(q, k, v, table.clamp(0, pages - 1), [min(n, 32) for n in lens], attention.chain(4, nodes))
+    at = torch.tensor(lens, dtype=torch.int32).cuda()
+    attention.compare(fq.attention_tree_kv4(q.cuda(), device, page, hk, table.cuda(), at), want, tol, "ends")
+    assert not bool(fq.attention_tree_kv4(q.cuda(), device, page, hk, table[:, :0].cuda(), at).any())
+    assert not bool(fq.attention_tree_kv4(q.cuda(), device, page, hk, table.cuda(), torch.full_like(at, -1)).any())
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with a workspace of its own."""
+    hk, D, page, width = 4, 128, 16, 300
+    n = 2 * width * page
+    cache = fq.kv4_cache(2 * width, page, hk, D)
+    fq.kv4_write(_normal((n, hk, D), F16, 1).cuda(), _normal((n, hk, D), F16, 2).cuda(), cache, page, torch.arange(n).cuda())
+    table = torch.randperm(2 * width, generator=torch.Generator().manual_seed(1)).int().view(2, width).cuda()
+    calls = []
+    for nodes in (1, 50):
+        q, lens = _normal((2, nodes, 16, D), F16, nodes).cuda(), torch.tensor([4000, 4700], dtype=torch.int32).cuda()
+        calls.append((q, lens, fq.attention_tree_kv4(q, cache, page, hk, table, lens), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for q, lens, _, stream in calls:
+            with torch.cuda.stream(stream):
+                got.append(fq.attention_tree_kv4(q, cache, page, hk, table, lens))
+        torch.cuda.synchronize()
+        for x, (_, _, want, _) in zip(got, calls):
+            assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("lens,nodes,hq,hk,D,page,how", [([900, 0, 2100], 65, 8, 4, 128, 64, None), ([300, 5], 200, 4, 4, 64, 16, "tree"), ([1500, 40, 700], 70, 4, 2, 96, 48, "tree"),
+                                                         ([130], 300, 2, 2, 128, 32, None), ([77, 1000], 150, 2, 2, 32, 16, "tree"), ([0, 3000], 48, 16, 4, 80, 128, "late"),
+                                                         ([400, 260], 131, 2, 2, 128, 16, "nan")])
+def test_blocks_of_256_rows(lens, nodes, hq, hk, D, page, how, dtype):
+    """Tables as long as such calls have, of which these sequences take a part."""
+    device, table, k, v = _context(lens, nodes, hk, D, page, dtype, nodes)
+    B = len(lens)
+    table = torch.cat([table, torch.full((B, 200000 // page), 1 << 30, dtype=torch.int32)], 1)
+    q = _normal((B, nodes, hq, D), dtype, nodes + 1, 20.0 if how == "late" else 1.5)
+    sees = attention.chain(B, nodes)
+    mask = None
+    if how in ("tree", "nan"):
+        sees = torch.rand((B, nodes, nodes), generator=torch.Generator().manual_seed(2)) < 0.3
+        sees[:, nodes // 3] = False
+        if how == "nan":
+            sees[:, :, 9] = False
+            sees[:, 100, 9] = True
+            slots = torch.stack([table[b].long()[(c + 9) // page] * page + (c + 9) % page for b, c in enumerate(lens)])
+            rows, values = _normal((B, hk, D), dtype, 6), _normal((B, hk, D), dtype, 7)
+            values[:, 1, 40] = math.inf
+            fq.kv4_write(rows.cuda(), values.cuda(), device, page, slots.cuda())
+            k.view(-1, hk, D)[slots], v.view(-1, hk, D)[slots] = ref.quantise(rows)[2].to(dtype), ref.quantise(values)[2].to(dtype)
+        mask = attention.words(sees).cuda()
+    got = fq.attention_tree_kv4(q.cuda(), device, page, hk, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), mask=mask).cpu()
+    want, tol = attention.tree(q, k, v, table[:, :(max(lens) + nodes + page - 1) // page].clamp_max(k.shape[0] - 1), lens, sees)
+    fine = want.isfinite()
+    assert torch.equal(got.isfinite(), fine) and bool(fine.all()) == (how != "nan")
+    assert bool(((got.double() - want).abs() <= tol)[fine].all())

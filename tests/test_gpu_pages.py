@@ -287,3 +287,39 @@ def test_captured_steps():
             model(new)
         p.check(f"replay {i}")
         p.check_holds(f"replay {i}")
+
+
+def test_pages_beyond_four_gigabytes():
+    pages, words = 5000, 1 << 18       # 1 MiB a page
+    cache = torch.zeros((pages, words), dtype=torch.int32, device="cuda")
+    cache[4999] = torch.arange(words, device="cuda").int()
+    cache[4500] = 7
+    fq.pages_copy([cache], torch.tensor([4999, 4500], dtype=torch.int32).cuda(), torch.tensor([4300, 2], dtype=torch.int32).cuda())
+    assert torch.equal(cache[4300], cache[4999]) and bool((cache[2] == 7).all())
+    assert int(cache[4299].any()) + int(cache[4301].any()) + int(cache[3].any()) == 0
+
+
+@pytest.mark.parametrize("rows,children,width", [(0, 3, 4), (3, 0, 4), (5, 7, 0), (1, 1, 1), (1024, 1024, 60), (1025, 3, 2), (1, 1025, 3), (1024, 1024, 70)])
+def test_forks_of_any_size(rows, children, width):
+    """No rows, no children, tables without entries; where one block ends to do it all."""
+    rng = random.Random(rows + children)
+    page = 4
+    m = Model(3 * rows + children + 5000, page, width)
+    m.rows, m.lens = [[-1] * width for _ in range(rows)], [0] * rows
+    p = Pool(m, words=2)
+    if rows:
+        wanted = [rng.randrange(0, 3 * page) for _ in range(rows)]
+        p.take(wanted)
+        m.take(wanted)
+        p.check("take")
+    for release in (False, True):
+        parents = [rng.randrange(-1, rows + 1) for _ in range(children)]
+        if not release:
+            kept = (p.table, p.lens, m.rows, m.lens)
+        p.fork(parents, release)
+        m.fork(parents, release)
+        p.check(f"fork {release}")
+        p.check_holds(f"fork {release}")
+        if not release:
+            p.table, p.lens = kept[:2]
+            m.rows, m.lens = [list(r) for r in kept[2]], list(kept[3])
