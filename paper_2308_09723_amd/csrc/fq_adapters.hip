@@ -277,7 +277,12 @@ struct split8 {
         for (int i = 0; i < 4; ++i) {
             float u = t[2 * i], v = t[2 * i + 1];
             if (ACT == FQ_F16) u = __builtin_amdgcn_ldexpf(u, -e), v = __builtin_amdgcn_ldexpf(v, -e);
-            (*high)[i] = pack2<ACT>(u, v);
+            uint32_t both = pack2<ACT>(u, v);
+            if (ACT == FQ_BF16) {                       // (a number that rounds to infinity: the largest one, and the rest below)
+                if ((both & 0x7fffu) == 0x7f80u && __builtin_fabsf(u) < __builtin_inff()) both -= 1u;
+                if ((both >> 16 & 0x7fffu) == 0x7f80u && __builtin_fabsf(v) < __builtin_inff()) both -= 0x10000u;
+            }
+            (*high)[i] = both;
             const float du = u - half_of<ACT, 0>((*high)[i]), dv = v - half_of<ACT, 1>((*high)[i]);
             (*low)[i] = pack2<ACT>(du == du ? du : 0.0f, dv == dv ? dv : 0.0f);        // (of an infinity: nothing)
         }

@@ -172,3 +172,17 @@ def test_adapters_beyond_four_gigabytes(rows):
     other = torch.ones(N, dtype=torch.bool, device="cuda")
     other[at.cuda()] = False
     assert not bool((out * other).any())
+
+
+@pytest.mark.parametrize("rows", [20, 600])
+def test_inner_sums_that_bfloat16_would_round_to_infinity(rows):
+    """t between bfloat16's largest number and binary32's, exactly the scale here."""
+    x, a = torch.zeros((rows, 64), dtype=BF16), torch.zeros((1, 8, 64), dtype=BF16)
+    x[:, 0], a[0, :, 0] = 1.0, torch.tensor([1.0, -1.0] * 4)
+    b = (torch.arange(16 * 8).view(1, 16, 8) % 11 * 2.0 ** -128).to(BF16)
+    before = _normal((rows, 16), BF16, 1)
+    scales = torch.tensor([3.4e38])
+    assert float(scales[0]) > torch.finfo(BF16).max
+    got = fq.adapters(x.cuda(), a.cuda(), b.cuda(), torch.zeros(rows, dtype=torch.int32).cuda(), before.cuda(), scales.cuda()).cpu().double()
+    want, tol = _reference(x, a, b, torch.zeros(rows, dtype=torch.int32), before, scales)
+    assert bool(((got - want).abs() <= tol).all())
