@@ -13,6 +13,11 @@ import sys
 import warnings
 from concurrent.futures import ThreadPoolExecutor
 
+if __package__:
+    from . import waits
+else:
+    import waits
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
@@ -75,7 +80,7 @@ NO_SPILL_FAMILIES = ["fq_gemm_mid_kernel", "fq_gemm_mid_items_kernel", "fq_w4a8_
                      "fq_attention_tree_stream_kernel", "fq_attention_tree_tile_kernel", "fq_attention_kv4_stream_kernel",
                      "fq_attention_kv4_tile_kernel", "fq_adapter_down_few_kernel", "fq_adapter_down_kernel", "fq_adapter_up_kernel"]
 # Kernels of which no instantiation may have accumulation registers: where the adapters' sums were in them, this compiler read the first of them behind the
-# loop without waiting for the loop's last product.
+# loop without waiting for the loop's last product.  (All kernels are searched for such reads, whatever registers: check_waits.)
 NO_ACCUMULATORS = ["fq_attention_kv4_stream_kernel", "fq_attention_kv4_tile_kernel", "fq_adapter_down_few_kernel", "fq_adapter_down_kernel", "fq_adapter_up_kernel"]
 
 
@@ -151,6 +156,35 @@ def _resource_report(rows, verbose):
         raise RuntimeError("NO_SPILL names kernels that were not compiled: " + ", ".join(missing))
 
 
+def short_waits(obj):
+    """waits.short_waits of an object's code for gfx950."""
+    tools = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin")
+    bundle, code = obj + ".bundle", obj + ".code"
+    try:
+        for cmd in ([os.path.join(tools, "llvm-objcopy"), "--dump-section", ".hip_fatbin=" + bundle, obj, os.devnull],
+                    [os.path.join(tools, "clang-offload-bundler"), "--unbundle", "--type=o", "--targets=hipv4-amdgcn-amd-amdhsa--gfx950",
+                     "--input=" + bundle, "--output=" + code],
+                    [os.path.join(tools, "llvm-objdump"), "-d", "--no-show-raw-insn", "--no-leading-addr", "--symbolize-operands", code]):
+            rc, out = _run(cmd)
+            if "section '.hip_fatbin' not found" in out:       # (host code alone)
+                return []
+            if rc != 0:
+                raise RuntimeError(f"{cmd[0]} failed on {obj}:\n{out}")
+    finally:
+        for path in (bundle, code):
+            if os.path.exists(path):
+                os.remove(path)
+    return waits.short_waits(out)
+
+
+def check_waits(found):
+    """found: (source, short_waits() of what it became).  Fails where a kernel reads a matrix product's result too early."""
+    early = [f"{source}: {kernel}: '{use}' {states} wait states behind '{product}', which needs {need}"
+             for source, short in found for kernel, product, use, states, need in short]
+    if early:
+        raise RuntimeError("results of matrix products that are read too early:\n" + "\n".join(early))
+
+
 def _native_command():
     """The command that compiles the native calls: host code only, against torch's headers (torch itself is not imported).
     None without torch."""
@@ -202,7 +236,7 @@ def build_lib(verbose: bool = True, jobs: int | None = None) -> str:
         rest = _strip_remarks(out)
         if verbose and rest.strip():
             print(rest)
-        return obj, _parse_resources(out)
+        return obj, _parse_resources(out), (src, short_waits(obj))
 
     with ThreadPoolExecutor(max_workers=jobs) as pool:
         native = pool.submit(build_native, verbose)
@@ -210,6 +244,7 @@ def build_lib(verbose: bool = True, jobs: int | None = None) -> str:
         native.result()
     objs = [r[0] for r in results]
     _resource_report([row for r in results for row in r[1]], verbose)
+    check_waits([r[2] for r in results])
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", LIB_PATH]
     if verbose:
         print(" ".join(cmd), flush=True)

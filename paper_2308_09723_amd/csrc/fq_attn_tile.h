@@ -303,6 +303,11 @@ struct wave_state {
                     for (int i = 0; i < 16; ++i) o[t][i] *= again;
             }
         }
+        if (ACT == FQ_BF16) {
+            // (where a branch leads past the search, the compiler leaves one or two wait states for the last product's scores out)
+            asm volatile("s_nop 3");
+            __builtin_amdgcn_sched_barrier(0);
+        }
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int t = 0; t < H; ++t) {
