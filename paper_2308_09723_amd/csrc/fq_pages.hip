@@ -175,7 +175,9 @@ __device__ inline void fork_last(const fq_fork_args& a, int* sums, int wanted, c
 
 // All of it by one block, up to SMALL children and rows: what becomes of each is worked out once, and the entries' reads do not wait for each other.
 // References change once for each page of an old row, by its children's number (less one where it is given up), since one compute unit counts but one at a
-// time.  Bound by latency: 4 children of 4 rows 6.4 us, 256 of 256 of up to 33 pages 16 (17.5 where each child and each old row counted its own).
+// time; where old rows stay that are more than twice the children, once for each child's, so that a large table is not gone through for a few of its rows.  Bound by latency: 4
+// children of 4 rows 6.4 us, 256 of 256 of up to 33 pages 16 (17.5 where each child and each old row counted its own).  With the copies' launch, old rows staying, 4 children
+// of 1024 rows of 2048 entries 13.5, by rows 417; 256 of 257 rows of 64 17.8 by rows, by children 23.6.
 constexpr int SMALL = 1024;
 __global__ __launch_bounds__(THREADS) void fq_pages_fork_kernel(fq_fork_args a, fqa::divisor by_width) {
     __shared__ int sums[THREADS / 64 + 1];
@@ -213,7 +215,8 @@ __global__ __launch_bounds__(THREADS) void fq_pages_fork_kernel(fq_fork_args a, 
         changed[t] = count[t] == (a.release ? 1 : 0) ? 0 : row.whole + (a.release && count[t] == 0 && row.part ? 1 : 0);
     }
     __syncthreads();
-    const int entries = a.children * width, old = a.rows * width;
+    const bool by_row = a.release || a.rows <= 2 * a.children;
+    const int entries = a.children * width, old = by_row ? a.rows * width : 0;       // (no more than twice what the launch has counted)
     for (int e0 = t; e0 < max(entries, old); e0 += THREADS * EACH) {
         int32_t page[EACH], of[EACH];
 #pragma unroll
@@ -230,6 +233,7 @@ __global__ __launch_bounds__(THREADS) void fq_pages_fork_kernel(fq_fork_args a, 
         for (int y = 0; y < EACH; ++y) {
             const int e = e0 + y * THREADS;
             if (e < entries) a.table_out[e] = page[y];
+            if (!by_row) refer(a.refs, a.pages, page[y], 1);       // (full pages: the copy of one that is not comes later)
             if (e < old) refer(a.refs, a.pages, of[y], count[by_width.quotient(e)] - (a.release ? 1 : 0));
         }
     }
