@@ -266,10 +266,11 @@ struct split8 {
 #pragma unroll
         for (int i = 0; i < 8; ++i) t[i] = x[i >> 2][i & 3] * scale;
     }
+    // the largest magnitude of those that are finite (a division by it leaves infinities and NaNs what they are)
     __device__ __forceinline__ float most() const {
         float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = __builtin_fmaxf(m, __builtin_fabsf(t[i]));
+        for (int i = 0; i < 8; ++i) m = __builtin_fabsf(t[i]) < __builtin_inff() ? __builtin_fmaxf(m, __builtin_fabsf(t[i])) : m;
         return m;
     }
     __device__ __forceinline__ void split(int e, u32x4* high, u32x4* low) const {
@@ -300,7 +301,7 @@ __global__ __launch_bounds__(256) void fq_adapter_fold_kernel(fq_adapter_args a,
     float most = id >= 0 ? s.most() : 0.0f;
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, d));
-    const int e = ACT == FQ_F16 ? __builtin_amdgcn_frexp_expf(most) : 0;       // (0 for an infinity)
+    const int e = ACT == FQ_F16 ? __builtin_amdgcn_frexp_expf(most) : 0;
     if (id < 0 || rank0 >= wide) return;
     u32x4 high, low;
     s.split(e, &high, &low);
