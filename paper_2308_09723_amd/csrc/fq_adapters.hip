@@ -273,19 +273,26 @@ struct split8 {
         for (int i = 0; i < 8; ++i) m = __builtin_fabsf(t[i]) < __builtin_inff() ? __builtin_fmaxf(m, __builtin_fabsf(t[i])) : m;
         return m;
     }
+    // Rounded to zero, and to the number before where next to nothing would be left: what is left then has the same sign and is no zero, so that an infinite
+    // weight times both is the infinity that it is times t.  (Of a number of exponent E bfloat16 is off by 2^(E - 16) at most; binary16 by 2^(E - 22), or 2^-24 of a row whose
+    // largest is 1/2 .. 1.  There, sums below 2^-23 count as zeros for an infinite weight, as do bfloat16's below 2^-118.)
     __device__ __forceinline__ void split(int e, u32x4* high, u32x4* low) const {
+        constexpr float LEAST = ACT == FQ_F16 ? 0x1p-24f : 0x1p-126f, MOST = ACT == FQ_F16 ? 0x1p-23f : 0x1p-118f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float u = t[2 * i], v = t[2 * i + 1];
-            if (ACT == FQ_F16) u = __builtin_amdgcn_ldexpf(u, -e), v = __builtin_amdgcn_ldexpf(v, -e);
-            uint32_t both = pack2<ACT>(u, v);
-            if (ACT == FQ_BF16) {                       // (a number that rounds to infinity: the largest one, and the rest below)
-                if ((both & 0x7fffu) == 0x7f80u && __builtin_fabsf(u) < __builtin_inff()) both -= 1u;
-                if ((both >> 16 & 0x7fffu) == 0x7f80u && __builtin_fabsf(v) < __builtin_inff()) both -= 0x10000u;
+            float rest[2];
+            uint32_t both = 0;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const float u = ACT == FQ_F16 ? __builtin_amdgcn_ldexpf(t[2 * i + x], -e) : t[2 * i + x];
+                uint32_t h = ACT == FQ_F16 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(u, 0.0f)) : __float_as_uint(u) >> 16;
+                if (__builtin_fabsf(u - half_of<ACT, 0>(h)) < LEAST && __builtin_fabsf(u) >= MOST) --h;
+                const float d = u - half_of<ACT, 0>(h);
+                rest[x] = d == d ? d : u;                     // (of an infinity: another)
+                both |= h << 16 * x;
             }
             (*high)[i] = both;
-            const float du = u - half_of<ACT, 0>((*high)[i]), dv = v - half_of<ACT, 1>((*high)[i]);
-            (*low)[i] = pack2<ACT>(du == du ? du : 0.0f, dv == dv ? dv : 0.0f);        // (of an infinity: nothing)
+            (*low)[i] = pack2<ACT>(rest[0], rest[1]);
         }
     }
 };
