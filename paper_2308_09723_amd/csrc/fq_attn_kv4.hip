@@ -113,6 +113,16 @@ __device__ __forceinline__ uint32_t times16(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(vec2, a) * __builtin_bit_cast(vec2, b));
 }
 
+// Whether a 16-byte unit of a query has a value of 2^120 or more: a group's codes (up to 7, 32 of them) times those may pass 2^128 where keys, codes times scales, do not, and a
+// score of -infinity would pass for one that counts nothing.  (bfloat16; such rows are computed one by one.)
+__device__ __forceinline__ bool beyond_codes(const u32x4& q) {
+    typedef uint16_t vec2 __attribute__((ext_vector_type(2)));
+    vec2 m = __builtin_bit_cast(vec2, q[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(vec2, q[i] & 0x7fff7fffu));
+    return (m[0] > m[1] ? m[0] : m[1]) >= 0x7b80;
+}
+
 // Of four neighbouring tokens' scales (two words) those of the first `count`: what lies behind the last key may be anything.
 __device__ __forceinline__ uint32_t first_mask(int count) { return count >= 2 ? ~0u : count == 1 ? 0xffffu : 0u; }
 
@@ -175,7 +185,7 @@ struct few_rows {
     u32x4 q[NT][S];
     f32x4 o[NT][2 * S];              // values 16 i + 4 h .. + 3 of the lane's row
     float m[NT], c[NT], l[NT];       // as wave_state's
-    bool stale;
+    bool stale, beyond;              // beyond: beyond_codes(), of any row
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -186,6 +196,7 @@ struct few_rows {
             c[n] = l[n] = 0.0f;
         }
         stale = true;
+        beyond = false;
     }
     template <typename ROWS>
     __device__ __forceinline__ void load_query(const ROWS& rows, int D) {
@@ -204,10 +215,15 @@ struct few_rows {
     __device__ __forceinline__ void take_query(const char*) {}
     // (waits for the queries here: see wave_state)
     __device__ __forceinline__ void query_is_here() {
+        bool any = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int t = 0; t < S; ++t) asm volatile("" : "+v"(q[n][t]));
+            for (int t = 0; t < S; ++t) {
+                asm volatile("" : "+v"(q[n][t]));
+                if (ACT == FQ_BF16) any = any || beyond_codes(q[n][t]);
+            }
+        beyond = __any(any);
     }
 
     // S^T of a record: score r belongs to key 4 h + r
@@ -386,7 +402,7 @@ struct few_rows {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) x = __builtin_fmaf(o[n][i][r], 0.0f, x);
         }
-        return __all(x == 0.0f);
+        return __all(x == 0.0f) && !beyond;
     }
 };
 
@@ -410,7 +426,7 @@ struct four_rows {
     u32x2 q[S][4][2];                // [t][a][half]: values 32 t + 8 a + 4 half .. + 3 of row j
     f32x4 o[1][2 * S];               // values 16 i + 4 h .. + 3 of row (lane % 16) % 4
     float m[1], c[1], l[1];
-    bool stale;
+    bool stale, beyond;
 
     __device__ __forceinline__ static int own_row() { return threadIdx.x & 3; }
     __device__ __forceinline__ static float rows_max(float x) {      // over the lanes of a row
@@ -430,6 +446,7 @@ struct four_rows {
         m[0] = -__builtin_inff();
         c[0] = l[0] = 0.0f;
         stale = true;
+        beyond = false;
     }
     // Each lane loads 16 bytes of the four rows and takes its row out of LDS (loaded as they are needed, a row 16 times, they took 3 us)
     u32x4 loaded;
@@ -438,7 +455,10 @@ struct four_rows {
         const int lane = threadIdx.x & 63, d = (lane & 15) * 8;
         loaded = d < D ? *(const u32x4*)(rows.query(min(lane >> 4, rows.count - 1)) + d) : u32x4{0, 0, 0, 0};
     }
-    __device__ __forceinline__ void query_is_here() { asm volatile("" : "+v"(loaded)); }
+    __device__ __forceinline__ void query_is_here() {
+        asm volatile("" : "+v"(loaded));
+        beyond = ACT == FQ_BF16 && __any(beyond_codes(loaded));
+    }
     __device__ __forceinline__ void pass_query(char* room) {
         const int lane = threadIdx.x & 63;
         if ((lane & 15) < 4 * S) *(u32x4*)(room + ((lane >> 4) * 4 * S + (lane & 15)) * 16) = loaded;
@@ -612,7 +632,7 @@ struct four_rows {
         for (int i = 0; i < 2 * S; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) x = __builtin_fmaf(o[0][i][r], 0.0f, x);
-        return __all(x == 0.0f);
+        return __all(x == 0.0f) && !beyond;
     }
 };
 
