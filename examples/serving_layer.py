@@ -20,8 +20,15 @@ from examples.attention_layer import AttentionLayer  # noqa: E402
 from paper_2308_09723_amd import fq  # noqa: E402
 
 
+def room(prompts, beams, tokens, page=64):
+    """Tokens of a table's rows, and pages of a pool, for beams of prompts that go on for so many tokens: the prompts' pages, and of each beam those of its own."""
+    pages = sum((n + page - 1) // page for n in prompts) + len(prompts) * beams * ((tokens + page - 1) // page + 1)
+    return max(prompts) + tokens, pages
+
+
 class SharedCache:
-    """A pool of pages held in 4 bits, and the rows of a table that hold them."""
+    """A pool of pages held in 4 bits, and the rows of a table that hold them.  Rows that there is no room for are an error (grow, fork: the host waits for the lengths; a
+    captured step would look at them behind its replays)."""
 
     def __init__(self, pages, rows, tokens, kv_heads, head_dim, page=64):
         self.page, self.kv_heads = page, kv_heads
@@ -33,7 +40,11 @@ class SharedCache:
     def grow(self, tokens):
         """Room for so many more tokens in every row (int32 [rows], on the device); the lengths from before."""
         before = self.lens.clone()
-        fq.pages_take(self.refs, self.page, self.table, self.lens, before + tokens)
+        wanted = before + tokens
+        fq.pages_take(self.refs, self.page, self.table, self.lens, wanted)
+        short = (self.lens != wanted).nonzero()[:, 0].tolist()
+        if short:       # (their next keys have no place, and attention would read another row's in it)
+            raise RuntimeError(f"no room for the next tokens of rows {short}: too few pages, or too few entries in the table")
         return before
 
     def slots(self, rows, positions):
@@ -43,6 +54,9 @@ class SharedCache:
 
     def fork(self, parents, release=True):
         self.table, self.lens = fq.pages_fork(self.refs, self.page, self.table, self.lens, parents, [self.pages], release=release)
+        short = (self.lens < 0).nonzero()[:, 0].tolist()
+        if short:
+            raise RuntimeError(f"no pages for children {short}")
 
     def free(self, rows=None):
         fq.pages_free(self.refs, self.page, self.table, self.lens, rows)
@@ -102,8 +116,8 @@ def main():
     dtype = torch.float16 if a.dtype == "f16" else torch.bfloat16
     layer = ServingLayer(a.hidden, a.heads, a.kv_heads, rank=a.rank, dtype=dtype)
     n = len(a.prompts)
-    longest = max(a.prompts) + a.tokens
-    cache = SharedCache(2 * n * (a.beams + longest // 64 + 1), n, longest, a.kv_heads, layer.D)
+    longest, pages = room(a.prompts, a.beams, a.tokens + 1)        # (the loop's tokens, and one that is timed)
+    cache = SharedCache(pages, n, longest, a.kv_heads, layer.D)
     gen = torch.Generator(device="cuda").manual_seed(1)
 
     def rows(n):
