@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256, 2) void fq_attention_prompt_kernel(fq_heads q,
                 keep_seen(s[0], low_bits(end - base));
                 keep_seen(s[1], low_bits(end - base - HALF));
             }
-            w.template soften<2>(s, p.factor, x);
+            w.template soften<2, false>(s, p.factor, x);
             w.template accumulate<2>(at + TILE_BYTES, x);
         }
     }

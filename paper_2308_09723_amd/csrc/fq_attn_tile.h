@@ -283,7 +283,9 @@ struct wave_state {
     }
 
     // Numerators of the scores, in the order that accumulate() takes; maximum, sum and results brought along.
-    template <int H>
+    // WAIT: where a branch leads past the search for the maximum (bfloat16), the compiler may leave one or two wait states for the last product's scores out, and
+    // four stand there.  (The build says where they are missing; a prompt of 8192 tokens has all of its own: 479.4 us without, 480.8 with.)
+    template <int H, bool WAIT = true>
     __device__ __forceinline__ void soften(f32x16 (&s)[H], float factor, u32x4 (&p)[2 * H]) {
         if (ACT == FQ_F16 || stale) {
             if (ACT == FQ_BF16) level();
@@ -303,8 +305,7 @@ struct wave_state {
                     for (int i = 0; i < 16; ++i) o[t][i] *= again;
             }
         }
-        if (ACT == FQ_BF16) {
-            // (where a branch leads past the search, the compiler leaves one or two wait states for the last product's scores out)
+        if (ACT == FQ_BF16 && WAIT) {
             asm volatile("s_nop 3");
             __builtin_amdgcn_sched_barrier(0);
         }
