@@ -10,9 +10,9 @@
 // address unit four times as long as one of four rows' 256).  t goes into the second product as the sum of two 16-bit numbers (16 bits and
 // more of it), in binary16 after a division by a power of two that brings the row's largest to about one.
 //
-// Bound by memory: A and B of each adapter, x once, the output twice.  One row, K and N 1024, rank 8: 2.8 + 3.2 us, launches; 64 rows of 64 adapters, K 4096, N 6144,
-// rank 16, 20 MB: 6.2 + 6.2; 2900 rows of 5 requests, K 12288, N 36864, rank 64: 28.4 for the inner sums (71 MB of x: 2.5 TB/s), 5.2 to fold them, 105 for the output (428 MB
-// read and written: 4.1 TB/s).
+// Bound by memory: A and B of each adapter, x once, the output twice.  One row, K and N 1024, rank 8: 2.6 + 3.0 us, launches; 64 rows of 64 adapters, K 4096, N 6144,
+// rank 16, 20 MB: 6.0 + 6.2; 2900 rows of 5 requests, K 12288, N 36864, rank 64: 28.6 for the inner sums (71 MB of x: 2.5 TB/s), 5.2 to fold them, 106 for the output (428 MB
+// read and written: 4.0 TB/s), 138 in all.
 #include <hip/hip_runtime.h>
 #include <atomic>
 
@@ -29,9 +29,9 @@ using fqa::type16;
 using fqa::u32x2;
 using fqa::u32x4;
 
-// Rows that are taken to have adapters of their own: where that costs little if they have not, and up to 256 where there are many adapters.  us, K 4096 and N 6144, so and with
-// 64 rows a block: 64 rows of rank 64, 64 adapters in turn 21.5, 149, three requests' 14.1, 16.4; 256 of rank 16, 19.7, 88.6 and 12.0, 13.2; 256 of rank 64, 42.5, 150 and 25.1,
-// 15.9; 512 of rank 16, 31.8, 97.3 and 17.3, 14.1.
+// Rows that are taken to have adapters of their own: where that costs little if they have not, and up to 256 where there are many adapters (the host does not see the rows' ids).  us,
+// K 4096 and N 6144, 64 adapters of which the rows have one after the other, or three requests one each, so and with 64 rows a block: 64 rows of rank 64 21.4, 150, requests'
+// 16.5, 17.3; 256 of rank 16 19.5, 106, and 17.3, 14.3; 256 of rank 64 41, 150, and 39.8, 16.8; 512 of rank 16 31, 106, and 29.8, 15.3.
 inline bool few_rows(int64_t rows, int64_t adapters, int rank) { return rows * rank <= 4096 || (adapters > 8 && rows <= 256); }
 
 template <int ACT>
@@ -440,12 +440,12 @@ adapter_plan plan(int64_t rows, int adapters, int rank, int64_t N, int64_t K) {
     adapter_plan p;
     p.few = few_rows(rows, adapters, rank);
     const int64_t tiles = (rows + (p.few ? 15 : 63)) / (p.few ? 16 : 64), most = rows < 16 ? rows : 16;
-    // More rows: of a prompt's tiles most have one adapter, some two, whose second turn is another block's (rows of 5 requests, as below: 43.7 us by the same, 29.0).
+    // More rows: of a prompt's tiles most have one adapter, some two, whose second turn is another block's (rows of 5 requests, as below: 147.6 us in all by the same, 137.8).
     p.slots = p.few ? (int)(adapters < most ? adapters : most) : adapters < 4 ? adapters : 4;
     const int64_t pieces = p.few ? (K + 31) / 32 : (K + 127) / 128, least = p.few ? 16 : 4;        // pieces of K; of a block, at least
     const int64_t wanted = p.few ? 512 / (tiles * p.slots) : 464 / tiles, fit = (pieces + least - 1) / least;
     p.parts = (int)(wanted < 1 ? 1 : wanted < fit ? wanted : fit);
-    // (blocks go to the eight dies in turn: a part's columns of A stay in one die's cache; eight parts 29.0 us, ten 35.6, sixteen 31.7)
+    // (blocks go to the eight dies in turn: a part's columns of A stay in one die's cache; in all, eight parts 137.8 us, ten 144.7, sixteen 142.0)
     if (p.parts > 8) p.parts = p.parts / 8 * 8;
     const int64_t each = (pieces + p.parts - 1) / p.parts;
     p.parts = (int)((pieces + each - 1) / each);
@@ -454,12 +454,13 @@ adapter_plan plan(int64_t rows, int adapters, int rank, int64_t N, int64_t K) {
         int lanes = 1;
         while (8 * lanes < rank) lanes *= 2;
         const int64_t steps = (N * lanes + 63) / 64;           // of a row, all columns
-        // (four waves a SIMD: 64 rows, N 6144, rank 16, 10.2 us; sixteen 12.2; rank 64, N and K 12288, 37.7 and 40.1)
+        // (four waves a SIMD, of four steps at least: 64 rows, N 6144, rank 16, 12.2 us in all; of one, sixteen 15.6; 16 rows four steps 8.2, of one 9.6; 64 rows of rank 64, N and K
+        // 12288, 51.8, sixteen 51.0)
         turns = (rows * steps + 4095) / 4096;
         turns = turns < 4 ? 4 : turns > 32 ? 32 : turns;
     } else {
         const int64_t all = tiles * ((N + 127) / 128);
-        // (eight blocks a compute unit: 2900 rows, N 36864, rank 64, 127.5 us in all; two 137.8, a turn each 138.4)
+        // (eight blocks a compute unit: 2900 rows, N 36864, rank 64, 137.8 us in all; two 145.6, a turn each 148.7)
         turns = all / 2048;
         turns = turns < 1 ? 1 : turns > 8 ? 8 : turns;
     }

@@ -2,8 +2,8 @@
 //
 // Work is dealt out as over a cache of 16 bits (fq_attn_units.h).  A key and its value are 1.125 D bytes, and taking their codes to 16 bits
 // is 2 D / 8 times 9 instructions, beside 4 D operations for each row on the matrix cores: with few rows the cache's bytes and
-// the conversions bind it about equally.  A token each of 64 sequences of 100 - 8191, 8 heads of 128, four rows each: 123 MB in 28.7 us, 4.3 TB/s (bytes 17.5 at the rate of
-// a kernel that only reads; 5 us of it are blocks' beginnings), 7.0 to join; over 16 bits 76 and 7.4.
+// the conversions bind it about equally.  A token each of 64 sequences of 100 - 8191, 8 heads of 128, four rows each: 123 MB in 28.5 us, 4.3 TB/s (bytes 17.5 at the rate of
+// a kernel that only reads; 5 us of it are blocks' beginnings), 7.0 to join, binary16 30.8 and 7.2; over 16 bits 76 and 7.4.  8 and 16 rows 39.8 (binary16 37.6), 32 58 (54), and 9 - 11.
 //
 // Up to 32 rows (fq_attention_kv4_stream_kernel) every wave brings 32 keys at a time into LDS of its own, as they lie in the cache: a
 // record of 16 tokens is what one product of 16 x 16 x 32 takes, lane by lane.  S^T = K Q^T goes over the keys' codes, group by group, and
@@ -13,8 +13,8 @@
 //
 // Above 32 rows (fq_attention_kv4_tile_kernel) the waves of a block take a tile's codes to 16 bits once, each a record, into tiles that all of them read: keys
 // as over a cache of 16 bits, values turned over (a lane has four tokens of a value).  Bound by instructions: for 32 rows and 64 keys a wave has 32 products, 170
-// instructions' time for the numerators and, of four waves, 200 for the codes, of eight 100.  Pieces of 700 tokens over 2500 - 3900, two sequences, 32 heads over 8: 134 us with
-// the join, 0.72 PFLOP/s; over 16 bits 151.
+// instructions' time for the numerators and, of four waves, 200 for the codes, of eight 100.  Pieces of 700 tokens over 2500 - 3900, two sequences, 32 heads over 8: 131 us with
+// the join where the card has been at rest, 0.73 PFLOP/s, 145 one call after the other (in a trace 134 and 17, binary16 144 and 17); over 16 bits 143.
 #include <hip/hip_runtime.h>
 #include <atomic>
 
@@ -1032,16 +1032,17 @@ int launch(const fq_tree_args& a, const tree_plan& p, hipStream_t stream) {
 }  // namespace
 
 // Above 128 rows blocks of 256, which take a key to 16 bits half as often as blocks of 128, where there are six tiles for each of them or more (a block begins
-// with 5 us in which it multiplies nothing).  us, 256 rows and 128: two sequences of 2500 - 3900 tokens, 2800 rows of eight heads 108, 121; eight of 500 - 4095, 192 rows
-// 39.3, 46.5; one of 20 000, 192 rows, which has five, 46.6, 42.1; one of 8000, eight heads of 64, 200 rows, two, 29.1, 23.2.
+// with 5 us in which it multiplies nothing), by the table's width.  us with the join, one call after the other, 256 rows and 128: two sequences of 2500 - 3900 tokens, 2800
+// rows of eight heads, 145, 163; eight of 500 - 4095, 192 rows, 39.0, 42.5; eight of 1000 in tables for 4000 34.3, 34.7; one of 20 000, 192 rows, which has five, 48.1, 43.4; of 8000 in
+// such a table 36.5, 33.6; one of 8000, eight heads of 64, which has two: a chain of 200 tokens 33.4, 27.5, but a tree of 25, eight query heads each, 20.2, 25.4.
 static bool wide(const fq_tree_args& a, int64_t rows) {
     const int64_t tiles = (a.table_width * a.cache.page_size + 127) / 128, units = a.sequences * a.kv_heads * ((rows + 255) / 256);
     return rows > 128 && tiles * units >= 6 * (int64_t)fq_cu_count();
 }
 
 // Few rows: waves take heads of their own where there are enough, so that pieces are four times as long, and few are joined in LDS.
-// The beginning and end of a unit count as three tiles, one of 128 keys (a token each of 64 sequences of 100 - 8191: 40.8 us where they count as none, 29.1 so; two
-// sequences' pieces as above, none 108.8, one 108.4, two 107.6, eight sequences' trees 42.6, 39.3, 42.1).
+// The beginning and end of a unit count as three tiles, one of 128 keys (with the join: a token each of 64 sequences of 100 - 8191 41.2 us where they count as none, 36.5 so; two
+// sequences' pieces as above, none 145.6, one 144.7, two 143.2, eight sequences' trees 40.8, 38.9, 42.4).
 static tree_plan plan_kv4(const fq_tree_args& a) {
     const int64_t rows = (int64_t)a.nodes * (a.q_heads / a.kv_heads);
     const int heads = rows > 16 ? 1 : a.kv_heads % 4 == 0 ? 4 : a.kv_heads % 2 == 0 ? 2 : 1;
