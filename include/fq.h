@@ -526,7 +526,8 @@ int fq_pages_free(int32_t* refs, int64_t pages, int page_size, int32_t* table, i
 
 /*
  * fq_pages_compact -- gathers the pool's U used pages in pages 0 .. U - 1: those behind go into free ones before, both in their order; refs and the table's entries
- * follow, and what the pages hold.  (A pool's rows must all be in the table.  What lay in the pages that become free stays there.)
+ * follow, and what the pages hold.  (A pool's rows must all be in the table: a page that somebody keeps by its refs alone is moved
+ * like any other, and only rows are told.  What lay in the pages that become free stays there.)
  *   workspace   device scratch, >= fq_pages_compact_workspace_bytes(pages) bytes
  */
 size_t fq_pages_compact_workspace_bytes(int64_t pages);

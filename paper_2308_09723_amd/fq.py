@@ -1079,7 +1079,7 @@ def pages_free(refs, page_size, page_table, lens, rows=None):
 
 
 def pages_compact(refs, page_size, page_table, lens, buffers=(), workspace=None):
-    """Gathers the pool's used pages at its beginning: refs and page_table (all rows that hold pages) are changed in place, pages copied in the buffers (as
+    """Gathers the pool's used pages at its beginning: refs and page_table (all rows that hold pages; one kept by refs alone moves untold) are changed in place, pages copied in the buffers (as
     pages_copy's).  workspace: pages_compact_workspace_bytes."""
     if _torch_mod is None:
         _torch()
